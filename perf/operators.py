@@ -294,7 +294,9 @@ def prepare(case, seed):
         if k in ("fused", "policy"):
             s["opts"] = cd.policy_opts(clip_low=CLIP_LOW, clip_high=CLIP_HIGH, dual_clip=DUAL, kl_coef=c["kl"],
                                        entropy_coef=c["ent"], reduction=c["reduction"])
-            n = cd.policy_loss_workspace(c["B"], c["T"])
+            n = cd.policy_loss_logits_workspace(s["logits"]) if k == "fused" else cd.policy_loss_workspace(c["B"], c["T"])
+        elif k == "logprobs":
+            n = cd.token_logprobs_workspace(s["logits"])
         elif k == "preference":
             s["opts"] = cd.preference_opts(beta=BETA, loss=c["loss"], label_smoothing=c["smoothing"],
                                            length_norm=c["length_norm"])
@@ -303,7 +305,7 @@ def prepare(case, seed):
             n = cd.head_logprobs_workspace(s["hidden"], s["weight"])
         elif k == "headgrad":
             n = cd.head_logprobs_backward_workspace(s["hidden"], s["weight"])
-        s["workspace"] = torch.empty(n, dtype=torch.uint8, device="cuda")
+        s["workspace"] = cd.workspace(n)
     return s
 
 
@@ -322,7 +324,7 @@ def _run_own(s):
     if k == "logprobs":
         logp, lse, entropy = s["out"]
         cd.conduit_token_logprobs(s["logits"], s["tokens"], logp, lse=lse, entropy=entropy, mask=s["mask"],
-                                  temperature=TAU)
+                                  temperature=TAU, workspace=ws)
         return {"logp": logp, "lse": lse, "entropy": entropy}
     if k == "backward":
         cd.conduit_token_logprobs_backward(s["logits"], s["tokens"], s["lse"], s["dlogp"], s["dlogits"],
