@@ -559,6 +559,175 @@ conduit_status conduit_minibatch_gather(const void* src, int64_t row_bytes, int6
                                         void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Token log-probabilities and losses: what a learner does with a delivered
+ * batch (PPO, Schulman et al., which the paper's on-policy workloads run, and
+ * its token form in the paper's post-training workload, App. A).
+ *
+ * A call works on B sequences of T tokens.  Every per-token array of a call
+ * (tokens, mask, log-probabilities, advantages, gradients, ...) is [B, T] with
+ * rows `stride` >= T elements apart, the same for all of them, so the delivered
+ * arrays and their columns [1, T) alike can be passed as they are.  mask is
+ * uint8 (NULL: every token counts): at tokens where it is 0 nothing else is
+ * read, whatever stands there, per-token outputs and gradients are written as
+ * 0, and no sum or mean sees them.  B * T < 2^31.  Sums over tokens run in
+ * fp64 and are joined in a fixed order: results are the same on every run.
+ * Tokens outside [0, V) that the mask counts are flagged, and are treated as
+ * masked but for the token counts.
+ * Per-token outputs may be one of the call's per-token float inputs (in place),
+ * and overlap none otherwise.
+ *
+ * Workspaces: `workspace` is device memory of at least the size that the
+ * call's _workspace function reports, 256-byte aligned, made ready once by
+ * conduit_workspace_init.  A call leaves it ready for the next one, of any of
+ * these functions and any sizes that fit; calls that may overlap in time need
+ * one each.
+ * ------------------------------------------------------------------------- */
+
+/* Rows of `width` elements for B x T tokens: row (b, t) starts at element
+ * b * stride_b + t * stride_t of `data` (device). */
+typedef struct {
+    void* data;
+    int32_t dtype;   /* CONDUIT_F32 or CONDUIT_BF16 */
+    int32_t reserved;
+    int64_t width;
+    int64_t stride_b, stride_t;
+} conduit_rows;
+
+/* Clear a new workspace (in stream order).  Errors: EINVAL (NULL or misaligned
+ * workspace, bytes not a multiple of 4), EDEVICE. */
+conduit_status conduit_workspace_init(void* workspace, uint64_t bytes, void* stream);
+
+/*
+ * Log-probabilities of the taken tokens under logits of V choices at a
+ * sampling temperature, with z_j = x_j / temperature:
+ *     lse = log sum_j exp z_j,  logp = z_token - lse,
+ *     entropy = lse - sum_j p_j z_j,  p_j = exp(z_j - lse).
+ * logits: float or bf16 rows of V = logits->width elements, 1 <= V <= 2^28, at
+ * any element alignment; tokens int32.  logp, lse, entropy: float outputs, each
+ * may be NULL.  A choice whose logit is -inf has probability 0 (and adds 0 to
+ * the entropy); a row of nothing else gives logp = lse = -inf and entropy 0.
+ * fp32 inside.  Rows of up to 512 choices share a wavefront or take one, wider
+ * ones a wavefront or a workgroup; fewer rows than the GPU has compute units
+ * are split into parts that the row's last workgroup joins.
+ * Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_token_logprobs_workspace(int64_t B, int64_t T, const conduit_rows* logits, uint64_t* bytes);
+conduit_status conduit_token_logprobs(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
+                                      const int32_t* tokens, const uint8_t* mask, double temperature, float* logp,
+                                      float* lse, float* entropy, void* workspace, uint64_t workspace_bytes,
+                                      void* stream);
+
+/*
+ * The gradient of conduit_token_logprobs: for gradients dlogp of the
+ * log-probabilities and dentropy of the entropies (NULL: none; either or both),
+ *     dx_j = (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)) / temperature
+ * from the logits and the forward call's lse (and entropy, with dentropy).
+ * dlogits: rows of the logits' dtype and width, rounded once; it may be the
+ * logits themselves (in place).  Masked rows are written as 0, and so are rows
+ * whose lse is -inf.  Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_token_logprobs_backward(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
+                                               const int32_t* tokens, const uint8_t* mask, double temperature,
+                                               const float* lse, const float* entropy, const float* dlogp,
+                                               const float* dentropy, const conduit_rows* dlogits, void* stream);
+
+/* how the terms of the counted tokens become one loss */
+typedef int32_t conduit_reduction;
+enum {
+    CONDUIT_TOKEN_MEAN = 0,    /* mean over the counted tokens of the batch */
+    CONDUIT_SEQUENCE_MEAN = 1, /* mean over the rows with any of the mean over the row's counted tokens */
+    CONDUIT_SUM = 2,           /* sum (a caller's own normalisation: `scale`) */
+};
+
+typedef struct {
+    double clip_low, clip_high; /* the ratio is clipped into [1 - clip_low, 1 + clip_high]; default 0.2, 0.2 */
+    double dual_clip;           /* > 1: ceiling -A dual_clip of the term where A < 0; 0 (default): none */
+    double kl_coef;             /* of the KL term to the reference; default 0 */
+    double entropy_coef;        /* of the entropy bonus; default 0 */
+    double scale;               /* of the loss and its gradients; default 1 */
+    conduit_reduction reduction;
+    int32_t reserved;
+} conduit_policy_opts;
+
+void conduit_policy_opts_default(conduit_policy_opts* opts);
+
+/*
+ * The clipped policy loss (PPO) with a KL term to a reference policy and an
+ * entropy bonus, and its gradient.  Per counted token, with r = exp(logp - old):
+ *     s = max(-A r, -A clip(r, 1 - clip_low, 1 + clip_high)),
+ *         and at most -A dual_clip where A < 0 (dual_clip > 0)
+ *     k = exp(x) - 1 - x,  x = ref - logp
+ *     loss = scale * sum w (s + kl_coef k - entropy_coef entropy),  w by `reduction`
+ *     dlogp = scale w ([s follows r] (-A r) + kl_coef (1 - exp x))
+ *     dentropy = -scale w entropy_coef
+ * At a tie (r on the clip's edge) s follows r.  old_logp NULL: r = 1 (the
+ * policy that acted); ref_logp NULL: k = 0; entropy NULL: 0.  stats: float [8]:
+ * loss; sum w s; sum w k; sum w entropy; fraction of counted tokens that a clip
+ * decided; mean of old - logp; mean ratio; counted tokens.  dlogp and dentropy
+ * may be NULL.  A batch without counted tokens gives zeros.
+ * Up to 16,384 tokens in whole rows take one launch, larger batches one without
+ * and two with a mask.  Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_policy_loss_workspace(int64_t B, int64_t T, uint64_t* bytes);
+conduit_status conduit_policy_loss(const conduit_policy_opts* opts, int64_t B, int64_t T, int64_t stride,
+                                   const float* logp, const float* old_logp, const float* ref_logp, const float* adv,
+                                   const float* entropy, const uint8_t* mask, float* stats, float* dlogp,
+                                   float* dentropy, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * conduit_token_logprobs, conduit_policy_loss and
+ * conduit_token_logprobs_backward as one call: logits in, the loss's statistics
+ * and the gradient of the logits out.  The logits cross memory once in each
+ * direction where a row fits a workgroup's registers (up to 256 KB); dlogits may
+ * be the logits themselves.  logp and entropy receive the per-token values
+ * (required; 0 where the mask is).  Other arguments as in the three calls.
+ * Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_policy_loss_logits_workspace(int64_t B, int64_t T, const conduit_rows* logits, uint64_t* bytes);
+conduit_status conduit_policy_loss_logits(const conduit_policy_opts* opts, const conduit_rows* logits, int64_t B,
+                                          int64_t T, int64_t stride, const int32_t* tokens, const float* old_logp,
+                                          const float* ref_logp, const float* adv, const uint8_t* mask,
+                                          double temperature, float* logp, float* entropy, float* stats,
+                                          const conduit_rows* dlogits, void* workspace, uint64_t workspace_bytes,
+                                          void* stream);
+
+/* the form of the preference loss */
+typedef int32_t conduit_preference_kind;
+enum {
+    CONDUIT_PREFERENCE_SIGMOID = 0, /* -(1 - e) log s(u) - e log s(-u), s the logistic function, e = label_smoothing */
+    CONDUIT_PREFERENCE_SQUARED = 1, /* (u / beta - 1 / (2 beta))^2 */
+};
+
+typedef struct {
+    double beta;             /* > 0; default 0.1 */
+    double label_smoothing;  /* in [0, 1); default 0 */
+    double scale;            /* of the loss's mean and its gradient; default 1 */
+    conduit_preference_kind loss;
+    int32_t length_norm;     /* 1: a row's sum is divided by its counted tokens */
+} conduit_preference_opts;
+
+void conduit_preference_opts_default(conduit_preference_opts* opts);
+
+/*
+ * The preference loss over P pairs of answers and its gradient.  Rows 0..P-1 of
+ * the [2 P, T] arrays are the preferred (chosen) answers, row P + i the rejected
+ * answer to row i's.  With d = sum over a row's counted tokens of logp - ref
+ * (ref_logp NULL: 0), divided by their number with length_norm, and
+ * u = beta (d_chosen - d_rejected): loss[i] as in conduit_preference_kind,
+ * chosen[i] = beta d_chosen, rejected[i] = beta d_rejected; stats: float [4]:
+ * scale * mean loss; fraction of pairs with u > 0; mean u; counted tokens.
+ * dlogp = the gradient of stats[0].  loss float [P]; chosen, rejected float [P]
+ * or NULL; dlogp or NULL.  A row without counted tokens has d = 0.  P = 0 gives
+ * zeros.  2 P T < 2^31.  One launch, or two where few pairs of long rows are
+ * split into parts of 4,096 tokens.  Errors: EINVAL, EDEVICE.
+ */
+conduit_status conduit_preference_loss_workspace(int64_t P, int64_t T, uint64_t* bytes);
+conduit_status conduit_preference_loss(const conduit_preference_opts* opts, int64_t P, int64_t T, int64_t stride,
+                                       const float* logp, const float* ref_logp, const uint8_t* mask, float* loss,
+                                       float* chosen, float* rejected, float* stats, float* dlogp, void* workspace,
+                                       uint64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * State, introspection, errors
  * ------------------------------------------------------------------------- */
 typedef struct {

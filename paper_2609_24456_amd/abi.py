@@ -119,6 +119,28 @@ class CkptHeader(C.Structure):
                 ("section", CkptSection * CKPT_MAX_SECTIONS)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("reserved", C.c_int32), ("width", C.c_int64),
+                ("stride_b", C.c_int64), ("stride_t", C.c_int64)]
+
+
+TOKEN_MEAN, SEQUENCE_MEAN, SUM = 0, 1, 2
+REDUCTIONS = {"token_mean": TOKEN_MEAN, "sequence_mean": SEQUENCE_MEAN, "sum": SUM}
+PREFERENCE_SIGMOID, PREFERENCE_SQUARED = 0, 1
+PREFERENCE_LOSSES = {"sigmoid": PREFERENCE_SIGMOID, "squared": PREFERENCE_SQUARED}
+
+
+class PolicyOpts(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("dual_clip", C.c_double),
+                ("kl_coef", C.c_double), ("entropy_coef", C.c_double), ("scale", C.c_double),
+                ("reduction", C.c_int32), ("reserved", C.c_int32)]
+
+
+class PreferenceOpts(C.Structure):
+    _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double), ("scale", C.c_double),
+                ("loss", C.c_int32), ("length_norm", C.c_int32)]
+
+
 # every symbol include/conduit.h declares, with its ctypes signature
 P = C.c_void_p
 I64 = C.c_int64
@@ -163,6 +185,18 @@ SIGNATURES = {
     "conduit_run_onpolicy": (ST, [P, P, P, P, P, P, P]),
     "conduit_placement_profile": (ST, [I64, I32_, P]),
     "conduit_place": (ST, [P, I32_, I64, F64, P, I32_, P, P]),
+    "conduit_workspace_init": (ST, [P, C.c_uint64, P]),
+    "conduit_token_logprobs_workspace": (ST, [I64, I64, P, P]),
+    "conduit_token_logprobs": (ST, [P, I64, I64, I64, P, P, F64, P, P, P, P, C.c_uint64, P]),
+    "conduit_token_logprobs_backward": (ST, [P, I64, I64, I64, P, P, F64, P, P, P, P, P, P]),
+    "conduit_policy_opts_default": (None, [P]),
+    "conduit_policy_loss_workspace": (ST, [I64, I64, P]),
+    "conduit_policy_loss": (ST, [P, I64, I64, I64, P, P, P, P, P, P, P, P, P, P, C.c_uint64, P]),
+    "conduit_policy_loss_logits_workspace": (ST, [I64, I64, P, P]),
+    "conduit_policy_loss_logits": (ST, [P, P, I64, I64, I64, P, P, P, P, P, F64, P, P, P, P, P, C.c_uint64, P]),
+    "conduit_preference_opts_default": (None, [P]),
+    "conduit_preference_loss_workspace": (ST, [I64, I64, P]),
+    "conduit_preference_loss": (ST, [P, I64, I64, I64, P, P, P, P, P, P, P, P, P, C.c_uint64, P]),
     "conduit_run_offpolicy": (ST, [P, P, P, P, P, P, P]),
 }
 

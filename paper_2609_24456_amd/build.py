@@ -12,7 +12,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libconduit.so")
 SOURCES = ["api.hip", "k_ingest.hip", "k_update.hip", "k_sample.hip", "k_gather.hip", "k_sample_gather.hip",
            "k_gae.hip", "sched.hip", "loop.hip", "place.hip", "k_nstep.hip", "k_update_ingest.hip",
-           "k_reference.hip"]
+           "k_reference.hip", "losses.hip", "k_logits.hip", "k_policy.hip", "k_preference.hip"]
 ARCH = os.environ.get("CONDUIT_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
@@ -88,14 +88,14 @@ def try_tensor_check(verbose: bool = False):
 
 # The ABI's host code (api.hip: argument checks, layouts, ring state,
 # checkpoint images; sched.hip: the scheduling cost model; place.hip: the
-# placement algorithm) built with AddressSanitizer and UndefinedBehaviorSanitizer,
+# placement algorithm; losses.hip: the loss calls' checks) built with AddressSanitizer and UndefinedBehaviorSanitizer,
 # linked with the kernel sources' objects of the regular build (_build/, whose
-# host parts are only the launchers).  These three sources hold no kernels, so
+# host parts are only the launchers).  These sources hold no kernels, so
 # they compile for the host alone; the result runs the ABI's host paths under
 # the sanitizers on a machine with no GPU.
 SANITIZE = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
             "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-fno-sanitize-recover=all"]
-HOST_SOURCES = ["api.hip", "sched.hip", "place.hip"]
+HOST_SOURCES = ["api.hip", "sched.hip", "place.hip", "losses.hip"]
 
 
 def build_host_sanitized(out_dir: str, verbose: bool = False) -> str:

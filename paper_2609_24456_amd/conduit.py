@@ -452,6 +452,217 @@ def conduit_minibatch_gather(src, row_bytes, n_src, perm, xf, out, cols=(), cols
                                           ca if ncols else None, co if ncols else None, ncols, _stream(stream)))
 
 
+# ---------------------------------------------------------------------------
+# token log-probabilities and losses: per-token tensors are [B, T] (or [T]: one
+# sequence) with elements next to each other along T and the same step between
+# rows, e.g. all contiguous, or all the columns [:, 1:] of contiguous ones
+# ---------------------------------------------------------------------------
+_U8 = (torch.uint8, torch.bool)
+
+
+def _batch_shape(t, name):
+    """(shape, B, T, step between rows) of a per-token tensor."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (1, 2):
+        raise ValueError(f"{name} must be a [B, T] or [T] tensor")
+    shape = t.shape
+    if len(shape) == 1:
+        return shape, 1, shape[0], shape[0]
+    B, T = shape
+    return shape, B, T, (t.stride(0) if B > 1 and T > 0 else T)
+
+
+def _token_ptr(t, dtype, name, batch):
+    """Device address of a per-token tensor laid out as `batch` (_batch_shape), after checking it."""
+    if t is None:
+        return None
+    shape, B, T, stride = batch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if stride == T:  # contiguous
+        return _ptr(t, dtype, name)
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.stride(0) != stride or (T > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have rows {stride} elements apart, like the call's other per-token tensors")
+    if not _on_device(t):
+        raise ValueError(f"{name} must be on a HIP device")
+    return t.data_ptr()
+
+
+_ROW_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _rows_struct(t, name):
+    """conduit_rows of a [B, T, width] (or [T, width]) tensor."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a [B, T, width] or [T, width] tensor")
+    dtype = _ROW_DTYPE.get(t.dtype)
+    if dtype is None:
+        raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    width = t.shape[-1]
+    if width > 1 and t.numel() > 0 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have its row's elements next to each other")
+    r = Rows()
+    r.data, r.dtype, r.reserved, r.width, r.stride_t = t.data_ptr(), dtype, 0, width, t.stride(-2)
+    r.stride_b = t.stride(0) if t.dim() == 3 else 0
+    return r
+
+
+def _rows_ptr(t, name, shape):
+    """conduit_rows of the rows of a batch whose per-token tensors have `shape`."""
+    r = _rows_struct(t, name)
+    if t.shape[:-1] != shape:
+        raise ValueError(f"{name} must be {tuple(shape)} rows, got {tuple(t.shape[:-1])}")
+    if not _on_device(t):
+        raise ValueError(f"{name} must be on a HIP device")
+    return r
+
+
+def _rows_bytes(entry, t):
+    n = C.c_uint64()
+    B, T = (t.shape[0], t.shape[1]) if t.dim() == 3 else (1, t.shape[0])
+    _check(entry(B, T, C.byref(_rows_struct(t, "logits")), C.byref(n)))
+    return n.value
+
+
+def workspace(nbytes, stream=None):
+    """A new workspace of at least `nbytes` for the loss calls, ready for use (conduit_workspace_init)."""
+    n = max(256, (int(nbytes) + 255) // 256 * 256)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    _check(lib().conduit_workspace_init(ws.data_ptr(), n, _stream(stream)))
+    return ws
+
+
+def _workspace(ws, nbytes, stream):
+    """(tensor, address, size): the caller's workspace, or a new one of nbytes() for this call."""
+    if ws is None:
+        ws = workspace(nbytes(), stream)
+        if stream is not None:  # torch hands its memory on in the order of the tensor's own stream
+            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    return ws, _ptr(ws, torch.uint8, "workspace"), ws.numel()
+
+
+def token_logprobs_workspace(logits):
+    """Bytes of workspace that conduit_token_logprobs needs for these logits."""
+    return _rows_bytes(lib().conduit_token_logprobs_workspace, logits)
+
+
+def conduit_token_logprobs(logits, tokens, logp, lse=None, entropy=None, mask=None, temperature=1.0, workspace=None,
+                           stream=None):
+    """Log-probabilities of the taken tokens, log-normalisers and entropies of logits [B, T, V]."""
+    batch = _batch_shape(tokens, "tokens")
+    x = _rows_ptr(logits, "logits", batch[0])
+    ws, wp, wn = _workspace(workspace, lambda: token_logprobs_workspace(logits), stream)
+    _check(lib().conduit_token_logprobs(C.byref(x), batch[1], batch[2], batch[3],
+                                        _token_ptr(tokens, torch.int32, "tokens", batch),
+                                        _token_ptr(mask, _U8, "mask", batch), float(temperature),
+                                        _token_ptr(logp, torch.float32, "logp", batch),
+                                        _token_ptr(lse, torch.float32, "lse", batch),
+                                        _token_ptr(entropy, torch.float32, "entropy", batch), wp, wn, _stream(stream)))
+
+
+def conduit_token_logprobs_backward(logits, tokens, lse, dlogp, dlogits, entropy=None, dentropy=None, mask=None,
+                                    temperature=1.0, stream=None):
+    """The gradient of conduit_token_logprobs's logits, into dlogits (the logits themselves: in place)."""
+    batch = _batch_shape(tokens, "tokens")
+    x, dx = _rows_ptr(logits, "logits", batch[0]), _rows_ptr(dlogits, "dlogits", batch[0])
+    f = torch.float32
+    _check(lib().conduit_token_logprobs_backward(
+        C.byref(x), batch[1], batch[2], batch[3], _token_ptr(tokens, torch.int32, "tokens", batch),
+        _token_ptr(mask, _U8, "mask", batch), float(temperature), _token_ptr(lse, f, "lse", batch),
+        _token_ptr(entropy, f, "entropy", batch), _token_ptr(dlogp, f, "dlogp", batch),
+        _token_ptr(dentropy, f, "dentropy", batch), C.byref(dx), _stream(stream)))
+
+
+def policy_opts(reduction="token_mean", **kw):
+    """Options of the policy loss: clip_low, clip_high, dual_clip, kl_coef, entropy_coef, scale, reduction."""
+    o = PolicyOpts()
+    lib().conduit_policy_opts_default(C.byref(o))
+    o.reduction = REDUCTIONS[reduction]
+    for k, v in kw.items():
+        if k not in ("clip_low", "clip_high", "dual_clip", "kl_coef", "entropy_coef", "scale"):
+            raise TypeError(f"unknown option {k}")
+        setattr(o, k, float(v))
+    return o
+
+
+POLICY_STATS = ("loss", "policy", "kl", "entropy", "clip_fraction", "old_kl", "ratio", "tokens")
+PREFERENCE_STATS = ("loss", "accuracy", "margin", "tokens")
+
+
+def policy_loss_workspace(B, T):
+    """Bytes of workspace that conduit_policy_loss needs for B sequences of T tokens."""
+    n = C.c_uint64()
+    _check(lib().conduit_policy_loss_workspace(int(B), int(T), C.byref(n)))
+    return n.value
+
+
+def conduit_policy_loss(opts, logp, adv, stats, dlogp=None, old_logp=None, ref_logp=None, entropy=None, dentropy=None,
+                        mask=None, workspace=None, stream=None):
+    """The clipped policy loss with its KL term and entropy bonus: stats (POLICY_STATS) and gradients."""
+    batch = _batch_shape(logp, "logp")
+    f = torch.float32
+    ws, wp, wn = _workspace(workspace, lambda: policy_loss_workspace(batch[1], batch[2]), stream)
+    _check(lib().conduit_policy_loss(
+        C.byref(opts), batch[1], batch[2], batch[3], _token_ptr(logp, f, "logp", batch),
+        _token_ptr(old_logp, f, "old_logp", batch), _token_ptr(ref_logp, f, "ref_logp", batch),
+        _token_ptr(adv, f, "adv", batch), _token_ptr(entropy, f, "entropy", batch),
+        _token_ptr(mask, _U8, "mask", batch), _ptr(stats, f, "stats", numel=8), _token_ptr(dlogp, f, "dlogp", batch),
+        _token_ptr(dentropy, f, "dentropy", batch), wp, wn, _stream(stream)))
+
+
+def policy_loss_logits_workspace(logits):
+    """Bytes of workspace that conduit_policy_loss_logits needs for these logits."""
+    return _rows_bytes(lib().conduit_policy_loss_logits_workspace, logits)
+
+
+def conduit_policy_loss_logits(opts, logits, tokens, adv, stats, dlogits, logp, entropy, old_logp=None, ref_logp=None,
+                               mask=None, temperature=1.0, workspace=None, stream=None):
+    """The policy loss from logits [B, T, V] to their gradient dlogits (the logits themselves: in place)."""
+    batch = _batch_shape(tokens, "tokens")
+    x, dx = _rows_ptr(logits, "logits", batch[0]), _rows_ptr(dlogits, "dlogits", batch[0])
+    f = torch.float32
+    ws, wp, wn = _workspace(workspace, lambda: policy_loss_logits_workspace(logits), stream)
+    _check(lib().conduit_policy_loss_logits(
+        C.byref(opts), C.byref(x), batch[1], batch[2], batch[3], _token_ptr(tokens, torch.int32, "tokens", batch),
+        _token_ptr(old_logp, f, "old_logp", batch), _token_ptr(ref_logp, f, "ref_logp", batch),
+        _token_ptr(adv, f, "adv", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
+        _token_ptr(logp, f, "logp", batch), _token_ptr(entropy, f, "entropy", batch),
+        _ptr(stats, f, "stats", numel=8), C.byref(dx), wp, wn, _stream(stream)))
+
+
+def preference_opts(loss="sigmoid", beta=0.1, label_smoothing=0.0, scale=1.0, length_norm=False):
+    """Options of the preference loss."""
+    o = PreferenceOpts()
+    o.beta, o.label_smoothing, o.scale = float(beta), float(label_smoothing), float(scale)
+    o.loss, o.length_norm = PREFERENCE_LOSSES[loss], int(bool(length_norm))
+    return o
+
+
+def preference_loss_workspace(P, T):
+    """Bytes of workspace that conduit_preference_loss needs for P pairs of sequences of T tokens."""
+    n = C.c_uint64()
+    _check(lib().conduit_preference_loss_workspace(int(P), int(T), C.byref(n)))
+    return n.value
+
+
+def conduit_preference_loss(opts, logp, loss, stats, dlogp=None, ref_logp=None, mask=None, chosen=None, rejected=None,
+                            workspace=None, stream=None):
+    """The preference loss over pairs (rows i and P + i of [2 P, T]): per pair, stats (PREFERENCE_STATS), gradient."""
+    batch = _batch_shape(logp, "logp")
+    if logp.dim() != 2 or batch[1] % 2:
+        raise ValueError("logp must be [2 P, T]: the chosen answers, then the rejected ones")
+    P, f = batch[1] // 2, torch.float32
+    ws, wp, wn = _workspace(workspace, lambda: preference_loss_workspace(P, batch[2]), stream)
+    _check(lib().conduit_preference_loss(
+        C.byref(opts), P, batch[2], batch[3], _token_ptr(logp, f, "logp", batch),
+        _token_ptr(ref_logp, f, "ref_logp", batch), _token_ptr(mask, _U8, "mask", batch),
+        _ptr(loss, f, "loss", numel=P), _ptr(chosen, f, "chosen", numel=P), _ptr(rejected, f, "rejected", numel=P),
+        _ptr(stats, f, "stats", numel=4), _token_ptr(dlogp, f, "dlogp", batch), wp, wn, _stream(stream)))
+
+
 def conduit_buffer_get_info(handle):
     return _info(handle)
 

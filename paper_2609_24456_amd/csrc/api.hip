@@ -87,6 +87,7 @@ const char* kErrText[kErrKinds] = {
     "GAE segment never published by its workgroup (GAE calls overlapping on one GPU?)",
     "sum-tree descent found no child",
     "ragged ingest offsets decreasing or outside [0, src_elems]",
+    "token outside [0, V)",
 };
 
 // Returns ESTATE if any flag of `slot` is set (no synchronisation).
@@ -115,6 +116,16 @@ conduit_status standalone_flags() {
     }
     return check_flags(0);
 }
+
+}  // namespace
+
+conduit_status conduit::standalone_error_words(uint32_t** err) {
+    const conduit_status st = standalone_flags();
+    if (st == CONDUIT_OK) *err = err_words(0);
+    return st;
+}
+
+namespace {
 
 struct DeviceGuard {
     int prev = -1;

@@ -25,7 +25,8 @@ enum ErrKind : int {
     ERR_GAE_WAIT = 5,       // split GAE: a later segment never published (overlapping calls)
     ERR_DESCENT = 6,        // tree descent found no child (never expected)
     ERR_OFFSETS = 7,        // ragged ingest offsets decreasing or outside [0, src_elems]
-    kErrKinds = 8,
+    ERR_TOKEN = 8,          // token outside [0, V) in a loss call
+    kErrKinds = 9,
 };
 
 // Small device-resident state of one buffer.
@@ -484,6 +485,8 @@ struct GatherArgs {
 
 // record `msg` as the calling thread's last error and return `s`
 conduit_status report_error(conduit_status s, const char* msg);
+// the stand-alone calls' sticky error words; ESTATE (reported) if one is set
+conduit_status standalone_error_words(uint32_t** err);
 
 // what the host code outside api.hip needs to know of a buffer's layout
 struct BufferGeometry {

@@ -1,0 +1,691 @@
+// Log-probabilities of the taken tokens from logits, their gradient, and the
+// policy loss from logits to the logits' gradient in one pass over them
+// (conduit_token_logprobs, _backward, conduit_policy_loss_logits).
+//
+// With d_j = c (x_j - max x), c = log2(e) / temperature, S = sum_j 2^d_j and
+// U = sum_j 2^d_j d_j, in fp32:
+//     lse = max x / temperature + ln2 log2 S,   logp = ln2 (d_a - log2 S),
+//     entropy = ln2 (log2 S - U / S),           p_j = 2^d_j / S,
+//     dx_j = (g ([j = a] - p_j) - h p_j (log p_j + entropy)) / temperature
+// for gradients g of logp and h of the entropy.  The maximum goes before the
+// scale: d_j then has two roundings of its own size however large the logits
+// are, and a row at the type's lowest value is as good as any other.  A choice
+// at -inf has no weight; a row of nothing else has logp = lse = -inf, entropy 0
+// and gradient 0.
+//
+// Each lane keeps its own running maximum, sum and weighted sum over the
+// elements it loads (rescaled when the maximum grows), and the lanes are joined
+// once a row, so a row costs one pass and one barrier.  The loss kernel keeps
+// the row's vectors in registers between the two uses, so that its logits cross
+// HBM once in each direction.
+#include <type_traits>
+
+#include "loss_dev.h"
+
+namespace conduit {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+enum LogitsMode { LOGPROBS, LOSS };
+
+constexpr float kNone = -INFINITY;
+constexpr float kFloor = -1024.0f;  // 2^d is 0 below; keeps 0 * d from being NaN at d = -inf
+
+template <bool BF16>
+struct Elem;
+template <>
+struct Elem<true> {
+    using T = uint16_t;
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float one(T x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+    static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[kPer]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __builtin_bit_cast(float, v[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ T round(float x) { return __builtin_bit_cast(T, (__bf16)x); }
+    static __device__ __forceinline__ u32x4 pack(const float (&x)[kPer]) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (uint32_t)round(x[2 * i]) | (uint32_t)round(x[2 * i + 1]) << 16;
+        return v;
+    }
+};
+template <>
+struct Elem<false> {
+    using T = float;
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ float one(T x) { return x; }
+    static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[kPer]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = v[i];  // (a value: bit_cast of a vector's element as an lvalue reads element 0)
+            x[i] = __builtin_bit_cast(float, w);
+        }
+    }
+    static __device__ __forceinline__ T round(float x) { return x; }
+    static __device__ __forceinline__ u32x4 pack(const float (&x)[kPer]) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, x[i]);
+        return v;
+    }
+};
+
+// 16-byte accesses at the elements' own alignment (rows of any width start anywhere)
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* p) {
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, u32x4 v) {
+    __builtin_memcpy(p, &v, 16);
+}
+
+// Running statistics of a part of a row: m = max x, s = sum 2^d, u = sum 2^d d
+// with d = c (x - m).
+struct Stat {
+    float m, s, u;
+};
+
+__device__ __forceinline__ Stat no_stat() { return Stat{kNone, 0.0f, 0.0f}; }
+
+__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float c) {
+    Stat r;
+    r.m = a.m > b.m ? a.m : b.m;
+    // equal maxima, -inf ones among them, have no distance
+    const float da = a.m == r.m ? 0.0f : (a.m - r.m) * c, db = b.m == r.m ? 0.0f : (b.m - r.m) * c;
+    const float ea = exp2_fast(da), eb = exp2_fast(db);
+    const float sa = a.s * ea, sb = b.s * eb;
+    r.s = sa + sb;
+    r.u = fmaf(a.u, ea, sa * fmaxf(da, kFloor)) + fmaf(b.u, eb, sb * fmaxf(db, kFloor));
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ float top_of(const float (&x)[N], float top) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
+    return top;
+}
+
+// the running maximum becomes at least `top`
+__device__ __forceinline__ void raise(Stat& st, float top, float c) {
+    if (top > st.m) {
+        const float d = (st.m - top) * c, e = exp2_fast(d);
+        st.u = fmaf(st.s, fmaxf(d, kFloor), st.u) * e;
+        st.s *= e;
+        st.m = top;
+    }
+}
+
+// elements that are no larger than the running maximum
+template <int N>
+__device__ __forceinline__ void add(Stat& st, const float (&x)[N], float c) {
+    const float base = st.m == kNone ? 0.0f : st.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float d = (x[i] - base) * c, e = exp2_fast(d);
+        st.s += e;
+        st.u = fmaf(e, fmaxf(d, kFloor), st.u);
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void accumulate(Stat& st, const float (&x)[N], float c) {
+    raise(st, top_of(x, kNone), c);
+    add(st, x, c);
+}
+
+// keeps a vector packed: without it the unpacked halves of one use would be kept
+// in registers for the next
+__device__ __forceinline__ u32x4 again(u32x4 v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// K vectors of a lane
+template <bool BF16, int K>
+__device__ __forceinline__ void accumulate_tile(Stat& st, const u32x4 (&v)[K], float c) {
+    using E = Elem<BF16>;
+    float top = kNone;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(v[k], f);
+        top = top_of(f, top);
+    }
+    raise(st, top, c);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(again(v[k]), f);
+        add(st, f, c);
+    }
+}
+
+__device__ __forceinline__ Stat shfl_xor(const Stat& a, int d) {
+    return Stat{__shfl_xor(a.m, d, kWave), __shfl_xor(a.s, d, kWave), __shfl_xor(a.u, d, kWave)};
+}
+
+template <int LANES>
+__device__ __forceinline__ Stat join_lanes(Stat s, float c) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) s = join(s, shfl_xor(s, d), c);
+    return s;
+}
+
+// joined over WAVES wavefronts of a workgroup, in every thread
+template <int WAVES>
+__device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
+    s = join_lanes<kWave>(s, c);
+    if constexpr (WAVES == 1) return s;
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = s;
+    __syncthreads();
+    Stat r = lds[lane_id() % WAVES];
+    return join_lanes<WAVES>(r, c);
+}
+
+// what a row's statistics say
+struct RowValues {
+    float base;     // m, or 0 in a row without weight
+    float inv_s;    // 1 / S, 0 in a row without weight
+    float log2_s;
+    float lse, entropy, logp, one_minus_p;
+};
+
+__device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float c, float inv_t) {
+    RowValues r;
+    if (st.s == 0.0f) {
+        r.base = r.inv_s = r.log2_s = r.entropy = r.one_minus_p = 0.0f;
+        r.lse = r.logp = kNone;
+        return r;
+    }
+    r.base = st.m;
+    r.inv_s = 1.0f / st.s;
+    r.log2_s = log2_fast(st.s);
+    r.lse = fmaf(st.m, inv_t, r.log2_s * kLn2);
+    r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
+    r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
+    r.one_minus_p = -expm1f(r.logp);
+    return r;
+}
+
+// the gradient of one logit: d = c (x - base)
+struct GradCoef {
+    float gp;    // -g / (temperature S)
+    float hp;    // -h / (temperature S)
+    float off;   // entropy - ln2 log2 S
+};
+
+template <bool ENT>
+__device__ __forceinline__ float logit_gradient(const GradCoef& k, float x, float c, float base) {
+    const float d = (x - base) * c, e = exp2_fast(d);
+    if constexpr (!ENT) return k.gp * e;
+    return e * fmaf(k.hp, fmaf(fmaxf(d, kFloor), kLn2, k.off), k.gp);
+}
+
+// the loss's part of a row: gradients of its log-probability and entropy
+struct RowGrad {
+    float g = 0.0f, h = 0.0f;
+};
+
+__device__ __forceinline__ RowGrad row_loss(const PolicyArgs& p, int64_t at, uint32_t b, float logp, TokenLoss* out,
+                                            double* weight) {
+    uint32_t tokens = (uint32_t)(p.shape.B * p.shape.T), rows = (uint32_t)p.shape.B, row = (uint32_t)p.shape.T;
+    if (p.mask) {
+        tokens = p.head->tokens;
+        rows = p.head->rows;
+        if (p.o.reduction == CONDUIT_SEQUENCE_MEAN) row = p.row_count[b];
+    }
+    const double w = token_weight(p.o, tokens, rows, row);
+    const TokenLoss t = policy_token(p.o, logp, p.old_logp != nullptr, p.old_logp ? p.old_logp[at] : 0.0f,
+                                     p.ref_logp != nullptr, p.ref_logp ? p.ref_logp[at] : 0.0f, p.adv[at]);
+    const float wf = (float)(w * p.o.scale);
+    if (out) {
+        *out = t;
+        *weight = w;
+    }
+    return RowGrad{wf * t.slope, -p.o.ent * wf};
+}
+
+__device__ __forceinline__ bool token_ok(const LogitsArgs& a, int32_t tok) {
+    if (tok >= 0 && tok < a.V) return true;
+    flag_error(a.err, ERR_TOKEN);
+    return false;
+}
+
+// ---------------------------------------------------------------------------
+// short rows: LANES lanes a row, up to E elements a lane
+// ---------------------------------------------------------------------------
+constexpr int kShortThreads = 256;
+constexpr int kShortElems = 8;
+
+template <bool BF16, int MODE, int LANES>
+__global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, PolicyArgs p, bool counted) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kRows = kShortThreads / LANES;
+    __shared__ double lds[MODE == LOSS ? kPolicySums * kShortThreads / kWave : 1];
+    const int l = threadIdx.x % LANES;
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    PolicySums sums;
+    for (uint32_t n = blockIdx.x * kRows + threadIdx.x / LANES; n < n_rows; n += gridDim.x * kRows) {
+        const int64_t at = a.shape.at(n);
+        const bool on = !a.mask || a.mask[at];
+        const int32_t tok = on ? a.tokens[at] : 0;
+        const bool ok = on && (l != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
+        const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+        float v[kShortElems];
+        RowValues r;
+        if (ok) {
+            float xa = E::one(x[tok]);
+#pragma unroll
+            for (int i = 0; i < kShortElems; ++i) v[i] = l + i * LANES < a.V ? E::one(x[l + i * LANES]) : kNone;
+            Stat st = no_stat();
+            accumulate(st, v, a.c);
+            r = row_values(join_lanes<LANES>(st, a.c), xa, a.c, a.inv_t);
+        }
+        if (l == 0) {
+            if (a.logp) a.logp[at] = ok ? r.logp : 0.0f;
+            if (a.lse) a.lse[at] = ok ? r.lse : 0.0f;
+            if (a.entropy) a.entropy[at] = ok ? r.entropy : 0.0f;
+        }
+        if constexpr (MODE == LOSS) {
+            T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
+            RowGrad rg;
+            if (ok) {
+                TokenLoss t;
+                double w;
+                rg = row_loss(p, at, div31(n, a.shape.by_T), r.logp, &t, &w);
+                if (l == 0) sums.add(w, t, r.entropy);
+            }
+            const GradCoef k{ok ? -rg.g * a.inv_t * r.inv_s : 0.0f, ok ? -rg.h * a.inv_t * r.inv_s : 0.0f,
+                             ok ? r.entropy - kLn2 * r.log2_s : 0.0f};
+#pragma unroll
+            for (int i = 0; i < kShortElems; ++i) {
+                const int j = l + i * LANES;
+                if (j >= a.V) break;
+                float d = 0.0f;
+                if (ok && r.inv_s != 0.0f) {
+                    if (j == tok)
+                        d = a.inv_t * (rg.g * r.one_minus_p) +
+                            (rg.h != 0.0f ? logit_gradient<true>(GradCoef{0.0f, k.hp, k.off}, v[i], a.c, r.base) : 0.0f);
+                    else if (rg.h != 0.0f)
+                        d = logit_gradient<true>(k, v[i], a.c, r.base);
+                    else
+                        d = logit_gradient<false>(k, v[i], a.c, r.base);
+                }
+                dx[j] = E::round(d);
+            }
+        }
+    }
+    if constexpr (MODE == LOSS)
+        finish_policy<kShortThreads>(p, sums, p.mask ? p.head->tokens : n_rows, counted, lds);
+}
+
+// ---------------------------------------------------------------------------
+// longer rows: WAVES wavefronts a row, K vectors a lane in registers
+// ---------------------------------------------------------------------------
+template <bool BF16, int MODE, int WAVES, int K>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(LogitsArgs a, PolicyArgs p) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    constexpr int NT = WAVES * kWave;
+    constexpr int kTile = NT * K;  // vectors
+    __shared__ Stat lds[WAVES];
+    uint32_t n = blockIdx.x;
+    if constexpr (WAVES == 1) {
+        n = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    }
+    const uint32_t tid = threadIdx.x % NT;
+    const int64_t at = a.shape.at(n);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const bool on = !a.mask || a.mask[at];
+    const int32_t tok = on ? a.tokens[at] : 0;
+    const bool ok = on && (tid != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
+    T* dx = MODE == LOSS ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
+    if (!ok) {
+        if (tid == 0) {
+            if (a.logp) a.logp[at] = 0.0f;
+            if (a.lse) a.lse[at] = 0.0f;
+            if (a.entropy) a.entropy[at] = 0.0f;
+        }
+        if constexpr (MODE == LOSS) {
+            for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
+        }
+        return;
+    }
+    const float xa = E::one(x[tok]);
+    const float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
+    Stat st = no_stat();
+    u32x4 v[K];
+    const u32x4 none = BF16 ? u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}
+                            : u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+    // from the last tile to the first, which then stays in registers
+    for (int32_t base = nv > 0 ? (int32_t)((nv - 1) / kTile * kTile) : 0; base >= 0; base -= kTile) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const uint32_t i = base + k * NT + tid;
+            v[k] = i < nv ? load16(x + (size_t)i * kPer) : none;
+        }
+        accumulate_tile<BF16>(st, v, a.c);
+    }
+    {
+        const float f[1] = {xt};
+        accumulate(st, f, a.c);
+    }
+    const RowValues r = row_values(join_block<WAVES>(st, lds, a.c), xa, a.c, a.inv_t);
+    if (tid == 0) {
+        if (a.logp) a.logp[at] = r.logp;
+        if (a.lse) a.lse[at] = r.lse;
+        if (a.entropy) a.entropy[at] = r.entropy;
+    }
+    if constexpr (MODE == LOSS) {
+        const RowGrad rg = row_loss(p, at, div31(n, a.shape.by_T), r.logp, nullptr, nullptr);
+        const GradCoef k{-rg.g * a.inv_t * r.inv_s, -rg.h * a.inv_t * r.inv_s, r.entropy - kLn2 * r.log2_s};
+        const bool empty = r.inv_s == 0.0f;
+        auto write = [&](auto ent) {
+            constexpr bool ENT = decltype(ent)::value;
+            auto vector = [&](uint32_t i, u32x4 raw) {
+                float f[kPer];
+                E::unpack(raw, f);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) f[j] = empty ? 0.0f : logit_gradient<ENT>(k, f[j], a.c, r.base);
+                store16(dx + (size_t)i * kPer, E::pack(f));
+            };
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const uint32_t i = q * NT + tid;
+                if (i < nv) vector(i, again(v[q]));
+            }
+            for (uint32_t i = kTile + tid; i < nv; i += NT) vector(i, load16(x + (size_t)i * kPer));
+            if (tid < tail) dx[nv * kPer + tid] = E::round(empty ? 0.0f : logit_gradient<ENT>(k, xt, a.c, r.base));
+            // the taken token's own, by the lane that wrote its vector
+            const uint32_t i = (uint32_t)tok / kPer;
+            if (i < nv ? tid == i % NT : tid == (uint32_t)tok - nv * kPer) {
+                float d = a.inv_t * (rg.g * r.one_minus_p);
+                if constexpr (ENT) d += logit_gradient<true>(GradCoef{0.0f, k.hp, k.off}, xa, a.c, r.base);
+                dx[tok] = E::round(empty ? 0.0f : d);
+            }
+        };
+        if (rg.h != 0.0f) write(std::true_type{});
+        else write(std::false_type{});
+    }
+}
+
+// ---------------------------------------------------------------------------
+// few long rows: parts of rows, joined by the last workgroup of each row
+// ---------------------------------------------------------------------------
+constexpr int kPartThreads = 512;
+constexpr int kPartK = 8;
+
+template <bool BF16>
+__global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    __shared__ Stat lds[kPartThreads / kWave];
+    __shared__ bool s_last;
+    const uint32_t n = blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
+    const int64_t at = a.shape.at(n);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const bool on = !a.mask || a.mask[at];
+    const int32_t tok = on ? a.tokens[at] : 0;
+    const bool ok = on && (tid != 0 || part != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
+    if (!ok) {
+        if (part == 0 && tid == 0) {
+            if (a.logp) a.logp[at] = 0.0f;
+            if (a.lse) a.lse[at] = 0.0f;
+            if (a.entropy) a.entropy[at] = 0.0f;
+        }
+        return;
+    }
+    const uint32_t per = (nv + a.parts - 1) / a.parts, lo = part * per, hi = lo + per < nv ? lo + per : nv;
+    const u32x4 none = BF16 ? u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}
+                            : u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+    Stat st = no_stat();
+    for (uint32_t base = lo; base < hi; base += kPartThreads * kPartK) {
+        u32x4 v[kPartK];
+#pragma unroll
+        for (int k = 0; k < kPartK; ++k) {
+            const uint32_t i = base + k * kPartThreads + tid;
+            v[k] = i < hi ? load16(x + (size_t)i * kPer) : none;
+        }
+        accumulate_tile<BF16>(st, v, a.c);
+    }
+    if (part == 0 && tid < tail) {
+        const float f[1] = {E::one(x[nv * kPer + tid])};
+        accumulate(st, f, a.c);
+    }
+    st = join_block<kPartThreads / kWave>(st, lds, a.c);
+    float* mine = a.part + 3 * ((int64_t)n * a.parts + part);
+    if (tid == 0) {
+        __hip_atomic_store(mine, st.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 1, st.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 2, st.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // acknowledged before the ticket is drawn
+        const uint32_t t = __hip_atomic_fetch_add(a.row_ticket + n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = t == (uint32_t)a.parts - 1;
+        if (s_last) __hip_atomic_store(a.row_ticket + n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!s_last || tid >= (uint32_t)kWave) return;
+    Stat all = no_stat();
+    for (int k = tid; k < a.parts; k += kWave) {
+        const float* q = a.part + 3 * ((int64_t)n * a.parts + k);
+        Stat o;
+        o.m = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        o.s = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        o.u = __hip_atomic_load(q + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        all = join(all, o, a.c);
+    }
+    const RowValues r = row_values(join_lanes<kWave>(all, a.c), E::one(x[tok]), a.c, a.inv_t);
+    if (tid == 0) {
+        if (a.logp) a.logp[at] = r.logp;
+        if (a.lse) a.lse[at] = r.lse;
+        if (a.entropy) a.entropy[at] = r.entropy;
+        if (a.lse_n) a.lse_n[n] = r.lse;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the gradient of the logits from the row's saved log-normaliser: wavefronts
+// take parts of kGradK vectors a lane of a row
+// ---------------------------------------------------------------------------
+constexpr int kGradThreads = 256;
+constexpr int kGradK = 4;
+
+template <bool BF16, bool POLICY>
+__global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, PolicyArgs p, uint32_t items,
+                                                                uint32_t per_row, Div31 by_row) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    const uint32_t item = blockIdx.x * (kGradThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (item >= items) return;
+    const uint32_t n = div31(item, by_row), part = item - n * per_row, lane = lane_id();
+    const int64_t at = a.shape.at(n);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const bool on = !a.mask || a.mask[at];
+    const int32_t tok = on ? a.tokens[at] : 0;
+    const bool ok = on && (lane != 0 || part != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
+    const uint32_t base = part * kGradK * kWave + lane;
+    const bool mine = part == 0 && lane < tail;  // the elements after the last vector
+    float lse = 0.0f;
+    RowGrad rg;
+    float entropy = 0.0f;
+    if (ok) {
+        lse = POLICY ? a.lse_n[n] : a.lse_in[at];
+        if constexpr (POLICY) {  // (lse_n, logp and entropy_in: from the launch before)
+            rg = row_loss(p, at, div31(n, a.shape.by_T), a.logp[at], nullptr, nullptr);
+        } else {
+            rg.g = a.g ? a.g[at] : 0.0f;
+            rg.h = a.h ? a.h[at] : 0.0f;
+        }
+        if (a.entropy_in) entropy = a.entropy_in[at];
+    }
+    if (!ok || lse == kNone) {  // nothing counts, or a row without weight
+#pragma unroll
+        for (int k = 0; k < kGradK; ++k) {
+            const uint32_t i = base + k * kWave;
+            if (i < nv) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+        }
+        if (mine) dx[nv * kPer + lane] = E::round(0.0f);
+        return;
+    }
+    u32x4 v[kGradK];
+#pragma unroll
+    for (int k = 0; k < kGradK; ++k) {
+        const uint32_t i = base + k * kWave;
+        v[k] = i < nv ? load16(x + (size_t)i * kPer) : u32x4{0, 0, 0, 0};
+    }
+    const float xt = mine ? E::one(x[nv * kPer + lane]) : 0.0f;
+    const float xa = E::one(x[tok]);
+    auto one = [&](float f, float g, auto ent) {
+        const float q = fmaf(f, a.inv_t, -lse), e = exp2_fast(q * kLog2e);  // log p_j, p_j
+        if constexpr (!decltype(ent)::value) return -g * a.inv_t * e;
+        return -a.inv_t * e * fmaf(rg.h, fmaxf(q, kFloor) + entropy, g);
+    };
+    auto write = [&](auto ent) {
+#pragma unroll
+        for (int k = 0; k < kGradK; ++k) {
+            const uint32_t i = base + k * kWave;
+            float f[kPer];
+            E::unpack(v[k], f);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) f[j] = one(f[j], rg.g, ent);
+            if (i < nv) store16(dx + (size_t)i * kPer, E::pack(f));
+        }
+        if (mine) dx[nv * kPer + lane] = E::round(one(xt, rg.g, ent));
+        // the taken token's own, by the lane that wrote its vector
+        const uint32_t i = (uint32_t)tok / kPer;
+        const bool holds = i < nv ? i / (kGradK * kWave) == part && i % kWave == lane
+                                  : part == 0 && (uint32_t)tok - nv * kPer == lane;
+        if (holds) {
+            float d = a.inv_t * (rg.g * -expm1f(fmaf(xa, a.inv_t, -lse)));
+            if constexpr (decltype(ent)::value) d += one(xa, 0.0f, ent);
+            dx[tok] = E::round(d);
+        }
+    };
+    if (rg.h != 0.0f) write(std::true_type{});
+    else write(std::false_type{});
+}
+
+template <bool BF16, bool POLICY>
+hipError_t launch_gradient(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+    const int64_t nv = a.V / Elem<BF16>::kPer;
+    const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
+    const int64_t rows = a.shape.B * a.shape.T;
+    // one launch takes fewer than 2^31 parts (the division's range)
+    const int64_t items = rows * per_row;
+    if (items >= 1ll << 31) return hipErrorInvalidValue;
+    const unsigned grid = (unsigned)((items + kGradThreads / kWave - 1) / (kGradThreads / kWave));
+    hipLaunchKernelGGL((k_rows_gradient<BF16, POLICY>), dim3(grid), dim3(kGradThreads), 0, s, a, p, (uint32_t)items,
+                       (uint32_t)per_row, make_div31((uint32_t)per_row));
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// which kernel a row's width takes
+// ---------------------------------------------------------------------------
+template <bool BF16, int MODE>
+hipError_t launch_short(const LogitsArgs& a, const PolicyArgs& p, bool counted, hipStream_t s) {
+    const int64_t rows = a.shape.B * a.shape.T;
+    auto go = [&](auto lanes) {
+        constexpr int LANES = decltype(lanes)::value;
+        const int64_t want = (rows + kShortThreads / LANES - 1) / (kShortThreads / LANES);
+        const int64_t cap = MODE == LOSS ? kPolicyBlocks : 16LL * device_cus();
+        hipLaunchKernelGGL((k_rows_short<BF16, MODE, LANES>), dim3((unsigned)(want < cap ? want : cap)),
+                           dim3(kShortThreads), 0, s, a, p, counted);
+        return hipGetLastError();
+    };
+    if (a.V <= 4 * kShortElems) return go(std::integral_constant<int, 4>{});
+    if (a.V <= 8 * kShortElems) return go(std::integral_constant<int, 8>{});
+    if (a.V <= 16 * kShortElems) return go(std::integral_constant<int, 16>{});
+    if (a.V <= 32 * kShortElems) return go(std::integral_constant<int, 32>{});
+    return go(std::integral_constant<int, 64>{});
+}
+
+constexpr int64_t kShortWidth = 64 * kShortElems;
+
+template <bool BF16, int MODE>
+hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+    const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
+    if (nv <= 8 * kWave)
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p);
+    else if (nv <= 4096)
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), dim3((unsigned)rows), dim3(256), 0, s, a, p);
+    else
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), dim3((unsigned)rows), dim3(1024), 0, s, a, p);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t launch_parts(const LogitsArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL((k_rows_parts<BF16>), dim3((unsigned)a.parts, (unsigned)(a.shape.B * a.shape.T)),
+                       dim3(kPartThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t logprobs(const LogitsArgs& a, hipStream_t s) {
+    if (a.V <= kShortWidth) return launch_short<BF16, LOGPROBS>(a, PolicyArgs{}, false, s);
+    if (a.parts > 1) return launch_parts<BF16>(a, s);
+    return launch_long<BF16, LOGPROBS>(a, PolicyArgs{}, s);
+}
+
+template <bool BF16>
+hipError_t loss_logits(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+    hipError_t e = hipSuccess;
+    if (p.mask) e = launch_token_count(p, s);  // the tokens' weight needs their number
+    if (e != hipSuccess) return e;
+    if (a.V <= kShortWidth) return launch_short<BF16, LOSS>(a, p, p.mask != nullptr, s);
+    if (a.parts > 1) {
+        e = launch_parts<BF16>(a, s);
+        if (e == hipSuccess) e = launch_gradient<BF16, true>(a, p, s);
+    } else {
+        e = launch_long<BF16, LOSS>(a, p, s);
+    }
+    if (e != hipSuccess) return e;
+    return launch_policy_loss(p, p.mask != nullptr, s);
+}
+
+}  // namespace
+
+// Parts of a row: rows are split where the rows alone would leave compute units
+// without a workgroup, into parts of at least two rounds of a workgroup's loads.
+int logits_parts(int64_t rows, int64_t V, bool bf16) {
+    const int64_t cus = device_cus(), nv = V / (bf16 ? 8 : 4);
+    if (V <= kShortWidth || rows >= cus || rows <= 0) return 1;
+    const int64_t want = (2 * cus + rows - 1) / rows, most = nv / (2 * kPartThreads);
+    const int64_t parts = want < most ? want : most;
+    return parts > 1 ? (int)parts : 1;
+}
+
+hipError_t launch_token_logprobs(const LogitsArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? logprobs<true>(a, s) : logprobs<false>(a, s);
+}
+
+hipError_t launch_token_logprobs_backward(const LogitsArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? launch_gradient<true, false>(a, PolicyArgs{}, s) : launch_gradient<false, false>(a, PolicyArgs{}, s);
+}
+
+hipError_t launch_policy_loss_logits(const LogitsArgs& a, const PolicyArgs& p, bool bf16, hipStream_t s) {
+    return bf16 ? loss_logits<true>(a, p, s) : loss_logits<false>(a, p, s);
+}
+
+}  // namespace conduit

@@ -1,0 +1,309 @@
+// Device code and launch arguments shared by the loss kernels (k_logits.hip,
+// k_policy.hip, k_preference.hip, k_head.hip): per-token arrays, the policy
+// loss of one token, reductions in a fixed order.
+#pragma once
+
+#include "common.h"
+
+namespace conduit {
+
+// Every per-token array of a call is [B, T] with rows `stride` elements apart.
+struct TokenShape {
+    int64_t B, T, stride;
+    Div31 by_T;  // of n = b * T + t
+    __device__ __forceinline__ int64_t at(uint32_t n) const {
+        const uint32_t b = div31(n, by_T);
+        return (int64_t)b * stride + (n - b * (uint32_t)T);
+    }
+};
+
+inline TokenShape make_shape(int64_t B, int64_t T, int64_t stride) {
+    return TokenShape{B, T, stride, make_div31((uint32_t)(T > 0 ? T : 1))};
+}
+
+// [B, T] rows of `width` elements: row (b, t) starts at b * stride_b + t * stride_t
+struct RowsView {
+    void* data;
+    int64_t stride_b, stride_t;
+    __device__ __forceinline__ int64_t at(uint32_t n, const TokenShape& s) const {
+        const uint32_t b = div31(n, s.by_T);
+        return (int64_t)b * stride_b + (int64_t)(n - b * (uint32_t)s.T) * stride_t;
+    }
+};
+
+// The options of the policy loss as the kernels take them.
+struct PolicyTerms {
+    float lo, hi;    // 1 - clip_low, 1 + clip_high
+    float dual;      // 0: no dual clip
+    float kl, ent;
+    int32_t reduction;
+    double scale;
+};
+
+// Head of a workspace: counters that every call finds and leaves at zero.
+struct WorkspaceHead {
+    uint32_t ticket;
+    uint32_t tokens;  // tokens that count
+    uint32_t rows;    // rows (sequences) with at least one
+    uint32_t pad[61];
+};
+static_assert(sizeof(WorkspaceHead) == 256, "workspace head");
+
+constexpr int kPolicySums = 6;     // weighted loss, KL and entropy; clipped, log ratio and ratio
+constexpr int kPolicyBlocks = 512; // most workgroups that a sum over the tokens is spread over
+
+struct PolicyArgs {
+    TokenShape shape;
+    PolicyTerms o;
+    const float* logp;
+    const float* old_logp;
+    const float* ref_logp;
+    const float* adv;
+    const float* entropy;
+    const uint8_t* mask;
+    const int32_t* tokens;  // with V: tokens outside [0, V) add nothing (NULL: every token is valid)
+    int64_t V;
+    float* stats;
+    float* dlogp;
+    float* dentropy;
+    WorkspaceHead* head;
+    uint32_t* row_count;  // [B] counted tokens, with the mean over rows
+    double* partial;      // [kPolicyBlocks][kPolicySums]
+};
+
+struct LogitsArgs {
+    TokenShape shape;
+    RowsView x, dx;
+    int64_t V;
+    float c;      // log2(e) / temperature
+    float inv_t;  // 1 / temperature
+    const int32_t* tokens;
+    const uint8_t* mask;
+    float* logp;
+    float* lse;
+    float* entropy;
+    const float* lse_in;
+    const float* entropy_in;
+    const float* g;  // gradient of logp
+    const float* h;  // gradient of the entropy
+    uint32_t* err;
+    // split rows: (maximum, sum, weighted sum) of each part of a row, and a ticket a row
+    float* part;
+    uint32_t* row_ticket;
+    int32_t parts;
+    float* lse_n;  // lse by token number, for the gradient launch of the split loss (or NULL)
+};
+
+hipError_t launch_token_count(const PolicyArgs& a, hipStream_t s);
+hipError_t launch_policy_loss(const PolicyArgs& a, bool counted, hipStream_t s);
+hipError_t launch_token_logprobs(const LogitsArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_token_logprobs_backward(const LogitsArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_policy_loss_logits(const LogitsArgs& a, const PolicyArgs& p, bool bf16, hipStream_t s);
+int logits_parts(int64_t rows, int64_t V, bool bf16);
+
+struct PreferenceArgs {
+    int64_t P, T, stride;
+    double beta, smoothing, scale;
+    int32_t squared, length_norm;
+    const float* logp;
+    const float* ref;
+    const uint8_t* mask;
+    float* loss;
+    float* chosen;
+    float* rejected;
+    float* stats;
+    float* dlogp;
+    WorkspaceHead* head;
+    double* pair;     // [P][4]: loss, u, margin > 0, tokens
+    double* partial;  // [2 P][parts][2]: sum, tokens
+    int32_t parts;
+};
+
+hipError_t launch_preference_loss(const PreferenceArgs& a, hipStream_t s);
+int preference_parts(int64_t P, int64_t T);
+
+// ---------------------------------------------------------------------------
+// constants and small functions
+// ---------------------------------------------------------------------------
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// exp(x) - 1 - x, x^2 / 2 at small x: the series up to x^9 below |x| = 1/2 (the
+// first term left out is x^8 * 2 / 10! of the whole, under 3e-9), where the
+// difference would cancel
+__device__ __forceinline__ float exp_remainder(float x, float em1) {
+    if (fabsf(x) >= 0.5f) return em1 - x;
+    float p = 1.0f / 362880.0f;
+    p = fmaf(p, x, 1.0f / 40320.0f);
+    p = fmaf(p, x, 1.0f / 5040.0f);
+    p = fmaf(p, x, 1.0f / 720.0f);
+    p = fmaf(p, x, 1.0f / 120.0f);
+    p = fmaf(p, x, 1.0f / 24.0f);
+    p = fmaf(p, x, 1.0f / 6.0f);
+    p = fmaf(p, x, 0.5f);
+    return p * x * x;
+}
+
+// ---------------------------------------------------------------------------
+// the policy loss of one token
+// ---------------------------------------------------------------------------
+struct TokenLoss {
+    float term, kl, ratio, log_ratio;
+    float slope;  // derivative of term + kl_coef * kl with respect to logp
+    float held;   // 1 if the clip or the dual clip decides
+};
+
+// r = exp(logp - old); term = max(-A r, -A clip(r, lo, hi)), and where A < 0
+// at most -A dual; kl = exp(ref - logp) - (ref - logp) - 1.  A NaN stays one
+// (no fmax, which would drop it); an advantage of 0 has no term however large
+// the ratio.  The old log-probability may be absent (r = 1: the policy that
+// acted is the one that learns), and so may the reference (kl = 0).
+__device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float logp, bool has_old, float old,
+                                                  bool has_ref, float ref, float adv) {
+    TokenLoss r;
+    r.log_ratio = has_old ? logp - old : 0.0f;
+    r.ratio = has_old ? expf(r.log_ratio) : 1.0f;
+    const float plain = adv == 0.0f ? 0.0f : -adv * r.ratio;
+    const float kept = r.ratio < o.lo ? o.lo : r.ratio > o.hi ? o.hi : r.ratio;
+    const float bound = -adv * kept;
+    bool held = bound > plain;
+    r.term = held ? bound : plain;
+    if (o.dual > 0.0f && adv < 0.0f && r.term > -adv * o.dual) {
+        r.term = -adv * o.dual;
+        held = true;
+    }
+    r.held = held ? 1.0f : 0.0f;
+    r.slope = held ? 0.0f : plain;
+    r.kl = 0.0f;
+    if (has_ref) {
+        const float x = ref - logp, em1 = expm1f(x);
+        r.kl = exp_remainder(x, em1);
+        if (o.kl != 0.0f) r.slope -= o.kl * em1;
+    }
+    return r;
+}
+
+// weight of a token: of the mean over tokens, of the mean over rows of each
+// row's mean, or 1
+__device__ __forceinline__ double token_weight(const PolicyTerms& o, uint32_t tokens, uint32_t rows, uint32_t row) {
+    if (o.reduction == CONDUIT_SUM) return 1.0;
+    if (o.reduction == CONDUIT_TOKEN_MEAN) return 1.0 / (double)(tokens > 0 ? tokens : 1);
+    return 1.0 / ((double)(rows > 0 ? rows : 1) * (double)(row > 0 ? row : 1));
+}
+
+struct PolicySums {
+    double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
+    __device__ __forceinline__ void add(double w, const TokenLoss& t, float entropy) {
+        v[0] += w * t.term;
+        v[1] += w * t.kl;
+        v[2] += w * entropy;
+        v[3] += t.held;
+        v[4] += t.log_ratio;
+        v[5] += t.ratio;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// reductions in a fixed order
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, kWave);
+    return x;
+}
+
+// sums of N doubles over a workgroup of NT threads, in every thread (every
+// thread takes part; `lds` holds N * NT / 64 doubles and may be reused after
+// the next barrier)
+template <int NT, int N>
+__device__ __forceinline__ void block_sum(double (&x)[N], double* lds) {
+    constexpr int W = NT / kWave;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+    if constexpr (W == 1) return;
+    const int w = threadIdx.x / kWave;
+    if (lane_id() == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[i * W + w] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        double t = 0.0;
+        for (int k = 0; k < W; ++k) t += lds[i * W + k];
+        x[i] = t;
+    }
+    __syncthreads();
+}
+
+// Last arrival of a launch's workgroups: true in every thread of the one that
+// drew the last of `total` tickets.  What thread 0 stored with store_agent
+// before is at the device's point of coherence by then (its stores are waited
+// for before the ticket is drawn), where load_agent reads it, so no fence, and
+// with it no write-back of the L2 under the outputs, is needed.  The ticket is
+// left at 0.
+__device__ __forceinline__ void store_agent(double* p, double v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ double load_agent(const double* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ bool last_block(uint32_t* ticket, uint32_t total) {
+    __shared__ bool s_last;
+    if (threadIdx.x == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores above are acknowledged
+        const uint32_t t = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = t == total - 1;
+        if (s_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return s_last;
+}
+
+// The 8 statistics from the sums over every token.
+__device__ __forceinline__ void write_policy_stats(const PolicyTerms& o, const double* v, uint32_t tokens, float* stats) {
+    const double n = tokens > 0 ? (double)tokens : 1.0;
+    double loss = v[0];
+    if (o.kl != 0.0f) loss += (double)o.kl * v[1];
+    if (o.ent != 0.0f) loss -= (double)o.ent * v[2];
+    stats[0] = (float)(o.scale * loss);
+    stats[1] = (float)v[0];
+    stats[2] = (float)v[1];
+    stats[3] = (float)v[2];
+    stats[4] = (float)(v[3] / n);
+    stats[5] = (float)(-v[4] / n);
+    stats[6] = (float)(v[5] / n);
+    stats[7] = (float)tokens;
+}
+
+// A workgroup's sums into its slot; the last workgroup adds the slots up (each
+// thread some of them, then block_sum: a fixed order), writes the statistics
+// and clears the counters.
+template <int NT>
+__device__ __forceinline__ void finish_policy(const PolicyArgs& a, PolicySums& s, uint32_t tokens, bool counted,
+                                              double* lds) {
+    block_sum<NT, kPolicySums>(s.v, lds);
+    if (gridDim.x == 1) {
+        if (threadIdx.x == 0) write_policy_stats(a.o, s.v, tokens, a.stats);
+    } else {
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < kPolicySums; ++i) store_agent(a.partial + (int64_t)blockIdx.x * kPolicySums + i, s.v[i]);
+        }
+        if (!last_block(&a.head->ticket, gridDim.x)) return;
+        double t[kPolicySums] = {0, 0, 0, 0, 0, 0};
+        for (uint32_t k = threadIdx.x; k < gridDim.x; k += NT) {
+#pragma unroll
+            for (int i = 0; i < kPolicySums; ++i) t[i] += load_agent(a.partial + (int64_t)k * kPolicySums + i);
+        }
+        block_sum<NT, kPolicySums>(t, lds);
+        if (threadIdx.x == 0) write_policy_stats(a.o, t, tokens, a.stats);
+    }
+    if (counted && threadIdx.x == 0) a.head->tokens = a.head->rows = 0;  // for the next call
+}
+
+}  // namespace conduit
