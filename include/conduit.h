@@ -727,6 +727,46 @@ conduit_status conduit_preference_loss(const conduit_preference_opts* opts, int6
                                        float* chosen, float* rejected, float* stats, float* dlogp, void* workspace,
                                        uint64_t workspace_bytes, void* stream);
 
+/*
+ * conduit_token_logprobs where the logits are hidden . weight^T and are never
+ * in memory whole (at 256 x 4096 tokens and 128,000 choices they would be 268
+ * GB): hidden: bf16 rows of H elements for B x T tokens, 1 <= H <= 2^16;
+ * weight: V bf16 rows of H elements, row v at v * weight->stride_t (stride_b is
+ * not used), 1 <= V <= 2^22; B * T <= 2^21.  Products of bf16 on the matrix
+ * cores, summed in fp32.  Rows that are not 16-byte aligned with H a multiple of
+ * 8, and with a mask the counted tokens' hidden rows, are copied into the
+ * workspace first.  The workspace's size depends on the addresses and strides.
+ * Other arguments and the outputs as in conduit_token_logprobs.
+ * Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_head_logprobs_workspace(int64_t B, int64_t T, const conduit_rows* hidden,
+                                               const conduit_rows* weight, int64_t V, uint64_t* bytes);
+conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_rows* weight, int64_t V, int64_t B,
+                                     int64_t T, int64_t stride, const int32_t* tokens, const uint8_t* mask,
+                                     double temperature, float* logp, float* lse, float* entropy, void* workspace,
+                                     uint64_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of conduit_head_logprobs with respect to the hidden states and
+ * the projection, for gradients dlogp and dentropy (either may be NULL) of its
+ * outputs and the lse (and, with dentropy, entropy) that it gave.  The logits
+ * are computed again; their gradient (that of
+ * conduit_token_logprobs_backward) is rounded once to bf16 between the
+ * products, whose sums are fp32.  dhidden: bf16 rows like hidden (0 at masked
+ * tokens); dweight: V bf16 rows; both are overwritten and apart from every
+ * input.  The workspace holds the logits' gradient of up to all choices in both
+ * orders, at most 8 GB of it; more tokens run in chunks of choices.
+ * Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_head_logprobs_backward_workspace(int64_t B, int64_t T, const conduit_rows* hidden,
+                                                        const conduit_rows* weight, int64_t V, uint64_t* bytes);
+conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const conduit_rows* weight, int64_t V,
+                                              int64_t B, int64_t T, int64_t stride, const int32_t* tokens,
+                                              const uint8_t* mask, double temperature, const float* lse,
+                                              const float* entropy, const float* dlogp, const float* dentropy,
+                                              const conduit_rows* dhidden, const conduit_rows* dweight,
+                                              void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------
  * State, introspection, errors
  * ------------------------------------------------------------------------- */

@@ -197,6 +197,10 @@ SIGNATURES = {
     "conduit_preference_opts_default": (None, [P]),
     "conduit_preference_loss_workspace": (ST, [I64, I64, P]),
     "conduit_preference_loss": (ST, [P, I64, I64, I64, P, P, P, P, P, P, P, P, P, C.c_uint64, P]),
+    "conduit_head_logprobs_workspace": (ST, [I64, I64, P, P, I64, P]),
+    "conduit_head_logprobs": (ST, [P, P, I64, I64, I64, I64, P, P, F64, P, P, P, P, C.c_uint64, P]),
+    "conduit_head_logprobs_backward_workspace": (ST, [I64, I64, P, P, I64, P]),
+    "conduit_head_logprobs_backward": (ST, [P, P, I64, I64, I64, I64, P, P, F64, P, P, P, P, P, P, P, C.c_uint64, P]),
     "conduit_run_offpolicy": (ST, [P, P, P, P, P, P, P]),
 }
 

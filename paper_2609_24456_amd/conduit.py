@@ -663,6 +663,65 @@ def conduit_preference_loss(opts, logp, loss, stats, dlogp=None, ref_logp=None, 
         _ptr(stats, f, "stats", numel=4), _token_ptr(dlogp, f, "dlogp", batch), wp, wn, _stream(stream)))
 
 
+def _head_rows(hidden, weight):
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise ValueError("weight must be a [V, H] tensor")
+    if not _on_device(weight):
+        raise ValueError("weight must be on a HIP device")
+    return _rows_struct(hidden, "hidden"), _rows_struct(weight, "weight")
+
+
+def _head_bytes(entry, hidden, weight):
+    x, w = _head_rows(hidden, weight)
+    n = C.c_uint64()
+    B, T = (hidden.shape[0], hidden.shape[1]) if hidden.dim() == 3 else (1, hidden.shape[0])
+    _check(entry(B, T, C.byref(x), C.byref(w), weight.shape[0], C.byref(n)))
+    return n.value
+
+
+def head_logprobs_workspace(hidden, weight):
+    """Bytes of workspace that conduit_head_logprobs needs for these tensors."""
+    return _head_bytes(lib().conduit_head_logprobs_workspace, hidden, weight)
+
+
+def head_logprobs_backward_workspace(hidden, weight):
+    """Bytes of workspace that conduit_head_logprobs_backward needs for these tensors."""
+    return _head_bytes(lib().conduit_head_logprobs_backward_workspace, hidden, weight)
+
+
+def conduit_head_logprobs(hidden, weight, tokens, logp, lse=None, entropy=None, mask=None, temperature=1.0,
+                          workspace=None, stream=None):
+    """conduit_token_logprobs of the logits hidden [B, T, H] . weight [V, H]^T, which are never whole in memory."""
+    batch = _batch_shape(tokens, "tokens")
+    x = _rows_ptr(hidden, "hidden", batch[0])
+    _, w = _head_rows(hidden, weight)
+    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_workspace(hidden, weight), stream)
+    f = torch.float32
+    _check(lib().conduit_head_logprobs(
+        C.byref(x), C.byref(w), weight.shape[0], batch[1], batch[2], batch[3],
+        _token_ptr(tokens, torch.int32, "tokens", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
+        _token_ptr(logp, f, "logp", batch), _token_ptr(lse, f, "lse", batch), _token_ptr(entropy, f, "entropy", batch),
+        wp, wn, _stream(stream)))
+
+
+def conduit_head_logprobs_backward(hidden, weight, tokens, lse, dlogp, dhidden, dweight, entropy=None, dentropy=None,
+                                   mask=None, temperature=1.0, workspace=None, stream=None):
+    """The gradients dhidden and dweight of conduit_head_logprobs."""
+    batch = _batch_shape(tokens, "tokens")
+    x, dx = _rows_ptr(hidden, "hidden", batch[0]), _rows_ptr(dhidden, "dhidden", batch[0])
+    _, w = _head_rows(hidden, weight)
+    if not isinstance(dweight, torch.Tensor) or dweight.shape != weight.shape:
+        raise ValueError("dweight must have the projection's shape")
+    _, dw = _head_rows(hidden, dweight)
+    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_backward_workspace(hidden, weight), stream)
+    f = torch.float32
+    _check(lib().conduit_head_logprobs_backward(
+        C.byref(x), C.byref(w), weight.shape[0], batch[1], batch[2], batch[3],
+        _token_ptr(tokens, torch.int32, "tokens", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
+        _token_ptr(lse, f, "lse", batch), _token_ptr(entropy, f, "entropy", batch), _token_ptr(dlogp, f, "dlogp", batch),
+        _token_ptr(dentropy, f, "dentropy", batch), C.byref(dx), C.byref(dw), wp, wn, _stream(stream)))
+
+
 def conduit_buffer_get_info(handle):
     return _info(handle)
 

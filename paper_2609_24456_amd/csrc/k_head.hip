@@ -1,0 +1,535 @@
+// Log-probabilities of the taken tokens from the last hidden states X and the
+// output projection W, and the gradients of both, without the [tokens, V] logits
+// ever being in memory whole (conduit_head_logprobs, _backward).
+//
+// Forward: logits z = X W^T / temperature are produced 256 x 256 at a time on
+// the matrix cores (gemm_dev.h); each tile leaves every token's maximum, sum and
+// weighted sum over its 256 choices (as in k_logits.hip) and, where the taken
+// token is among them, its score.  A second launch joins a token's tiles.  The
+// tile holds choices as rows and tokens as columns of the product, so that a
+// lane has 32 choices of one token and most of the reduction is its own.
+//
+// Backward: the tiles are produced again, turned into the logits' gradient
+//     d = (g ([j = token] - p_j) - h p_j (log p_j + entropy)) / temperature
+// and rounded once to bf16 (the type of W and X: its relative error, 2^-9 at
+// worst and independent from element to element, is that of the gradients' own
+// rounding), in both orders: [token][choice] and [choice][token].  Then
+//     dX = d W  (split along the choices, parts joined in a fixed order),
+//     dW = d^T X
+// by the same product, with W and X transposed once.  Batches whose d would pass
+// kHeadChunkBytes run in chunks of choices; dX accumulates over them in fp32.
+//
+// Tokens that the mask leaves out take no part: a first launch lists the others
+// in order, and the hidden rows are packed by that list.  Their number stays on
+// the device: grids are sized for all tokens, workgroups beyond return at once.
+#include <type_traits>
+
+#include "gemm_dev.h"
+#include "head_dev.h"
+
+namespace conduit {
+
+namespace {
+
+constexpr int kListThreads = 1024;
+constexpr int kHeadXcds = 8;
+constexpr int kHeadGroup = 8;  // column tiles that neighbours in a launch share
+
+__device__ __forceinline__ int64_t live_tokens(const HeadArgs& a) { return a.count ? (int64_t)*a.count : a.N; }
+
+// The tokens that count, in order: list[k] = token, place[token] = k or -1, and
+// their number.  One workgroup; a lane takes 16 tokens a round.
+__global__ __launch_bounds__(kListThreads) void k_head_list(HeadArgs a) {
+    __shared__ uint32_t s_wave[kListThreads / kWave + 1];
+    constexpr int kPer = 16;
+    uint32_t done = 0;
+    for (int64_t base = 0; base < a.N; base += kListThreads * kPer) {
+        const int64_t n0 = base + (int64_t)threadIdx.x * kPer;
+        uint32_t on = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int64_t n = n0 + i;
+            if (n >= a.N) break;
+            const int64_t at = a.shape.at((uint32_t)n);
+            if (!a.mask[at]) continue;
+            const int32_t tok = a.tokens[at];
+            if (tok >= 0 && tok < a.V) on |= 1u << i;
+            else flag_error(a.err, ERR_TOKEN);
+        }
+        const uint32_t mine = __builtin_popcount(on);
+        uint32_t incl = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t up = __shfl_up(incl, d, kWave);
+            if (lane_id() >= d) incl += up;
+        }
+        if (lane_id() == kWave - 1) s_wave[threadIdx.x / kWave] = incl;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint32_t sum = 0;
+            for (int w = 0; w < kListThreads / kWave; ++w) {
+                const uint32_t c = s_wave[w];
+                s_wave[w] = sum;
+                sum += c;
+            }
+            s_wave[kListThreads / kWave] = sum;
+        }
+        __syncthreads();
+        uint32_t k = done + s_wave[threadIdx.x / kWave] + incl - mine;
+        done += s_wave[kListThreads / kWave];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (n0 + i >= a.N) break;
+            const bool counts = on >> i & 1;
+            a.place[n0 + i] = counts ? (int32_t)k : -1;
+            if (counts) a.list[k++] = (int32_t)(n0 + i);
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.count_out = done;
+}
+
+// dst[k][0..ld) = src row of the k-th token, zeros beyond `width`; with `rows`
+// given, plain rows (the projection's) instead of tokens
+__global__ __launch_bounds__(256) void k_head_pack(HeadArgs a, const uint16_t* src, int64_t src_ld, int64_t width, uint16_t* dst,
+                                                   int64_t ld, int64_t rows, bool tokens) {
+    const int64_t n_rows = tokens ? live_tokens(a) : rows;
+    for (int64_t k = blockIdx.x; k < n_rows; k += gridDim.x) {
+        const uint16_t* x = src + (tokens ? a.x.at((uint32_t)(a.list ? a.list[k] : k), a.shape) : k * src_ld);
+        uint16_t* y = dst + k * ld;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < ld; c += 8 * 256) {
+            u32x4_t v = {0, 0, 0, 0};
+            if (c + 8 <= width) {
+                __builtin_memcpy(&v, x + c, 16);
+            } else {
+                uint16_t e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = c + i < width ? x[c + i] : (uint16_t)0;
+                __builtin_memcpy(&v, e, 16);
+            }
+            *reinterpret_cast<u32x4_t*>(y + c) = v;
+        }
+    }
+}
+
+// dst[c][r] = src[r][c] for 64 x 64 tiles; rows r >= the live tokens (or `rows`)
+// read as zeros, columns r up to dst_ld are written
+__global__ __launch_bounds__(256) void k_head_transpose(HeadArgs a, const uint16_t* src, int64_t src_ld, int64_t rows,
+                                                        int64_t cols, uint16_t* dst, int64_t dst_ld, bool tokens) {
+    __shared__ uint16_t tile[64][64 + 8];
+    const int64_t n_rows = tokens ? live_tokens(a) : rows;
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    if (r0 >= (n_rows + kGemmK - 1) / kGemmK * kGemmK) return;  // nothing reads those columns
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int q = threadIdx.x + i * 256, r = q / 8, c = q % 8 * 8;
+        u32x4_t v = {0, 0, 0, 0};
+        if (r0 + r < n_rows) {
+            const uint16_t* p = src + (r0 + r) * src_ld + c0 + c;
+            if (c0 + c + 8 <= cols) {
+                __builtin_memcpy(&v, p, 16);
+            } else {
+                uint16_t e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = c0 + c + j < cols ? p[j] : (uint16_t)0;
+                __builtin_memcpy(&v, e, 16);
+            }
+        }
+        *reinterpret_cast<u32x4_t*>(&tile[r][c]) = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int q = threadIdx.x + i * 256, c = q / 8, r = q % 8 * 8;
+        if (c0 + c >= cols || r0 + r >= dst_ld) continue;
+        u32x4_t v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (uint32_t)tile[r + 2 * j][c] | (uint32_t)tile[r + 2 * j + 1][c] << 16;
+        *reinterpret_cast<u32x4_t*>(dst + (c0 + c) * dst_ld + r0 + r) = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// which tile of C a workgroup takes
+// ---------------------------------------------------------------------------
+// Workgroup b runs on die b % 8 (of 8, with an L2 each).  A die takes an eighth
+// of the row tiles, and walks them kHeadGroup column tiles at a time, so that the
+// 32 workgroups it runs at once share 4 row tiles and 8 column tiles.
+struct TilePlace {
+    int32_t row, col;
+    bool ok;
+};
+
+__device__ __forceinline__ TilePlace tile_place(uint32_t block, int32_t row_tiles, int32_t col_tiles) {
+    const int32_t x = block % kHeadXcds, j = block / kHeadXcds;
+    const int32_t lo = (int32_t)((int64_t)row_tiles * x / kHeadXcds), n = (int32_t)((int64_t)row_tiles * (x + 1) / kHeadXcds) - lo;
+    TilePlace t{0, 0, false};
+    if (n == 0 || col_tiles == 0) return t;
+    const int32_t g = j / (n * kHeadGroup), r = j - g * n * kHeadGroup, c0 = g * kHeadGroup;
+    const int32_t width = col_tiles - c0 < kHeadGroup ? col_tiles - c0 : kHeadGroup;
+    if (width <= 0 || r >= n * width) return t;
+    t.row = lo + r / width;
+    t.col = c0 + r % width;
+    t.ok = true;
+    return t;
+}
+
+unsigned tile_grid(int64_t row_tiles, int64_t col_tiles) {
+    return (unsigned)(kHeadXcds * ((row_tiles + kHeadXcds - 1) / kHeadXcds) * col_tiles);
+}
+
+__device__ __forceinline__ int64_t tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
+
+// ---------------------------------------------------------------------------
+// forward: the statistics of a tile
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
+    __shared__ __align__(1024) uint8_t lds[kGemmLds];
+    const int64_t n = live_tokens(a);
+    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(a.V), (int32_t)tiles(n));
+    if (!tp.ok) return;
+    const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
+    GemmAcc acc;
+    gemm_tile(a.W, v0, a.V, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+    Stat* stat = reinterpret_cast<Stat*>(lds);  // [2][256]
+#pragma unroll
+    for (int ni = 0; ni < 4; ++ni) {
+        const int64_t k = n0 + wn * 64 + ni * 16 + col;
+        const int32_t tok = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
+        const int64_t first = v0 + wm * 128 + 4 * q;
+        // places of this lane's choices below the last one, and of the taken one
+        const int32_t end = a.V - first < 256 ? (int32_t)(a.V - first) : 256;
+        const int64_t from = (int64_t)tok - first;
+        const int32_t at = from >= 0 && from < 128 ? (int32_t)from : -1;
+        float top = kNone, xt = 0.0f;
+        bool here = false;
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (mi * 16 + i >= end) acc.c[mi][ni][i] = kNone;
+                if (mi * 16 + i == at) {
+                    xt = acc.c[mi][ni][i];
+                    here = true;
+                }
+                top = fmaxf(top, acc.c[mi][ni][i]);
+            }
+        }
+        if (here) a.taken[k] = xt;
+        Stat st = no_stat();
+        raise(st, top, a.c);
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) {
+            const float x[4] = {acc.c[mi][ni][0], acc.c[mi][ni][1], acc.c[mi][ni][2], acc.c[mi][ni][3]};
+            add(st, x, a.c);
+        }
+        st = join(st, shfl_xor(st, 16), a.c);
+        st = join(st, shfl_xor(st, 32), a.c);
+        if (q == 0) stat[wm * kGemmTile + wn * 64 + ni * 16 + col] = st;
+    }
+    __syncthreads();
+    if (threadIdx.x < kGemmTile && n0 + threadIdx.x < n) {
+        const Stat st = join(stat[threadIdx.x], stat[kGemmTile + threadIdx.x], a.c);
+        float* p = a.part + ((int64_t)tp.row * a.N + n0 + threadIdx.x) * 3;
+        p[0] = st.m;
+        p[1] = st.s;
+        p[2] = st.u;
+    }
+}
+
+// a token's tiles joined: 16 tokens a workgroup, 16 lanes each
+__global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
+    const int64_t t = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int l = threadIdx.x % 16;
+    if (t >= a.N) return;
+    const int64_t at = a.shape.at((uint32_t)t);
+    int64_t k = t;
+    bool ok = true;
+    if (a.place) {
+        k = a.place[t];
+        ok = k >= 0;
+    } else {
+        const int32_t tok = a.tokens[at];
+        ok = tok >= 0 && tok < a.V;
+        if (!ok && l == 0) flag_error(a.err, ERR_TOKEN);
+    }
+    if (!ok) {
+        if (l == 0) {
+            if (a.logp) a.logp[at] = 0.0f;
+            if (a.lse) a.lse[at] = 0.0f;
+            if (a.entropy) a.entropy[at] = 0.0f;
+        }
+        return;
+    }
+    Stat st = no_stat();
+    const int32_t n_tiles = (int32_t)tiles(a.V);
+    for (int32_t r = l; r < n_tiles; r += 16) {
+        const float* p = a.part + ((int64_t)r * a.N + k) * 3;
+        st = join(st, Stat{p[0], p[1], p[2]}, a.c);
+    }
+    st = join_lanes<16>(st, a.c);
+    const RowValues r = row_values(st, a.taken[k], a.c, a.inv_t);
+    if (l == 0) {
+        if (a.logp) a.logp[at] = r.logp;
+        if (a.lse) a.lse[at] = r.lse;
+        if (a.entropy) a.entropy[at] = r.entropy;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+// the logits' gradient of a tile of choices [v_base, v_base + v_count) of W, into
+// d [token][choice - v_base] and dt [choice - v_base][token]
+__global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int64_t v_base, int64_t v_count) {
+    __shared__ __align__(1024) uint8_t lds[kGemmLds];
+    const int64_t n = live_tokens(a);
+    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(v_count), (int32_t)tiles(n));
+    if (!tp.ok) return;
+    const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
+    GemmAcc acc;
+    const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld};
+    gemm_tile(W, v0, v_count, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+    // [token][choice] with rows of 512 bytes; the 8-byte piece c of row r lies at piece c ^ (r & 15)
+    uint2* out = reinterpret_cast<uint2*>(lds);
+#pragma unroll
+    for (int ni = 0; ni < 4; ++ni) {
+        const int c = wn * 64 + ni * 16 + col;
+        const int64_t k = n0 + c;
+        float g = 0.0f, h = 0.0f, lse = 0.0f, entropy = 0.0f;
+        int64_t tok = -1;
+        if (k < n) {
+            const int64_t at = a.shape.at((uint32_t)(a.list ? a.list[k] : k));
+            tok = a.tokens[at];
+            const bool ok = tok >= 0 && tok < a.V;  // (without a mask there is no list that leaves others out)
+            if (!ok && v_base == 0 && tp.row == 0 && wm == 0 && q == 0) flag_error(a.err, ERR_TOKEN);
+            lse = a.lse_in[at];
+            if (ok && a.g) g = a.g[at] * a.inv_t;
+            if (ok && a.h) h = a.h[at] * a.inv_t;
+            if (ok && a.h) entropy = a.entropy_in[at];
+        }
+        const int64_t first = v_base + v0 + wm * 128 + 4 * q;
+        const bool live = (g != 0.0f || h != 0.0f) && lse != kNone;
+        const int32_t end = !live ? 0 : v_base + v_count - first < 256 ? (int32_t)(v_base + v_count - first) : 256;
+        const int64_t from = tok - first;
+        const int32_t at = from >= 0 && from < 128 ? (int32_t)from : -1;
+        float taken = 0.0f;  // log p of the taken token
+        bool here = false;
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) {
+            uint16_t d[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lp = fmaf(acc.c[mi][ni][i], a.inv_t, -lse), p = exp2_fast(lp * kLog2e);
+                const float x = -p * fmaf(h, fmaxf(lp, kFloor) + entropy, g);
+                if (mi * 16 + i == at) {
+                    taken = lp;
+                    here = live;
+                }
+                d[i] = __builtin_bit_cast(uint16_t, (__bf16)(mi * 16 + i < end ? x : 0.0f));
+            }
+            const int piece = wm * 32 + mi * 4 + q;
+            out[c * 64 + (piece ^ (c & 15))] = make_uint2((uint32_t)d[0] | (uint32_t)d[1] << 16, (uint32_t)d[2] | (uint32_t)d[3] << 16);
+        }
+        if (here) {  // g (1 - p) without the cancellation of a probability near 1
+            const float x = -g * expm1f(taken) - h * exp2_fast(taken * kLog2e) * (fmaxf(taken, kFloor) + entropy);
+            const int v = wm * 128 + 4 * q + at;
+            reinterpret_cast<uint16_t*>(lds)[c * 256 + ((v / 4) ^ (c & 15)) * 4 + v % 4] = __builtin_bit_cast(uint16_t, (__bf16)x);
+        }
+    }
+    __syncthreads();
+    // [token][choice]: 16 bytes a lane, 32 lanes a row
+    for (int e = threadIdx.x; e < kGemmTile * 32; e += kGemmThreads) {
+        const int r = e / 32, p = e % 32 * 2;
+        if (n0 + r >= n) break;
+        const uint2 x = out[r * 64 + (p ^ (r & 15))], y = out[r * 64 + ((p + 1) ^ (r & 15))];
+        *reinterpret_cast<u32x4_t*>(a.d + (n0 + r) * a.d_ld + v0 + p * 4) = u32x4_t{x.x, x.y, y.x, y.y};
+    }
+    // [choice][token]: a lane gathers 8 tokens of one choice
+    const uint16_t* flat = reinterpret_cast<const uint16_t*>(lds);
+    for (int e = threadIdx.x; e < kGemmTile * 32; e += kGemmThreads) {
+        const int v = e % 256, t = e / 256 * 8;
+        if (v0 + v >= v_count) continue;
+        uint32_t x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r0 = t + 2 * j, r1 = r0 + 1;
+            x[j] = (uint32_t)flat[r0 * 256 + ((v / 4) ^ (r0 & 15)) * 4 + v % 4] |
+                   (uint32_t)flat[r1 * 256 + ((v / 4) ^ (r1 & 15)) * 4 + v % 4] << 16;
+        }
+        *reinterpret_cast<u32x4_t*>(a.dt + (v0 + v) * a.dt_ld + n0 + t) = u32x4_t{x[0], x[1], x[2], x[3]};
+    }
+}
+
+// Parts along k that a product of `tiles` tiles is split into, so that its work
+// fills rounds of the compute units: the fewest of at most `most` for which
+// the rounds cost least (a part also costs the writing of its sums).
+__device__ __forceinline__ int32_t splits(int64_t n_tiles, int32_t steps, int32_t cus, int32_t most) {
+    int32_t best = 1;
+    float cost = 1e30f;
+    for (int32_t s = 1; s <= most && s * 8 <= steps + 7; ++s) {
+        const float rounds = (float)((n_tiles * s + cus - 1) / cus);
+        const float c = rounds * ((float)steps / s + 8.0f);
+        if (c < cost) {
+            cost = c;
+            best = s;
+        }
+    }
+    return best;
+}
+
+// part s of dX^T tiles: rows = hidden units (W transposed), columns = tokens
+__global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64_t v_count) {
+    __shared__ __align__(1024) uint8_t lds[kGemmLds];
+    const int64_t n = live_tokens(a);
+    const int32_t row_tiles = (int32_t)tiles(a.H), col_tiles = (int32_t)tiles(n), steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
+    const int32_t S = splits((int64_t)row_tiles * col_tiles, steps, a.cus, a.splits);
+    const TilePlace tp = tile_place(blockIdx.x, row_tiles * S, col_tiles);
+    if (!tp.ok) return;
+    const int32_t s = tp.row / row_tiles, row = tp.row % row_tiles;
+    const int64_t h0 = (int64_t)row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
+    GemmAcc acc;
+    gemm_tile(a.WT, h0, a.H, GemmOperand{a.d, a.d_ld}, n0, n, v_count, (int32_t)((int64_t)steps * s / S),
+              (int32_t)((int64_t)steps * (s + 1) / S), lds, acc);
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+    float* part = a.dx_part + (int64_t)s * a.N * a.h_ld;
+#pragma unroll
+    for (int ni = 0; ni < 4; ++ni) {
+        const int64_t k = n0 + wn * 64 + ni * 16 + col;
+        if (k >= n) continue;
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) {
+            const int64_t h = h0 + wm * 128 + mi * 16 + 4 * q;
+            if (h < a.h_ld) *reinterpret_cast<f32x4_t*>(part + k * a.h_ld + h) = acc.c[mi][ni];
+        }
+    }
+}
+
+// the parts of dX of this chunk of choices (and, beyond the first, of those
+// before) in their order; after the last chunk bf16 rows, zeros where nothing
+// counts
+__global__ __launch_bounds__(256) void k_head_dhidden_join(HeadArgs a, int64_t v_count, bool first, bool last) {
+    const int64_t t = blockIdx.x;
+    const int64_t k = a.place ? a.place[t] : t;
+    const int64_t n = live_tokens(a);
+    const int32_t steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
+    const int32_t S = splits(tiles(a.H) * tiles(n), steps, a.cus, a.splits);
+    uint16_t* out = static_cast<uint16_t*>(a.dx.data) + a.dx.at((uint32_t)t, a.shape);
+    for (int64_t h = 4 * (int64_t)threadIdx.x; h < a.h_ld; h += 4 * 256) {
+        f32x4_t sum = {0, 0, 0, 0};
+        if (k >= 0) {
+            f32x4_t* total = reinterpret_cast<f32x4_t*>(a.dx_sum + k * a.h_ld + h);
+            if (!first) sum = *total;
+            for (int32_t s = 0; s < S; ++s)
+                sum += *reinterpret_cast<const f32x4_t*>(a.dx_part + ((int64_t)s * a.N + k) * a.h_ld + h);
+            if (!last) *total = sum;
+        }
+        if (last) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (h + i < a.H) out[h + i] = __builtin_bit_cast(uint16_t, (__bf16)sum[i]);
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void k_head_zero(HeadArgs a) {
+    for (int64_t v = blockIdx.x; v < a.V; v += gridDim.x)
+        for (int64_t h = threadIdx.x; h < a.H; h += 256) a.dw[v * a.dw_ld + h] = 0;
+}
+
+// dW of a chunk: rows = hidden units (X transposed), columns = choices, k = tokens
+__global__ __launch_bounds__(kGemmThreads) void k_head_dweight(HeadArgs a, int64_t v_base, int64_t v_count) {
+    __shared__ __align__(1024) uint8_t lds[kGemmLds];
+    const int64_t n = live_tokens(a);
+    // column tiles are many here: they take the rows' part in the walk
+    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(v_count), (int32_t)tiles(a.H));
+    if (!tp.ok) return;
+    const int64_t h0 = (int64_t)tp.col * kGemmTile, v0 = (int64_t)tp.row * kGemmTile;
+    const int64_t K = (n + kGemmK - 1) / kGemmK * kGemmK;  // both operands hold zeros up to there
+    GemmAcc acc;
+    gemm_tile(a.XT, h0, a.H, GemmOperand{a.dt, a.dt_ld}, v0, v_count, K, 0, (int32_t)(K / kGemmK), lds, acc);
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+#pragma unroll
+    for (int ni = 0; ni < 4; ++ni) {
+        const int64_t v = v0 + wn * 64 + ni * 16 + col;
+        if (v >= v_count) continue;
+        uint16_t* out = a.dw + (v_base + v) * a.dw_ld;
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) {
+            const int64_t h = h0 + wm * 128 + mi * 16 + 4 * q;
+            uint16_t e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = __builtin_bit_cast(uint16_t, (__bf16)acc.c[mi][ni][i]);
+            if (h + 4 <= a.H) {
+                __builtin_memcpy(out + h, e, 8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (h + i < a.H) out[h + i] = e[i];
+            }
+        }
+    }
+}
+
+}  // namespace
+
+#define HEAD_LAUNCH(kernel, grid, threads, ...)                                 \
+    do {                                                                        \
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, __VA_ARGS__);     \
+        const hipError_t e_ = hipGetLastError();                                \
+        if (e_ != hipSuccess) return e_;                                        \
+    } while (0)
+
+namespace {
+
+// the list of tokens that count, and operands whose rows the product can read
+hipError_t prepare_operands(HeadArgs& a, hipStream_t s) {
+    if (a.mask) HEAD_LAUNCH(k_head_list, dim3(1), kListThreads, a);
+    if (a.x_pack) {
+        HEAD_LAUNCH(k_head_pack, dim3((unsigned)(a.N < 65536 ? a.N : 65536)), 256, a, static_cast<const uint16_t*>(a.x.data), 0,
+                    a.H, a.x_pack, a.X.ld, 0, true);
+    }
+    if (a.w_pack) {
+        HEAD_LAUNCH(k_head_pack, dim3((unsigned)(a.V < 65536 ? a.V : 65536)), 256, a, a.w_src, a.w_ld, a.H, a.w_pack, a.W.ld, a.V,
+                    false);
+    }
+    return hipSuccess;
+}
+
+int64_t host_tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
+
+}  // namespace
+
+hipError_t launch_head_logprobs(HeadArgs a, hipStream_t s) {
+    hipError_t e = prepare_operands(a, s);
+    if (e != hipSuccess) return e;
+    HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N))), kGemmThreads, a);
+    HEAD_LAUNCH(k_head_join, dim3((unsigned)((a.N + 15) / 16)), 256, a);
+    return hipSuccess;
+}
+
+hipError_t launch_head_backward(HeadArgs a, hipStream_t s) {
+    if (a.N == 0) {  // no tokens: the projection's gradient is 0
+        HEAD_LAUNCH(k_head_zero, dim3((unsigned)(a.V < 65536 ? a.V : 65536)), 256, a);
+        return hipSuccess;
+    }
+    hipError_t e = prepare_operands(a, s);
+    if (e != hipSuccess) return e;
+    const dim3 by_token((unsigned)((a.N + 63) / 64), (unsigned)((a.H + 63) / 64));
+    HEAD_LAUNCH(k_head_transpose, by_token, 256, a, a.X.p, a.X.ld, 0, a.H, a.xt, a.XT.ld, true);
+    for (int64_t v = 0; v < a.V; v += a.chunk) {
+        const int64_t count = a.V - v < a.chunk ? a.V - v : a.chunk;
+        const bool first = v == 0, last = v + count == a.V;
+        HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N))), kGemmThreads, a, v, count);
+        const dim3 by_choice((unsigned)((count + 63) / 64), (unsigned)((a.H + 63) / 64));
+        HEAD_LAUNCH(k_head_transpose, by_choice, 256, a, a.W.p + v * a.W.ld, a.W.ld, count, a.H, a.wt, a.WT.ld, false);
+        HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N))), kGemmThreads, a, count);
+        HEAD_LAUNCH(k_head_dhidden_join, dim3((unsigned)a.N), 256, a, count, first, last);
+        HEAD_LAUNCH(k_head_dweight, dim3(tile_grid(host_tiles(count), host_tiles(a.H))), kGemmThreads, a, v, count);
+    }
+    return hipSuccess;
+}
+
+}  // namespace conduit

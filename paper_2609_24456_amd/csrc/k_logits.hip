@@ -20,7 +20,7 @@
 // HBM once in each direction.
 #include <type_traits>
 
-#include "loss_dev.h"
+#include "softmax_dev.h"
 
 namespace conduit {
 
@@ -29,9 +29,6 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 enum LogitsMode { LOGPROBS, LOSS };
-
-constexpr float kNone = -INFINITY;
-constexpr float kFloor = -1024.0f;  // 2^d is 0 below; keeps 0 * d from being NaN at d = -inf
 
 template <bool BF16>
 struct Elem;
@@ -88,61 +85,6 @@ __device__ __forceinline__ void store16(T* p, u32x4 v) {
     __builtin_memcpy(p, &v, 16);
 }
 
-// Running statistics of a part of a row: m = max x, s = sum 2^d, u = sum 2^d d
-// with d = c (x - m).
-struct Stat {
-    float m, s, u;
-};
-
-__device__ __forceinline__ Stat no_stat() { return Stat{kNone, 0.0f, 0.0f}; }
-
-__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float c) {
-    Stat r;
-    r.m = a.m > b.m ? a.m : b.m;
-    // equal maxima, -inf ones among them, have no distance
-    const float da = a.m == r.m ? 0.0f : (a.m - r.m) * c, db = b.m == r.m ? 0.0f : (b.m - r.m) * c;
-    const float ea = exp2_fast(da), eb = exp2_fast(db);
-    const float sa = a.s * ea, sb = b.s * eb;
-    r.s = sa + sb;
-    r.u = fmaf(a.u, ea, sa * fmaxf(da, kFloor)) + fmaf(b.u, eb, sb * fmaxf(db, kFloor));
-    return r;
-}
-
-template <int N>
-__device__ __forceinline__ float top_of(const float (&x)[N], float top) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
-    return top;
-}
-
-// the running maximum becomes at least `top`
-__device__ __forceinline__ void raise(Stat& st, float top, float c) {
-    if (top > st.m) {
-        const float d = (st.m - top) * c, e = exp2_fast(d);
-        st.u = fmaf(st.s, fmaxf(d, kFloor), st.u) * e;
-        st.s *= e;
-        st.m = top;
-    }
-}
-
-// elements that are no larger than the running maximum
-template <int N>
-__device__ __forceinline__ void add(Stat& st, const float (&x)[N], float c) {
-    const float base = st.m == kNone ? 0.0f : st.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = (x[i] - base) * c, e = exp2_fast(d);
-        st.s += e;
-        st.u = fmaf(e, fmaxf(d, kFloor), st.u);
-    }
-}
-
-template <int N>
-__device__ __forceinline__ void accumulate(Stat& st, const float (&x)[N], float c) {
-    raise(st, top_of(x, kNone), c);
-    add(st, x, c);
-}
-
 // keeps a vector packed: without it the unpacked halves of one use would be kept
 // in registers for the next
 __device__ __forceinline__ u32x4 again(u32x4 v) {
@@ -170,17 +112,6 @@ __device__ __forceinline__ void accumulate_tile(Stat& st, const u32x4 (&v)[K], f
     }
 }
 
-__device__ __forceinline__ Stat shfl_xor(const Stat& a, int d) {
-    return Stat{__shfl_xor(a.m, d, kWave), __shfl_xor(a.s, d, kWave), __shfl_xor(a.u, d, kWave)};
-}
-
-template <int LANES>
-__device__ __forceinline__ Stat join_lanes(Stat s, float c) {
-#pragma unroll
-    for (int d = LANES / 2; d > 0; d >>= 1) s = join(s, shfl_xor(s, d), c);
-    return s;
-}
-
 // joined over WAVES wavefronts of a workgroup, in every thread
 template <int WAVES>
 __device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
@@ -190,31 +121,6 @@ __device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
     __syncthreads();
     Stat r = lds[lane_id() % WAVES];
     return join_lanes<WAVES>(r, c);
-}
-
-// what a row's statistics say
-struct RowValues {
-    float base;     // m, or 0 in a row without weight
-    float inv_s;    // 1 / S, 0 in a row without weight
-    float log2_s;
-    float lse, entropy, logp, one_minus_p;
-};
-
-__device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float c, float inv_t) {
-    RowValues r;
-    if (st.s == 0.0f) {
-        r.base = r.inv_s = r.log2_s = r.entropy = r.one_minus_p = 0.0f;
-        r.lse = r.logp = kNone;
-        return r;
-    }
-    r.base = st.m;
-    r.inv_s = 1.0f / st.s;
-    r.log2_s = log2_fast(st.s);
-    r.lse = fmaf(st.m, inv_t, r.log2_s * kLn2);
-    r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
-    r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
-    r.one_minus_p = -expm1f(r.logp);
-    return r;
 }
 
 // the gradient of one logit: d = c (x - base)

@@ -4,7 +4,7 @@
 #include <initializer_list>
 #include <string>
 
-#include "loss_dev.h"
+#include "head_dev.h"
 
 using namespace conduit;
 
@@ -197,6 +197,127 @@ LogitsArgs logits_args(const conduit_rows* x, int64_t B, int64_t T, int64_t stri
     a.mask = mask;
     a.err = err;
     a.parts = 1;
+    return a;
+}
+
+// ---------------------------------------------------------------------------
+// the projection head
+// ---------------------------------------------------------------------------
+// (byte offsets within 256 rows of an operand, rows of at most 2^21 elements, stay below 2^31)
+constexpr int64_t kHeadMaxTokens = 1ll << 21, kHeadMaxChoices = 1ll << 22, kHeadMaxHidden = 1ll << 16;
+constexpr int64_t kHeadMaxLd = 1ll << 21;
+constexpr int64_t kHeadChunkBytes = 8ll << 30;  // of the logits' gradient in both orders
+constexpr int64_t kHeadPartBytes = 4ll << 30;   // of the parts of the hidden states' gradient
+
+int64_t ceil_to(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// can the product's copies read these rows where they are (16-byte pieces, whole ones)
+bool readable(const void* p, int64_t ld, int64_t width) {
+    return !misaligned(p, 16) && ld % 8 == 0 && width % 8 == 0 && ld <= kHeadMaxLd;
+}
+
+bool one_after_another(const conduit_rows* r, int64_t B, int64_t T) {
+    return B <= 1 || T <= 0 || r->stride_b == T * r->stride_t || T == 1;
+}
+
+int64_t row_step(const conduit_rows* r, int64_t T) { return T == 1 ? r->stride_b : r->stride_t; }
+
+struct HeadLayout {
+    bool pack_w, pack_x;  // pack_x: even without a mask
+    int64_t K, ld, np, chunk, h_ld;
+    int32_t splits;
+    uint64_t count, list, place, taken, part, x_pack, w_pack, xt, wt, d, dt, dx_part, dx_sum, bytes;
+};
+
+// Everything but the chunk's arrays is sized for all B * T tokens counting; the
+// hidden rows' copy is there whether or not a mask will ask for it.
+HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const conduit_rows* weight, int64_t V, bool backward) {
+    HeadLayout l{};
+    const int64_t N = B * T, H = hidden->width;
+    l.pack_w = !readable(weight->data, weight->stride_t, H);
+    l.pack_x = !readable(hidden->data, row_step(hidden, T), H) || !one_after_another(hidden, B, T);
+    l.ld = ceil_to(H, 8);
+    l.K = l.ld;
+    l.np = ceil_to(N, kGemmTile);
+    l.h_ld = ceil_to(H, 8);
+    uint64_t at = layout(0, 0).bytes;
+    auto take = [&](int64_t bytes) {
+        const uint64_t p = at;
+        at += up((uint64_t)bytes);
+        return p;
+    };
+    l.count = take(4);
+    l.list = take(4 * N);
+    l.place = take(4 * N);
+    l.x_pack = take(2 * N * l.ld);
+    l.w_pack = take(l.pack_w ? 2 * V * l.ld : 0);
+    if (!backward) {
+        l.taken = take(4 * N);
+        l.part = take(12 * N * ((V + kGemmTile - 1) / kGemmTile));
+    } else {
+        const int64_t fit = l.np > 0 ? kHeadChunkBytes / (4 * l.np) / kGemmTile * kGemmTile : V;
+        l.chunk = ceil_to(V < kHeadMaxLd ? V : kHeadMaxLd, kGemmTile);
+        if (l.chunk > fit) l.chunk = fit > 4 * kGemmTile ? fit : 4 * kGemmTile;
+        const int64_t most = N > 0 ? kHeadPartBytes / (4 * N * l.h_ld) : 1;
+        l.splits = (int32_t)(most < 1 ? 1 : most < kHeadSplits ? most : kHeadSplits);
+        l.xt = take(2 * H * l.np);
+        l.wt = take(2 * H * l.chunk);
+        l.d = take(2 * N * l.chunk);
+        l.dt = take(2 * l.chunk * l.np);
+        l.dx_part = take(4 * N * l.h_ld * l.splits);
+        l.dx_sum = take(l.chunk < V ? 4 * N * l.h_ld : 0);
+    }
+    l.bytes = at;
+    return l;
+}
+
+conduit_status check_head(const conduit_rows* hidden, const conduit_rows* weight, int64_t V, int64_t B, int64_t T) {
+    CONDUIT_TRY(check_rows(hidden, B, T, false, "hidden"));
+    CONDUIT_TRY(check_rows(weight, 1, V, false, "weight"));
+    if (hidden->dtype != CONDUIT_BF16 || weight->dtype != CONDUIT_BF16) return bad("hidden and weight must be BF16");
+    if (hidden->width != weight->width) return bad("hidden and weight must have the same width");
+    if (hidden->width > kHeadMaxHidden) return bad("the hidden width must be at most 2^16");
+    if (V < 1 || V > kHeadMaxChoices) return bad("the number of choices must be in [1, 2^22]");
+    if (B * T > kHeadMaxTokens) return bad("the batch must hold at most 2^21 tokens");
+    return CONDUIT_OK;
+}
+
+HeadArgs head_args(const conduit_rows* hidden, const conduit_rows* weight, int64_t V, int64_t B, int64_t T, int64_t stride,
+                   const int32_t* tokens, const uint8_t* mask, double temperature, uint32_t* err, void* ws,
+                   const HeadLayout& l) {
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    auto u16 = [&](uint64_t at) { return reinterpret_cast<uint16_t*>(w + at); };
+    HeadArgs a{};
+    a.shape = make_shape(B, T, stride);
+    a.N = B * T;
+    a.V = V;
+    a.H = hidden->width;
+    a.x = view(hidden);
+    a.K = l.K;
+    a.tokens = tokens;
+    a.mask = mask;
+    a.c = (float)((double)1.4426950408889634074 / temperature);
+    a.inv_t = (float)(1.0 / temperature);
+    a.err = err;
+    a.cus = device_cus();
+    if (mask) {
+        a.list = reinterpret_cast<int32_t*>(w + l.list);
+        a.place = reinterpret_cast<int32_t*>(w + l.place);
+        a.count_out = reinterpret_cast<uint32_t*>(w + l.count);
+        a.count = a.count_out;
+    }
+    a.X = GemmOperand{static_cast<const uint16_t*>(hidden->data), row_step(hidden, T)};
+    if (mask || l.pack_x) {
+        a.x_pack = u16(l.x_pack);
+        a.X = GemmOperand{a.x_pack, l.ld};
+    }
+    a.w_src = static_cast<const uint16_t*>(weight->data);
+    a.w_ld = weight->stride_t;
+    a.W = GemmOperand{a.w_src, a.w_ld};
+    if (l.pack_w) {
+        a.w_pack = u16(l.w_pack);
+        a.W = GemmOperand{a.w_pack, l.ld};
+    }
     return a;
 }
 
@@ -421,6 +542,104 @@ conduit_status conduit_preference_loss(const conduit_preference_opts* opts, int6
     a.pair = reinterpret_cast<double*>(w + l.rest);
     a.partial = a.pair + 4 * P;
     return launched(launch_preference_loss(a, s), "preference loss launch");
+}
+
+conduit_status conduit_head_logprobs_workspace(int64_t B, int64_t T, const conduit_rows* hidden, const conduit_rows* weight,
+                                               int64_t V, uint64_t* bytes) {
+    if (!bytes) return bad("NULL size pointer");
+    CONDUIT_TRY(check_batch(B, T, T));
+    CONDUIT_TRY(check_head(hidden, weight, V, B, T));
+    *bytes = head_layout(B, T, hidden, weight, V, false).bytes;
+    return CONDUIT_OK;
+}
+
+conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_rows* weight, int64_t V, int64_t B, int64_t T,
+                                     int64_t stride, const int32_t* tokens, const uint8_t* mask, double temperature,
+                                     float* logp, float* lse, float* entropy, void* workspace, uint64_t workspace_bytes,
+                                     void* stream) {
+    CONDUIT_TRY(check_batch(B, T, stride));
+    CONDUIT_TRY(check_head(hidden, weight, V, B, T));
+    CONDUIT_TRY(check_temperature(temperature));
+    if (B == 0 || T == 0) return CONDUIT_OK;
+    if (!tokens) return bad("tokens must not be NULL");
+    CONDUIT_TRY(check_outputs({logp, lse, entropy}, {tokens}, B, T, stride));
+    const HeadLayout l = head_layout(B, T, hidden, weight, V, false);
+    CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
+    uint32_t* err = nullptr;
+    CONDUIT_TRY(standalone_error_words(&err));
+    HeadArgs a = head_args(hidden, weight, V, B, T, stride, tokens, mask, temperature, err, workspace, l);
+    uint8_t* w = static_cast<uint8_t*>(workspace);
+    a.taken = reinterpret_cast<float*>(w + l.taken);
+    a.part = reinterpret_cast<float*>(w + l.part);
+    a.logp = logp;
+    a.lse = lse;
+    a.entropy = entropy;
+    return launched(launch_head_logprobs(a, static_cast<hipStream_t>(stream)), "head logprobs launch");
+}
+
+conduit_status conduit_head_logprobs_backward_workspace(int64_t B, int64_t T, const conduit_rows* hidden,
+                                                        const conduit_rows* weight, int64_t V, uint64_t* bytes) {
+    if (!bytes) return bad("NULL size pointer");
+    CONDUIT_TRY(check_batch(B, T, T));
+    CONDUIT_TRY(check_head(hidden, weight, V, B, T));
+    *bytes = head_layout(B, T, hidden, weight, V, true).bytes;
+    return CONDUIT_OK;
+}
+
+conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const conduit_rows* weight, int64_t V, int64_t B,
+                                              int64_t T, int64_t stride, const int32_t* tokens, const uint8_t* mask,
+                                              double temperature, const float* lse, const float* entropy, const float* dlogp,
+                                              const float* dentropy, const conduit_rows* dhidden, const conduit_rows* dweight,
+                                              void* workspace, uint64_t workspace_bytes, void* stream) {
+    CONDUIT_TRY(check_batch(B, T, stride));
+    CONDUIT_TRY(check_head(hidden, weight, V, B, T));
+    CONDUIT_TRY(check_rows(dhidden, B, T, true, "dhidden"));
+    CONDUIT_TRY(check_rows(dweight, 1, V, true, "dweight"));
+    if (dhidden->dtype != CONDUIT_BF16 || dweight->dtype != CONDUIT_BF16) return bad("dhidden and dweight must be BF16");
+    if (dhidden->width != hidden->width || dweight->width != hidden->width)
+        return bad("dhidden and dweight must have the hidden width");
+    CONDUIT_TRY(check_temperature(temperature));
+    const bool empty = B == 0 || T == 0;
+    if (!empty) {
+        if (!tokens || !lse) return bad("tokens and lse must not be NULL");
+        if (dentropy && !entropy) return bad("the gradient of the entropy needs the entropy");
+        CONDUIT_TRY(check_outputs({}, {tokens, lse, entropy, dlogp, dentropy}, B, T, stride));
+        if (!apart(dhidden->data, rows_extent(dhidden, B, T), hidden->data, rows_extent(hidden, B, T)) ||
+            !apart(dhidden->data, rows_extent(dhidden, B, T), weight->data, rows_extent(weight, 1, V)) ||
+            !apart(dweight->data, rows_extent(dweight, 1, V), hidden->data, rows_extent(hidden, B, T)) ||
+            !apart(dhidden->data, rows_extent(dhidden, B, T), dweight->data, rows_extent(dweight, 1, V)))
+            return bad("dhidden and dweight must be apart from each other and from the inputs");
+    }
+    if (!apart(dweight->data, rows_extent(dweight, 1, V), weight->data, rows_extent(weight, 1, V)))
+        return bad("dhidden and dweight must be apart from each other and from the inputs");
+    const HeadLayout l = head_layout(B, T, hidden, weight, V, true);
+    CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
+    uint32_t* err = nullptr;
+    CONDUIT_TRY(standalone_error_words(&err));
+    HeadArgs a = head_args(hidden, weight, V, empty ? 0 : B, empty ? 0 : T, empty ? 0 : stride, tokens, mask, temperature, err,
+                           workspace, l);
+    uint8_t* w = static_cast<uint8_t*>(workspace);
+    a.lse_in = lse;
+    a.entropy_in = entropy;
+    a.g = dlogp;
+    a.h = dentropy;
+    a.dx = view(dhidden);
+    a.dw = static_cast<uint16_t*>(dweight->data);
+    a.dw_ld = dweight->stride_t;
+    a.chunk = l.chunk;
+    a.splits = l.splits;
+    a.xt = reinterpret_cast<uint16_t*>(w + l.xt);
+    a.wt = reinterpret_cast<uint16_t*>(w + l.wt);
+    a.d = reinterpret_cast<uint16_t*>(w + l.d);
+    a.dt = reinterpret_cast<uint16_t*>(w + l.dt);
+    a.XT = GemmOperand{a.xt, l.np};
+    a.WT = GemmOperand{a.wt, l.chunk};
+    a.d_ld = l.chunk;
+    a.dt_ld = l.np;
+    a.dx_part = reinterpret_cast<float*>(w + l.dx_part);
+    a.dx_sum = reinterpret_cast<float*>(w + l.dx_sum);
+    a.h_ld = l.h_ld;
+    return launched(launch_head_backward(a, static_cast<hipStream_t>(stream)), "head gradient launch");
 }
 
 }  // extern "C"
