@@ -180,6 +180,12 @@ unsigned tile_grid(int64_t row_tiles, int64_t col_tiles) {
 
 __device__ __forceinline__ int64_t tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
 
+// joined over the four lanes 16 apart
+__device__ __forceinline__ Stat join_quarters(Stat s, float c) {
+    s = join(s, Stat{partner<4>(s.m), partner<4>(s.s), partner<4>(s.u)}, c);
+    return join(s, Stat{partner<5>(s.m), partner<5>(s.s), partner<5>(s.u)}, c);
+}
+
 // ---------------------------------------------------------------------------
 // forward: the statistics of a tile
 // ---------------------------------------------------------------------------
@@ -224,8 +230,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
             const float x[4] = {acc.c[mi][ni][0], acc.c[mi][ni][1], acc.c[mi][ni][2], acc.c[mi][ni][3]};
             add(st, x, a.c);
         }
-        st = join(st, shfl_xor(st, 16), a.c);
-        st = join(st, shfl_xor(st, 32), a.c);
+        st = join_quarters(st, a.c);
         if (q == 0) stat[wm * kGemmTile + wn * 64 + ni * 16 + col] = st;
     }
     __syncthreads();

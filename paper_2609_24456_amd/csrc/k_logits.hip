@@ -142,22 +142,32 @@ struct RowGrad {
     float g = 0.0f, h = 0.0f;
 };
 
-__device__ __forceinline__ RowGrad row_loss(const PolicyArgs& p, int64_t at, uint32_t b, float logp, TokenLoss* out,
-                                            double* weight) {
+// what the loss of a row needs beside its log-probability, loaded ahead of it
+struct RowData {
+    float old, ref, adv;
+    double w;
+};
+
+__device__ __forceinline__ RowData row_data(const PolicyArgs& p, int64_t at, uint32_t b) {
+    RowData d;
+    d.old = p.old_logp ? p.old_logp[at] : 0.0f;
+    d.ref = p.ref_logp ? p.ref_logp[at] : 0.0f;
+    d.adv = p.adv[at];
     uint32_t tokens = (uint32_t)(p.shape.B * p.shape.T), rows = (uint32_t)p.shape.B, row = (uint32_t)p.shape.T;
     if (p.mask) {
-        tokens = p.head->tokens;
-        rows = p.head->rows;
+        const uint64_t counts = p.head->counts;
+        tokens = (uint32_t)counts;
+        rows = (uint32_t)(counts >> 32);
         if (p.o.reduction == CONDUIT_SEQUENCE_MEAN) row = p.row_count[b];
     }
-    const double w = token_weight(p.o, tokens, rows, row);
-    const TokenLoss t = policy_token(p.o, logp, p.old_logp != nullptr, p.old_logp ? p.old_logp[at] : 0.0f,
-                                     p.ref_logp != nullptr, p.ref_logp ? p.ref_logp[at] : 0.0f, p.adv[at]);
-    const float wf = (float)(w * p.o.scale);
-    if (out) {
-        *out = t;
-        *weight = w;
-    }
+    d.w = token_weight(p.o, tokens, rows, row);
+    return d;
+}
+
+__device__ __forceinline__ RowGrad row_loss(const PolicyArgs& p, const RowData& d, float logp, TokenLoss* out) {
+    const TokenLoss t = policy_token(p.o, logp, p.old_logp != nullptr, d.old, p.ref_logp != nullptr, d.ref, d.adv);
+    const float wf = (float)(d.w * p.o.scale);
+    if (out) *out = t;
     return RowGrad{wf * t.slope, -p.o.ent * wf};
 }
 
@@ -190,13 +200,19 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
         const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
         float v[kShortElems];
         RowValues r;
+        RowData rd;
         if (ok) {
-            float xa = E::one(x[tok]);
+            if constexpr (MODE == LOSS) rd = row_data(p, at, div31(n, a.shape.by_T));
+            float xa = 0.0f;  // the taken one's, in the lane that holds it
 #pragma unroll
-            for (int i = 0; i < kShortElems; ++i) v[i] = l + i * LANES < a.V ? E::one(x[l + i * LANES]) : kNone;
+            for (int i = 0; i < kShortElems; ++i) {
+                v[i] = l + i * LANES < a.V ? E::one(x[l + i * LANES]) : kNone;
+                if (l + i * LANES == tok) xa = v[i];
+            }
             Stat st = no_stat();
             accumulate(st, v, a.c);
-            r = row_values(join_lanes<LANES>(st, a.c), xa, a.c, a.inv_t);
+            // (a plain sum over the lanes: the others hold 0)
+            r = row_values(join_lanes<LANES>(st, a.c), lanes_sum<LANES>(xa), a.c, a.inv_t);
         }
         if (l == 0) {
             if (a.logp) a.logp[at] = ok ? r.logp : 0.0f;
@@ -208,9 +224,12 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
             RowGrad rg;
             if (ok) {
                 TokenLoss t;
-                double w;
-                rg = row_loss(p, at, div31(n, a.shape.by_T), r.logp, &t, &w);
-                if (l == 0) sums.add(w, t, r.entropy);
+                rg = row_loss(p, rd, r.logp, &t);
+                if (l == 0) {
+                    TokenSums one;
+                    one.add(t, r.entropy);
+                    sums.add(rd.w, one);
+                }
             }
             const GradCoef k{ok ? -rg.g * a.inv_t * r.inv_s : 0.0f, ok ? -rg.h * a.inv_t * r.inv_s : 0.0f,
                              ok ? r.entropy - kLn2 * r.log2_s : 0.0f};
@@ -233,7 +252,7 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
         }
     }
     if constexpr (MODE == LOSS)
-        finish_policy<kShortThreads>(p, sums, p.mask ? p.head->tokens : n_rows, counted, lds);
+        finish_policy<kShortThreads>(p, sums, p.mask ? (uint32_t)p.head->counts : n_rows, counted, lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -272,6 +291,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
         }
         return;
     }
+    RowData rd;
+    if constexpr (MODE == LOSS) rd = row_data(p, at, div31(n, a.shape.by_T));
     const float xa = E::one(x[tok]);
     const float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
     Stat st = no_stat();
@@ -298,7 +319,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
         if (a.entropy) a.entropy[at] = r.entropy;
     }
     if constexpr (MODE == LOSS) {
-        const RowGrad rg = row_loss(p, at, div31(n, a.shape.by_T), r.logp, nullptr, nullptr);
+        const RowGrad rg = row_loss(p, rd, r.logp, nullptr);
         const GradCoef k{-rg.g * a.inv_t * r.inv_s, -rg.h * a.inv_t * r.inv_s, r.entropy - kLn2 * r.log2_s};
         const bool empty = r.inv_s == 0.0f;
         auto write = [&](auto ent) {
@@ -437,7 +458,7 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, Po
     if (ok) {
         lse = POLICY ? a.lse_n[n] : a.lse_in[at];
         if constexpr (POLICY) {  // (lse_n, logp and entropy_in: from the launch before)
-            rg = row_loss(p, at, div31(n, a.shape.by_T), a.logp[at], nullptr, nullptr);
+            rg = row_loss(p, row_data(p, at, div31(n, a.shape.by_T)), a.logp[at], nullptr);
         } else {
             rg.g = a.g ? a.g[at] : 0.0f;
             rg.h = a.h ? a.h[at] : 0.0f;
@@ -533,6 +554,8 @@ hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) 
     const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
     if (nv <= 8 * kWave)
         hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p);
+    else if (MODE == LOGPROBS)  // nothing stays: any width goes by in tiles of 8 vectors a lane
+        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), dim3((unsigned)rows), dim3(256), 0, s, a, p);
     else if (nv <= 4096)
         hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), dim3((unsigned)rows), dim3(256), 0, s, a, p);
     else

@@ -20,10 +20,11 @@ namespace conduit {
 namespace {
 
 constexpr int kPolicyThreads = 256;
-constexpr int kSmallThreads = 512;
+constexpr int kSmallThreads = 1024;
 constexpr int kChunk = 4;             // tokens a lane takes at once
-constexpr int kSmallChunks = 4096;    // most chunks, and most rows, that one workgroup takes by itself
-constexpr int kCountBytes = 16 * kWave;  // mask bytes a wavefront counts at once
+constexpr int kSmallChunks = 2048;    // most chunks, and most rows, that one workgroup takes by itself
+constexpr int kCountThreads = 1024;
+constexpr int kCountBlocks = 64;      // few: each ends in an atomic on one word
 
 struct Chunks {
     int64_t T;
@@ -68,32 +69,62 @@ __device__ __forceinline__ uint32_t count_bytes(uint32_t x) {
     return __builtin_popcount((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
 }
 
-__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, int64_t at, uint32_t mask, int n, double w,
-                                             PolicySums& sums) {
-    float lp[kChunk], old[kChunk], ref[kChunk], adv[kChunk], ent[kChunk], g[kChunk], h[kChunk];
-    load4(a.logp + at, n, lp);
-    load4(a.adv + at, n, adv);
-    if (a.old_logp) load4(a.old_logp + at, n, old);
-    if (a.ref_logp) load4(a.ref_logp + at, n, ref);
-    if (a.entropy) load4(a.entropy + at, n, ent);
+// a chunk's inputs, loaded ahead of what they wait for
+struct ChunkData {
+    float lp[kChunk], old[kChunk], ref[kChunk], adv[kChunk], ent[kChunk];
+    uint32_t mask;
+    int n;
+    int64_t at;
+    uint32_t row;
+};
+
+__device__ __forceinline__ ChunkData load_chunk(const PolicyArgs& a, const Chunks& ch, uint32_t c) {
+    ChunkData d;
+    d.row = div31(c, ch.by_row);
+    const int64_t t = (int64_t)(c - d.row * ch.per_row) * kChunk;
+    d.at = (int64_t)d.row * a.shape.stride + t;
+    d.n = ch.T - t < kChunk ? (int)(ch.T - t) : kChunk;
+    d.mask = a.mask ? load_mask4(a.mask + d.at, d.n) : 0x01010101u;
+    load4(a.logp + d.at, d.n, d.lp);
+    load4(a.adv + d.at, d.n, d.adv);
+    if (a.old_logp) load4(a.old_logp + d.at, d.n, d.old);
+    if (a.ref_logp) load4(a.ref_logp + d.at, d.n, d.ref);
+    if (a.entropy) load4(a.entropy + d.at, d.n, d.ent);
+    return d;
+}
+
+__device__ __forceinline__ ChunkData load_chunk_mask(const PolicyArgs& a, const Chunks& ch, uint32_t c) {
+    ChunkData d;
+    d.row = div31(c, ch.by_row);
+    const int64_t t = (int64_t)(c - d.row * ch.per_row) * kChunk;
+    d.n = ch.T - t < kChunk ? (int)(ch.T - t) : kChunk;
+    d.mask = load_mask4(a.mask + (int64_t)d.row * a.shape.stride + t, d.n);
+    return d;
+}
+
+__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, const ChunkData& d, double w, PolicySums& sums) {
     const float wf = (float)(w * a.o.scale), we = -a.o.ent * wf;
+    float g[kChunk], h[kChunk];
+    TokenSums few;
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) {
         g[i] = h[i] = 0.0f;
-        bool on = i < n && (mask >> (8 * i) & 255u) != 0;
+        bool on = i < d.n && (d.mask >> (8 * i) & 255u) != 0;
         if (on && a.tokens) {
-            const int32_t tok = a.tokens[at + i];
+            const int32_t tok = a.tokens[d.at + i];
             on = tok >= 0 && tok < a.V;
         }
-        if (!on) continue;
-        const TokenLoss t = policy_token(a.o, lp[i], a.old_logp != nullptr, a.old_logp ? old[i] : 0.0f,
-                                         a.ref_logp != nullptr, a.ref_logp ? ref[i] : 0.0f, adv[i]);
-        sums.add(w, t, a.entropy ? ent[i] : 0.0f);
-        g[i] = wf * t.slope;
-        h[i] = we;
+        if (on) {
+            const TokenLoss t = policy_token(a.o, d.lp[i], a.old_logp != nullptr, d.old[i], a.ref_logp != nullptr, d.ref[i], d.adv[i]);
+            few.add(t, a.entropy ? d.ent[i] : 0.0f);
+            g[i] = wf * t.slope;
+            h[i] = we;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // one token after the other: interleaved, they would need twice the registers
     }
-    if (a.dlogp) store4(a.dlogp + at, n, g);
-    if (a.dentropy) store4(a.dentropy + at, n, h);
+    sums.add(w, few);
+    if (a.dlogp) store4(a.dlogp + d.at, d.n, g);
+    if (a.dentropy) store4(a.dentropy + d.at, d.n, h);
 }
 
 template <int NT, bool SMALL>
@@ -102,48 +133,37 @@ __global__ __launch_bounds__(NT) void k_policy_loss(PolicyArgs a, Chunks ch, boo
     __shared__ uint32_t s_count[SMALL ? kSmallChunks : 1];
     uint32_t tokens = (uint32_t)(a.shape.B * a.shape.T), rows = (uint32_t)a.shape.B;
     const uint32_t first = blockIdx.x * NT + threadIdx.x, step = gridDim.x * NT;
-    auto place = [&](uint32_t c, uint32_t* b, int64_t* at, int* n) {
-        *b = div31(c, ch.by_row);
-        const int64_t t = (int64_t)(c - *b * ch.per_row) * kChunk;
-        *at = (int64_t)*b * a.shape.stride + t;
-        *n = ch.T - t < kChunk ? (int)(ch.T - t) : kChunk;
-    };
+    ChunkData d;
+    if (first < ch.total) d = load_chunk(a, ch, first);
     if (SMALL && a.mask) {
-        for (uint32_t b = threadIdx.x; b < (uint32_t)a.shape.B; b += NT) s_count[b] = 0;
-        __syncthreads();
-        for (uint32_t c = first; c < ch.total; c += step) {
-            uint32_t b;
-            int64_t at;
-            int n;
-            place(c, &b, &at, &n);
-            const uint32_t k = count_bytes(load_mask4(a.mask + at, n));
-            if (k) atomicAdd(&s_count[b], k);
+        const bool by_row = a.o.reduction == CONDUIT_SEQUENCE_MEAN;
+        if (by_row) {
+            for (uint32_t b = threadIdx.x; b < (uint32_t)a.shape.B; b += NT) s_count[b] = 0;
+            __syncthreads();
         }
-        __syncthreads();
         double t[2] = {0, 0};
-        for (uint32_t b = threadIdx.x; b < (uint32_t)a.shape.B; b += NT) {
-            t[0] += s_count[b];
-            t[1] += s_count[b] != 0;
+        for (uint32_t c = first; c < ch.total; c += step) {
+            const ChunkData o = c == first ? d : load_chunk_mask(a, ch, c);
+            const uint32_t k = count_bytes(o.n == kChunk ? o.mask : o.mask & ((1u << (8 * o.n)) - 1u));
+            t[0] += k;
+            if (by_row && k && atomicAdd(&s_count[o.row], k) == 0) t[1] += 1.0;
         }
-        block_sum<NT, 2>(t, lds);
+        block_sum<NT, 2>(t, lds);  // (its barriers also end the counting)
         tokens = (uint32_t)t[0];
         rows = (uint32_t)t[1];
     } else if (counted) {
-        tokens = a.head->tokens;
-        rows = a.head->rows;
+        const uint64_t counts = a.head->counts;
+        tokens = (uint32_t)counts;
+        rows = (uint32_t)(counts >> 32);
     }
     PolicySums sums;
     const double flat = token_weight(a.o, tokens, rows, (uint32_t)a.shape.T);
     for (uint32_t c = first; c < ch.total; c += step) {
-        uint32_t b;
-        int64_t at;
-        int n;
-        place(c, &b, &at, &n);
-        const uint32_t mask = a.mask ? load_mask4(a.mask + at, n) : 0x01010101u;
+        if (c != first) d = load_chunk(a, ch, c);
         double w = flat;
         if (a.o.reduction == CONDUIT_SEQUENCE_MEAN && a.mask)
-            w = token_weight(a.o, tokens, rows, SMALL ? s_count[b] : a.row_count[b]);
-        policy_chunk(a, at, mask, n, w, sums);
+            w = token_weight(a.o, tokens, rows, SMALL ? s_count[d.row] : a.row_count[d.row]);
+        policy_chunk(a, d, w, sums);
     }
     finish_policy<NT>(a, sums, tokens, counted, lds);
 }
@@ -160,69 +180,64 @@ __device__ __forceinline__ uint32_t count16(const uint8_t* row, int64_t t0, int6
     return k;
 }
 
-// Counted tokens of the batch: wavefronts take parts of kCountBytes mask bytes
-// of a row.  Whole numbers, so the order of the additions is free.
-__global__ __launch_bounds__(kPolicyThreads) void k_token_count(PolicyArgs a, uint32_t items, uint32_t per_row,
-                                                                Div31 by_row) {
-    __shared__ double lds[kPolicyThreads / kWave];
-    const uint32_t waves = gridDim.x * (kPolicyThreads / kWave);
-    double tokens[1] = {0};
-    for (uint32_t i = blockIdx.x * (kPolicyThreads / kWave) + threadIdx.x / kWave; i < items; i += waves) {
-        const uint32_t b = div31(i, by_row);
-        const int64_t t0 = (int64_t)(i - b * per_row) * kCountBytes + lane_id() * 16;
-        tokens[0] += count16(a.mask + (int64_t)b * a.shape.stride, t0, a.shape.T);
-    }
-    block_sum<kPolicyThreads, 1>(tokens, lds);
-    if (threadIdx.x == 0 && tokens[0] > 0) atomicAdd(&a.head->tokens, (uint32_t)tokens[0]);
-}
-
-// Counted tokens of every row, of the batch, and the rows with any: NT threads a
-// row, kRows rows a workgroup at once.
-template <int NT, int kRows>
-__global__ __launch_bounds__(NT * kRows) void k_row_count(PolicyArgs a) {
-    constexpr int kAll = NT * kRows;
-    __shared__ double lds[2 * kAll / kWave];
+// Counted tokens of every row, of the batch, and the rows with any.  LANES lanes
+// take a row (a wavefront, or the workgroup); rows that follow each other
+// without a gap and have no weight of their own are one row, cut into parts.
+// Whole numbers, so the order of the additions is free.
+template <int LANES>
+__global__ __launch_bounds__(kCountThreads) void k_count(PolicyArgs a, int64_t rows, int64_t T, int64_t stride, int64_t last_T) {
+    __shared__ double lds[2 * kCountThreads / kWave];
+    constexpr int kRows = kCountThreads / LANES;
     double sums[2] = {0, 0};
-    const int tid = threadIdx.x % NT;
-    for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.shape.B; first += (int64_t)gridDim.x * kRows) {
-        const int64_t b = first + threadIdx.x / NT;
-        double k[1] = {0};
-        if (b < a.shape.B) {
-            const uint8_t* row = a.mask + b * a.shape.stride;
-            for (int64_t t0 = 16 * (int64_t)tid; t0 < a.shape.T; t0 += 16 * NT) k[0] += count16(row, t0, a.shape.T);
+    const int tid = threadIdx.x % LANES;
+    const bool each = a.o.reduction == CONDUIT_SEQUENCE_MEAN;
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows) {
+        const int64_t b = r0 + threadIdx.x / LANES, end = b == rows - 1 ? last_T : T;
+        uint32_t k = 0;
+        if (b < rows) {
+            const uint8_t* row = a.mask + b * stride;
+#pragma unroll 4
+            for (int64_t t0 = 16 * (int64_t)tid; t0 < end; t0 += 16 * LANES) k += count16(row, t0, end);
         }
-        if constexpr (kRows > 1) k[0] = wave_sum(k[0]);  // NT = 64: a wavefront a row
-        else block_sum<NT, 1>(k, lds);
-        if (tid == 0 && b < a.shape.B) {
-            a.row_count[b] = (uint32_t)k[0];
-            sums[0] += k[0];
-            sums[1] += k[0] > 0;
+        if (!each) {
+            sums[0] += k;
+            continue;
+        }
+        double n[1] = {(double)k};
+        if constexpr (LANES == kWave) n[0] = wave_sum(n[0]);
+        else block_sum<kCountThreads, 1>(n, lds);
+        if (tid == 0 && b < rows) {
+            a.row_count[b] = (uint32_t)n[0];
+            sums[0] += n[0];
+            sums[1] += n[0] > 0;
         }
     }
-    block_sum<kAll, 2>(sums, lds);
-    if (threadIdx.x == 0 && sums[0] > 0) {
-        atomicAdd(&a.head->tokens, (uint32_t)sums[0]);
-        atomicAdd(&a.head->rows, (uint32_t)sums[1]);
-    }
+    block_sum<kCountThreads, 2>(sums, lds);
+    if (threadIdx.x == 0 && sums[0] > 0)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&a.head->counts),
+                  (unsigned long long)sums[0] | (unsigned long long)sums[1] << 32);
 }
 
 }  // namespace
 
-// A row of up to 1,024 tokens takes a wavefront, up to 16,384 a workgroup of 256
-// lanes, a longer one 1,024 lanes: 16 bytes a lane and round.
+// A row of up to 16,384 tokens takes a wavefront, a longer one a workgroup; with
+// one weight for all tokens, contiguous rows are taken as parts of 16,384.
 hipError_t launch_token_count(const PolicyArgs& a, hipStream_t s) {
-    auto grid = [](int64_t want) { return dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)); };
-    const int64_t B = a.shape.B, T = a.shape.T;
-    if (a.o.reduction == CONDUIT_SEQUENCE_MEAN) {
-        if (T <= kCountBytes) hipLaunchKernelGGL((k_row_count<64, 4>), grid((B + 3) / 4), dim3(256), 0, s, a);
-        else if (T <= 16 * kCountBytes) hipLaunchKernelGGL((k_row_count<256, 1>), grid(B), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((k_row_count<1024, 1>), grid(B), dim3(1024), 0, s, a);
+    constexpr int64_t kPart = 16 * kCountThreads;
+    int64_t rows = a.shape.B, T = a.shape.T, stride = a.shape.stride, last = a.shape.T;
+    if (a.o.reduction != CONDUIT_SEQUENCE_MEAN && (stride == T || rows == 1)) {
+        const int64_t n = rows * T;
+        T = stride = n < kPart ? n : kPart;
+        rows = (n + T - 1) / T;
+        last = n - (rows - 1) * T;
+    } else if (T <= kPart) {
+        const int64_t want = (rows + kCountThreads / kWave - 1) / (kCountThreads / kWave);
+        hipLaunchKernelGGL((k_count<kWave>), dim3((unsigned)(want < kCountBlocks ? want : kCountBlocks)), dim3(kCountThreads), 0, s,
+                           a, rows, T, stride, last);
         return hipGetLastError();
     }
-    const uint32_t per_row = (uint32_t)((T + kCountBytes - 1) / kCountBytes);
-    const int64_t items = B * per_row;
-    hipLaunchKernelGGL(k_token_count, grid((items + kPolicyThreads / kWave - 1) / (kPolicyThreads / kWave)),
-                       dim3(kPolicyThreads), 0, s, a, (uint32_t)items, per_row, make_div31(per_row));
+    hipLaunchKernelGGL((k_count<kCountThreads>), dim3((unsigned)(rows < kCountBlocks ? rows : kCountBlocks)), dim3(kCountThreads),
+                       0, s, a, rows, T, stride, last);
     return hipGetLastError();
 }
 

@@ -91,11 +91,11 @@ __device__ __forceinline__ Pair pair_loss(const PreferenceArgs& a, const double 
         p.loss = off * off;
         q = 2.0 * off;
     } else {
-        // -log s(u) = max(-u, 0) + log(1 + exp(-|u|)), and s(-u) = 1 / (1 + exp(u))
-        const double e = a.smoothing, z = log1p(exp(-fabs(p.u)));
+        // with t = exp(-|u|): -log s(u) = max(-u, 0) + log(1 + t), s(u) = 1 / (1 + t) for u > 0, else t / (1 + t)
+        const double e = a.smoothing, t = exp(-fabs(p.u)), z = log1p(t), low = t / (1.0 + t), high = 1.0 / (1.0 + t);
         p.loss = (1.0 - e) * ((p.u < 0 ? -p.u : 0.0) + z);
         if (e > 0.0) p.loss += e * ((p.u > 0 ? p.u : 0.0) + z);
-        q = beta * (e / (1.0 + exp(-p.u)) - (1.0 - e) / (1.0 + exp(p.u)));
+        q = beta * (p.u > 0 ? e * high - (1.0 - e) * low : e * low - (1.0 - e) * high);
     }
     p.tokens = s[1] + s[3];
     const double each = a.scale * q / (double)a.P;

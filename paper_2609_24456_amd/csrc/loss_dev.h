@@ -43,9 +43,9 @@ struct PolicyTerms {
 // Head of a workspace: counters that every call finds and leaves at zero.
 struct WorkspaceHead {
     uint32_t ticket;
-    uint32_t tokens;  // tokens that count
-    uint32_t rows;    // rows (sequences) with at least one
-    uint32_t pad[61];
+    uint32_t reserved;
+    uint64_t counts;  // tokens that count, and from bit 32 on rows (sequences) with at least one
+    uint32_t pad[60];
 };
 static_assert(sizeof(WorkspaceHead) == 256, "workspace head");
 
@@ -131,11 +131,20 @@ constexpr float kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
+// exp(x) in a few instructions: 2^t for t = x log2(e) rounded, times 1 + ln2 r for
+// what the rounding of t (and of log2(e)) left out, so that the error does not
+// grow with x
+__device__ __forceinline__ float exp_fast(float x) {
+    const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.925963033500762e-8f;  // (the last: log2(e) - kLog2e)
+    const float e = exp2_fast(t);
+    return fabsf(t) < 1e30f ? fmaf(e, r * kLn2, e) : e;  // (r is no number beyond)
+}
+
 // exp(x) - 1 - x, x^2 / 2 at small x: the series up to x^9 below |x| = 1/2 (the
 // first term left out is x^8 * 2 / 10! of the whole, under 3e-9), where the
 // difference would cancel
-__device__ __forceinline__ float exp_remainder(float x, float em1) {
-    if (fabsf(x) >= 0.5f) return em1 - x;
+__device__ __forceinline__ float exp_remainder(float x) {
+    if (!(fabsf(x) < 0.5f)) return exp_fast(x) - 1.0f - x;
     float p = 1.0f / 362880.0f;
     p = fmaf(p, x, 1.0f / 40320.0f);
     p = fmaf(p, x, 1.0f / 5040.0f);
@@ -165,7 +174,7 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float lo
                                                   bool has_ref, float ref, float adv) {
     TokenLoss r;
     r.log_ratio = has_old ? logp - old : 0.0f;
-    r.ratio = has_old ? expf(r.log_ratio) : 1.0f;
+    r.ratio = has_old ? exp_fast(r.log_ratio) : 1.0f;
     const float plain = adv == 0.0f ? 0.0f : -adv * r.ratio;
     const float kept = r.ratio < o.lo ? o.lo : r.ratio > o.hi ? o.hi : r.ratio;
     const float bound = -adv * kept;
@@ -179,9 +188,9 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float lo
     r.slope = held ? 0.0f : plain;
     r.kl = 0.0f;
     if (has_ref) {
-        const float x = ref - logp, em1 = expm1f(x);
-        r.kl = exp_remainder(x, em1);
-        if (o.kl != 0.0f) r.slope -= o.kl * em1;
+        const float x = ref - logp;
+        r.kl = exp_remainder(x);
+        if (o.kl != 0.0f) r.slope -= o.kl * (fabsf(x) < 0.5f ? r.kl + x : exp_fast(x) - 1.0f);
     }
     return r;
 }
@@ -194,26 +203,68 @@ __device__ __forceinline__ double token_weight(const PolicyTerms& o, uint32_t to
     return 1.0 / ((double)(rows > 0 ? rows : 1) * (double)(row > 0 ? row : 1));
 }
 
-struct PolicySums {
-    double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
-    __device__ __forceinline__ void add(double w, const TokenLoss& t, float entropy) {
-        v[0] += w * t.term;
-        v[1] += w * t.kl;
-        v[2] += w * entropy;
+// A lane's sums: a few tokens of one weight in 32 bits, then in 64.
+struct TokenSums {
+    float v[kPolicySums] = {0, 0, 0, 0, 0, 0};
+    __device__ __forceinline__ void add(const TokenLoss& t, float entropy) {
+        v[0] += t.term;
+        v[1] += t.kl;
+        v[2] += entropy;
         v[3] += t.held;
         v[4] += t.log_ratio;
         v[5] += t.ratio;
     }
 };
 
+struct PolicySums {
+    double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
+    __device__ __forceinline__ void add(double w, const TokenSums& t) {
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) v[i] += i < 3 ? w * (double)t.v[i] : (double)t.v[i];
+    }
+};
+
 // ---------------------------------------------------------------------------
 // reductions in a fixed order
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, kWave);
+// one step of a butterfly over groups of LANES lanes: every lane's partner's
+// value (lanes 1, 2, 7 - i and 15 - i of a row by DPP moves, then 16 and 32 away)
+template <int STEP>
+__device__ __forceinline__ uint32_t partner(uint32_t x) {
+    constexpr int kCtrl[4] = {0xB1, 0x4E, 0x141, 0x140};  // quad_perm 1032, quad_perm 2301, row_half_mirror, row_mirror
+    if constexpr (STEP < 4) return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, kCtrl[STEP], 0xf, 0xf, false);
+    else return (uint32_t)__shfl_xor((int)x, STEP == 4 ? 16 : 32, kWave);
+}
+
+template <int STEP>
+__device__ __forceinline__ float partner(float x) {
+    return __builtin_bit_cast(float, partner<STEP>(__builtin_bit_cast(uint32_t, x)));
+}
+
+template <int STEP>
+__device__ __forceinline__ double partner(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)partner<STEP>((uint32_t)u) | (uint64_t)partner<STEP>((uint32_t)(u >> 32)) << 32);
+}
+
+// reduction over groups of LANES lanes, the same value in every lane of a group
+template <int LANES, typename T, typename Op>
+__device__ __forceinline__ T lanes_reduce(T x, Op op) {
+    if constexpr (LANES > 1) x = op(x, partner<0>(x));
+    if constexpr (LANES > 2) x = op(x, partner<1>(x));
+    if constexpr (LANES > 4) x = op(x, partner<2>(x));
+    if constexpr (LANES > 8) x = op(x, partner<3>(x));
+    if constexpr (LANES > 16) x = op(x, partner<4>(x));
+    if constexpr (LANES > 32) x = op(x, partner<5>(x));
     return x;
 }
+
+template <int LANES, typename T>
+__device__ __forceinline__ T lanes_sum(T x) {
+    return lanes_reduce<LANES>(x, [](T a, T b) { return a + b; });
+}
+
+__device__ __forceinline__ double wave_sum(double x) { return lanes_sum<kWave>(x); }
 
 // sums of N doubles over a workgroup of NT threads, in every thread (every
 // thread takes part; `lds` holds N * NT / 64 doubles and may be reused after
@@ -231,11 +282,7 @@ __device__ __forceinline__ void block_sum(double (&x)[N], double* lds) {
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        double t = 0.0;
-        for (int k = 0; k < W; ++k) t += lds[i * W + k];
-        x[i] = t;
-    }
+    for (int i = 0; i < N; ++i) x[i] = lanes_sum<W>(lds[i * W + lane_id() % W]);
     __syncthreads();
 }
 
@@ -303,7 +350,7 @@ __device__ __forceinline__ void finish_policy(const PolicyArgs& a, PolicySums& s
         block_sum<NT, kPolicySums>(t, lds);
         if (threadIdx.x == 0) write_policy_stats(a.o, t, tokens, a.stats);
     }
-    if (counted && threadIdx.x == 0) a.head->tokens = a.head->rows = 0;  // for the next call
+    if (counted && threadIdx.x == 0) a.head->counts = 0;  // for the next call
 }
 
 }  // namespace conduit

@@ -64,15 +64,16 @@ __device__ __forceinline__ void accumulate(Stat& st, const float (&x)[N], float 
     add(st, x, c);
 }
 
-__device__ __forceinline__ Stat shfl_xor(const Stat& a, int d) {
-    return Stat{__shfl_xor(a.m, d, kWave), __shfl_xor(a.s, d, kWave), __shfl_xor(a.u, d, kWave)};
-}
-
+// joined over groups of LANES lanes, in every lane: their largest maximum first,
+// then one rescaling a lane and plain sums
 template <int LANES>
-__device__ __forceinline__ Stat join_lanes(Stat s, float c) {
-#pragma unroll
-    for (int d = LANES / 2; d > 0; d >>= 1) s = join(s, shfl_xor(s, d), c);
-    return s;
+__device__ __forceinline__ Stat join_lanes(const Stat& a, float c) {
+    Stat r;
+    r.m = lanes_reduce<LANES>(a.m, [](float x, float y) { return x > y ? x : y; });
+    const float d = a.m == r.m ? 0.0f : (a.m - r.m) * c, e = exp2_fast(d), s = a.s * e;
+    r.s = lanes_sum<LANES>(s);
+    r.u = lanes_sum<LANES>(fmaf(a.u, e, s * fmaxf(d, kFloor)));
+    return r;
 }
 
 // what a row's statistics say
