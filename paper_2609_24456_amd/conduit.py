@@ -18,7 +18,11 @@ try:  # built beside libconduit.so; without it, or for another torch, every chec
     if getattr(_tensor_check, "torch_version", None) != torch.__version__:
         raise ImportError("built against another torch")
     _address = _tensor_check.address
+    _native_batch = getattr(_tensor_check, "token_batch", None)
+    _native_rows = getattr(_tensor_check, "rows", None)
 except ImportError:
+    _native_batch = _native_rows = None
+
     def _address(t, dtype, nbytes, numel):
         return None
 
@@ -491,6 +495,17 @@ def _token_ptr(t, dtype, name, batch):
     return t.data_ptr()
 
 
+def _token_ptrs(*args):
+    """(B, T, step between rows, address, address, ...) of per-token tensors given as (tensor, dtype, name) one after
+    the other, all laid out like the first.  Natively where they are plain ones (_tensor_check), else checked here."""
+    if _native_batch is not None:
+        got = _native_batch(*[a for i, a in enumerate(args) if i % 3 != 2])
+        if got is not None:
+            return got
+    batch = _batch_shape(args[0], args[2])
+    return batch[1:] + tuple(_token_ptr(args[i], args[i + 1], args[i + 2], batch) for i in range(0, len(args), 3))
+
+
 _ROW_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -510,11 +525,15 @@ def _rows_struct(t, name):
     return r
 
 
-def _rows_ptr(t, name, shape):
-    """conduit_rows of the rows of a batch whose per-token tensors have `shape`."""
+def _rows_ptr(t, name, tokens):
+    """conduit_rows of the rows of a batch whose per-token tensors are shaped like `tokens`."""
+    if _native_rows is not None:
+        r = Rows()
+        if _native_rows(C.addressof(r), t, tokens, F32, BF16):
+            return r
     r = _rows_struct(t, name)
-    if t.shape[:-1] != shape:
-        raise ValueError(f"{name} must be {tuple(shape)} rows, got {tuple(t.shape[:-1])}")
+    if t.shape[:-1] != tokens.shape:
+        raise ValueError(f"{name} must be {tuple(tokens.shape)} rows, got {tuple(t.shape[:-1])}")
     if not _on_device(t):
         raise ValueError(f"{name} must be on a HIP device")
     return r
@@ -552,28 +571,23 @@ def token_logprobs_workspace(logits):
 def conduit_token_logprobs(logits, tokens, logp, lse=None, entropy=None, mask=None, temperature=1.0, workspace=None,
                            stream=None):
     """Log-probabilities of the taken tokens, log-normalisers and entropies of logits [B, T, V]."""
-    batch = _batch_shape(tokens, "tokens")
-    x = _rows_ptr(logits, "logits", batch[0])
+    f = torch.float32
+    B, T, step, tok, lp, ls, en, mk = _token_ptrs(tokens, torch.int32, "tokens", logp, f, "logp", lse, f, "lse",
+                                                  entropy, f, "entropy", mask, _U8, "mask")
+    x = _rows_ptr(logits, "logits", tokens)
     ws, wp, wn = _workspace(workspace, lambda: token_logprobs_workspace(logits), stream)
-    _check(lib().conduit_token_logprobs(C.byref(x), batch[1], batch[2], batch[3],
-                                        _token_ptr(tokens, torch.int32, "tokens", batch),
-                                        _token_ptr(mask, _U8, "mask", batch), float(temperature),
-                                        _token_ptr(logp, torch.float32, "logp", batch),
-                                        _token_ptr(lse, torch.float32, "lse", batch),
-                                        _token_ptr(entropy, torch.float32, "entropy", batch), wp, wn, _stream(stream)))
+    _check(lib().conduit_token_logprobs(C.byref(x), B, T, step, tok, mk, temperature, lp, ls, en, wp, wn, _stream(stream)))
 
 
 def conduit_token_logprobs_backward(logits, tokens, lse, dlogp, dlogits, entropy=None, dentropy=None, mask=None,
                                     temperature=1.0, stream=None):
     """The gradient of conduit_token_logprobs's logits, into dlogits (the logits themselves: in place)."""
-    batch = _batch_shape(tokens, "tokens")
-    x, dx = _rows_ptr(logits, "logits", batch[0]), _rows_ptr(dlogits, "dlogits", batch[0])
     f = torch.float32
-    _check(lib().conduit_token_logprobs_backward(
-        C.byref(x), batch[1], batch[2], batch[3], _token_ptr(tokens, torch.int32, "tokens", batch),
-        _token_ptr(mask, _U8, "mask", batch), float(temperature), _token_ptr(lse, f, "lse", batch),
-        _token_ptr(entropy, f, "entropy", batch), _token_ptr(dlogp, f, "dlogp", batch),
-        _token_ptr(dentropy, f, "dentropy", batch), C.byref(dx), _stream(stream)))
+    B, T, step, tok, ls, g, en, h, mk = _token_ptrs(tokens, torch.int32, "tokens", lse, f, "lse", dlogp, f, "dlogp",
+                                                    entropy, f, "entropy", dentropy, f, "dentropy", mask, _U8, "mask")
+    x, dx = _rows_ptr(logits, "logits", tokens), _rows_ptr(dlogits, "dlogits", tokens)
+    _check(lib().conduit_token_logprobs_backward(C.byref(x), B, T, step, tok, mk, temperature, ls, en, g, h, C.byref(dx),
+                                                 _stream(stream)))
 
 
 def policy_opts(reduction="token_mean", **kw):
@@ -602,15 +616,13 @@ def policy_loss_workspace(B, T):
 def conduit_policy_loss(opts, logp, adv, stats, dlogp=None, old_logp=None, ref_logp=None, entropy=None, dentropy=None,
                         mask=None, workspace=None, stream=None):
     """The clipped policy loss with its KL term and entropy bonus: stats (POLICY_STATS) and gradients."""
-    batch = _batch_shape(logp, "logp")
     f = torch.float32
-    ws, wp, wn = _workspace(workspace, lambda: policy_loss_workspace(batch[1], batch[2]), stream)
-    _check(lib().conduit_policy_loss(
-        C.byref(opts), batch[1], batch[2], batch[3], _token_ptr(logp, f, "logp", batch),
-        _token_ptr(old_logp, f, "old_logp", batch), _token_ptr(ref_logp, f, "ref_logp", batch),
-        _token_ptr(adv, f, "adv", batch), _token_ptr(entropy, f, "entropy", batch),
-        _token_ptr(mask, _U8, "mask", batch), _ptr(stats, f, "stats", numel=8), _token_ptr(dlogp, f, "dlogp", batch),
-        _token_ptr(dentropy, f, "dentropy", batch), wp, wn, _stream(stream)))
+    B, T, step, lp, ad, old, rf, en, g, h, mk = _token_ptrs(
+        logp, f, "logp", adv, f, "adv", old_logp, f, "old_logp", ref_logp, f, "ref_logp", entropy, f, "entropy",
+        dlogp, f, "dlogp", dentropy, f, "dentropy", mask, _U8, "mask")
+    ws, wp, wn = _workspace(workspace, lambda: policy_loss_workspace(B, T), stream)
+    _check(lib().conduit_policy_loss(C.byref(opts), B, T, step, lp, old, rf, ad, en, mk, _ptr(stats, f, "stats", numel=8),
+                                     g, h, wp, wn, _stream(stream)))
 
 
 def policy_loss_logits_workspace(logits):
@@ -621,16 +633,14 @@ def policy_loss_logits_workspace(logits):
 def conduit_policy_loss_logits(opts, logits, tokens, adv, stats, dlogits, logp, entropy, old_logp=None, ref_logp=None,
                                mask=None, temperature=1.0, workspace=None, stream=None):
     """The policy loss from logits [B, T, V] to their gradient dlogits (the logits themselves: in place)."""
-    batch = _batch_shape(tokens, "tokens")
-    x, dx = _rows_ptr(logits, "logits", batch[0]), _rows_ptr(dlogits, "dlogits", batch[0])
     f = torch.float32
+    B, T, step, tok, ad, lp, en, old, rf, mk = _token_ptrs(
+        tokens, torch.int32, "tokens", adv, f, "adv", logp, f, "logp", entropy, f, "entropy", old_logp, f, "old_logp",
+        ref_logp, f, "ref_logp", mask, _U8, "mask")
+    x, dx = _rows_ptr(logits, "logits", tokens), _rows_ptr(dlogits, "dlogits", tokens)
     ws, wp, wn = _workspace(workspace, lambda: policy_loss_logits_workspace(logits), stream)
-    _check(lib().conduit_policy_loss_logits(
-        C.byref(opts), C.byref(x), batch[1], batch[2], batch[3], _token_ptr(tokens, torch.int32, "tokens", batch),
-        _token_ptr(old_logp, f, "old_logp", batch), _token_ptr(ref_logp, f, "ref_logp", batch),
-        _token_ptr(adv, f, "adv", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
-        _token_ptr(logp, f, "logp", batch), _token_ptr(entropy, f, "entropy", batch),
-        _ptr(stats, f, "stats", numel=8), C.byref(dx), wp, wn, _stream(stream)))
+    _check(lib().conduit_policy_loss_logits(C.byref(opts), C.byref(x), B, T, step, tok, old, rf, ad, mk, temperature, lp, en,
+                                            _ptr(stats, f, "stats", numel=8), C.byref(dx), wp, wn, _stream(stream)))
 
 
 def preference_opts(loss="sigmoid", beta=0.1, label_smoothing=0.0, scale=1.0, length_norm=False):
@@ -651,28 +661,28 @@ def preference_loss_workspace(P, T):
 def conduit_preference_loss(opts, logp, loss, stats, dlogp=None, ref_logp=None, mask=None, chosen=None, rejected=None,
                             workspace=None, stream=None):
     """The preference loss over pairs (rows i and P + i of [2 P, T]): per pair, stats (PREFERENCE_STATS), gradient."""
-    batch = _batch_shape(logp, "logp")
-    if logp.dim() != 2 or batch[1] % 2:
+    f = torch.float32
+    B, T, step, lp, rf, g, mk = _token_ptrs(logp, f, "logp", ref_logp, f, "ref_logp", dlogp, f, "dlogp", mask, _U8, "mask")
+    if logp.dim() != 2 or B % 2:
         raise ValueError("logp must be [2 P, T]: the chosen answers, then the rejected ones")
-    P, f = batch[1] // 2, torch.float32
-    ws, wp, wn = _workspace(workspace, lambda: preference_loss_workspace(P, batch[2]), stream)
+    P = B // 2
+    ws, wp, wn = _workspace(workspace, lambda: preference_loss_workspace(P, T), stream)
     _check(lib().conduit_preference_loss(
-        C.byref(opts), P, batch[2], batch[3], _token_ptr(logp, f, "logp", batch),
-        _token_ptr(ref_logp, f, "ref_logp", batch), _token_ptr(mask, _U8, "mask", batch),
-        _ptr(loss, f, "loss", numel=P), _ptr(chosen, f, "chosen", numel=P), _ptr(rejected, f, "rejected", numel=P),
-        _ptr(stats, f, "stats", numel=4), _token_ptr(dlogp, f, "dlogp", batch), wp, wn, _stream(stream)))
+        C.byref(opts), P, T, step, lp, rf, mk, _ptr(loss, f, "loss", numel=P), _ptr(chosen, f, "chosen", numel=P),
+        _ptr(rejected, f, "rejected", numel=P), _ptr(stats, f, "stats", numel=4), g, wp, wn, _stream(stream)))
 
 
-def _head_rows(hidden, weight):
+def _weight_rows(weight, name):
+    """conduit_rows of a [V, H] projection."""
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
-        raise ValueError("weight must be a [V, H] tensor")
+        raise ValueError(f"{name} must be a [V, H] tensor")
     if not _on_device(weight):
-        raise ValueError("weight must be on a HIP device")
-    return _rows_struct(hidden, "hidden"), _rows_struct(weight, "weight")
+        raise ValueError(f"{name} must be on a HIP device")
+    return _rows_struct(weight, name)
 
 
 def _head_bytes(entry, hidden, weight):
-    x, w = _head_rows(hidden, weight)
+    x, w = _rows_struct(hidden, "hidden"), _weight_rows(weight, "weight")
     n = C.c_uint64()
     B, T = (hidden.shape[0], hidden.shape[1]) if hidden.dim() == 3 else (1, hidden.shape[0])
     _check(entry(B, T, C.byref(x), C.byref(w), weight.shape[0], C.byref(n)))
@@ -692,34 +702,28 @@ def head_logprobs_backward_workspace(hidden, weight):
 def conduit_head_logprobs(hidden, weight, tokens, logp, lse=None, entropy=None, mask=None, temperature=1.0,
                           workspace=None, stream=None):
     """conduit_token_logprobs of the logits hidden [B, T, H] . weight [V, H]^T, which are never whole in memory."""
-    batch = _batch_shape(tokens, "tokens")
-    x = _rows_ptr(hidden, "hidden", batch[0])
-    _, w = _head_rows(hidden, weight)
-    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_workspace(hidden, weight), stream)
     f = torch.float32
-    _check(lib().conduit_head_logprobs(
-        C.byref(x), C.byref(w), weight.shape[0], batch[1], batch[2], batch[3],
-        _token_ptr(tokens, torch.int32, "tokens", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
-        _token_ptr(logp, f, "logp", batch), _token_ptr(lse, f, "lse", batch), _token_ptr(entropy, f, "entropy", batch),
-        wp, wn, _stream(stream)))
+    B, T, step, tok, lp, ls, en, mk = _token_ptrs(tokens, torch.int32, "tokens", logp, f, "logp", lse, f, "lse",
+                                                  entropy, f, "entropy", mask, _U8, "mask")
+    x, w = _rows_ptr(hidden, "hidden", tokens), _weight_rows(weight, "weight")
+    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_workspace(hidden, weight), stream)
+    _check(lib().conduit_head_logprobs(C.byref(x), C.byref(w), weight.shape[0], B, T, step, tok, mk, temperature, lp, ls, en,
+                                       wp, wn, _stream(stream)))
 
 
 def conduit_head_logprobs_backward(hidden, weight, tokens, lse, dlogp, dhidden, dweight, entropy=None, dentropy=None,
                                    mask=None, temperature=1.0, workspace=None, stream=None):
     """The gradients dhidden and dweight of conduit_head_logprobs."""
-    batch = _batch_shape(tokens, "tokens")
-    x, dx = _rows_ptr(hidden, "hidden", batch[0]), _rows_ptr(dhidden, "dhidden", batch[0])
-    _, w = _head_rows(hidden, weight)
-    if not isinstance(dweight, torch.Tensor) or dweight.shape != weight.shape:
-        raise ValueError("dweight must have the projection's shape")
-    _, dw = _head_rows(hidden, dweight)
-    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_backward_workspace(hidden, weight), stream)
     f = torch.float32
-    _check(lib().conduit_head_logprobs_backward(
-        C.byref(x), C.byref(w), weight.shape[0], batch[1], batch[2], batch[3],
-        _token_ptr(tokens, torch.int32, "tokens", batch), _token_ptr(mask, _U8, "mask", batch), float(temperature),
-        _token_ptr(lse, f, "lse", batch), _token_ptr(entropy, f, "entropy", batch), _token_ptr(dlogp, f, "dlogp", batch),
-        _token_ptr(dentropy, f, "dentropy", batch), C.byref(dx), C.byref(dw), wp, wn, _stream(stream)))
+    B, T, step, tok, ls, g, en, h, mk = _token_ptrs(tokens, torch.int32, "tokens", lse, f, "lse", dlogp, f, "dlogp",
+                                                    entropy, f, "entropy", dentropy, f, "dentropy", mask, _U8, "mask")
+    x, dx = _rows_ptr(hidden, "hidden", tokens), _rows_ptr(dhidden, "dhidden", tokens)
+    w, dw = _weight_rows(weight, "weight"), _weight_rows(dweight, "dweight")
+    if dweight.shape != weight.shape:
+        raise ValueError("dweight must have the projection's shape")
+    ws, wp, wn = _workspace(workspace, lambda: head_logprobs_backward_workspace(hidden, weight), stream)
+    _check(lib().conduit_head_logprobs_backward(C.byref(x), C.byref(w), weight.shape[0], B, T, step, tok, mk, temperature, ls,
+                                                en, g, h, C.byref(dx), C.byref(dw), wp, wn, _stream(stream)))
 
 
 def conduit_buffer_get_info(handle):
