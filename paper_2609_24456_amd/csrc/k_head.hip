@@ -181,10 +181,12 @@ unsigned tile_grid(int64_t row_tiles, int64_t col_tiles) {
 __device__ __forceinline__ int64_t tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
 
 // joined over the four lanes 16 apart
-__device__ __forceinline__ Stat join_quarters(Stat s, float c) {
-    s = join(s, Stat{partner<4>(s.m), partner<4>(s.s), partner<4>(s.u)}, c);
-    return join(s, Stat{partner<5>(s.m), partner<5>(s.s), partner<5>(s.u)}, c);
+template <int STEP>
+__device__ __forceinline__ Stat join_step(const Stat& s, float c) {
+    const Sides<float> m = sides<STEP>(s.m), t = sides<STEP>(s.s), u = sides<STEP>(s.u);
+    return join(Stat{m.a, t.a, u.a}, Stat{m.b, t.b, u.b}, c);
 }
+__device__ __forceinline__ Stat join_quarters(const Stat& s, float c) { return join_step<5>(join_step<4>(s, c), c); }
 
 // ---------------------------------------------------------------------------
 // forward: the statistics of a tile

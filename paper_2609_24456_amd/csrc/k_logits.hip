@@ -144,14 +144,17 @@ struct RowGrad {
 
 // what the loss of a row needs beside its log-probability, loaded ahead of it
 struct RowData {
-    float old, ref, adv;
-    double w;
+    float old, ref, adv, w;
+    bool has_old, has_ref;
 };
 
 __device__ __forceinline__ RowData row_data(const PolicyArgs& p, int64_t at, uint32_t b) {
     RowData d;
-    d.old = p.old_logp ? p.old_logp[at] : 0.0f;
-    d.ref = p.ref_logp ? p.ref_logp[at] : 0.0f;
+    // (an absent policy's is logp itself, which the call has yet to write)
+    d.has_old = p.old_logp != p.logp;
+    d.has_ref = p.ref_logp != p.logp;
+    d.old = p.old_logp[at];
+    d.ref = p.ref_logp[at];
     d.adv = p.adv[at];
     uint32_t tokens = (uint32_t)(p.shape.B * p.shape.T), rows = (uint32_t)p.shape.B, row = (uint32_t)p.shape.T;
     if (p.mask) {
@@ -165,8 +168,8 @@ __device__ __forceinline__ RowData row_data(const PolicyArgs& p, int64_t at, uin
 }
 
 __device__ __forceinline__ RowGrad row_loss(const PolicyArgs& p, const RowData& d, float logp, TokenLoss* out) {
-    const TokenLoss t = policy_token(p.o, logp, p.old_logp != nullptr, d.old, p.ref_logp != nullptr, d.ref, d.adv);
-    const float wf = (float)(d.w * p.o.scale);
+    const TokenLoss t = policy_token(p.o, logp, d.has_old ? d.old : logp, d.has_ref ? d.ref : logp, d.adv);
+    const float wf = (float)((double)d.w * p.o.scale);
     if (out) *out = t;
     return RowGrad{wf * t.slope, -p.o.ent * wf};
 }
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
                 rg = row_loss(p, rd, r.logp, &t);
                 if (l == 0) {
                     TokenSums one;
-                    one.add(t, r.entropy);
+                    one.add(true, t, r.entropy);
                     sums.add(rd.w, one);
                 }
             }
@@ -275,8 +278,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const int32_t tok = a.tokens[at];  // (beside the mask's load, not after it)
     const bool on = !a.mask || a.mask[at];
-    const int32_t tok = on ? a.tokens[at] : 0;
     const bool ok = on && (tid != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
     T* dx = MODE == LOSS ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
     if (!ok) {

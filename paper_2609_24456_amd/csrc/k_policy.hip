@@ -19,7 +19,7 @@ namespace conduit {
 
 namespace {
 
-constexpr int kPolicyThreads = 256;
+constexpr int kPolicyThreads = 512;
 constexpr int kSmallThreads = 1024;
 constexpr int kChunk = 4;             // tokens a lane takes at once
 constexpr int kSmallChunks = 2048;    // most chunks, and most rows, that one workgroup takes by itself
@@ -33,15 +33,6 @@ struct Chunks {
     Div31 by_row;
 };
 
-__device__ __forceinline__ void load4(const float* p, int n, float (&v)[kChunk]) {
-    if (n == kChunk) {
-        __builtin_memcpy(v, p, 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = i < n ? p[i] : 0.0f;
-    }
-}
-
 __device__ __forceinline__ void store4(float* p, int n, const float (&v)[kChunk]) {
     if (n == kChunk) {
         __builtin_memcpy(p, v, 16);
@@ -52,15 +43,9 @@ __device__ __forceinline__ void store4(float* p, int n, const float (&v)[kChunk]
     }
 }
 
-__device__ __forceinline__ uint32_t load_mask4(const uint8_t* p, int n) {
+__device__ __forceinline__ uint32_t mask_tail(const uint8_t* p, int n) {
     uint32_t m = 0;
-    if (n == kChunk) {
-        __builtin_memcpy(&m, p, 4);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (i < n) m |= (uint32_t)p[i] << (8 * i);
-    }
+    for (int i = 0; i < n; ++i) m |= (uint32_t)p[i] << (8 * i);
     return m;
 }
 
@@ -84,12 +69,27 @@ __device__ __forceinline__ ChunkData load_chunk(const PolicyArgs& a, const Chunk
     const int64_t t = (int64_t)(c - d.row * ch.per_row) * kChunk;
     d.at = (int64_t)d.row * a.shape.stride + t;
     d.n = ch.T - t < kChunk ? (int)(ch.T - t) : kChunk;
-    d.mask = a.mask ? load_mask4(a.mask + d.at, d.n) : 0x01010101u;
-    load4(a.logp + d.at, d.n, d.lp);
-    load4(a.adv + d.at, d.n, d.adv);
-    if (a.old_logp) load4(a.old_logp + d.at, d.n, d.old);
-    if (a.ref_logp) load4(a.ref_logp + d.at, d.n, d.ref);
-    if (a.entropy) load4(a.entropy + d.at, d.n, d.ent);
+    // one branch around all loads: a branch at each would wait for each
+    if (d.n == kChunk) {
+        d.mask = 0x01010101u;
+        if (a.mask) __builtin_memcpy(&d.mask, a.mask + d.at, 4);
+        __builtin_memcpy(d.lp, a.logp + d.at, 16);
+        __builtin_memcpy(d.adv, a.adv + d.at, 16);
+        __builtin_memcpy(d.old, a.old_logp + d.at, 16);
+        __builtin_memcpy(d.ref, a.ref_logp + d.at, 16);
+        __builtin_memcpy(d.ent, a.entropy + d.at, 16);
+    } else {
+        d.mask = a.mask ? mask_tail(a.mask + d.at, d.n) : 0x01010101u;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const int64_t k = d.at + (i < d.n ? i : 0);
+            d.lp[i] = a.logp[k];
+            d.adv[i] = a.adv[k];
+            d.old[i] = a.old_logp[k];
+            d.ref[i] = a.ref_logp[k];
+            d.ent[i] = a.entropy[k];
+        }
+    }
     return d;
 }
 
@@ -98,29 +98,29 @@ __device__ __forceinline__ ChunkData load_chunk_mask(const PolicyArgs& a, const 
     d.row = div31(c, ch.by_row);
     const int64_t t = (int64_t)(c - d.row * ch.per_row) * kChunk;
     d.n = ch.T - t < kChunk ? (int)(ch.T - t) : kChunk;
-    d.mask = load_mask4(a.mask + (int64_t)d.row * a.shape.stride + t, d.n);
+    const uint8_t* p = a.mask + (int64_t)d.row * a.shape.stride + t;
+    if (d.n == kChunk) __builtin_memcpy(&d.mask, p, 4);
+    else d.mask = mask_tail(p, d.n);
     return d;
 }
 
-__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, const ChunkData& d, double w, PolicySums& sums) {
-    const float wf = (float)(w * a.o.scale), we = -a.o.ent * wf;
+__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, const ChunkData& d, float w, PolicySums& sums) {
+    const float wf = (float)((double)w * a.o.scale), we = -a.o.ent * wf;
     float g[kChunk], h[kChunk];
     TokenSums few;
+    int32_t tok[kChunk];
+    if (a.tokens) {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) tok[i] = i < d.n ? a.tokens[d.at + i] : -1;
+    }
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) {
-        g[i] = h[i] = 0.0f;
-        bool on = i < d.n && (d.mask >> (8 * i) & 255u) != 0;
-        if (on && a.tokens) {
-            const int32_t tok = a.tokens[d.at + i];
-            on = tok >= 0 && tok < a.V;
-        }
-        if (on) {
-            const TokenLoss t = policy_token(a.o, d.lp[i], a.old_logp != nullptr, d.old[i], a.ref_logp != nullptr, d.ref[i], d.adv[i]);
-            few.add(t, a.entropy ? d.ent[i] : 0.0f);
-            g[i] = wf * t.slope;
-            h[i] = we;
-        }
-        __builtin_amdgcn_sched_barrier(0);  // one token after the other: interleaved, they would need twice the registers
+        bool on = (i < d.n) & ((d.mask >> (8 * i) & 255u) != 0);
+        if (a.tokens) on = on & (tok[i] >= 0) & (tok[i] < a.V);
+        const TokenLoss t = policy_token(a.o, d.lp[i], d.old[i], d.ref[i], d.adv[i]);
+        few.add(on, t, a.has_entropy ? d.ent[i] : 0.0f);
+        g[i] = on ? wf * t.slope : 0.0f;
+        h[i] = on ? we : 0.0f;
     }
     sums.add(w, few);
     if (a.dlogp) store4(a.dlogp + d.at, d.n, g);
@@ -157,10 +157,10 @@ __global__ __launch_bounds__(NT) void k_policy_loss(PolicyArgs a, Chunks ch, boo
         rows = (uint32_t)(counts >> 32);
     }
     PolicySums sums;
-    const double flat = token_weight(a.o, tokens, rows, (uint32_t)a.shape.T);
+    const float flat = token_weight(a.o, tokens, rows, (uint32_t)a.shape.T);
     for (uint32_t c = first; c < ch.total; c += step) {
         if (c != first) d = load_chunk(a, ch, c);
-        double w = flat;
+        float w = flat;
         if (a.o.reduction == CONDUIT_SEQUENCE_MEAN && a.mask)
             w = token_weight(a.o, tokens, rows, SMALL ? s_count[d.row] : a.row_count[d.row]);
         policy_chunk(a, d, w, sums);
@@ -244,6 +244,8 @@ hipError_t launch_token_count(const PolicyArgs& a, hipStream_t s) {
 // counted: the counts stand in the workspace already (and are cleared here)
 hipError_t launch_policy_loss(const PolicyArgs& args, bool counted, hipStream_t s) {
     PolicyArgs a = args;
+    a.has_entropy = a.entropy != nullptr;
+    if (!a.entropy) a.entropy = a.logp;  // (read, not used)
     // rows that follow each other without a gap are one, unless each has its own weight
     if (a.shape.stride == a.shape.T && (a.o.reduction != CONDUIT_SEQUENCE_MEAN || !a.mask))
         a.shape = make_shape(1, a.shape.B * a.shape.T, a.shape.B * a.shape.T);

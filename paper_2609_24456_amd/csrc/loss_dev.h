@@ -56,10 +56,11 @@ struct PolicyArgs {
     TokenShape shape;
     PolicyTerms o;
     const float* logp;
-    const float* old_logp;
-    const float* ref_logp;
+    const float* old_logp;  // (absent: logp)
+    const float* ref_logp;  // (absent: logp)
     const float* adv;
     const float* entropy;
+    bool has_entropy;
     const uint8_t* mask;
     const int32_t* tokens;  // with V: tokens outside [0, V) add nothing (NULL: every token is valid)
     int64_t V;
@@ -140,11 +141,10 @@ __device__ __forceinline__ float exp_fast(float x) {
     return fabsf(t) < 1e30f ? fmaf(e, r * kLn2, e) : e;  // (r is no number beyond)
 }
 
-// exp(x) - 1 - x, x^2 / 2 at small x: the series up to x^9 below |x| = 1/2 (the
-// first term left out is x^8 * 2 / 10! of the whole, under 3e-9), where the
-// difference would cancel
-__device__ __forceinline__ float exp_remainder(float x) {
-    if (!(fabsf(x) < 0.5f)) return exp_fast(x) - 1.0f - x;
+// k = exp(x) - 1 - x (x^2 / 2 at small x) and em1 = exp(x) - 1: the series up to
+// x^9 below |x| = 1/2 (the first term left out is x^8 * 2 / 10! of the whole,
+// under 3e-9), where the difference would cancel
+__device__ __forceinline__ void exp_remainder(float x, float* k, float* em1) {
     float p = 1.0f / 362880.0f;
     p = fmaf(p, x, 1.0f / 40320.0f);
     p = fmaf(p, x, 1.0f / 5040.0f);
@@ -153,7 +153,11 @@ __device__ __forceinline__ float exp_remainder(float x) {
     p = fmaf(p, x, 1.0f / 24.0f);
     p = fmaf(p, x, 1.0f / 6.0f);
     p = fmaf(p, x, 0.5f);
-    return p * x * x;
+    p = p * x * x;
+    const float e = exp_fast(x) - 1.0f;
+    const bool small = fabsf(x) < 0.5f;
+    *k = small ? p : e - x;
+    *em1 = small ? p + x : e;
 }
 
 // ---------------------------------------------------------------------------
@@ -168,94 +172,111 @@ struct TokenLoss {
 // r = exp(logp - old); term = max(-A r, -A clip(r, lo, hi)), and where A < 0
 // at most -A dual; kl = exp(ref - logp) - (ref - logp) - 1.  A NaN stays one
 // (no fmax, which would drop it); an advantage of 0 has no term however large
-// the ratio.  The old log-probability may be absent (r = 1: the policy that
-// acted is the one that learns), and so may the reference (kl = 0).
-__device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float logp, bool has_old, float old,
-                                                  bool has_ref, float ref, float adv) {
+// the ratio.  Equal log-probabilities, -inf among them, have ratio 1 and kl 0,
+// so an absent old or reference policy is passed as logp itself.  Without
+// branches: the lanes of a wavefront hold tokens of every kind.
+__device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float logp, float old, float ref, float adv) {
     TokenLoss r;
-    r.log_ratio = has_old ? logp - old : 0.0f;
-    r.ratio = has_old ? exp_fast(r.log_ratio) : 1.0f;
+    r.log_ratio = logp == old ? 0.0f : logp - old;
+    r.ratio = exp_fast(r.log_ratio);
     const float plain = adv == 0.0f ? 0.0f : -adv * r.ratio;
     const float kept = r.ratio < o.lo ? o.lo : r.ratio > o.hi ? o.hi : r.ratio;
-    const float bound = -adv * kept;
-    bool held = bound > plain;
-    r.term = held ? bound : plain;
-    if (o.dual > 0.0f && adv < 0.0f && r.term > -adv * o.dual) {
-        r.term = -adv * o.dual;
-        held = true;
-    }
-    r.held = held ? 1.0f : 0.0f;
-    r.slope = held ? 0.0f : plain;
-    r.kl = 0.0f;
-    if (has_ref) {
-        const float x = ref - logp;
-        r.kl = exp_remainder(x);
-        if (o.kl != 0.0f) r.slope -= o.kl * (fabsf(x) < 0.5f ? r.kl + x : exp_fast(x) - 1.0f);
-    }
+    const float bound = -adv * kept, ceiling = -adv * o.dual;
+    const bool held = bound > plain;
+    const float term = held ? bound : plain;
+    const bool dual = (o.dual > 0.0f) & (adv < 0.0f) & (term > ceiling);
+    r.term = dual ? ceiling : term;
+    r.held = held | dual ? 1.0f : 0.0f;
+    const float x = ref == logp ? 0.0f : ref - logp;
+    float em1;
+    exp_remainder(x, &r.kl, &em1);
+    r.slope = held | dual ? 0.0f : plain;
+    r.slope = o.kl != 0.0f ? fmaf(-o.kl, em1, r.slope) : r.slope;
     return r;
 }
 
 // weight of a token: of the mean over tokens, of the mean over rows of each
 // row's mean, or 1
-__device__ __forceinline__ double token_weight(const PolicyTerms& o, uint32_t tokens, uint32_t rows, uint32_t row) {
-    if (o.reduction == CONDUIT_SUM) return 1.0;
-    if (o.reduction == CONDUIT_TOKEN_MEAN) return 1.0 / (double)(tokens > 0 ? tokens : 1);
-    return 1.0 / ((double)(rows > 0 ? rows : 1) * (double)(row > 0 ? row : 1));
+__device__ __forceinline__ float token_weight(const PolicyTerms& o, uint32_t tokens, uint32_t rows, uint32_t row) {
+    if (o.reduction == CONDUIT_SUM) return 1.0f;
+    if (o.reduction == CONDUIT_TOKEN_MEAN) return 1.0f / (float)(tokens > 0 ? tokens : 1);
+    return 1.0f / ((float)(rows > 0 ? rows : 1) * (float)(row > 0 ? row : 1));
 }
 
 // A lane's sums: a few tokens of one weight in 32 bits, then in 64.
 struct TokenSums {
     float v[kPolicySums] = {0, 0, 0, 0, 0, 0};
-    __device__ __forceinline__ void add(const TokenLoss& t, float entropy) {
-        v[0] += t.term;
-        v[1] += t.kl;
-        v[2] += entropy;
-        v[3] += t.held;
-        v[4] += t.log_ratio;
-        v[5] += t.ratio;
+    __device__ __forceinline__ void add(bool on, const TokenLoss& t, float entropy) {
+        v[0] += on ? t.term : 0.0f;
+        v[1] += on ? t.kl : 0.0f;
+        v[2] += on ? entropy : 0.0f;
+        v[3] += on ? t.held : 0.0f;
+        v[4] += on ? t.log_ratio : 0.0f;
+        v[5] += on ? t.ratio : 0.0f;
     }
 };
 
 struct PolicySums {
     double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
-    __device__ __forceinline__ void add(double w, const TokenSums& t) {
+    __device__ __forceinline__ void add(float w, const TokenSums& t) {
 #pragma unroll
-        for (int i = 0; i < kPolicySums; ++i) v[i] += i < 3 ? w * (double)t.v[i] : (double)t.v[i];
+        for (int i = 0; i < kPolicySums; ++i) v[i] += i < 3 ? (double)w * (double)t.v[i] : (double)t.v[i];
     }
 };
 
 // ---------------------------------------------------------------------------
 // reductions in a fixed order
 // ---------------------------------------------------------------------------
-// one step of a butterfly over groups of LANES lanes: every lane's partner's
-// value (lanes 1, 2, 7 - i and 15 - i of a row by DPP moves, then 16 and 32 away)
+// The two sides of one step of a butterfly, in every lane: its own value and the
+// lane's 1 or 2 away, or mirrored in its 8 or 16 (DPP moves), then, by swaps of
+// rows, those of the even and the odd row of 16 and of the two halves.
+template <typename T>
+struct Sides {
+    T a, b;
+};
+
 template <int STEP>
-__device__ __forceinline__ uint32_t partner(uint32_t x) {
+__device__ __forceinline__ Sides<uint32_t> sides(uint32_t x) {
     constexpr int kCtrl[4] = {0xB1, 0x4E, 0x141, 0x140};  // quad_perm 1032, quad_perm 2301, row_half_mirror, row_mirror
-    if constexpr (STEP < 4) return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, kCtrl[STEP], 0xf, 0xf, false);
-    else return (uint32_t)__shfl_xor((int)x, STEP == 4 ? 16 : 32, kWave);
+    if constexpr (STEP < 4) {
+        return {x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl[STEP], 0xf, 0xf, true)};
+    } else {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 r = STEP == 4 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false))
+                                  : __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, x, false, false));
+        return {r.x, r.y};
+    }
 }
 
 template <int STEP>
-__device__ __forceinline__ float partner(float x) {
-    return __builtin_bit_cast(float, partner<STEP>(__builtin_bit_cast(uint32_t, x)));
+__device__ __forceinline__ Sides<float> sides(float x) {
+    const Sides<uint32_t> r = sides<STEP>(__builtin_bit_cast(uint32_t, x));
+    return {__builtin_bit_cast(float, r.a), __builtin_bit_cast(float, r.b)};
 }
 
 template <int STEP>
-__device__ __forceinline__ double partner(double x) {
+__device__ __forceinline__ Sides<double> sides(double x) {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    return __builtin_bit_cast(double, (uint64_t)partner<STEP>((uint32_t)u) | (uint64_t)partner<STEP>((uint32_t)(u >> 32)) << 32);
+    const Sides<uint32_t> lo = sides<STEP>((uint32_t)u), hi = sides<STEP>((uint32_t)(u >> 32));
+    return {__builtin_bit_cast(double, (uint64_t)lo.a | (uint64_t)hi.a << 32),
+            __builtin_bit_cast(double, (uint64_t)lo.b | (uint64_t)hi.b << 32)};
+}
+
+template <int STEP, typename T, typename Op>
+__device__ __forceinline__ T reduce_step(T x, Op op) {
+    const Sides<T> r = sides<STEP>(x);
+    return op(r.a, r.b);
 }
 
 // reduction over groups of LANES lanes, the same value in every lane of a group
 template <int LANES, typename T, typename Op>
 __device__ __forceinline__ T lanes_reduce(T x, Op op) {
-    if constexpr (LANES > 1) x = op(x, partner<0>(x));
-    if constexpr (LANES > 2) x = op(x, partner<1>(x));
-    if constexpr (LANES > 4) x = op(x, partner<2>(x));
-    if constexpr (LANES > 8) x = op(x, partner<3>(x));
-    if constexpr (LANES > 16) x = op(x, partner<4>(x));
-    if constexpr (LANES > 32) x = op(x, partner<5>(x));
+    if constexpr (LANES > 1) x = reduce_step<0>(x, op);
+    if constexpr (LANES > 2) x = reduce_step<1>(x, op);
+    if constexpr (LANES > 4) x = reduce_step<2>(x, op);
+    if constexpr (LANES > 8) x = reduce_step<3>(x, op);
+    if constexpr (LANES > 16) x = reduce_step<4>(x, op);
+    if constexpr (LANES > 32) x = reduce_step<5>(x, op);
     return x;
 }
 
@@ -287,8 +308,8 @@ __device__ __forceinline__ void block_sum(double (&x)[N], double* lds) {
 }
 
 // Last arrival of a launch's workgroups: true in every thread of the one that
-// drew the last of `total` tickets.  What thread 0 stored with store_agent
-// before is at the device's point of coherence by then (its stores are waited
+// drew the last of `total` tickets.  What the first wavefront stored with
+// store_agent before is at the device's point of coherence by then (its stores are waited
 // for before the ticket is drawn), where load_agent reads it, so no fence, and
 // with it no write-back of the L2 under the outputs, is needed.  The ticket is
 // left at 0.
@@ -327,25 +348,43 @@ __device__ __forceinline__ void write_policy_stats(const PolicyTerms& o, const d
     stats[7] = (float)tokens;
 }
 
-// A workgroup's sums into its slot; the last workgroup adds the slots up (each
-// thread some of them, then block_sum: a fixed order), writes the statistics
-// and clears the counters.
+// A wavefront's lanes are added up in 32 bits (a tree of 64 values: six
+// roundings), everything above in 64: lane i of the first wavefront adds the
+// wavefronts' i-th sums and stores them in the workgroup's slot; the last
+// workgroup adds the slots up, in a fixed order, writes the statistics and
+// clears the counters.
 template <int NT>
-__device__ __forceinline__ void finish_policy(const PolicyArgs& a, PolicySums& s, uint32_t tokens, bool counted,
+__device__ __forceinline__ void finish_policy(const PolicyArgs& a, const PolicySums& s, uint32_t tokens, bool counted,
                                               double* lds) {
-    block_sum<NT, kPolicySums>(s.v, lds);
-    if (gridDim.x == 1) {
-        if (threadIdx.x == 0) write_policy_stats(a.o, s.v, tokens, a.stats);
-    } else {
-        if (threadIdx.x == 0) {
+    constexpr int W = NT / kWave;
+    float v[kPolicySums];
 #pragma unroll
-            for (int i = 0; i < kPolicySums; ++i) store_agent(a.partial + (int64_t)blockIdx.x * kPolicySums + i, s.v[i]);
-        }
+    for (int i = 0; i < kPolicySums; ++i) v[i] = lanes_sum<kWave>((float)s.v[i]);
+    if (lane_id() == 0) {
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) lds[i * W + threadIdx.x / kWave] = v[i];
+    }
+    __syncthreads();
+    double mine = 0.0;
+    if (threadIdx.x < kPolicySums) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) mine += lds[threadIdx.x * W + k];
+    }
+    if (gridDim.x == 1) {
+        __syncthreads();
+        if (threadIdx.x < kPolicySums) lds[threadIdx.x] = mine;
+        __syncthreads();
+        if (threadIdx.x == 0) write_policy_stats(a.o, lds, tokens, a.stats);
+    } else {
+        if (threadIdx.x < kPolicySums) store_agent(a.partial + (int64_t)blockIdx.x * kPolicySums + threadIdx.x, mine);
         if (!last_block(&a.head->ticket, gridDim.x)) return;
         double t[kPolicySums] = {0, 0, 0, 0, 0, 0};
         for (uint32_t k = threadIdx.x; k < gridDim.x; k += NT) {
+            double p[kPolicySums];
 #pragma unroll
-            for (int i = 0; i < kPolicySums; ++i) t[i] += load_agent(a.partial + (int64_t)k * kPolicySums + i);
+            for (int i = 0; i < kPolicySums; ++i) p[i] = load_agent(a.partial + (int64_t)k * kPolicySums + i);
+#pragma unroll
+            for (int i = 0; i < kPolicySums; ++i) t[i] += p[i];
         }
         block_sum<NT, kPolicySums>(t, lds);
         if (threadIdx.x == 0) write_policy_stats(a.o, t, tokens, a.stats);

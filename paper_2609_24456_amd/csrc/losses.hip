@@ -418,8 +418,8 @@ conduit_status conduit_policy_loss(const conduit_policy_opts* opts, int64_t B, i
     if (B == 0 || T == 0) B = T = stride = 0;
     p.shape = make_shape(B, T, stride);
     p.logp = logp;
-    p.old_logp = old_logp;
-    p.ref_logp = ref_logp;
+    p.old_logp = old_logp ? old_logp : logp;
+    p.ref_logp = ref_logp ? ref_logp : logp;
     p.adv = adv;
     p.entropy = entropy;
     p.mask = mask;
@@ -475,8 +475,8 @@ conduit_status conduit_policy_loss_logits(const conduit_policy_opts* opts, const
     place_workspace(a, workspace, l);
     p.shape = a.shape;
     p.logp = logp;
-    p.old_logp = old_logp;
-    p.ref_logp = ref_logp;
+    p.old_logp = old_logp ? old_logp : logp;
+    p.ref_logp = ref_logp ? ref_logp : logp;
     p.adv = adv;
     p.entropy = entropy;
     p.mask = mask;
