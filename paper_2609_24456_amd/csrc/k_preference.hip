@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kPairThreads) void k_preference(PreferenceArgs a) {
         write_gradient(a, p, 0, a.T, (float)x.q_chosen);
         write_gradient(a, a.P + p, 0, a.T, (float)x.q_rejected);
     }
-    if (last_block(&a.head->ticket, gridDim.x)) write_means(a, lds);
+    if (last_block(a.head, blockIdx.x, gridDim.x)) write_means(a, lds);
 }
 
 // parts of rows: grid (parts, 2 P)
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kPairThreads) void k_preference_join(PreferenceArgs
                        (float)(b < a.P ? x.q_chosen : x.q_rejected));
     if (blockIdx.x == 0 && b < a.P) {  // one workgroup a pair
         if (threadIdx.x == 0) write_pair(a, p, x);
-        if (last_block(&a.head->ticket, (uint32_t)a.P)) write_means(a, lds);
+        if (last_block(a.head, (uint32_t)p, (uint32_t)a.P)) write_means(a, lds);
     }
 }
 

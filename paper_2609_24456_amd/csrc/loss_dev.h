@@ -41,13 +41,17 @@ struct PolicyTerms {
 };
 
 // Head of a workspace: counters that every call finds and leaves at zero.
+constexpr int kTicketGroups = 32;
 struct WorkspaceHead {
-    uint32_t ticket;
-    uint32_t reserved;
     uint64_t counts;  // tokens that count, and from bit 32 on rows (sequences) with at least one
-    uint32_t pad[60];
+    uint32_t ticket;
+    uint32_t pad[61];
+    struct {
+        uint32_t ticket;
+        uint32_t pad[31];
+    } group[kTicketGroups];  // a cache line each
 };
-static_assert(sizeof(WorkspaceHead) == 256, "workspace head");
+static_assert(sizeof(WorkspaceHead) == 256 + 128 * kTicketGroups, "workspace head");
 
 constexpr int kPolicySums = 6;     // weighted loss, KL and entropy; clipped, log ratio and ratio
 constexpr int kPolicyBlocks = 512; // most workgroups that a sum over the tokens is spread over
@@ -308,11 +312,13 @@ __device__ __forceinline__ void block_sum(double (&x)[N], double* lds) {
 }
 
 // Last arrival of a launch's workgroups: true in every thread of the one that
-// drew the last of `total` tickets.  What the first wavefront stored with
-// store_agent before is at the device's point of coherence by then (its stores are waited
-// for before the ticket is drawn), where load_agent reads it, so no fence, and
-// with it no write-back of the L2 under the outputs, is needed.  The ticket is
-// left at 0.
+// drew the last ticket.  What the first wavefront stored with store_agent before
+// is at the device's point of coherence by then (its stores are waited for
+// before the ticket is drawn), where load_agent reads it, so no fence, and with
+// it no write-back of the L2 under the outputs, is needed.  An atomic on one word
+// takes 13 ns after the one before it (512 workgroups: 7 us), so more than 32
+// workgroups draw from 32 words, and the last of each from the common one.  The
+// tickets are left at 0.
 __device__ __forceinline__ void store_agent(double* p, double v) {
     __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -320,13 +326,24 @@ __device__ __forceinline__ double load_agent(const double* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-__device__ __forceinline__ bool last_block(uint32_t* ticket, uint32_t total) {
+__device__ __forceinline__ bool draw_last(uint32_t* ticket, uint32_t total) {
+    const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == total - 1;
+    if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return last;
+}
+
+__device__ __forceinline__ bool last_block(WorkspaceHead* head, uint32_t block, uint32_t total) {
     __shared__ bool s_last;
     if (threadIdx.x == 0) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores above are acknowledged
-        const uint32_t t = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = t == total - 1;
-        if (s_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        bool last = true;
+        uint32_t words = total;
+        if (total > kTicketGroups) {
+            const uint32_t g = block % kTicketGroups;
+            last = draw_last(&head->group[g].ticket, (total - g + kTicketGroups - 1) / kTicketGroups);
+            words = kTicketGroups;
+        }
+        s_last = last && draw_last(&head->ticket, words);
     }
     __syncthreads();
     return s_last;
@@ -377,7 +394,7 @@ __device__ __forceinline__ void finish_policy(const PolicyArgs& a, const PolicyS
         if (threadIdx.x == 0) write_policy_stats(a.o, lds, tokens, a.stats);
     } else {
         if (threadIdx.x < kPolicySums) store_agent(a.partial + (int64_t)blockIdx.x * kPolicySums + threadIdx.x, mine);
-        if (!last_block(&a.head->ticket, gridDim.x)) return;
+        if (!last_block(a.head, blockIdx.x, gridDim.x)) return;
         double t[kPolicySums] = {0, 0, 0, 0, 0, 0};
         for (uint32_t k = threadIdx.x; k < gridDim.x; k += NT) {
             double p[kPolicySums];
