@@ -191,48 +191,63 @@ __device__ __forceinline__ Stat join_quarters(const Stat& s, float c) { return j
 // ---------------------------------------------------------------------------
 // forward: the statistics of a tile
 // ---------------------------------------------------------------------------
+// The statistics of ROWS x 16 choices of one token in four lanes 16 apart: lane
+// group q holds choices 16 i + 4 q + j as x[i][j].  `first` is the first choice
+// of this lane's; the taken token's score is left in `taken` where it is here.
+template <int ROWS>
+__device__ __forceinline__ Stat score_stat(f32x4_t (&x)[ROWS], int64_t first, int64_t V, int32_t tok, float c, float* taken) {
+    // places of this lane's choices below the last one, and of the taken one
+    const int32_t end = V - first < 16 * ROWS ? (int32_t)(V - first) : 16 * ROWS;
+    const int64_t from = (int64_t)tok - first;
+    const int32_t at = from >= 0 && from < 16 * ROWS ? (int32_t)from : -1;
+    float top = kNone, xt = 0.0f;
+    bool here = false;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (i * 16 + j >= end) x[i][j] = kNone;
+            if (i * 16 + j == at) {
+                xt = x[i][j];
+                here = true;
+            }
+            top = fmaxf(top, x[i][j]);
+        }
+    }
+    if (here) *taken = xt;
+    Stat st = no_stat();
+    raise(st, top, c);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const float v[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+        add(st, v, c);
+    }
+    return join_quarters(st, c);
+}
+
 __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
     const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(a.V), (int32_t)tiles(n));
     if (!tp.ok) return;
     const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+    int32_t tok[4];  // ahead of the product, which hides the loads
+#pragma unroll
+    for (int ni = 0; ni < 4; ++ni) {
+        const int64_t k = n0 + wn * 64 + ni * 16 + col;
+        tok[ni] = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
+    }
     GemmAcc acc;
     gemm_tile(a.W, v0, a.V, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
-    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
     Stat* stat = reinterpret_cast<Stat*>(lds);  // [2][256]
 #pragma unroll
     for (int ni = 0; ni < 4; ++ni) {
         const int64_t k = n0 + wn * 64 + ni * 16 + col;
-        const int32_t tok = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
-        const int64_t first = v0 + wm * 128 + 4 * q;
-        // places of this lane's choices below the last one, and of the taken one
-        const int32_t end = a.V - first < 256 ? (int32_t)(a.V - first) : 256;
-        const int64_t from = (int64_t)tok - first;
-        const int32_t at = from >= 0 && from < 128 ? (int32_t)from : -1;
-        float top = kNone, xt = 0.0f;
-        bool here = false;
+        f32x4_t x[8];
 #pragma unroll
-        for (int mi = 0; mi < 8; ++mi) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (mi * 16 + i >= end) acc.c[mi][ni][i] = kNone;
-                if (mi * 16 + i == at) {
-                    xt = acc.c[mi][ni][i];
-                    here = true;
-                }
-                top = fmaxf(top, acc.c[mi][ni][i]);
-            }
-        }
-        if (here) a.taken[k] = xt;
-        Stat st = no_stat();
-        raise(st, top, a.c);
-#pragma unroll
-        for (int mi = 0; mi < 8; ++mi) {
-            const float x[4] = {acc.c[mi][ni][0], acc.c[mi][ni][1], acc.c[mi][ni][2], acc.c[mi][ni][3]};
-            add(st, x, a.c);
-        }
-        st = join_quarters(st, a.c);
+        for (int mi = 0; mi < 8; ++mi) x[mi] = acc.c[mi][ni];
+        const Stat st = score_stat<8>(x, v0 + wm * 128 + 4 * q, a.V, tok[ni], a.c, a.taken + k);
         if (q == 0) stat[wm * kGemmTile + wn * 64 + ni * 16 + col] = st;
     }
     __syncthreads();
@@ -245,10 +260,82 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
     }
 }
 
-// a token's tiles joined: 16 tokens a workgroup, 16 lanes each
+// The same for at most 16 tokens, which W's bytes bound: a wavefront takes 64
+// choices and reads its rows of W straight into registers, a set of kFewSteps x
+// 32 hidden units ahead of the one it multiplies, without LDS or barriers.  The
+// hidden states come out of the caches, a quarter as many bytes again: with 32
+// tokens they would be half, and the tiles of 256 are as fast (16 tokens of 2,048
+// units, 128,000 choices: 119 us, 4.4 TB/s, against 150; 32 tokens 147 against 138).
+constexpr int kFewThreads = 256;
+constexpr int kFewTokens = 16;
+constexpr int kFewSteps = 4;
+
+__global__ __launch_bounds__(kFewThreads) void k_head_stats_few(HeadArgs a) {
+    __shared__ Stat stat[kFewThreads / kWave][kFewTokens];
+    const int64_t n = live_tokens(a);
+    if (n == 0) return;
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, col = lane % 16;
+    const int64_t v0 = (int64_t)blockIdx.x * kGemmTile + w * 64;
+    __amdgpu_buffer_rsrc_t rw =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.W.p + v0 * a.W.ld), 0, 0x7fffffff, 0x00027000);
+    __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.X.p), 0, 0x7fffffff, 0x00027000);
+    uint32_t vw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vw[i] = v0 + i * 16 + col < a.V ? (uint32_t)((i * 16 + col) * a.W.ld * 2 + q * 16) : kGemmOut;
+    const uint32_t vx = col < n ? (uint32_t)(col * a.X.ld * 2 + q * 16) : kGemmOut;
+    const int32_t tok = col < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[col] : col))] : -1;
+    f32x4_t acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
+    u32x4_t fw[2][kFewSteps][4], fx[2][kFewSteps];
+    const int32_t sets = (int32_t)((a.K + 32 * kFewSteps - 1) / (32 * kFewSteps));
+    auto load = [&](int32_t set, u32x4_t (&x)[kFewSteps][4], u32x4_t (&y)[kFewSteps]) {
+#pragma unroll
+        for (int t = 0; t < kFewSteps; ++t) {
+            const int32_t k0 = (set * kFewSteps + t) * 32;
+            const bool in = k0 + q * 8 < a.K;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[t][i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, in ? vw[i] : kGemmOut, k0 * 2, 0));
+            y[t] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rx, in ? vx : kGemmOut, k0 * 2, 0));
+        }
+    };
+    auto multiply = [&](const u32x4_t (&x)[kFewSteps][4], const u32x4_t (&y)[kFewSteps]) {
+#pragma unroll
+        for (int t = 0; t < kFewSteps; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t][i]), __builtin_bit_cast(bf16x8, y[t]),
+                                                                 acc[i], 0, 0, 0);
+        }
+    };
+    load(0, fw[0], fx[0]);
+    for (int32_t set = 0; set < sets; set += 2) {
+        load(set + 1, fw[1], fx[1]);  // (beyond the last: zeros)
+        multiply(fw[0], fx[0]);
+        load(set + 2, fw[0], fx[0]);
+        multiply(fw[1], fx[1]);
+    }
+    const Stat mine = score_stat<4>(acc, v0 + 4 * q, a.V, tok, a.c, a.taken + col);
+    if (q == 0) stat[w][col] = mine;
+    __syncthreads();
+    if (threadIdx.x < kFewTokens && threadIdx.x < n) {
+        Stat st = stat[0][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < kFewThreads / kWave; ++i) st = join(st, stat[i][threadIdx.x], a.c);
+        float* p = a.part + ((int64_t)blockIdx.x * a.N + threadIdx.x) * 3;
+        p[0] = st.m;
+        p[1] = st.s;
+        p[2] = st.u;
+    }
+}
+
+// a token's tiles joined, by LANES lanes (16, or a workgroup)
+template <int LANES>
 __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
-    const int64_t t = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const int l = threadIdx.x % 16;
+    __shared__ Stat lds[256 / kWave];
+    const int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int l = threadIdx.x % LANES;
     if (t >= a.N) return;
     const int64_t at = a.shape.at((uint32_t)t);
     int64_t k = t;
@@ -271,11 +358,19 @@ __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
     }
     Stat st = no_stat();
     const int32_t n_tiles = (int32_t)tiles(a.V);
-    for (int32_t r = l; r < n_tiles; r += 16) {
+#pragma unroll 4
+    for (int32_t r = l; r < n_tiles; r += LANES) {
         const float* p = a.part + ((int64_t)r * a.N + k) * 3;
         st = join(st, Stat{p[0], p[1], p[2]}, a.c);
     }
-    st = join_lanes<16>(st, a.c);
+    if constexpr (LANES == 16) {
+        st = join_lanes<16>(st, a.c);
+    } else {
+        st = join_lanes<kWave>(st, a.c);
+        if (lane_id() == 0) lds[threadIdx.x / kWave] = st;
+        __syncthreads();
+        st = join_lanes<256 / kWave>(lds[lane_id() % (256 / kWave)], a.c);
+    }
     const RowValues r = row_values(st, a.taken[k], a.c, a.inv_t);
     if (l == 0) {
         if (a.logp) a.logp[at] = r.logp;
@@ -512,8 +607,11 @@ int64_t host_tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
 hipError_t launch_head_logprobs(HeadArgs a, hipStream_t s) {
     hipError_t e = prepare_operands(a, s);
     if (e != hipSuccess) return e;
-    HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N))), kGemmThreads, a);
-    HEAD_LAUNCH(k_head_join, dim3((unsigned)((a.N + 15) / 16)), 256, a);
+    if (a.N <= kFewTokens) HEAD_LAUNCH(k_head_stats_few, dim3((unsigned)host_tiles(a.V)), kFewThreads, a);
+    else HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N))), kGemmThreads, a);
+    // few tokens: a workgroup each
+    if (a.N <= 4 * a.cus) HEAD_LAUNCH(k_head_join<256>, dim3((unsigned)a.N), 256, a);
+    else HEAD_LAUNCH(k_head_join<16>, dim3((unsigned)((a.N + 15) / 16)), 256, a);
     return hipSuccess;
 }
 
