@@ -754,8 +754,8 @@ conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_r
  * conduit_token_logprobs_backward) is rounded once to bf16 between the
  * products, whose sums are fp32.  dhidden: bf16 rows like hidden (0 at masked
  * tokens); dweight: V bf16 rows; both are overwritten and apart from every
- * input.  The workspace holds the logits' gradient of up to all choices in both
- * orders, at most 8 GB of it; more tokens run in chunks of choices.
+ * input.  The workspace holds the logits' gradient of up to all choices, at
+ * most 4 GiB of it; more tokens run in chunks of choices.
  * Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_head_logprobs_backward_workspace(int64_t B, int64_t T, const conduit_rows* hidden,

@@ -41,12 +41,8 @@ struct HeadArgs {
     RowsView dx;
     uint16_t* dw;
     int64_t dw_ld;
-    GemmOperand XT, WT;
-    uint16_t* xt;
-    uint16_t* wt;
-    uint16_t* d;
-    uint16_t* dt;
-    int64_t d_ld, dt_ld;
+    uint16_t* d;     // [N][d_ld]: the logits' gradient of a chunk
+    int64_t d_ld;
     float* dx_part;  // [splits][N][h_ld]
     float* dx_sum;   // [N][h_ld]
     int64_t h_ld;

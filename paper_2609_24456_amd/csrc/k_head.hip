@@ -11,12 +11,12 @@
 //
 // Backward: the tiles are produced again, turned into the logits' gradient
 //     d = (g ([j = token] - p_j) - h p_j (log p_j + entropy)) / temperature
-// and rounded once to bf16 (the type of W and X: its relative error, 2^-9 at
+// and rounded once to bf16 (the type of W and X: its relative error, 2^-8 at
 // worst and independent from element to element, is that of the gradients' own
-// rounding), in both orders: [token][choice] and [choice][token].  Then
+// rounding).  Then
 //     dX = d W  (split along the choices, parts joined in a fixed order),
 //     dW = d^T X
-// by the same product, with W and X transposed once.  Batches whose d would pass
+// by the same product, which turns W, X and d as it reads them.  Batches whose d would pass
 // kHeadChunkBytes run in chunks of choices; dX accumulates over them in fp32.
 //
 // Tokens that the mask leaves out take no part: a first launch lists the others
@@ -112,43 +112,6 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs a, const uint16_t* s
     }
 }
 
-// dst[c][r] = src[r][c] for 64 x 64 tiles; rows r >= the live tokens (or `rows`)
-// read as zeros, columns r up to dst_ld are written
-__global__ __launch_bounds__(256) void k_head_transpose(HeadArgs a, const uint16_t* src, int64_t src_ld, int64_t rows,
-                                                        int64_t cols, uint16_t* dst, int64_t dst_ld, bool tokens) {
-    __shared__ uint16_t tile[64][64 + 8];
-    const int64_t n_rows = tokens ? live_tokens(a) : rows;
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-    if (r0 >= (n_rows + kGemmK - 1) / kGemmK * kGemmK) return;  // nothing reads those columns
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int q = threadIdx.x + i * 256, r = q / 8, c = q % 8 * 8;
-        u32x4_t v = {0, 0, 0, 0};
-        if (r0 + r < n_rows) {
-            const uint16_t* p = src + (r0 + r) * src_ld + c0 + c;
-            if (c0 + c + 8 <= cols) {
-                __builtin_memcpy(&v, p, 16);
-            } else {
-                uint16_t e[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = c0 + c + j < cols ? p[j] : (uint16_t)0;
-                __builtin_memcpy(&v, e, 16);
-            }
-        }
-        *reinterpret_cast<u32x4_t*>(&tile[r][c]) = v;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int q = threadIdx.x + i * 256, c = q / 8, r = q % 8 * 8;
-        if (c0 + c >= cols || r0 + r >= dst_ld) continue;
-        u32x4_t v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (uint32_t)tile[r + 2 * j][c] | (uint32_t)tile[r + 2 * j + 1][c] << 16;
-        *reinterpret_cast<u32x4_t*>(dst + (c0 + c) * dst_ld + r0 + r) = v;
-    }
-}
-
 // ---------------------------------------------------------------------------
 // which tile of C a workgroup takes
 // ---------------------------------------------------------------------------
@@ -239,7 +202,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
         tok[ni] = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
     }
     GemmAcc acc;
-    gemm_tile(a.W, v0, a.V, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
+    gemm_tile<false, false>(a.W, v0, a.V, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
     Stat* stat = reinterpret_cast<Stat*>(lds);  // [2][256]
 #pragma unroll
     for (int ni = 0; ni < 4; ++ni) {
@@ -383,7 +346,7 @@ __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
 // backward
 // ---------------------------------------------------------------------------
 // the logits' gradient of a tile of choices [v_base, v_base + v_count) of W, into
-// d [token][choice - v_base] and dt [choice - v_base][token]
+// d [token][choice - v_base]
 __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
@@ -392,7 +355,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
     const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
     GemmAcc acc;
     const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld};
-    gemm_tile(W, v0, v_count, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
+    gemm_tile<false, false>(W, v0, v_count, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
     // [token][choice] with rows of 512 bytes; the 8-byte piece c of row r lies at piece c ^ (r & 15)
     uint2* out = reinterpret_cast<uint2*>(lds);
@@ -449,20 +412,6 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
         const uint2 x = out[r * 64 + (p ^ (r & 15))], y = out[r * 64 + ((p + 1) ^ (r & 15))];
         *reinterpret_cast<u32x4_t*>(a.d + (n0 + r) * a.d_ld + v0 + p * 4) = u32x4_t{x.x, x.y, y.x, y.y};
     }
-    // [choice][token]: a lane gathers 8 tokens of one choice
-    const uint16_t* flat = reinterpret_cast<const uint16_t*>(lds);
-    for (int e = threadIdx.x; e < kGemmTile * 32; e += kGemmThreads) {
-        const int v = e % 256, t = e / 256 * 8;
-        if (v0 + v >= v_count) continue;
-        uint32_t x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r0 = t + 2 * j, r1 = r0 + 1;
-            x[j] = (uint32_t)flat[r0 * 256 + ((v / 4) ^ (r0 & 15)) * 4 + v % 4] |
-                   (uint32_t)flat[r1 * 256 + ((v / 4) ^ (r1 & 15)) * 4 + v % 4] << 16;
-        }
-        *reinterpret_cast<u32x4_t*>(a.dt + (v0 + v) * a.dt_ld + n0 + t) = u32x4_t{x[0], x[1], x[2], x[3]};
-    }
 }
 
 // Parts along k that a product of `tiles` tiles is split into, so that its work
@@ -482,8 +431,8 @@ __device__ __forceinline__ int32_t splits(int64_t n_tiles, int32_t steps, int32_
     return best;
 }
 
-// part s of dX^T tiles: rows = hidden units (W transposed), columns = tokens
-__global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64_t v_count) {
+// part s of dX^T tiles: rows = hidden units, columns = tokens, k = choices (W as it stands is transposed here)
+__global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
     const int32_t row_tiles = (int32_t)tiles(a.H), col_tiles = (int32_t)tiles(n), steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
@@ -493,7 +442,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64
     const int32_t s = tp.row / row_tiles, row = tp.row % row_tiles;
     const int64_t h0 = (int64_t)row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
     GemmAcc acc;
-    gemm_tile(a.WT, h0, a.H, GemmOperand{a.d, a.d_ld}, n0, n, v_count, (int32_t)((int64_t)steps * s / S),
+    gemm_tile<true, false>(GemmOperand{a.W.p + v_base * a.W.ld, a.W.ld}, h0, a.K, GemmOperand{a.d, a.d_ld}, n0, n, v_count, (int32_t)((int64_t)steps * s / S),
               (int32_t)((int64_t)steps * (s + 1) / S), lds, acc);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
     float* part = a.dx_part + (int64_t)s * a.N * a.h_ld;
@@ -541,7 +490,7 @@ __global__ __launch_bounds__(256) void k_head_zero(HeadArgs a) {
         for (int64_t h = threadIdx.x; h < a.H; h += 256) a.dw[v * a.dw_ld + h] = 0;
 }
 
-// dW of a chunk: rows = hidden units (X transposed), columns = choices, k = tokens
+// dW of a chunk: rows = hidden units, columns = choices, k = tokens (X and d as they stand are transposed here)
 __global__ __launch_bounds__(kGemmThreads) void k_head_dweight(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
@@ -549,9 +498,9 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_dweight(HeadArgs a, int64
     const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(v_count), (int32_t)tiles(a.H));
     if (!tp.ok) return;
     const int64_t h0 = (int64_t)tp.col * kGemmTile, v0 = (int64_t)tp.row * kGemmTile;
-    const int64_t K = (n + kGemmK - 1) / kGemmK * kGemmK;  // both operands hold zeros up to there
     GemmAcc acc;
-    gemm_tile(a.XT, h0, a.H, GemmOperand{a.dt, a.dt_ld}, v0, v_count, K, 0, (int32_t)(K / kGemmK), lds, acc);
+    gemm_tile<true, true>(a.X, h0, a.K, GemmOperand{a.d, a.d_ld}, v0, (v_count + 7) / 8 * 8, n, 0, (int32_t)((n + kGemmK - 1) / kGemmK),
+                          lds, acc);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
 #pragma unroll
     for (int ni = 0; ni < 4; ++ni) {
@@ -622,15 +571,11 @@ hipError_t launch_head_backward(HeadArgs a, hipStream_t s) {
     }
     hipError_t e = prepare_operands(a, s);
     if (e != hipSuccess) return e;
-    const dim3 by_token((unsigned)((a.N + 63) / 64), (unsigned)((a.H + 63) / 64));
-    HEAD_LAUNCH(k_head_transpose, by_token, 256, a, a.X.p, a.X.ld, 0, a.H, a.xt, a.XT.ld, true);
     for (int64_t v = 0; v < a.V; v += a.chunk) {
         const int64_t count = a.V - v < a.chunk ? a.V - v : a.chunk;
         const bool first = v == 0, last = v + count == a.V;
         HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N))), kGemmThreads, a, v, count);
-        const dim3 by_choice((unsigned)((count + 63) / 64), (unsigned)((a.H + 63) / 64));
-        HEAD_LAUNCH(k_head_transpose, by_choice, 256, a, a.W.p + v * a.W.ld, a.W.ld, count, a.H, a.wt, a.WT.ld, false);
-        HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N))), kGemmThreads, a, count);
+        HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N))), kGemmThreads, a, v, count);
         HEAD_LAUNCH(k_head_dhidden_join, dim3((unsigned)a.N), 256, a, count, first, last);
         HEAD_LAUNCH(k_head_dweight, dim3(tile_grid(host_tiles(count), host_tiles(a.H))), kGemmThreads, a, v, count);
     }

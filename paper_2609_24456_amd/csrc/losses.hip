@@ -206,7 +206,7 @@ LogitsArgs logits_args(const conduit_rows* x, int64_t B, int64_t T, int64_t stri
 // (byte offsets within 256 rows of an operand, rows of at most 2^21 elements, stay below 2^31)
 constexpr int64_t kHeadMaxTokens = 1ll << 21, kHeadMaxChoices = 1ll << 22, kHeadMaxHidden = 1ll << 16;
 constexpr int64_t kHeadMaxLd = 1ll << 21;
-constexpr int64_t kHeadChunkBytes = 8ll << 30;  // of the logits' gradient in both orders
+constexpr int64_t kHeadChunkBytes = 4ll << 30;  // of the logits' gradient
 constexpr int64_t kHeadPartBytes = 4ll << 30;   // of the parts of the hidden states' gradient
 
 int64_t ceil_to(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -224,9 +224,9 @@ int64_t row_step(const conduit_rows* r, int64_t T) { return T == 1 ? r->stride_b
 
 struct HeadLayout {
     bool pack_w, pack_x;  // pack_x: even without a mask
-    int64_t K, ld, np, chunk, h_ld;
+    int64_t K, ld, chunk, h_ld;
     int32_t splits;
-    uint64_t count, list, place, taken, part, x_pack, w_pack, xt, wt, d, dt, dx_part, dx_sum, bytes;
+    uint64_t count, list, place, taken, part, x_pack, w_pack, d, dx_part, dx_sum, bytes;
 };
 
 // Everything but the chunk's arrays is sized for all B * T tokens counting; the
@@ -238,7 +238,6 @@ HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const c
     l.pack_x = !readable(hidden->data, row_step(hidden, T), H) || !one_after_another(hidden, B, T);
     l.ld = ceil_to(H, 8);
     l.K = l.ld;
-    l.np = ceil_to(N, kGemmTile);
     l.h_ld = ceil_to(H, 8);
     uint64_t at = layout(0, 0).bytes;
     auto take = [&](int64_t bytes) {
@@ -255,15 +254,12 @@ HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const c
         l.taken = take(4 * N);
         l.part = take(12 * N * ((V + kGemmTile - 1) / kGemmTile));
     } else {
-        const int64_t fit = l.np > 0 ? kHeadChunkBytes / (4 * l.np) / kGemmTile * kGemmTile : V;
+        const int64_t fit = N > 0 ? kHeadChunkBytes / (2 * N) / kGemmTile * kGemmTile : V;
         l.chunk = ceil_to(V < kHeadMaxLd ? V : kHeadMaxLd, kGemmTile);
         if (l.chunk > fit) l.chunk = fit > 4 * kGemmTile ? fit : 4 * kGemmTile;
         const int64_t most = N > 0 ? kHeadPartBytes / (4 * N * l.h_ld) : 1;
         l.splits = (int32_t)(most < 1 ? 1 : most < kHeadSplits ? most : kHeadSplits);
-        l.xt = take(2 * H * l.np);
-        l.wt = take(2 * H * l.chunk);
         l.d = take(2 * N * l.chunk);
-        l.dt = take(2 * l.chunk * l.np);
         l.dx_part = take(4 * N * l.h_ld * l.splits);
         l.dx_sum = take(l.chunk < V ? 4 * N * l.h_ld : 0);
     }
@@ -628,14 +624,8 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
     a.dw_ld = dweight->stride_t;
     a.chunk = l.chunk;
     a.splits = l.splits;
-    a.xt = reinterpret_cast<uint16_t*>(w + l.xt);
-    a.wt = reinterpret_cast<uint16_t*>(w + l.wt);
     a.d = reinterpret_cast<uint16_t*>(w + l.d);
-    a.dt = reinterpret_cast<uint16_t*>(w + l.dt);
-    a.XT = GemmOperand{a.xt, l.np};
-    a.WT = GemmOperand{a.wt, l.chunk};
     a.d_ld = l.chunk;
-    a.dt_ld = l.np;
     a.dx_part = reinterpret_cast<float*>(w + l.dx_part);
     a.dx_sum = reinterpret_cast<float*>(w + l.dx_sum);
     a.h_ld = l.h_ld;

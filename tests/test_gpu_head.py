@@ -178,7 +178,7 @@ def test_tokens_outside_the_choices_are_flagged():
 
 
 def test_gradient_in_chunks_of_choices():
-    """So many tokens that the logits' gradient passes the workspace's 8 GB: 69,632 tokens x 40,000 choices."""
+    """So many tokens that the logits' gradient passes the workspace's 4 GiB: 69,632 tokens x 40,000 choices."""
     B, T, H, V = 17, 4096, 64, 40000
     b = Batch(B, T, H, V, mask=True)
     lse = b.forward(1.0)[1].clone()
