@@ -214,109 +214,121 @@ struct GemmSide {
     }
 };
 
+// The tiles of a workgroup, one after the other: start() sets a tile and starts
+// the copies of its first two steps, which then run under the caller's work on
+// the tile before; run() multiplies.
+//
 // C of rows row0.. of A (of `rows` in all) and col0.. of B (of `cols`), over k in
 // [64 step0, min(64 step1, K)); where an operand stands by rows of k, K is a
 // multiple of 8 or the row holds zeros up to one; where it is transposed, rows
-// (cols) is, or the rows hold as many more elements.  `lds` holds kGemmLds bytes,
-// free again for the caller when every wavefront has returned.
+// (cols) is, or the rows hold as many more elements.  `lds`, kGemmLds bytes, is
+// this object's alone.
 template <bool TA, bool TB>
-__device__ __forceinline__ void gemm_tile(const GemmOperand& A, int64_t row0, int64_t rows, const GemmOperand& B,
-                                          int64_t col0, int64_t cols, int64_t K, int32_t step0, int32_t step1,
-                                          uint8_t* lds, GemmAcc& acc) {
-    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = w / 4, wn = w % 4;
-    const int32_t steps = step1 - step0;
-    const int64_t kleft = (K < (int64_t)step1 * kGemmK ? K : (int64_t)step1 * kGemmK) - (int64_t)step0 * kGemmK;
+struct GemmTiles {
     GemmSide<false, TA> sa;
     GemmSide<true, TB> sb;
-    sa.init(A, row0, rows, step0, kleft);
-    sb.init(B, col0, cols, step0, kleft);
-    // what this lane reads: [two steps of 32 k], or per 16 rows
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds;
-    uint32_t aa[TA ? 4 : 2], ab[2];
-    const uint32_t frag = (lane % 16) * 128 + (((lane / 16) ^ (lane & 7)) * 16);
-    const uint32_t trow = (lane / 16 * 8 + lane % 16 / 4) * 256 + lane % 4 * 8, turn = lane % 16 / 4 + 4 * (lane / 16 % 2);
-    if constexpr (TA) {
+    int32_t steps;
+    uint8_t* lds;
+
+    __device__ __forceinline__ void start(const GemmOperand& A, int64_t row0, int64_t rows, const GemmOperand& B, int64_t col0,
+                                          int64_t cols, int64_t K, int32_t step0, int32_t step1) {
+        steps = step1 - step0;
+        const int64_t kleft = (K < (int64_t)step1 * kGemmK ? K : (int64_t)step1 * kGemmK) - (int64_t)step0 * kGemmK;
+        sa.init(A, row0, rows, step0, kleft);
+        sb.init(B, col0, cols, step0, kleft);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) aa[i] = base + trow + ((wm * 4 + i) ^ turn) * 32;
-    } else {
-        aa[0] = base + wm * 16384 + frag;
-        aa[1] = base + wm * 16384 + (frag ^ 64);
+        for (int t = 0; t < 2; ++t) {
+            sb.stage(lds, 0, t);
+            sa.stage(lds, 0, t);
+            sb.stage(lds, 1, t);
+            sa.stage(lds, 1, t);
+        }
     }
-    if constexpr (TB) {
+
+    // (What the caller has loaded or stored since start() only makes the counted
+    // waits stricter: the copies among themselves end in order.)
+    __device__ __forceinline__ void run(GemmAcc& acc) {
+        const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = w / 4, wn = w % 4;
+        // what this lane reads: [two steps of 32 k], or per 16 rows
+        const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds;
+        uint32_t aa[TA ? 4 : 2], ab[2];
+        const uint32_t frag = (lane % 16) * 128 + (((lane / 16) ^ (lane & 7)) * 16);
+        const uint32_t trow = (lane / 16 * 8 + lane % 16 / 4) * 256 + lane % 4 * 8, turn = lane % 16 / 4 + 4 * (lane / 16 % 2);
+        if constexpr (TA) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ab[i] = base + 32768 + trow + ((wn * 2 + i) ^ turn) * 32;
-    } else {
-        ab[0] = base + 32768 + wn * 8192 + frag;
-        ab[1] = base + 32768 + wn * 8192 + (frag ^ 64);
-    }
+            for (int i = 0; i < 4; ++i) aa[i] = base + trow + ((wm * 4 + i) ^ turn) * 32;
+        } else {
+            aa[0] = base + wm * 16384 + frag;
+            aa[1] = base + wm * 16384 + (frag ^ 64);
+        }
+        if constexpr (TB) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 2; ++i) ab[i] = base + 32768 + trow + ((wn * 2 + i) ^ turn) * 32;
+        } else {
+            ab[0] = base + 32768 + wn * 8192 + frag;
+            ab[1] = base + 32768 + wn * 8192 + (frag ^ 64);
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc.c[i][j] = f32x4_t{0, 0, 0, 0};
-    }
-    typedef typename std::conditional<TA, GemmPair, u32x4_t>::type FA;
-    typedef typename std::conditional<TB, GemmPair, u32x4_t>::type FB;
-    FA a[4][2];
-    FB bl[2][2], bh[2][2];
-    // (macros: the offsets are the instructions' own)
-#define GEMM_READ_A(h)                              \
-    do {                                            \
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc.c[i][j] = f32x4_t{0, 0, 0, 0};
+        }
+        typedef typename std::conditional<TA, GemmPair, u32x4_t>::type FA;
+        typedef typename std::conditional<TB, GemmPair, u32x4_t>::type FB;
+        FA a[4][2];
+        FB bl[2][2], bh[2][2];
+        // (macros: the offsets are the instructions' own)
+#define GEMM_READ_A(h)                                     \
+    do {                                                   \
         if constexpr (TA) GEMM_TURN16(a, aa, (h) * 16384); \
         else GEMM_READ8(a, aa[0], aa[1], (h) * 8192);      \
     } while (0)
-#define GEMM_READ_B(r, h)                           \
-    do {                                            \
+#define GEMM_READ_B(r, h)                                  \
+    do {                                                   \
         if constexpr (TB) GEMM_TURN8(r, ab, (h) * 16384);  \
         else GEMM_READ4(r, ab[0], ab[1], (h) * 4096);      \
     } while (0)
-    sb.stage(lds, 0, 0);
-    sa.stage(lds, 0, 0);
-    sb.stage(lds, 1, 0);
-    sa.stage(lds, 1, 0);
-    sb.stage(lds, 0, 1);
-    sa.stage(lds, 0, 1);
-    sb.stage(lds, 1, 1);
-    sa.stage(lds, 1, 1);
-    asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
-    gemm_barrier();
-    GEMM_READ_B(bl, 0);
-    if (wm == 1) gemm_barrier();  // group 1 runs one barrier behind
-    for (int32_t t = 0; t < steps; ++t) {
-        // (0, 0)
-        sb.stage(lds, 0, t + 2);
-        GEMM_READ_A(0);
+        asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
         gemm_barrier();
-        gemm_multiply<0, 0>(acc, a, bl);
-        gemm_barrier();
-        // (0, 1)
-        sa.stage(lds, 0, t + 2);
-        GEMM_READ_B(bh, 1);
-        gemm_barrier();
-        gemm_multiply<0, 1>(acc, a, bh);
-        gemm_barrier();
-        // (1, 0)
-        sb.stage(lds, 1, t + 2);
-        GEMM_READ_A(1);
-        gemm_barrier();
-        gemm_multiply<1, 0>(acc, a, bl);
-        gemm_barrier();
-        // (1, 1), and the next step's columns half 0
-        const uint32_t next = (t & 1) ? 0u - kGemmStep : kGemmStep;
-#pragma unroll
-        for (int i = 0; i < (TA ? 4 : 2); ++i) aa[i] += next;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) ab[i] += next;
-        sa.stage(lds, 1, t + 2);
         GEMM_READ_B(bl, 0);
+        if (wm == 1) gemm_barrier();  // group 1 runs one barrier behind
+        for (int32_t t = 0; t < steps; ++t) {
+            // (0, 0)
+            sb.stage(lds, 0, t + 2);
+            GEMM_READ_A(0);
+            gemm_barrier();
+            gemm_multiply<0, 0>(acc, a, bl);
+            gemm_barrier();
+            // (0, 1)
+            sa.stage(lds, 0, t + 2);
+            GEMM_READ_B(bh, 1);
+            gemm_barrier();
+            gemm_multiply<0, 1>(acc, a, bh);
+            gemm_barrier();
+            // (1, 0)
+            sb.stage(lds, 1, t + 2);
+            GEMM_READ_A(1);
+            gemm_barrier();
+            gemm_multiply<1, 0>(acc, a, bl);
+            gemm_barrier();
+            // (1, 1), and the next step's columns half 0
+            const uint32_t next = (t & 1) ? 0u - kGemmStep : kGemmStep;
+#pragma unroll
+            for (int i = 0; i < (TA ? 4 : 2); ++i) aa[i] += next;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) ab[i] += next;
+            sa.stage(lds, 1, t + 2);
+            GEMM_READ_B(bl, 0);
+            gemm_barrier();
+            gemm_multiply<1, 1>(acc, a, bh);
+            gemm_barrier();
+        }
+        if (wm == 0) gemm_barrier();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the copies beyond the last step
         gemm_barrier();
-        gemm_multiply<1, 1>(acc, a, bh);
-        gemm_barrier();
-    }
-    if (wm == 0) gemm_barrier();
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the copies beyond the last step
-    gemm_barrier();
 #undef GEMM_READ_A
 #undef GEMM_READ_B
-}
+    }
+};
 
 }  // namespace conduit

@@ -115,30 +115,39 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs a, const uint16_t* s
 // ---------------------------------------------------------------------------
 // which tile of C a workgroup takes
 // ---------------------------------------------------------------------------
-// Workgroup b runs on die b % 8 (of 8, with an L2 each).  A die takes an eighth
-// of the row tiles, and walks them kHeadGroup column tiles at a time, so that the
-// 32 workgroups it runs at once share 4 row tiles and 8 column tiles.
-struct TilePlace {
+// A launch has a workgroup for every compute unit (LDS holds one), and workgroup
+// b, on die b % 8 (of 8, with an L2 each), takes the places b, b + gridDim, ...
+// A die has an eighth of the row tiles, and walks them kHeadGroup column tiles at
+// a time, so that the 32 workgroups it runs at once share 4 row tiles and 8
+// column tiles.
+struct TileWalk {
+    int32_t row_tiles, col_tiles, lo, n, place, end;
     int32_t row, col;
-    bool ok;
+
+    __device__ __forceinline__ TileWalk(int64_t rows, int64_t cols)
+        : row_tiles((int32_t)rows), col_tiles((int32_t)cols), row(0), col(0) {
+        const int32_t x = blockIdx.x % kHeadXcds;
+        lo = (int32_t)(rows * x / kHeadXcds);
+        n = (int32_t)(rows * (x + 1) / kHeadXcds) - lo;
+        place = blockIdx.x / kHeadXcds;
+        end = n * col_tiles;
+    }
+    // the next tile of this workgroup into row, col; false: there is none
+    __device__ __forceinline__ bool next() {
+        if (place >= end) return false;
+        const int32_t g = place / (n * kHeadGroup), r = place - g * n * kHeadGroup, c0 = g * kHeadGroup;
+        const int32_t width = col_tiles - c0 < kHeadGroup ? col_tiles - c0 : kHeadGroup;
+        row = lo + r / width;
+        col = c0 + r % width;
+        place += gridDim.x / kHeadXcds;
+        return true;
+    }
 };
 
-__device__ __forceinline__ TilePlace tile_place(uint32_t block, int32_t row_tiles, int32_t col_tiles) {
-    const int32_t x = block % kHeadXcds, j = block / kHeadXcds;
-    const int32_t lo = (int32_t)((int64_t)row_tiles * x / kHeadXcds), n = (int32_t)((int64_t)row_tiles * (x + 1) / kHeadXcds) - lo;
-    TilePlace t{0, 0, false};
-    if (n == 0 || col_tiles == 0) return t;
-    const int32_t g = j / (n * kHeadGroup), r = j - g * n * kHeadGroup, c0 = g * kHeadGroup;
-    const int32_t width = col_tiles - c0 < kHeadGroup ? col_tiles - c0 : kHeadGroup;
-    if (width <= 0 || r >= n * width) return t;
-    t.row = lo + r / width;
-    t.col = c0 + r % width;
-    t.ok = true;
-    return t;
-}
-
-unsigned tile_grid(int64_t row_tiles, int64_t col_tiles) {
-    return (unsigned)(kHeadXcds * ((row_tiles + kHeadXcds - 1) / kHeadXcds) * col_tiles);
+// workgroups: one a compute unit (and no more than places), a multiple of the dies
+unsigned tile_grid(int64_t row_tiles, int64_t col_tiles, int32_t cus) {
+    const int64_t places = (row_tiles + kHeadXcds - 1) / kHeadXcds * col_tiles, each = cus / kHeadXcds > 0 ? cus / kHeadXcds : 1;
+    return (unsigned)(kHeadXcds * (places < each ? places : each));
 }
 
 __device__ __forceinline__ int64_t tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
@@ -159,25 +168,35 @@ __device__ __forceinline__ Stat join_quarters(const Stat& s, float c) { return j
 // of this lane's; the taken token's score is left in `taken` where it is here.
 template <int ROWS>
 __device__ __forceinline__ Stat score_stat(f32x4_t (&x)[ROWS], int64_t first, int64_t V, int32_t tok, float c, float* taken) {
-    // places of this lane's choices below the last one, and of the taken one
-    const int32_t end = V - first < 16 * ROWS ? (int32_t)(V - first) : 16 * ROWS;
+    if (V - first < 16 * ROWS) {  // the last tile: choices beyond have no weight
+        const int32_t end = (int32_t)(V - first);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = i * 16 + j < end ? x[i][j] : kNone;
+        }
+    }
     const int64_t from = (int64_t)tok - first;
-    const int32_t at = from >= 0 && from < 16 * ROWS ? (int32_t)from : -1;
-    float top = kNone, xt = 0.0f;
-    bool here = false;
+    if (from >= 0 && from < 16 * ROWS) {  // in few tiles
+        const int32_t at = (int32_t)from;
+        float xt = 0.0f;
+        bool here = false;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                xt = i * 16 + j == at ? x[i][j] : xt;
+                here |= i * 16 + j == at;
+            }
+        }
+        if (here) *taken = xt;
+    }
+    float top = kNone;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (i * 16 + j >= end) x[i][j] = kNone;
-            if (i * 16 + j == at) {
-                xt = x[i][j];
-                here = true;
-            }
-            top = fmaxf(top, x[i][j]);
-        }
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, x[i][j]);
     }
-    if (here) *taken = xt;
     Stat st = no_stat();
     raise(st, top, c);
 #pragma unroll
@@ -190,36 +209,47 @@ __device__ __forceinline__ Stat score_stat(f32x4_t (&x)[ROWS], int64_t first, in
 
 __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
+    __shared__ Stat stat[2][kGemmTile];
     const int64_t n = live_tokens(a);
-    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(a.V), (int32_t)tiles(n));
-    if (!tp.ok) return;
-    const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
-    int32_t tok[4];  // ahead of the product, which hides the loads
+    const int32_t steps = (int32_t)((a.K + kGemmK - 1) / kGemmK);
+    TileWalk walk(tiles(a.V), tiles(n));
+    GemmTiles<false, false> gemm;
+    gemm.lds = lds;
+    bool more = walk.next();
+    if (more) gemm.start(a.W, (int64_t)walk.row * kGemmTile, a.V, a.X, (int64_t)walk.col * kGemmTile, n, a.K, 0, steps);
+    while (more) {
+        const int64_t row = walk.row, v0 = row * kGemmTile, n0 = (int64_t)walk.col * kGemmTile;
+        int32_t tok[4];  // ahead of the product, which hides the loads
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-        const int64_t k = n0 + wn * 64 + ni * 16 + col;
-        tok[ni] = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
-    }
-    GemmAcc acc;
-    gemm_tile<false, false>(a.W, v0, a.V, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
-    Stat* stat = reinterpret_cast<Stat*>(lds);  // [2][256]
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t k = n0 + wn * 64 + ni * 16 + col;
+            tok[ni] = k < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[k] : k))] : -1;
+        }
+        GemmAcc acc;
+        gemm.run(acc);
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-        const int64_t k = n0 + wn * 64 + ni * 16 + col;
-        f32x4_t x[8];
+        for (int ni = 0; ni < 4; ++ni) asm volatile("" : "+v"(tok[ni]));  // waited for before the next copies start
+        more = walk.next();
+        if (more) gemm.start(a.W, (int64_t)walk.row * kGemmTile, a.V, a.X, (int64_t)walk.col * kGemmTile, n, a.K, 0, steps);
 #pragma unroll
-        for (int mi = 0; mi < 8; ++mi) x[mi] = acc.c[mi][ni];
-        const Stat st = score_stat<8>(x, v0 + wm * 128 + 4 * q, a.V, tok[ni], a.c, a.taken + k);
-        if (q == 0) stat[wm * kGemmTile + wn * 64 + ni * 16 + col] = st;
-    }
-    __syncthreads();
-    if (threadIdx.x < kGemmTile && n0 + threadIdx.x < n) {
-        const Stat st = join(stat[threadIdx.x], stat[kGemmTile + threadIdx.x], a.c);
-        float* p = a.part + ((int64_t)tp.row * a.N + n0 + threadIdx.x) * 3;
-        p[0] = st.m;
-        p[1] = st.s;
-        p[2] = st.u;
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t k = n0 + wn * 64 + ni * 16 + col;
+            f32x4_t x[8];
+#pragma unroll
+            for (int mi = 0; mi < 8; ++mi) x[mi] = acc.c[mi][ni];
+            const Stat st = score_stat<8>(x, v0 + wm * 128 + 4 * q, a.V, tok[ni], a.c, a.taken + k);
+            if (q == 0) stat[wm][wn * 64 + ni * 16 + col] = st;
+        }
+        lds_barrier();
+        if (threadIdx.x < kGemmTile && n0 + threadIdx.x < n) {
+            const Stat st = join(stat[0][threadIdx.x], stat[1][threadIdx.x], a.c);
+            float* p = a.part + (row * a.N + n0 + threadIdx.x) * 3;
+            p[0] = st.m;
+            p[1] = st.s;
+            p[2] = st.u;
+        }
+        // (run() meets barriers before stat is written again)
     }
 }
 
@@ -350,67 +380,96 @@ __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
 __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
-    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(v_count), (int32_t)tiles(n));
-    if (!tp.ok) return;
-    const int64_t v0 = (int64_t)tp.row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
-    GemmAcc acc;
-    const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld};
-    gemm_tile<false, false>(W, v0, v_count, a.X, n0, n, a.K, 0, (int32_t)((a.K + kGemmK - 1) / kGemmK), lds, acc);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
-    // [token][choice] with rows of 512 bytes; the 8-byte piece c of row r lies at piece c ^ (r & 15)
-    uint2* out = reinterpret_cast<uint2*>(lds);
+    const int32_t steps = (int32_t)((a.K + kGemmK - 1) / kGemmK);
+    const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld};
+    TileWalk walk(tiles(v_count), tiles(n));
+    GemmTiles<false, false> gemm;
+    gemm.lds = lds;
+    bool more = walk.next();
+    if (more) gemm.start(W, (int64_t)walk.row * kGemmTile, v_count, a.X, (int64_t)walk.col * kGemmTile, n, a.K, 0, steps);
+    while (more) {
+        const int64_t v0 = (int64_t)walk.row * kGemmTile, n0 = (int64_t)walk.col * kGemmTile;
+        int32_t tok[4];
+        float g[4], h[4], lse[4], entropy[4];  // g and h over the temperature
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-        const int c = wn * 64 + ni * 16 + col;
-        const int64_t k = n0 + c;
-        float g = 0.0f, h = 0.0f, lse = 0.0f, entropy = 0.0f;
-        int64_t tok = -1;
-        if (k < n) {
-            const int64_t at = a.shape.at((uint32_t)(a.list ? a.list[k] : k));
-            tok = a.tokens[at];
-            const bool ok = tok >= 0 && tok < a.V;  // (without a mask there is no list that leaves others out)
-            if (!ok && v_base == 0 && tp.row == 0 && wm == 0 && q == 0) flag_error(a.err, ERR_TOKEN);
-            lse = a.lse_in[at];
-            if (ok && a.g) g = a.g[at] * a.inv_t;
-            if (ok && a.h) h = a.h[at] * a.inv_t;
-            if (ok && a.h) entropy = a.entropy_in[at];
-        }
-        const int64_t first = v_base + v0 + wm * 128 + 4 * q;
-        const bool live = (g != 0.0f || h != 0.0f) && lse != kNone;
-        const int32_t end = !live ? 0 : v_base + v_count - first < 256 ? (int32_t)(v_base + v_count - first) : 256;
-        const int64_t from = tok - first;
-        const int32_t at = from >= 0 && from < 128 ? (int32_t)from : -1;
-        float taken = 0.0f;  // log p of the taken token
-        bool here = false;
-#pragma unroll
-        for (int mi = 0; mi < 8; ++mi) {
-            uint16_t d[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float lp = fmaf(acc.c[mi][ni][i], a.inv_t, -lse), p = exp2_fast(lp * kLog2e);
-                const float x = -p * fmaf(h, fmaxf(lp, kFloor) + entropy, g);
-                if (mi * 16 + i == at) {
-                    taken = lp;
-                    here = live;
-                }
-                d[i] = __builtin_bit_cast(uint16_t, (__bf16)(mi * 16 + i < end ? x : 0.0f));
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t k = n0 + wn * 64 + ni * 16 + col;
+            tok[ni] = -1;
+            g[ni] = h[ni] = lse[ni] = entropy[ni] = 0.0f;
+            if (k < n) {
+                const int64_t at = a.shape.at((uint32_t)(a.list ? a.list[k] : k));
+                const int32_t t = a.tokens[at];
+                const bool ok = t >= 0 && t < a.V;  // (without a mask there is no list that leaves others out)
+                if (!ok && v_base == 0 && walk.row == 0 && wm == 0 && q == 0) flag_error(a.err, ERR_TOKEN);
+                tok[ni] = t;
+                lse[ni] = a.lse_in[at];
+                if (ok && a.g) g[ni] = a.g[at] * a.inv_t;
+                if (ok && a.h) h[ni] = a.h[at] * a.inv_t;
+                if (ok && a.h) entropy[ni] = a.entropy_in[at];
             }
-            const int piece = wm * 32 + mi * 4 + q;
-            out[c * 64 + (piece ^ (c & 15))] = make_uint2((uint32_t)d[0] | (uint32_t)d[1] << 16, (uint32_t)d[2] | (uint32_t)d[3] << 16);
         }
-        if (here) {  // g (1 - p) without the cancellation of a probability near 1
-            const float x = -g * expm1f(taken) - h * exp2_fast(taken * kLog2e) * (fmaxf(taken, kFloor) + entropy);
-            const int v = wm * 128 + 4 * q + at;
-            reinterpret_cast<uint16_t*>(lds)[c * 256 + ((v / 4) ^ (c & 15)) * 4 + v % 4] = __builtin_bit_cast(uint16_t, (__bf16)x);
+        GemmAcc acc;
+        gemm.run(acc);
+#pragma unroll
+        for (int ni = 0; ni < 4; ++ni)  // waited for before the next copies start
+            asm volatile("" : "+v"(tok[ni]), "+v"(g[ni]), "+v"(h[ni]), "+v"(lse[ni]), "+v"(entropy[ni]));
+        more = walk.next();
+        if (more) gemm.start(W, (int64_t)walk.row * kGemmTile, v_count, a.X, (int64_t)walk.col * kGemmTile, n, a.K, 0, steps);
+        const int64_t first = v0 + wm * 128 + 4 * q;  // of this lane's choices in the chunk
+#pragma unroll
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t k = n0 + wn * 64 + ni * 16 + col;
+            // the taken token's place among this lane's choices
+            const int64_t from = tok[ni] - (v_base + first);
+            const bool near = from >= 0 && from < 128 && from % 16 < 4;
+            const bool live = (g[ni] != 0.0f || h[ni] != 0.0f) && lse[ni] != kNone;
+            const float l2 = lse[ni] * kLog2e;
+            float x[8][4];
+#pragma unroll
+            for (int mi = 0; mi < 8; ++mi) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float d = fmaf(acc.c[mi][ni][i], a.c, -l2), p = exp2_fast(d);  // log2 p, p
+                    x[mi][i] = -p * (a.h ? fmaf(h[ni], fmaf(fmaxf(d, kFloor), kLn2, entropy[ni]), g[ni]) : g[ni]);
+                }
+            }
+            if (near) {  // in few tiles: g (1 - p) without the cancellation of a probability near 1
+#pragma unroll
+                for (int mi = 0; mi < 8; ++mi) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (from != mi * 16 + i) continue;
+                        const float lp = fmaf(acc.c[mi][ni][i], a.inv_t, -lse[ni]);
+                        x[mi][i] = -g[ni] * expm1_fast(lp);
+                        if (a.h) x[mi][i] -= h[ni] * exp2_fast(lp * kLog2e) * (fmaxf(lp, kFloor) + entropy[ni]);
+                    }
+                }
+            }
+            if (!live || first + 128 > v_count) {  // nothing from this token, or the last tile: zeros beyond
+#pragma unroll
+                for (int mi = 0; mi < 8; ++mi) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[mi][i] = live && first + mi * 16 + i < v_count ? x[mi][i] : 0.0f;
+                }
+            }
+            // 16 bytes a lane: of rows mi and mi + 1, lanes of q = 0, 2 take the first's choices 0-7 and 8-15, q = 1, 3 the second's
+            uint16_t* out = a.d + k * a.d_ld + v0 + wm * 128 + (q & 1) * 16 + (q / 2) * 8;
+#pragma unroll
+            for (int mi = 0; mi < 8; mi += 2) {
+                uint32_t e[2][2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        e[m][i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i]) |
+                                  (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i + 1]) << 16;
+                }
+                const u32x2_t s0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][0], e[1][0], false, false));
+                const u32x2_t s1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][1], e[1][1], false, false));
+                if (k < n) *reinterpret_cast<u32x4_t*>(out + mi * 16) = u32x4_t{s0.x, s1.x, s0.y, s1.y};
+            }
         }
-    }
-    __syncthreads();
-    // [token][choice]: 16 bytes a lane, 32 lanes a row
-    for (int e = threadIdx.x; e < kGemmTile * 32; e += kGemmThreads) {
-        const int r = e / 32, p = e % 32 * 2;
-        if (n0 + r >= n) break;
-        const uint2 x = out[r * 64 + (p ^ (r & 15))], y = out[r * 64 + ((p + 1) ^ (r & 15))];
-        *reinterpret_cast<u32x4_t*>(a.d + (n0 + r) * a.d_ld + v0 + p * 4) = u32x4_t{x.x, x.y, y.x, y.y};
     }
 }
 
@@ -437,23 +496,34 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64
     const int64_t n = live_tokens(a);
     const int32_t row_tiles = (int32_t)tiles(a.H), col_tiles = (int32_t)tiles(n), steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
     const int32_t S = splits((int64_t)row_tiles * col_tiles, steps, a.cus, a.splits);
-    const TilePlace tp = tile_place(blockIdx.x, row_tiles * S, col_tiles);
-    if (!tp.ok) return;
-    const int32_t s = tp.row / row_tiles, row = tp.row % row_tiles;
-    const int64_t h0 = (int64_t)row * kGemmTile, n0 = (int64_t)tp.col * kGemmTile;
-    GemmAcc acc;
-    gemm_tile<true, false>(GemmOperand{a.W.p + v_base * a.W.ld, a.W.ld}, h0, a.K, GemmOperand{a.d, a.d_ld}, n0, n, v_count, (int32_t)((int64_t)steps * s / S),
-              (int32_t)((int64_t)steps * (s + 1) / S), lds, acc);
+    const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld}, D{a.d, a.d_ld};
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
-    float* part = a.dx_part + (int64_t)s * a.N * a.h_ld;
+    TileWalk walk((int64_t)row_tiles * S, col_tiles);
+    GemmTiles<true, false> gemm;
+    gemm.lds = lds;
+    auto start = [&] {
+        const int32_t s = walk.row / row_tiles;
+        gemm.start(W, (int64_t)(walk.row % row_tiles) * kGemmTile, a.K, D, (int64_t)walk.col * kGemmTile, n, v_count,
+                   (int32_t)((int64_t)steps * s / S), (int32_t)((int64_t)steps * (s + 1) / S));
+    };
+    bool more = walk.next();
+    if (more) start();
+    while (more) {
+        const int64_t h0 = (int64_t)(walk.row % row_tiles) * kGemmTile, n0 = (int64_t)walk.col * kGemmTile;
+        float* part = a.dx_part + (int64_t)(walk.row / row_tiles) * a.N * a.h_ld;
+        GemmAcc acc;
+        gemm.run(acc);
+        more = walk.next();
+        if (more) start();
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-        const int64_t k = n0 + wn * 64 + ni * 16 + col;
-        if (k >= n) continue;
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t k = n0 + wn * 64 + ni * 16 + col;
+            if (k >= n) continue;
 #pragma unroll
-        for (int mi = 0; mi < 8; ++mi) {
-            const int64_t h = h0 + wm * 128 + mi * 16 + 4 * q;
-            if (h < a.h_ld) *reinterpret_cast<f32x4_t*>(part + k * a.h_ld + h) = acc.c[mi][ni];
+            for (int mi = 0; mi < 8; ++mi) {
+                const int64_t h = h0 + wm * 128 + mi * 16 + 4 * q;
+                if (h < a.h_ld) *reinterpret_cast<f32x4_t*>(part + k * a.h_ld + h) = acc.c[mi][ni];
+            }
         }
     }
 }
@@ -494,31 +564,49 @@ __global__ __launch_bounds__(256) void k_head_zero(HeadArgs a) {
 __global__ __launch_bounds__(kGemmThreads) void k_head_dweight(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
     const int64_t n = live_tokens(a);
-    // column tiles are many here: they take the rows' part in the walk
-    const TilePlace tp = tile_place(blockIdx.x, (int32_t)tiles(v_count), (int32_t)tiles(a.H));
-    if (!tp.ok) return;
-    const int64_t h0 = (int64_t)tp.col * kGemmTile, v0 = (int64_t)tp.row * kGemmTile;
-    GemmAcc acc;
-    gemm_tile<true, true>(a.X, h0, a.K, GemmOperand{a.d, a.d_ld}, v0, (v_count + 7) / 8 * 8, n, 0, (int32_t)((n + kGemmK - 1) / kGemmK),
-                          lds, acc);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
+    const GemmOperand D{a.d, a.d_ld};
+    const int32_t steps = (int32_t)((n + kGemmK - 1) / kGemmK);
+    TileWalk walk(tiles(v_count), tiles(a.H));  // (column tiles are many here: they take the rows' part in the walk)
+    GemmTiles<true, true> gemm;
+    gemm.lds = lds;
+    auto start = [&] {
+        gemm.start(a.X, (int64_t)walk.col * kGemmTile, a.K, D, (int64_t)walk.row * kGemmTile, (v_count + 7) / 8 * 8, n, 0, steps);
+    };
+    bool more = walk.next();
+    if (more) start();
+    while (more) {
+        const int64_t h0 = (int64_t)walk.col * kGemmTile, v0 = (int64_t)walk.row * kGemmTile;
+        GemmAcc acc;
+        gemm.run(acc);
+        more = walk.next();
+        if (more) start();
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-        const int64_t v = v0 + wn * 64 + ni * 16 + col;
-        if (v >= v_count) continue;
-        uint16_t* out = a.dw + (v_base + v) * a.dw_ld;
+        for (int ni = 0; ni < 4; ++ni) {
+            const int64_t v = v0 + wn * 64 + ni * 16 + col;
+            uint16_t* out = a.dw + (v_base + v) * a.dw_ld;
 #pragma unroll
-        for (int mi = 0; mi < 8; ++mi) {
-            const int64_t h = h0 + wm * 128 + mi * 16 + 4 * q;
-            uint16_t e[4];
+            for (int mi = 0; mi < 8; mi += 2) {
+                uint32_t e[2][2];  // as in k_head_gradient
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = __builtin_bit_cast(uint16_t, (__bf16)acc.c[mi][ni][i]);
-            if (h + 4 <= a.H) {
-                __builtin_memcpy(out + h, e, 8);
-            } else {
+                for (int m = 0; m < 2; ++m) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (h + i < a.H) out[h + i] = e[i];
+                    for (int i = 0; i < 2; ++i)
+                        e[m][i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc.c[mi + m][ni][2 * i]) |
+                                  (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc.c[mi + m][ni][2 * i + 1]) << 16;
+                }
+                const u32x2_t s0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][0], e[1][0], false, false));
+                const u32x2_t s1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][1], e[1][1], false, false));
+                const u32x4_t x = {s0.x, s1.x, s0.y, s1.y};
+                const int64_t h = h0 + wm * 128 + (mi + (q & 1)) * 16 + (q / 2) * 8;
+                if (v >= v_count) continue;
+                if (h + 8 <= a.H) {
+                    __builtin_memcpy(out + h, &x, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (h + i < a.H) out[h + i] = (uint16_t)(x[i / 2] >> (i % 2 * 16));
+                }
             }
         }
     }
@@ -557,7 +645,7 @@ hipError_t launch_head_logprobs(HeadArgs a, hipStream_t s) {
     hipError_t e = prepare_operands(a, s);
     if (e != hipSuccess) return e;
     if (a.N <= kFewTokens) HEAD_LAUNCH(k_head_stats_few, dim3((unsigned)host_tiles(a.V)), kFewThreads, a);
-    else HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N))), kGemmThreads, a);
+    else HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N), a.cus)), kGemmThreads, a);
     // few tokens: a workgroup each
     if (a.N <= 4 * a.cus) HEAD_LAUNCH(k_head_join<256>, dim3((unsigned)a.N), 256, a);
     else HEAD_LAUNCH(k_head_join<16>, dim3((unsigned)((a.N + 15) / 16)), 256, a);
@@ -574,10 +662,10 @@ hipError_t launch_head_backward(HeadArgs a, hipStream_t s) {
     for (int64_t v = 0; v < a.V; v += a.chunk) {
         const int64_t count = a.V - v < a.chunk ? a.V - v : a.chunk;
         const bool first = v == 0, last = v + count == a.V;
-        HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N))), kGemmThreads, a, v, count);
-        HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N))), kGemmThreads, a, v, count);
+        HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
+        HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
         HEAD_LAUNCH(k_head_dhidden_join, dim3((unsigned)a.N), 256, a, count, first, last);
-        HEAD_LAUNCH(k_head_dweight, dim3(tile_grid(host_tiles(count), host_tiles(a.H))), kGemmThreads, a, v, count);
+        HEAD_LAUNCH(k_head_dweight, dim3(tile_grid(host_tiles(count), host_tiles(a.H), a.cus)), kGemmThreads, a, v, count);
     }
     return hipSuccess;
 }

@@ -506,7 +506,7 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, Po
         const bool holds = i < nv ? i / (kGradK * kWave) == part && i % kWave == lane
                                   : part == 0 && (uint32_t)tok - nv * kPer == lane;
         if (holds) {
-            float d = a.inv_t * (rg.g * -expm1f(fmaf(xa, a.inv_t, -lse)));
+            float d = a.inv_t * (rg.g * -expm1_fast(fmaf(xa, a.inv_t, -lse)));
             if constexpr (decltype(ent)::value) d += one(xa, 0.0f, ent);
             dx[tok] = E::round(d);
         }

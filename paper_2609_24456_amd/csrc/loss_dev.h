@@ -164,6 +164,13 @@ __device__ __forceinline__ void exp_remainder(float x, float* k, float* em1) {
     *em1 = small ? p + x : e;
 }
 
+// exp(x) - 1
+__device__ __forceinline__ float expm1_fast(float x) {
+    float k, em1;
+    exp_remainder(x, &k, &em1);
+    return em1;
+}
+
 // ---------------------------------------------------------------------------
 // the policy loss of one token
 // ---------------------------------------------------------------------------

@@ -97,7 +97,7 @@ __device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float 
     r.lse = fmaf(st.m, inv_t, r.log2_s * kLn2);
     r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
     r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
-    r.one_minus_p = -expm1f(r.logp);
+    r.one_minus_p = -expm1_fast(r.logp);
     return r;
 }
 
