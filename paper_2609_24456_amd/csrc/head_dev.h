@@ -6,7 +6,7 @@
 
 namespace conduit {
 
-constexpr int kHeadSplits = 16;  // most parts of dX's sum over the choices
+constexpr int kHeadSplits = 128;  // most parts of dX's sum over the choices
 
 struct HeadArgs {
     TokenShape shape;

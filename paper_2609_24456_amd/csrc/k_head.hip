@@ -473,18 +473,23 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
     }
 }
 
-// Parts along k that a product of `tiles` tiles is split into, so that its work
-// fills rounds of the compute units: the fewest of at most `most` for which
-// the rounds cost least (a part also costs the writing of its sums).
+// Parts along k (of 8 steps at least) that a product of n_tiles tiles is split
+// into: as many as fill a number of rounds of the compute units, for the number
+// for which rounds times the length of a part, and 8 steps' time for a tile's
+// start and its sums, is least.
 __device__ __forceinline__ int32_t splits(int64_t n_tiles, int32_t steps, int32_t cus, int32_t most) {
+    if (n_tiles <= 0) return 1;
     int32_t best = 1;
-    float cost = 1e30f;
-    for (int32_t s = 1; s <= most && s * 8 <= steps + 7; ++s) {
-        const float rounds = (float)((n_tiles * s + cus - 1) / cus);
-        const float c = rounds * ((float)steps / s + 8.0f);
+    float cost = (float)((n_tiles + cus - 1) / cus) * ((float)steps + 8.0f);
+    if (most > steps / 8) most = steps / 8;
+    for (int32_t rounds = 1; rounds <= 8; ++rounds) {
+        int64_t s = (int64_t)rounds * cus / n_tiles;
+        if (s > most) s = most;
+        if (s < 1) continue;
+        const float c = (float)((n_tiles * s + cus - 1) / cus) * ((float)steps / (float)s + 8.0f);
         if (c < cost) {
             cost = c;
-            best = s;
+            best = (int32_t)s;
         }
     }
     return best;
@@ -543,8 +548,17 @@ __global__ __launch_bounds__(256) void k_head_dhidden_join(HeadArgs a, int64_t v
         if (k >= 0) {
             f32x4_t* total = reinterpret_cast<f32x4_t*>(a.dx_sum + k * a.h_ld + h);
             if (!first) sum = *total;
-            for (int32_t s = 0; s < S; ++s)
-                sum += *reinterpret_cast<const f32x4_t*>(a.dx_part + ((int64_t)s * a.N + k) * a.h_ld + h);
+            const float* part = a.dx_part + k * a.h_ld + h;
+            const int64_t step = a.N * a.h_ld;
+            int32_t s = 0;
+            for (; s + 8 <= S; s += 8) {  // eight under way at once, added in their order
+                f32x4_t x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(part + (s + i) * step);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += x[i];
+            }
+            for (; s < S; ++s) sum += *reinterpret_cast<const f32x4_t*>(part + s * step);
             if (!last) *total = sum;
         }
         if (last) {
