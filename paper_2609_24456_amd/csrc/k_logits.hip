@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
 // longer rows: WAVES wavefronts a row, K vectors a lane in registers
 // ---------------------------------------------------------------------------
 template <bool BF16, int MODE, int WAVES, int K>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(LogitsArgs a, PolicyArgs p) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(LogitsArgs a, PolicyArgs p, bool few_rows) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
@@ -289,6 +289,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
             if (a.entropy) a.entropy[at] = 0.0f;
         }
         if constexpr (MODE == LOSS) {
+            if (few_rows && tid < kWave) finish_row(p, n, false, TokenLoss{}, 0.0f, 0.0f);
             for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
             if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
         }
@@ -322,7 +323,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
         if (a.entropy) a.entropy[at] = r.entropy;
     }
     if constexpr (MODE == LOSS) {
-        const RowGrad rg = row_loss(p, rd, r.logp, nullptr);
+        TokenLoss loss;
+        const RowGrad rg = row_loss(p, rd, r.logp, &loss);
+        if (few_rows && tid < kWave) finish_row(p, n, true, loss, rd.w, r.entropy);
         const GradCoef k{-rg.g * a.inv_t * r.inv_s, -rg.h * a.inv_t * r.inv_s, r.entropy - kLn2 * r.log2_s};
         const bool empty = r.inv_s == 0.0f;
         auto write = [&](auto ent) {
@@ -360,8 +363,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
 constexpr int kPartThreads = 512;
 constexpr int kPartK = 8;
 
-template <bool BF16>
-__global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a) {
+template <bool BF16, int MODE>
+__global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a, PolicyArgs p) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
@@ -379,6 +382,9 @@ __global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a) {
             if (a.logp) a.logp[at] = 0.0f;
             if (a.lse) a.lse[at] = 0.0f;
             if (a.entropy) a.entropy[at] = 0.0f;
+        }
+        if constexpr (MODE == LOSS) {
+            if (part == 0 && tid < (uint32_t)kWave) finish_row(p, n, false, TokenLoss{}, 0.0f, 0.0f);
         }
         return;
     }
@@ -426,7 +432,17 @@ __global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a) {
         if (a.logp) a.logp[at] = r.logp;
         if (a.lse) a.lse[at] = r.lse;
         if (a.entropy) a.entropy[at] = r.entropy;
-        if (a.lse_n) a.lse_n[n] = r.lse;
+    }
+    if constexpr (MODE == LOSS) {
+        const RowData rd = row_data(p, at, div31(n, a.shape.by_T));
+        TokenLoss loss;
+        const RowGrad rg = row_loss(p, rd, r.logp, &loss);
+        if (tid == 0) {
+            a.lse_n[n] = r.lse;
+            a.g_n[n] = rg.g;
+            a.h_n[n] = rg.h;
+        }
+        finish_row(p, n, true, loss, rd.w, r.entropy);
     }
 }
 
@@ -437,9 +453,8 @@ __global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a) {
 constexpr int kGradThreads = 256;
 constexpr int kGradK = 4;
 
-template <bool BF16, bool POLICY>
-__global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, PolicyArgs p, uint32_t items,
-                                                                uint32_t per_row, Div31 by_row) {
+template <bool BF16>
+__global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, uint32_t items, uint32_t per_row, Div31 by_row) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
@@ -459,10 +474,12 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, Po
     RowGrad rg;
     float entropy = 0.0f;
     if (ok) {
-        lse = POLICY ? a.lse_n[n] : a.lse_in[at];
-        if constexpr (POLICY) {  // (lse_n, logp and entropy_in: from the launch before)
-            rg = row_loss(p, row_data(p, at, div31(n, a.shape.by_T)), a.logp[at], nullptr);
+        if (a.lse_n) {  // from the split loss
+            lse = a.lse_n[n];
+            rg.g = a.g_n[n];
+            rg.h = a.h_n[n];
         } else {
+            lse = a.lse_in[at];
             rg.g = a.g ? a.g[at] : 0.0f;
             rg.h = a.h ? a.h[at] : 0.0f;
         }
@@ -515,8 +532,8 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, Po
     else write(std::false_type{});
 }
 
-template <bool BF16, bool POLICY>
-hipError_t launch_gradient(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+template <bool BF16>
+hipError_t launch_gradient(const LogitsArgs& a, hipStream_t s) {
     const int64_t nv = a.V / Elem<BF16>::kPer;
     const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
     const int64_t rows = a.shape.B * a.shape.T;
@@ -524,8 +541,8 @@ hipError_t launch_gradient(const LogitsArgs& a, const PolicyArgs& p, hipStream_t
     const int64_t items = rows * per_row;
     if (items >= 1ll << 31) return hipErrorInvalidValue;
     const unsigned grid = (unsigned)((items + kGradThreads / kWave - 1) / (kGradThreads / kWave));
-    hipLaunchKernelGGL((k_rows_gradient<BF16, POLICY>), dim3(grid), dim3(kGradThreads), 0, s, a, p, (uint32_t)items,
-                       (uint32_t)per_row, make_div31((uint32_t)per_row));
+    hipLaunchKernelGGL((k_rows_gradient<BF16>), dim3(grid), dim3(kGradThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row,
+                       make_div31((uint32_t)per_row));
     return hipGetLastError();
 }
 
@@ -553,33 +570,36 @@ hipError_t launch_short(const LogitsArgs& a, const PolicyArgs& p, bool counted, 
 constexpr int64_t kShortWidth = 64 * kShortElems;
 
 template <bool BF16, int MODE>
-hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, bool few_rows, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
     if (nv <= 8 * kWave)
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p, few_rows);
     else if (MODE == LOGPROBS)  // nothing stays: any width goes by in tiles of 8 vectors a lane
-        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), dim3((unsigned)rows), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), dim3((unsigned)rows), dim3(256), 0, s, a, p, few_rows);
     else if (nv <= 4096)
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), dim3((unsigned)rows), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), dim3((unsigned)rows), dim3(256), 0, s, a, p, few_rows);
     else
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), dim3((unsigned)rows), dim3(1024), 0, s, a, p);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), dim3((unsigned)rows), dim3(1024), 0, s, a, p, few_rows);
     return hipGetLastError();
 }
 
-template <bool BF16>
-hipError_t launch_parts(const LogitsArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((k_rows_parts<BF16>), dim3((unsigned)a.parts, (unsigned)(a.shape.B * a.shape.T)),
-                       dim3(kPartThreads), 0, s, a);
+template <bool BF16, int MODE>
+hipError_t launch_parts(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
+    hipLaunchKernelGGL((k_rows_parts<BF16, MODE>), dim3((unsigned)a.parts, (unsigned)(a.shape.B * a.shape.T)),
+                       dim3(kPartThreads), 0, s, a, p);
     return hipGetLastError();
 }
 
 template <bool BF16>
 hipError_t logprobs(const LogitsArgs& a, hipStream_t s) {
     if (a.V <= kShortWidth) return launch_short<BF16, LOGPROBS>(a, PolicyArgs{}, false, s);
-    if (a.parts > 1) return launch_parts<BF16>(a, s);
-    return launch_long<BF16, LOGPROBS>(a, PolicyArgs{}, s);
+    if (a.parts > 1) return launch_parts<BF16, LOGPROBS>(a, PolicyArgs{}, s);
+    return launch_long<BF16, LOGPROBS>(a, PolicyArgs{}, false, s);
 }
 
+// Split rows (fewer than the GPU has compute units) and up to kPolicyBlocks
+// whole ones sum the statistics up as they go; more rows leave them to a launch
+// over the tokens (its 9 us against as many tickets, 13 ns each).
 template <bool BF16>
 hipError_t loss_logits(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) {
     hipError_t e = hipSuccess;
@@ -587,12 +607,13 @@ hipError_t loss_logits(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) 
     if (e != hipSuccess) return e;
     if (a.V <= kShortWidth) return launch_short<BF16, LOSS>(a, p, p.mask != nullptr, s);
     if (a.parts > 1) {
-        e = launch_parts<BF16>(a, s);
-        if (e == hipSuccess) e = launch_gradient<BF16, true>(a, p, s);
-    } else {
-        e = launch_long<BF16, LOSS>(a, p, s);
+        e = launch_parts<BF16, LOSS>(a, p, s);
+        if (e == hipSuccess) e = launch_gradient<BF16>(a, s);
+        return e;
     }
-    if (e != hipSuccess) return e;
+    const bool few = a.shape.B * a.shape.T <= kPolicyBlocks;
+    e = launch_long<BF16, LOSS>(a, p, few, s);
+    if (e != hipSuccess || few) return e;
     return launch_policy_loss(p, p.mask != nullptr, s);
 }
 
@@ -602,7 +623,7 @@ hipError_t loss_logits(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) 
 // without a workgroup, into parts of at least two rounds of a workgroup's loads.
 int logits_parts(int64_t rows, int64_t V, bool bf16) {
     const int64_t cus = device_cus(), nv = V / (bf16 ? 8 : 4);
-    if (V <= kShortWidth || rows >= cus || rows <= 0) return 1;
+    if (V <= kShortWidth || rows >= cus || rows > kPolicyBlocks || rows <= 0) return 1;
     const int64_t want = (2 * cus + rows - 1) / rows, most = nv / (2 * kPartThreads);
     const int64_t parts = want < most ? want : most;
     return parts > 1 ? (int)parts : 1;
@@ -613,7 +634,7 @@ hipError_t launch_token_logprobs(const LogitsArgs& a, bool bf16, hipStream_t s) 
 }
 
 hipError_t launch_token_logprobs_backward(const LogitsArgs& a, bool bf16, hipStream_t s) {
-    return bf16 ? launch_gradient<true, false>(a, PolicyArgs{}, s) : launch_gradient<false, false>(a, PolicyArgs{}, s);
+    return bf16 ? launch_gradient<true>(a, s) : launch_gradient<false>(a, s);
 }
 
 hipError_t launch_policy_loss_logits(const LogitsArgs& a, const PolicyArgs& p, bool bf16, hipStream_t s) {

@@ -96,7 +96,11 @@ struct LogitsArgs {
     float* part;
     uint32_t* row_ticket;
     int32_t parts;
-    float* lse_n;  // lse by token number, for the gradient launch of the split loss (or NULL)
+    // by token number, from the split loss to its gradient launch: lse, and the
+    // gradients of logp and of the entropy
+    float* lse_n;
+    float* g_n;
+    float* h_n;
 };
 
 hipError_t launch_token_count(const PolicyArgs& a, hipStream_t s);
@@ -339,19 +343,21 @@ __device__ __forceinline__ bool draw_last(uint32_t* ticket, uint32_t total) {
     return last;
 }
 
+// one lane's draw of a workgroup's (or a row's) ticket `k` of `total`
+__device__ __forceinline__ bool draw_ticket(WorkspaceHead* head, uint32_t k, uint32_t total) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores before it are acknowledged
+    uint32_t words = total;
+    if (total > kTicketGroups) {
+        const uint32_t g = k % kTicketGroups;
+        if (!draw_last(&head->group[g].ticket, (total - g + kTicketGroups - 1) / kTicketGroups)) return false;
+        words = kTicketGroups;
+    }
+    return draw_last(&head->ticket, words);
+}
+
 __device__ __forceinline__ bool last_block(WorkspaceHead* head, uint32_t block, uint32_t total) {
     __shared__ bool s_last;
-    if (threadIdx.x == 0) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores above are acknowledged
-        bool last = true;
-        uint32_t words = total;
-        if (total > kTicketGroups) {
-            const uint32_t g = block % kTicketGroups;
-            last = draw_last(&head->group[g].ticket, (total - g + kTicketGroups - 1) / kTicketGroups);
-            words = kTicketGroups;
-        }
-        s_last = last && draw_last(&head->ticket, words);
-    }
+    if (threadIdx.x == 0) s_last = draw_ticket(head, block, total);
     __syncthreads();
     return s_last;
 }
@@ -370,6 +376,48 @@ __device__ __forceinline__ void write_policy_stats(const PolicyTerms& o, const d
     stats[5] = (float)(-v[4] / n);
     stats[6] = (float)(v[5] / n);
     stats[7] = (float)tokens;
+}
+
+// this lane's share (every step-th from `first`) of the sums in n slots
+__device__ __forceinline__ void sum_slots(const double* slots, uint32_t first, uint32_t step, uint32_t n, double (&t)[kPolicySums]) {
+#pragma unroll
+    for (int i = 0; i < kPolicySums; ++i) t[i] = 0.0;
+    for (uint32_t k = first; k < n; k += step) {
+        double p[kPolicySums];
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) p[i] = load_agent(slots + (int64_t)k * kPolicySums + i);
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) t[i] += p[i];
+    }
+}
+
+// Batches of few rows (at most kPolicyBlocks): the row's own workgroup or
+// wavefront leaves its sums in slot n, and the last row's first wavefront adds
+// the slots up, in a fixed order.  Called by that first wavefront of every row,
+// lane 0 holding the row's values (`on`: it counts).
+__device__ __forceinline__ void finish_row(const PolicyArgs& a, uint32_t n, bool on, const TokenLoss& t, float w, float entropy) {
+    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T);
+    const uint32_t tokens = a.mask ? (uint32_t)a.head->counts : rows;
+    const int lane = threadIdx.x % kWave;
+    bool last = false;
+    if (lane == 0) {
+        TokenSums one;
+        one.add(on, t, entropy);
+        PolicySums s;
+        s.add(w, one);
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) store_agent(a.partial + (int64_t)n * kPolicySums + i, s.v[i]);
+        last = draw_ticket(a.head, n, rows);
+    }
+    if (!__builtin_amdgcn_readfirstlane((int)last)) return;
+    double v[kPolicySums];
+    sum_slots(a.partial, lane, kWave, rows, v);
+#pragma unroll
+    for (int i = 0; i < kPolicySums; ++i) v[i] = wave_sum(v[i]);
+    if (lane == 0) {
+        write_policy_stats(a.o, v, tokens, a.stats);
+        a.head->counts = 0;  // for the next call
+    }
 }
 
 // A wavefront's lanes are added up in 32 bits (a tree of 64 values: six
@@ -402,14 +450,8 @@ __device__ __forceinline__ void finish_policy(const PolicyArgs& a, const PolicyS
     } else {
         if (threadIdx.x < kPolicySums) store_agent(a.partial + (int64_t)blockIdx.x * kPolicySums + threadIdx.x, mine);
         if (!last_block(a.head, blockIdx.x, gridDim.x)) return;
-        double t[kPolicySums] = {0, 0, 0, 0, 0, 0};
-        for (uint32_t k = threadIdx.x; k < gridDim.x; k += NT) {
-            double p[kPolicySums];
-#pragma unroll
-            for (int i = 0; i < kPolicySums; ++i) p[i] = load_agent(a.partial + (int64_t)k * kPolicySums + i);
-#pragma unroll
-            for (int i = 0; i < kPolicySums; ++i) t[i] += p[i];
-        }
+        double t[kPolicySums];
+        sum_slots(a.partial, threadIdx.x, NT, gridDim.x, t);
         block_sum<NT, kPolicySums>(t, lds);
         if (threadIdx.x == 0) write_policy_stats(a.o, t, tokens, a.stats);
     }

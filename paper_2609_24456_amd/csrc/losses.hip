@@ -144,10 +144,10 @@ Layout layout(int64_t B, uint64_t rest) {
 
 Layout policy_layout(int64_t B) { return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks); }
 
-// split rows: their parts' statistics and the rows' log-normalisers behind the partial sums
+// split rows: their parts' statistics, and the rows' log-normalisers and gradients, behind the partial sums
 Layout logits_layout(int64_t B, int64_t T, const conduit_rows* x) {
     const int64_t rows = B * T, parts = logits_parts(rows, x->width, x->dtype == CONDUIT_BF16);
-    return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks + (parts > 1 ? 4 * (uint64_t)rows * (3 * parts + 1) : 0));
+    return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks + (parts > 1 ? 4 * (uint64_t)rows * (3 * parts + 3) : 0));
 }
 
 Layout preference_layout(int64_t P, int64_t T) {
@@ -167,6 +167,8 @@ void place_workspace(LogitsArgs& a, void* ws, const Layout& l) {
     a.row_ticket = reinterpret_cast<uint32_t*>(w + l.row_ticket);
     a.part = reinterpret_cast<float*>(w + l.rest + sizeof(double) * kPolicySums * kPolicyBlocks);
     a.lse_n = a.part + 3 * rows * a.parts;
+    a.g_n = a.lse_n + rows;
+    a.h_n = a.g_n + rows;
 }
 
 conduit_status policy_terms(const conduit_policy_opts* o, PolicyTerms* t) {
