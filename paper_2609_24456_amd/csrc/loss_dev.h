@@ -42,14 +42,15 @@ struct PolicyTerms {
 
 // Head of a workspace: counters that every call finds and leaves at zero.
 constexpr int kTicketGroups = 32;
+constexpr uint32_t kTicketStep = 32;  // words from a ticket to the next: a cache line each
 struct WorkspaceHead {
     uint64_t counts;  // tokens that count, and from bit 32 on rows (sequences) with at least one
     uint32_t ticket;
     uint32_t pad[61];
     struct {
         uint32_t ticket;
-        uint32_t pad[31];
-    } group[kTicketGroups];  // a cache line each
+        uint32_t pad[kTicketStep - 1];
+    } group[kTicketGroups];
 };
 static_assert(sizeof(WorkspaceHead) == 256 + 128 * kTicketGroups, "workspace head");
 

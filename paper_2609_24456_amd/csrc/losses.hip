@@ -26,7 +26,7 @@ conduit_status launched(hipError_t e, const char* what) {
 constexpr int64_t kMaxTokens = (1ll << 31) - 1;
 constexpr int64_t kMaxWidth = 1ll << 28;
 constexpr int64_t kMaxStride = 1ll << 40;  // products of strides and indices stay below 2^63 in bytes
-constexpr int64_t kSplitRows = 1024;       // row tickets of a workspace (rows are split below the number of CUs)
+constexpr int64_t kSplitRows = kPolicyBlocks;  // row tickets of a workspace (fewer rows than this are split)
 
 conduit_status check_batch(int64_t B, int64_t T, int64_t stride) {
     if (B < 0 || T < 0) return bad("the number of sequences and of tokens must be >= 0");
@@ -136,7 +136,7 @@ struct Layout {
 Layout layout(int64_t B, uint64_t rest) {
     Layout l;
     l.row_ticket = sizeof(WorkspaceHead);
-    l.row_count = l.row_ticket + 4 * kSplitRows;
+    l.row_count = l.row_ticket + 4 * kTicketStep * kSplitRows;
     l.rest = l.row_count + up(4 * (uint64_t)B);
     l.bytes = l.rest + up(rest);
     return l;
