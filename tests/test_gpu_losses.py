@@ -507,3 +507,35 @@ def test_calls_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(got, (lp, en, stats, dx)):
             assert torch.equal(a, b), k
+
+
+@pytest.mark.parametrize("n", [600, 20000])
+def test_ratios_and_divergences_beyond_the_type(n):
+    """exp of every argument past 88.73 is infinity, never NaN: a clipped token's loss and gradient stay finite, and
+    the means of the ratio and of the divergence say infinity.  (Both sizes, so that both kernels of the loss run.)"""
+    rng = np.random.default_rng(n)
+    x = np.concatenate([rng.uniform(88.8, 1e3, n // 2), rng.uniform(1e3, 1e6, n - n // 2)]).astype(np.float32)[None]
+    adv = rng.integers(-1, 2, (1, n)).astype(np.float32)
+    zero = torch.zeros((1, n), device="cuda")
+    stats, g = torch.empty(8, device="cuda"), torch.empty((1, n), device="cuda")
+    cd.conduit_policy_loss(cd.policy_opts(dual_clip=3.0, reduction="sum"), _gpu(x), _gpu(adv), stats, g, old_logp=zero)
+    s = host(stats)
+    want = -1.2 * (adv > 0).sum() + 3.0 * (adv < 0).sum()
+    assert abs(s[1] - want) <= 2.0 ** -20 * 3.0 * n and abs(s[0] - want) <= 2.0 ** -20 * 3.0 * n
+    assert s[6] == np.inf and not host(g).any()
+    cd.conduit_policy_loss(cd.policy_opts(kl_coef=0.1, reduction="sum"), zero, zero, stats, g, ref_logp=_gpu(x))
+    s = host(stats)
+    assert s[1] == 0.0 and s[2] == np.inf and s[0] == np.inf and (host(g) == -np.inf).all()
+
+
+def test_ratios_up_to_the_type_s_largest():
+    """Below the overflow exp is right to a few units of the last place, whatever the argument (2^-21: the instruction's
+    unit, the two products', and half of one for the sum's)."""
+    x = np.random.default_rng(5).uniform(-87.0, 88.7, 4000).astype(np.float32)
+    stats, one = torch.empty((len(x), 8), device="cuda"), torch.ones((1, 1), device="cuda")
+    lp = _gpu(x)
+    opts, zero, g = cd.policy_opts(reduction="sum"), torch.zeros((1, 1), device="cuda"), torch.empty((1, 1), device="cuda")
+    for i in range(len(x)):
+        cd.conduit_policy_loss(opts, lp[i].view(1, 1), one, stats[i], g, old_logp=zero)
+    want = np.exp(x.astype(np.float64))
+    assert (np.abs(host(stats)[:, 6] - want) <= 2.0 ** -21 * want).all()
