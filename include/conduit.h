@@ -40,7 +40,8 @@
  *   - The delivery and on-policy calls (conduit_sample, conduit_gather_transform,
  *     conduit_sample_gather, conduit_sample_gather_nstep, conduit_sample_pack_gae,
  *     conduit_update_priorities, conduit_nstep, the GAE
- *     calls, conduit_minibatch_gather) only enqueue kernels: no allocation,
+ *     calls, conduit_minibatch_gather, the log-probabilities and losses) only
+ *     enqueue kernels: no allocation,
  *     memset or synchronisation, so they may be captured into a HIP graph and
  *     replayed; a replay uses the arguments and the ring state (size, total)
  *     of the capture.  The ingest calls advance the ring's host-side head when
@@ -567,9 +568,9 @@ conduit_status conduit_minibatch_gather(const void* src, int64_t row_bytes, int6
  * (tokens, mask, log-probabilities, advantages, gradients, ...) is [B, T] with
  * rows `stride` >= T elements apart, the same for all of them, so the delivered
  * arrays and their columns [1, T) alike can be passed as they are.  mask is
- * uint8 (NULL: every token counts): at tokens where it is 0 nothing else is
- * read, whatever stands there, per-token outputs and gradients are written as
- * 0, and no sum or mean sees them.  B * T < 2^31.  Sums over tokens run in
+ * uint8 (NULL: every token counts): at tokens where it is 0 nothing counts,
+ * whatever stands there (a NaN, a token outside the vocabulary): per-token outputs
+ * and gradients are written as 0, and no sum or mean sees them.  B * T < 2^31.  Sums over tokens run in
  * fp64 and are joined in a fixed order: results are the same on every run.
  * Tokens outside [0, V) that the mask counts are flagged, and are treated as
  * masked but for the token counts.
@@ -661,12 +662,14 @@ void conduit_policy_opts_default(conduit_policy_opts* opts);
  *     dlogp = scale w ([s follows r] (-A r) + kl_coef (1 - exp x))
  *     dentropy = -scale w entropy_coef
  * At a tie (r on the clip's edge) s follows r.  old_logp NULL: r = 1 (the
- * policy that acted); ref_logp NULL: k = 0; entropy NULL: 0.  stats: float [8]:
+ * policy that acted); ref_logp NULL: k = 0; entropy NULL: 0.  Equal
+ * log-probabilities, -inf among them, have r = 1 and k = 0; a ratio or a k past the
+ * largest float is infinity, and the clip holds it like any other.  stats: float [8]:
  * loss; sum w s; sum w k; sum w entropy; fraction of counted tokens that a clip
  * decided; mean of old - logp; mean ratio; counted tokens.  dlogp and dentropy
  * may be NULL.  A batch without counted tokens gives zeros.
- * Up to 16,384 tokens in whole rows take one launch, larger batches one without
- * and two with a mask.  Errors: EINVAL, EDEVICE, ESTATE.
+ * Up to 8,192 tokens (2,048 chunks of 4 of a row) take one launch, larger batches
+ * one without and two with a mask.  Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_policy_loss_workspace(int64_t B, int64_t T, uint64_t* bytes);
 conduit_status conduit_policy_loss(const conduit_policy_opts* opts, int64_t B, int64_t T, int64_t stride,
@@ -680,7 +683,10 @@ conduit_status conduit_policy_loss(const conduit_policy_opts* opts, int64_t B, i
  * and the gradient of the logits out.  The logits cross memory once in each
  * direction where a row fits a workgroup's registers (up to 256 KB); dlogits may
  * be the logits themselves.  logp and entropy receive the per-token values
- * (required; 0 where the mask is).  Other arguments as in the three calls.
+ * (required, apart from the call's inputs; 0 where the mask is).  Up to three
+ * launches: the count of the tokens (with a mask), the rows, and the gradient
+ * where rows are split into parts or the sums of a batch of more than 512 rows
+ * wider than 512.  Other arguments as in the three calls.
  * Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_policy_loss_logits_workspace(int64_t B, int64_t T, const conduit_rows* logits, uint64_t* bytes);
@@ -915,7 +921,8 @@ conduit_status conduit_buffer_restore(conduit_buffer* buf, const void* src, uint
 /*
  * Wait for `stream`, then report the sticky device-side error flag of `buf`
  * (NULL: the flag shared by the stand-alone calls conduit_gae,
- * conduit_gae_packed and conduit_minibatch_gather, and then the words
+ * conduit_gae_packed, conduit_minibatch_gather and those that take tokens
+ * (conduit_token_logprobs to conduit_head_logprobs_backward), and then the words
  * conduit_gae_noalloc keeps in the current GPU's static table).  Returns OK or ESTATE (with
  * a description in conduit_last_error), or EDEVICE.
  */
