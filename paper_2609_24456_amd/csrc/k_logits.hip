@@ -505,8 +505,11 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
     }
     const float xt = mine ? E::one(x[nv * kPer + lane]) : 0.0f;
     const float xa = E::one(x[tok]);
+    // The scores are far from 0 where log p_j need not be, so a rounded 1 / temperature would cost |z_j| 2^-25 of p_j:
+    // its rest goes along (of the lowest finite value for a choice at -inf: the rest may be 0).
+    auto log_p = [&](float f) { return fmaf(f, a.inv_t, fmaf(fmaxf(f, -3.4028235e38f), a.inv_lo, -lse)); };
     auto one = [&](float f, float g, auto ent) {
-        const float q = fmaf(f, a.inv_t, -lse), e = exp2_fast(q * kLog2e);  // log p_j, p_j
+        const float q = log_p(f), e = exp2_fast(q * kLog2e);  // log p_j, p_j
         if constexpr (!decltype(ent)::value) return -g * a.inv_t * e;
         return -a.inv_t * e * fmaf(rg.h, fmaxf(q, kFloor) + entropy, g);
     };
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
         const bool holds = i < nv ? i / (kGradK * kWave) == part && i % kWave == lane
                                   : part == 0 && (uint32_t)tok - nv * kPer == lane;
         if (holds) {
-            float d = a.inv_t * (rg.g * -expm1_fast(fmaf(xa, a.inv_t, -lse)));
+            float d = a.inv_t * (rg.g * -expm1_fast(log_p(xa)));
             if constexpr (decltype(ent)::value) d += one(xa, 0.0f, ent);
             dx[tok] = E::round(d);
         }

@@ -83,6 +83,7 @@ struct LogitsArgs {
     int64_t V;
     float c;      // log2(e) / temperature
     float inv_t;  // 1 / temperature
+    float inv_lo; // what its rounding left
     const int32_t* tokens;
     const uint8_t* mask;
     float* logp;

@@ -195,6 +195,7 @@ LogitsArgs logits_args(const conduit_rows* x, int64_t B, int64_t T, int64_t stri
     a.V = x->width;
     a.c = (float)((double)1.4426950408889634074 / temperature);
     a.inv_t = (float)(1.0 / temperature);
+    a.inv_lo = (float)(1.0 / temperature - (double)a.inv_t);
     a.tokens = tokens;
     a.mask = mask;
     a.err = err;
