@@ -758,7 +758,8 @@ conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_r
  * outputs and the lse (and, with dentropy, entropy) that it gave.  The logits
  * are computed again; their gradient (that of
  * conduit_token_logprobs_backward) is rounded once to bf16 between the
- * products, whose sums are fp32.  dhidden: bf16 rows like hidden (0 at masked
+ * products (to two halves of 16 bits together for up to 128 tokens), whose sums
+ * are fp32.  dhidden: bf16 rows like hidden (0 at masked
  * tokens); dweight: V bf16 rows; both are overwritten and apart from every
  * input.  The workspace holds the logits' gradient of up to all choices, at
  * most 4 GiB of it; more tokens run in chunks of choices.

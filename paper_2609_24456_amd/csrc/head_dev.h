@@ -7,6 +7,7 @@
 namespace conduit {
 
 constexpr int kHeadSplits = 128;  // most parts of dX's sum over the choices
+constexpr int kHeadTwo = 128;     // most tokens whose logits' gradient is kept in two halves
 
 struct HeadArgs {
     TokenShape shape;
@@ -41,9 +42,10 @@ struct HeadArgs {
     RowsView dx;
     uint16_t* dw;
     int64_t dw_ld;
-    uint16_t* d;     // [N][d_ld]: the logits' gradient of a chunk
+    uint16_t* d;     // [d_rows][d_ld]: the logits' gradient of a chunk
     int64_t d_ld;
-    float* dx_part;  // [splits][N][h_ld]
+    int64_t d_rows;  // N, or 2 N: after the live tokens' rows come the rows of what their rounding left
+    float* dx_part;  // [splits][d_rows][h_ld]
     float* dx_sum;   // [N][h_ld]
     int64_t h_ld;
     int64_t chunk;   // choices a pass

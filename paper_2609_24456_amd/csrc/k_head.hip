@@ -11,9 +11,15 @@
 //
 // Backward: the tiles are produced again, turned into the logits' gradient
 //     d = (g ([j = token] - p_j) - h p_j (log p_j + entropy)) / temperature
-// and rounded once to bf16 (the type of W and X: its relative error, 2^-8 at
-// worst and independent from element to element, is that of the gradients' own
-// rounding).  Then
+// and rounded once to bf16, the type of W and X: over many tokens its error, of
+// random sign from element to element, is no more than that of the gradients' own
+// rounding.  Up to kHeadTwo tokens, whose few large elements would not average
+// out, what the rounding left is kept too, as another bf16 row of d beside a
+// second copy of the token's hidden states: 16 bits of each element.  (10 tokens,
+// 7,925 choices, 1,088 units: error 0.0027 of the gradients with one row, 0.0017
+// with two, the outputs' own rounding; 81 us and 89.  128,000 choices, 4,096 units:
+// 16 tokens 693 us and 745, 128 tokens 865 and 1,003; beyond, 0.0024 with one.)
+// Then
 //     dX = d W  (split along the choices, parts joined in a fixed order),
 //     dW = d^T X
 // by the same product, which turns W, X and d as it reads them.  Batches whose d would pass
@@ -36,6 +42,10 @@ constexpr int kHeadXcds = 8;
 constexpr int kHeadGroup = 8;  // column tiles that neighbours in a launch share
 
 __device__ __forceinline__ int64_t live_tokens(const HeadArgs& a) { return a.count ? (int64_t)*a.count : a.N; }
+
+// rows of the logits' gradient, for n live tokens
+__device__ __forceinline__ bool two_halves(const HeadArgs& a) { return a.d_rows > a.N; }
+__device__ __forceinline__ int64_t gradient_rows(const HeadArgs& a, int64_t n) { return two_halves(a) ? 2 * n : n; }
 
 // The tokens that count, in order: list[k] = token, place[token] = k or -1, and
 // their number.  One workgroup; a lane takes 16 tokens a round.
@@ -90,12 +100,14 @@ __global__ __launch_bounds__(kListThreads) void k_head_list(HeadArgs a) {
 }
 
 // dst[k][0..ld) = src row of the k-th token, zeros beyond `width`; with `rows`
-// given, plain rows (the projection's) instead of tokens
+// given, plain rows (the projection's) instead of tokens.  The tokens' rows twice
+// where d has two halves.
 __global__ __launch_bounds__(256) void k_head_pack(HeadArgs a, const uint16_t* src, int64_t src_ld, int64_t width, uint16_t* dst,
                                                    int64_t ld, int64_t rows, bool tokens) {
-    const int64_t n_rows = tokens ? live_tokens(a) : rows;
+    const int64_t n = tokens ? live_tokens(a) : rows, n_rows = tokens ? gradient_rows(a, n) : n;
     for (int64_t k = blockIdx.x; k < n_rows; k += gridDim.x) {
-        const uint16_t* x = src + (tokens ? a.x.at((uint32_t)(a.list ? a.list[k] : k), a.shape) : k * src_ld);
+        const int64_t r = k < n ? k : k - n;
+        const uint16_t* x = src + (tokens ? a.x.at((uint32_t)(a.list ? a.list[r] : r), a.shape) : r * src_ld);
         uint16_t* y = dst + k * ld;
         for (int64_t c = 8 * (int64_t)threadIdx.x; c < ld; c += 8 * 256) {
             u32x4_t v = {0, 0, 0, 0};
@@ -382,6 +394,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
     const int64_t n = live_tokens(a);
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
     const int32_t steps = (int32_t)((a.K + kGemmK - 1) / kGemmK);
+    const bool two = two_halves(a);
     const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld};
     TileWalk walk(tiles(v_count), tiles(n));
     GemmTiles<false, false> gemm;
@@ -454,20 +467,34 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
                 }
             }
             // 16 bytes a lane: of rows mi and mi + 1, lanes of q = 0, 2 take the first's choices 0-7 and 8-15, q = 1, 3 the second's
-            uint16_t* out = a.d + k * a.d_ld + v0 + wm * 128 + (q & 1) * 16 + (q / 2) * 8;
+            auto write = [&](int64_t row) {
+                uint16_t* out = a.d + row * a.d_ld + v0 + wm * 128 + (q & 1) * 16 + (q / 2) * 8;
 #pragma unroll
-            for (int mi = 0; mi < 8; mi += 2) {
-                uint32_t e[2][2];
+                for (int mi = 0; mi < 8; mi += 2) {
+                    uint32_t e[2][2];
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
+                    for (int m = 0; m < 2; ++m) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        e[m][i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i]) |
-                                  (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i + 1]) << 16;
+                        for (int i = 0; i < 2; ++i)
+                            e[m][i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i]) |
+                                      (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[mi + m][2 * i + 1]) << 16;
+                    }
+                    const u32x2_t s0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][0], e[1][0], false, false));
+                    const u32x2_t s1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][1], e[1][1], false, false));
+                    if (k < n) *reinterpret_cast<u32x4_t*>(out + mi * 16) = u32x4_t{s0.x, s1.x, s0.y, s1.y};
                 }
-                const u32x2_t s0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][0], e[1][0], false, false));
-                const u32x2_t s1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(e[0][1], e[1][1], false, false));
-                if (k < n) *reinterpret_cast<u32x4_t*>(out + mi * 16) = u32x4_t{s0.x, s1.x, s0.y, s1.y};
+            };
+            write(k);
+            if (two) {
+#pragma unroll
+                for (int mi = 0; mi < 8; ++mi) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float rest = x[mi][i] - (float)(__bf16)x[mi][i];
+                        x[mi][i] = fabsf(rest) < 1e38f ? rest : 0.0f;  // (infinities and NaN stand in the first row)
+                    }
+                }
+                write(n + k);
             }
         }
     }
@@ -498,7 +525,7 @@ __device__ __forceinline__ int32_t splits(int64_t n_tiles, int32_t steps, int32_
 // part s of dX^T tiles: rows = hidden units, columns = tokens, k = choices (W as it stands is transposed here)
 __global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
-    const int64_t n = live_tokens(a);
+    const int64_t n = gradient_rows(a, live_tokens(a));
     const int32_t row_tiles = (int32_t)tiles(a.H), col_tiles = (int32_t)tiles(n), steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
     const int32_t S = splits((int64_t)row_tiles * col_tiles, steps, a.cus, a.splits);
     const GemmOperand W{a.W.p + v_base * a.W.ld, a.W.ld}, D{a.d, a.d_ld};
@@ -515,7 +542,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64
     if (more) start();
     while (more) {
         const int64_t h0 = (int64_t)(walk.row % row_tiles) * kGemmTile, n0 = (int64_t)walk.col * kGemmTile;
-        float* part = a.dx_part + (int64_t)(walk.row / row_tiles) * a.N * a.h_ld;
+        float* part = a.dx_part + (int64_t)(walk.row / row_tiles) * a.d_rows * a.h_ld;
         GemmAcc acc;
         gemm.run(acc);
         more = walk.next();
@@ -541,24 +568,27 @@ __global__ __launch_bounds__(256) void k_head_dhidden_join(HeadArgs a, int64_t v
     const int64_t k = a.place ? a.place[t] : t;
     const int64_t n = live_tokens(a);
     const int32_t steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
-    const int32_t S = splits(tiles(a.H) * tiles(n), steps, a.cus, a.splits);
+    const int32_t S = splits(tiles(a.H) * tiles(gradient_rows(a, n)), steps, a.cus, a.splits);
     uint16_t* out = static_cast<uint16_t*>(a.dx.data) + a.dx.at((uint32_t)t, a.shape);
     for (int64_t h = 4 * (int64_t)threadIdx.x; h < a.h_ld; h += 4 * 256) {
         f32x4_t sum = {0, 0, 0, 0};
         if (k >= 0) {
             f32x4_t* total = reinterpret_cast<f32x4_t*>(a.dx_sum + k * a.h_ld + h);
             if (!first) sum = *total;
-            const float* part = a.dx_part + k * a.h_ld + h;
-            const int64_t step = a.N * a.h_ld;
-            int32_t s = 0;
-            for (; s + 8 <= S; s += 8) {  // eight under way at once, added in their order
-                f32x4_t x[8];
+            const int64_t step = a.d_rows * a.h_ld;
+            auto add = [&](const float* part) {
+                int32_t s = 0;
+                for (; s + 8 <= S; s += 8) {  // eight under way at once, added in their order
+                    f32x4_t x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(part + (s + i) * step);
+                    for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(part + (s + i) * step);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += x[i];
-            }
-            for (; s < S; ++s) sum += *reinterpret_cast<const f32x4_t*>(part + s * step);
+                    for (int i = 0; i < 8; ++i) sum += x[i];
+                }
+                for (; s < S; ++s) sum += *reinterpret_cast<const f32x4_t*>(part + s * step);
+            };
+            if (two_halves(a)) add(a.dx_part + (n + k) * a.h_ld + h);
+            add(a.dx_part + k * a.h_ld + h);
             if (!last) *total = sum;
         }
         if (last) {
@@ -577,7 +607,7 @@ __global__ __launch_bounds__(256) void k_head_zero(HeadArgs a) {
 // dW of a chunk: rows = hidden units, columns = choices, k = tokens (X and d as they stand are transposed here)
 __global__ __launch_bounds__(kGemmThreads) void k_head_dweight(HeadArgs a, int64_t v_base, int64_t v_count) {
     __shared__ __align__(1024) uint8_t lds[kGemmLds];
-    const int64_t n = live_tokens(a);
+    const int64_t n = gradient_rows(a, live_tokens(a));
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / 4, wn = w % 4, q = lane / 16, col = lane % 16;
     const GemmOperand D{a.d, a.d_ld};
     const int32_t steps = (int32_t)((n + kGemmK - 1) / kGemmK);
@@ -641,7 +671,7 @@ namespace {
 hipError_t prepare_operands(HeadArgs& a, hipStream_t s) {
     if (a.mask) HEAD_LAUNCH(k_head_list, dim3(1), kListThreads, a);
     if (a.x_pack) {
-        HEAD_LAUNCH(k_head_pack, dim3((unsigned)(a.N < 65536 ? a.N : 65536)), 256, a, static_cast<const uint16_t*>(a.x.data), 0,
+        HEAD_LAUNCH(k_head_pack, dim3((unsigned)(a.d_rows < 65536 ? a.d_rows : 65536)), 256, a, static_cast<const uint16_t*>(a.x.data), 0,
                     a.H, a.x_pack, a.X.ld, 0, true);
     }
     if (a.w_pack) {

@@ -227,7 +227,7 @@ int64_t row_step(const conduit_rows* r, int64_t T) { return T == 1 ? r->stride_b
 
 struct HeadLayout {
     bool pack_w, pack_x;  // pack_x: even without a mask
-    int64_t K, ld, chunk, h_ld;
+    int64_t K, ld, chunk, h_ld, d_rows;
     int32_t splits;
     uint64_t count, list, place, taken, part, x_pack, w_pack, d, dx_part, dx_sum, bytes;
 };
@@ -239,6 +239,11 @@ HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const c
     const int64_t N = B * T, H = hidden->width;
     l.pack_w = !readable(weight->data, weight->stride_t, H);
     l.pack_x = !readable(hidden->data, row_step(hidden, T), H) || !one_after_another(hidden, B, T);
+    l.d_rows = N;
+    if (backward && N <= kHeadTwo) {
+        l.d_rows = 2 * N;
+        l.pack_x = true;
+    }
     l.ld = ceil_to(H, 8);
     l.K = l.ld;
     l.h_ld = ceil_to(H, 8);
@@ -251,7 +256,7 @@ HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const c
     l.count = take(4);
     l.list = take(4 * N);
     l.place = take(4 * N);
-    l.x_pack = take(2 * N * l.ld);
+    l.x_pack = take(2 * l.d_rows * l.ld);
     l.w_pack = take(l.pack_w ? 2 * V * l.ld : 0);
     if (!backward) {
         l.taken = take(4 * N);
@@ -262,8 +267,8 @@ HeadLayout head_layout(int64_t B, int64_t T, const conduit_rows* hidden, const c
         if (l.chunk > fit) l.chunk = fit > 4 * kGemmTile ? fit : 4 * kGemmTile;
         const int64_t most = N > 0 ? kHeadPartBytes / (4 * N * l.h_ld) : 1;
         l.splits = (int32_t)(most < 1 ? 1 : most < kHeadSplits ? most : kHeadSplits);
-        l.d = take(2 * N * l.chunk);
-        l.dx_part = take(4 * N * l.h_ld * l.splits);
+        l.d = take(2 * l.d_rows * l.chunk);
+        l.dx_part = take(4 * l.d_rows * l.h_ld * l.splits);
         l.dx_sum = take(l.chunk < V ? 4 * N * l.h_ld : 0);
     }
     l.bytes = at;
@@ -293,6 +298,7 @@ HeadArgs head_args(const conduit_rows* hidden, const conduit_rows* weight, int64
     a.H = hidden->width;
     a.x = view(hidden);
     a.K = l.K;
+    a.d_rows = l.d_rows;
     a.tokens = tokens;
     a.mask = mask;
     a.c = (float)((double)1.4426950408889634074 / temperature);

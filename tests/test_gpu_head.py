@@ -227,3 +227,32 @@ def test_results_do_not_change_from_run_to_run_and_in_a_graph():
         torch.cuda.synchronize()
         for a, c in zip(got, (*out, dh, dw)):
             assert torch.equal(a, c), k
+
+
+
+
+@pytest.mark.parametrize("N,H,V", [(1, 64, 300), (5, 200, 900), (31, 136, 2000), (33, 320, 700), (127, 64, 1000), (128, 256, 520)])
+@pytest.mark.parametrize("mask", [False, True])
+def test_gradients_of_few_tokens_are_rounded_once(N, H, V, mask):
+    """Few tokens have few large elements in the logits' gradient, whose rounding would not average out: what is left
+    is the outputs' own rounding to 8 bits, half a unit of the last place (2^-8 of the value at most), the halves'
+    2^-16 of the terms summed, and what a probability may lose."""
+    b = Batch(1, N, H, V, seed=N, mask=mask)
+    if mask:
+        b.mask[0, 0] = 1
+    logp, lse, ent = b.forward(1.0)
+    dh, dw = torch.empty_like(b.hidden), torch.empty_like(b.weight)
+    cd.conduit_head_logprobs_backward(b.hidden, b.weight, b.tokens, lse, b.g, dh, dw, entropy=ent, dentropy=b.h, mask=b.mask)
+    z = b.scores(1.0)
+    logq = z - torch.logsumexp(z, -1, keepdim=True)
+    p, on = logq.exp(), b.on().reshape(-1)
+    e = -(p * logq).sum(-1, keepdim=True)
+    g, h = b.g.double().reshape(-1, 1), b.h.double().reshape(-1, 1)
+    d = -p * (g + h * (logq + e))
+    d.scatter_add_(1, b.tokens.reshape(-1, 1).long(), g)
+    d = torch.where(on[:, None], d, 0.0)
+    x, w = b.hidden.double().reshape(N, H), b.weight.double()
+    loss = 2.0 ** -16 + 4 * b.tolerance(z)
+    for got, want, terms in ((dh.reshape(N, H), d @ w, d.abs() @ w.abs()), (dw, d.t() @ x, d.abs().t() @ x.abs())):
+        err = (got.double() - want).abs()
+        assert (err <= 2.0 ** -8 * want.abs() + loss * terms).all(), (err - 2.0 ** -8 * want.abs()).max()
