@@ -17,7 +17,7 @@
 // out, what the rounding left is kept too, as another bf16 row of d beside a
 // second copy of the token's hidden states: 16 bits of each element.  (10 tokens,
 // 7,925 choices, 1,088 units: error 0.0027 of the gradients with one row, 0.0017
-// with two, the outputs' own rounding; 81 us and 89.  128,000 choices, 4,096 units:
+// with two, the outputs' own rounding; 81 us and 83.  128,000 choices, 4,096 units:
 // 16 tokens 693 us and 745, 128 tokens 865 and 1,003; beyond, 0.0024 with one.)
 // Then
 //     dX = d W  (split along the choices, parts joined in a fixed order),
@@ -566,36 +566,54 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_dhidden(HeadArgs a, int64
 }
 
 // the parts of dX of this chunk of choices (and, beyond the first, of those
-// before) in their order; after the last chunk bf16 rows, zeros where nothing
-// counts
+// before) in a fixed order; after the last chunk bf16 rows, zeros where nothing
+// counts.  GROUPS wavefronts share the parts of the same units, one after the
+// other's; blockIdx.y takes the units' next 1,024 / GROUPS.  (10 tokens of 1,088
+// units: four 7.6 us, one 14.3; 128 of 1,024: 15.0 and 16.4; 200 of 2,048: 15.5 and 13.6.)
+template <int GROUPS>
 __global__ __launch_bounds__(256) void k_head_dhidden_join(HeadArgs a, int64_t v_count, bool first, bool last) {
+    constexpr int kLanes = 256 / GROUPS;
+    __shared__ f32x4_t s_sum[GROUPS][kLanes];
     const int64_t t = blockIdx.x;
     const int64_t k = a.place ? a.place[t] : t;
     const int64_t n = live_tokens(a);
     const int32_t steps = (int32_t)((v_count + kGemmK - 1) / kGemmK);
     const int32_t S = splits(tiles(a.H) * tiles(gradient_rows(a, n)), steps, a.cus, a.splits);
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const int32_t s0 = S * group / GROUPS, s1 = S * (group + 1) / GROUPS;
     uint16_t* out = static_cast<uint16_t*>(a.dx.data) + a.dx.at((uint32_t)t, a.shape);
-    for (int64_t h = 4 * (int64_t)threadIdx.x; h < a.h_ld; h += 4 * 256) {
+    for (int64_t h0 = 4 * kLanes * (int64_t)blockIdx.y; h0 < a.h_ld; h0 += 4 * kLanes * (int64_t)gridDim.y) {
+        const int64_t h = h0 + 4 * lane;
         f32x4_t sum = {0, 0, 0, 0};
-        if (k >= 0) {
-            f32x4_t* total = reinterpret_cast<f32x4_t*>(a.dx_sum + k * a.h_ld + h);
-            if (!first) sum = *total;
+        f32x4_t* total = reinterpret_cast<f32x4_t*>(a.dx_sum + k * a.h_ld + h);
+        if (k >= 0 && h < a.h_ld) {
+            if (!first && group == 0) sum = *total;
             const int64_t step = a.d_rows * a.h_ld;
             auto add = [&](const float* part) {
-                int32_t s = 0;
-                for (; s + 8 <= S; s += 8) {  // eight under way at once, added in their order
+                int32_t s = s0;
+                for (; s + 8 <= s1; s += 8) {  // eight under way at once, added in their order
                     f32x4_t x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(part + (s + i) * step);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sum += x[i];
                 }
-                for (; s < S; ++s) sum += *reinterpret_cast<const f32x4_t*>(part + s * step);
+                for (; s < s1; ++s) sum += *reinterpret_cast<const f32x4_t*>(part + s * step);
             };
             if (two_halves(a)) add(a.dx_part + (n + k) * a.h_ld + h);
             add(a.dx_part + k * a.h_ld + h);
-            if (!last) *total = sum;
         }
+        if constexpr (GROUPS > 1) {
+            s_sum[group][lane] = sum;
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int i = 1; i < GROUPS; ++i) sum += s_sum[i][lane];
+            }
+            __syncthreads();
+        }
+        if (group != 0 || h >= a.h_ld) continue;
+        if (!last && k >= 0) *total = sum;
         if (last) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -713,7 +731,10 @@ hipError_t launch_head_backward(HeadArgs a, hipStream_t s) {
         const bool first = v == 0, last = v + count == a.V;
         HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
         HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
-        HEAD_LAUNCH(k_head_dhidden_join, dim3((unsigned)a.N), 256, a, count, first, last);
+        if (a.N <= kHeadTwo)  // few tokens' sums are of many parts
+            HEAD_LAUNCH(k_head_dhidden_join<4>, dim3((unsigned)a.N, (unsigned)((a.h_ld + 255) / 256)), 256, a, count, first, last);
+        else
+            HEAD_LAUNCH(k_head_dhidden_join<1>, dim3((unsigned)a.N), 256, a, count, first, last);
         HEAD_LAUNCH(k_head_dweight, dim3(tile_grid(host_tiles(count), host_tiles(a.H), a.cus)), kGemmThreads, a, v, count);
     }
     return hipSuccess;
