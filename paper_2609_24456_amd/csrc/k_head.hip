@@ -17,7 +17,7 @@
 // out, what the rounding left is kept too, as another bf16 row of d beside a
 // second copy of the token's hidden states: 16 bits of each element.  (10 tokens,
 // 7,925 choices, 1,088 units: error 0.0027 of the gradients with one row, 0.0017
-// with two, the outputs' own rounding; 81 us and 83.  128,000 choices, 4,096 units:
+// with two, the outputs' own rounding; 16 bits cost 8 us of 81.  128,000 choices, 4,096 units:
 // 16 tokens 693 us and 745, 128 tokens 865 and 1,003; beyond, 0.0024 with one.)
 // Then
 //     dX = d W  (split along the choices, parts joined in a fixed order),
@@ -279,22 +279,18 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_stats(HeadArgs a) {
 constexpr int kFewThreads = 256;
 constexpr int kFewTokens = 16;
 constexpr int kFewSteps = 4;
+constexpr int kFewHidden = 2048;
 
-__global__ __launch_bounds__(kFewThreads) void k_head_stats_few(HeadArgs a) {
-    __shared__ Stat stat[kFewThreads / kWave][kFewTokens];
-    const int64_t n = live_tokens(a);
-    if (n == 0) return;
-    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, col = lane % 16;
-    const int64_t v0 = (int64_t)blockIdx.x * kGemmTile + w * 64;
+// acc[i][j]: the product of row 16 i + 4 q + j from w on (of `rows` that exist) and token lane % 16
+__device__ __forceinline__ void few_scores(const HeadArgs& a, const uint16_t* w, int64_t rows, int64_t n, f32x4_t (&acc)[4]) {
+    const int lane = lane_id(), q = lane / 16, col = lane % 16;
     __amdgpu_buffer_rsrc_t rw =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.W.p + v0 * a.W.ld), 0, 0x7fffffff, 0x00027000);
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(w), 0, 0x7fffffff, 0x00027000);
     __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.X.p), 0, 0x7fffffff, 0x00027000);
     uint32_t vw[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vw[i] = v0 + i * 16 + col < a.V ? (uint32_t)((i * 16 + col) * a.W.ld * 2 + q * 16) : kGemmOut;
+    for (int i = 0; i < 4; ++i) vw[i] = i * 16 + col < rows ? (uint32_t)((i * 16 + col) * a.W.ld * 2 + q * 16) : kGemmOut;
     const uint32_t vx = col < n ? (uint32_t)(col * a.X.ld * 2 + q * 16) : kGemmOut;
-    const int32_t tok = col < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[col] : col))] : -1;
-    f32x4_t acc[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
     u32x4_t fw[2][kFewSteps][4], fx[2][kFewSteps];
@@ -326,6 +322,17 @@ __global__ __launch_bounds__(kFewThreads) void k_head_stats_few(HeadArgs a) {
         load(set + 2, fw[0], fx[0]);
         multiply(fw[1], fx[1]);
     }
+}
+
+__global__ __launch_bounds__(kFewThreads) void k_head_stats_few(HeadArgs a) {
+    __shared__ Stat stat[kFewThreads / kWave][kFewTokens];
+    const int64_t n = live_tokens(a);
+    if (n == 0) return;
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, col = lane % 16;
+    const int64_t v0 = (int64_t)blockIdx.x * kGemmTile + w * 64;
+    const int32_t tok = col < n ? a.tokens[a.shape.at((uint32_t)(a.list ? a.list[col] : col))] : -1;
+    f32x4_t acc[4];
+    few_scores(a, a.W.p + v0 * a.W.ld, a.V - v0, n, acc);
     const Stat mine = score_stat<4>(acc, v0 + 4 * q, a.V, tok, a.c, a.taken + col);
     if (q == 0) stat[w][col] = mine;
     __syncthreads();
@@ -392,6 +399,25 @@ __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
 // ---------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------
+// one logit's gradient from its product x; l2 = log2(e) lse, g and h over the temperature
+__device__ __forceinline__ float score_gradient(const HeadArgs& a, float x, float l2, float g, float h, float entropy) {
+    const float d = fmaf(x, a.c, -l2), p = exp2_fast(d);  // log2 p, p
+    return -p * (a.h ? fmaf(h, fmaf(fmaxf(d, kFloor), kLn2, entropy), g) : g);
+}
+
+// the taken token's own: g (1 - p) without the cancellation of a probability near 1
+__device__ __forceinline__ float taken_gradient(const HeadArgs& a, float x, float lse, float g, float h, float entropy) {
+    const float lp = fmaf(x, a.inv_t, -lse);
+    const float d = -g * expm1_fast(lp);
+    return a.h ? d - h * exp2_fast(lp * kLog2e) * (fmaxf(lp, kFloor) + entropy) : d;
+}
+
+// what the rounding to bf16 leaves (infinities and NaN stand in the first half)
+__device__ __forceinline__ float second_half(float x) {
+    const float rest = x - (float)(__bf16)x;
+    return fabsf(rest) < 1e38f ? rest : 0.0f;
+}
+
 // the logits' gradient of a tile of choices [v_base, v_base + v_count) of W, into
 // d [token][choice - v_base]
 __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int64_t v_base, int64_t v_count) {
@@ -447,20 +473,15 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
 #pragma unroll
             for (int mi = 0; mi < 8; ++mi) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float d = fmaf(acc.c[mi][ni][i], a.c, -l2), p = exp2_fast(d);  // log2 p, p
-                    x[mi][i] = -p * (a.h ? fmaf(h[ni], fmaf(fmaxf(d, kFloor), kLn2, entropy[ni]), g[ni]) : g[ni]);
-                }
+                for (int i = 0; i < 4; ++i) x[mi][i] = score_gradient(a, acc.c[mi][ni][i], l2, g[ni], h[ni], entropy[ni]);
             }
-            if (near) {  // in few tiles: g (1 - p) without the cancellation of a probability near 1
+            if (near) {  // in few tiles
 #pragma unroll
                 for (int mi = 0; mi < 8; ++mi) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (from != mi * 16 + i) continue;
-                        const float lp = fmaf(acc.c[mi][ni][i], a.inv_t, -lse[ni]);
-                        x[mi][i] = -g[ni] * expm1_fast(lp);
-                        if (a.h) x[mi][i] -= h[ni] * exp2_fast(lp * kLog2e) * (fmaxf(lp, kFloor) + entropy[ni]);
+                        x[mi][i] = taken_gradient(a, acc.c[mi][ni][i], lse[ni], g[ni], h[ni], entropy[ni]);
                     }
                 }
             }
@@ -494,14 +515,54 @@ __global__ __launch_bounds__(kGemmThreads) void k_head_gradient(HeadArgs a, int6
 #pragma unroll
                 for (int mi = 0; mi < 8; ++mi) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float rest = x[mi][i] - (float)(__bf16)x[mi][i];
-                        x[mi][i] = fabsf(rest) < 1e38f ? rest : 0.0f;  // (infinities and NaN stand in the first row)
-                    }
+                    for (int i = 0; i < 4; ++i) x[mi][i] = second_half(x[mi][i]);
                 }
                 write(n + k);
             }
         }
+    }
+}
+
+// The same for at most 16 tokens, as in k_head_stats_few: 64 choices a wavefront.
+__global__ __launch_bounds__(kFewThreads) void k_head_gradient_few(HeadArgs a, int64_t v_base, int64_t v_count) {
+    static_assert(kFewTokens <= kHeadTwo);
+    const int64_t n = live_tokens(a);
+    if (n == 0) return;
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, col = lane % 16;
+    const int64_t v0 = (int64_t)blockIdx.x * kGemmTile + w * 64, first = v0 + 4 * q;
+    int32_t tok = -1;
+    float g = 0.0f, h = 0.0f, lse = 0.0f, entropy = 0.0f;
+    if (col < n) {
+        const int64_t at = a.shape.at((uint32_t)(a.list ? a.list[col] : col));
+        tok = a.tokens[at];
+        const bool ok = tok >= 0 && tok < a.V;
+        if (!ok && v_base == 0 && v0 == 0 && q == 0) flag_error(a.err, ERR_TOKEN);
+        lse = a.lse_in[at];
+        if (ok && a.g) g = a.g[at] * a.inv_t;
+        if (ok && a.h) h = a.h[at] * a.inv_t;
+        if (ok && a.h) entropy = a.entropy_in[at];
+    }
+    f32x4_t acc[4];
+    few_scores(a, a.W.p + (v_base + v0) * a.W.ld, v_count - v0, n, acc);
+    if (col >= n) return;
+    const int64_t from = tok - (v_base + first);  // the taken token's place among this lane's choices
+    const bool live = (g != 0.0f || h != 0.0f) && lse != kNone;
+    const float l2 = lse * kLog2e;
+    uint16_t* out = a.d + col * a.d_ld + first;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint16_t e[2][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = 16 * i + j;
+            float x = score_gradient(a, acc[i][j], l2, g, h, entropy);
+            if (from == c) x = taken_gradient(a, acc[i][j], lse, g, h, entropy);
+            x = live && first + c < v_count ? x : 0.0f;
+            e[0][j] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            e[1][j] = __builtin_bit_cast(uint16_t, (__bf16)second_half(x));
+        }
+        __builtin_memcpy(out + 16 * i, e[0], 8);
+        __builtin_memcpy(out + n * a.d_ld + 16 * i, e[1], 8);
     }
 }
 
@@ -706,12 +767,21 @@ hipError_t prepare_operands(HeadArgs& a, hipStream_t s) {
 
 int64_t host_tiles(int64_t n) { return (n + kGemmTile - 1) / kGemmTile; }
 
+// At most 16 tokens, by rows of W in registers or by tiles: long rows of more
+// choices than one round of tiles are as fast or faster by tiles (16 tokens, 4,096
+// units: scores over 128,000 choices 214 us by tiles and 249 by rows, 70,000 210 and
+// 212, 32,000 90 and 76; of 8,192 units and 128,000 choices 411 and 406; the logits'
+// gradient 256 and 290, 107 and 106 over 32,000, 106 and 79 of 2,048 units and 64,000).
+bool few_tokens(const HeadArgs& a, int64_t choices) {
+    return a.N <= kFewTokens && (a.K <= kFewHidden || host_tiles(choices) <= a.cus);
+}
+
 }  // namespace
 
 hipError_t launch_head_logprobs(HeadArgs a, hipStream_t s) {
     hipError_t e = prepare_operands(a, s);
     if (e != hipSuccess) return e;
-    if (a.N <= kFewTokens) HEAD_LAUNCH(k_head_stats_few, dim3((unsigned)host_tiles(a.V)), kFewThreads, a);
+    if (few_tokens(a, a.V)) HEAD_LAUNCH(k_head_stats_few, dim3((unsigned)host_tiles(a.V)), kFewThreads, a);
     else HEAD_LAUNCH(k_head_stats, dim3(tile_grid(host_tiles(a.V), host_tiles(a.N), a.cus)), kGemmThreads, a);
     // few tokens: a workgroup each
     if (a.N <= 4 * a.cus) HEAD_LAUNCH(k_head_join<256>, dim3((unsigned)a.N), 256, a);
@@ -729,7 +799,8 @@ hipError_t launch_head_backward(HeadArgs a, hipStream_t s) {
     for (int64_t v = 0; v < a.V; v += a.chunk) {
         const int64_t count = a.V - v < a.chunk ? a.V - v : a.chunk;
         const bool first = v == 0, last = v + count == a.V;
-        HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
+        if (few_tokens(a, count)) HEAD_LAUNCH(k_head_gradient_few, dim3((unsigned)host_tiles(count)), kFewThreads, a, v, count);
+        else HEAD_LAUNCH(k_head_gradient, dim3(tile_grid(host_tiles(count), host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
         HEAD_LAUNCH(k_head_dhidden, dim3(tile_grid(host_tiles(a.H) * a.splits, host_tiles(a.N), a.cus)), kGemmThreads, a, v, count);
         if (a.N <= kHeadTwo)  // few tokens' sums are of many parts
             HEAD_LAUNCH(k_head_dhidden_join<4>, dim3((unsigned)a.N, (unsigned)((a.h_ld + 255) / 256)), 256, a, count, first, last);

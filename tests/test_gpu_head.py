@@ -256,3 +256,17 @@ def test_gradients_of_few_tokens_are_rounded_once(N, H, V, mask):
     for got, want, terms in ((dh.reshape(N, H), d @ w, d.abs() @ w.abs()), (dw, d.t() @ x, d.abs().t() @ x.abs())):
         err = (got.double() - want).abs()
         assert (err <= 2.0 ** -8 * want.abs() + loss * terms).all(), (err - 2.0 ** -8 * want.abs()).max()
+
+
+@pytest.mark.parametrize("B,T,H,V", [(16, 1, 2056, 70001), (2, 6, 2056, 65537), (1, 16, 2048, 66000), (1, 3, 4104, 500)])
+def test_few_tokens_by_rows_and_by_tiles(B, T, H, V):
+    """Up to 16 tokens, both sides of the widths at which rows of the projection or tiles of it are multiplied."""
+    b = Batch(B, T, H, V, mask=B == 2)
+    z, want = _wanted(b, 1.0)
+    tol = b.tolerance(z)
+    got = b.forward(1.0)
+    for name, g, w in zip(("logp", "lse", "entropy"), got, want):
+        _close(g, w, 2 * tol, name)
+    dh, dw = torch.full_like(b.hidden, float("nan")), torch.full_like(b.weight, float("nan"))
+    cd.conduit_head_logprobs_backward(b.hidden, b.weight, b.tokens, got[1], b.g, dh, dw, entropy=got[2], dentropy=b.h, mask=b.mask)
+    _check_gradients(b, 1.0, dh, dw, got[1], got[2], b.h)
