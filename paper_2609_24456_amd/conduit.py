@@ -546,8 +546,25 @@ def _rows_bytes(entry, t):
     return n.value
 
 
+def _stream_object(stream):
+    """The torch stream of a stream argument: one already, or a handle (0, 1: the legacy default stream)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(stream)
+    return torch.cuda.ExternalStream(handle) if handle > 1 else torch.cuda.default_stream()
+
+
 def workspace(nbytes, stream=None):
-    """A new workspace of at least `nbytes` for the loss calls, ready for use (conduit_workspace_init)."""
+    """A new workspace of at least `nbytes` for the loss calls, ready for use (conduit_workspace_init).  Its memory is
+    `stream`'s from the start (torch hands memory on in the order of the stream that is current at the allocation): what
+    other streams still have under way in memory freed on them stays apart from it."""
+    if stream is not None:
+        with torch.cuda.stream(_stream_object(stream)):
+            return _new_workspace(nbytes, stream)
+    return _new_workspace(nbytes, None)
+
+
+def _new_workspace(nbytes, stream):
     n = max(256, (int(nbytes) + 255) // 256 * 256)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     _check(lib().conduit_workspace_init(ws.data_ptr(), n, _stream(stream)))
@@ -555,11 +572,10 @@ def workspace(nbytes, stream=None):
 
 
 def _workspace(ws, nbytes, stream):
-    """(tensor, address, size): the caller's workspace, or a new one of nbytes() for this call."""
+    """(tensor, address, size): the caller's workspace, or a new one of nbytes() for this call, which goes back to
+    `stream`'s memory when the call returns."""
     if ws is None:
         ws = workspace(nbytes(), stream)
-        if stream is not None:  # torch hands its memory on in the order of the tensor's own stream
-            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
     return ws, _ptr(ws, torch.uint8, "workspace"), ws.numel()
 
 
