@@ -72,8 +72,8 @@ def policy_loss(logp, adv, old=None, ref=None, entropy=None, mask=None, clip_low
         kl = 0.0
         if ref is not None:
             x = float(ref[b, t]) - lp
-            kl = np.expm1(x) - x
-            slope -= kl_coef * np.expm1(x)
+            kl = np.expm1(x) - x if x < np.inf else x
+            slope -= kl_coef * np.expm1(x) if kl_coef else 0.0  # (no term: not 0 times infinity)
         e = float(entropy[b, t]) if entropy is not None else 0.0
         stats[1] += w * term
         stats[2] += w * kl
@@ -83,7 +83,8 @@ def policy_loss(logp, adv, old=None, ref=None, entropy=None, mask=None, clip_low
         ratio_sum += r
         g[b, t] = scale * w * slope
         h[b, t] = -scale * w * entropy_coef
-    stats[0] = scale * (stats[1] + kl_coef * stats[2] - entropy_coef * stats[3])
+    terms = [c * v for c, v in ((1.0, stats[1]), (kl_coef, stats[2]), (-entropy_coef, stats[3])) if c]
+    stats[0] = scale * sum(terms)
     stats[4], stats[5], stats[6] = held_n / n, -log_sum / n, ratio_sum / n
     return stats, g, h
 

@@ -153,7 +153,7 @@ __device__ __forceinline__ float exp_fast(float x) {
 
 // k = exp(x) - 1 - x (x^2 / 2 at small x) and em1 = exp(x) - 1: the series up to
 // x^9 below |x| = 1/2 (the first term left out is x^8 * 2 / 10! of the whole,
-// under 3e-9), where the difference would cancel
+// under 3e-9), where the difference would cancel.  Both are infinity at infinity.
 __device__ __forceinline__ void exp_remainder(float x, float* k, float* em1) {
     float p = 1.0f / 362880.0f;
     p = fmaf(p, x, 1.0f / 40320.0f);
@@ -166,7 +166,7 @@ __device__ __forceinline__ void exp_remainder(float x, float* k, float* em1) {
     p = p * x * x;
     const float e = exp_fast(x) - 1.0f;
     const bool small = fabsf(x) < 0.5f;
-    *k = small ? p : e - x;
+    *k = small ? p : x < INFINITY ? e - x : e;
     *em1 = small ? p + x : e;
 }
 
