@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256) void k_head_join(HeadArgs a) {
         __syncthreads();
         st = join_lanes<256 / kWave>(lds[lane_id() % (256 / kWave)], a.c);
     }
-    const RowValues r = row_values(st, a.taken[k], a.c, a.inv_t);
+    const RowValues r = row_values(st, a.taken[k], a.c, a.inv_t, 0.0f);
     if (l == 0) {
         if (a.logp) a.logp[at] = r.logp;
         if (a.lse) a.lse[at] = r.lse;

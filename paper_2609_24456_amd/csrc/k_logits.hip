@@ -142,6 +142,18 @@ struct RowGrad {
     float g = 0.0f, h = 0.0f;
 };
 
+__device__ __forceinline__ GradCoef grad_coef(const LogitsArgs& a, const RowGrad& g, const RowValues& r) {
+    return GradCoef{-g.g * a.inv_t * r.inv_s, -g.h * a.inv_t * r.inv_s, r.entropy - kLn2 * r.log2_s};
+}
+
+// the taken token's own, at logit xa
+template <bool ENT>
+__device__ __forceinline__ float taken_gradient(const LogitsArgs& a, const RowGrad& g, const RowValues& r, const GradCoef& k, float xa) {
+    const float d = a.inv_t * (g.g * r.one_minus_p);
+    if constexpr (!ENT) return d;
+    return d + logit_gradient<true>(GradCoef{0.0f, k.hp, k.off}, xa, a.c, r.base);
+}
+
 // what the loss of a row needs beside its log-probability, loaded ahead of it
 struct RowData {
     float old, ref, adv, w;
@@ -217,7 +229,7 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
             Stat st = no_stat();
             accumulate(st, v, a.c);
             // (a plain sum over the lanes: the others hold 0)
-            r = row_values(join_lanes<LANES>(st, a.c), lanes_sum<LANES>(xa), a.c, a.inv_t);
+            r = row_values(join_lanes<LANES>(st, a.c), lanes_sum<LANES>(xa), a.c, a.inv_t, a.inv_lo);
         }
         if (l == 0) {
             if (a.logp) a.logp[at] = ok ? r.logp : 0.0f;
@@ -245,8 +257,7 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
                 float d = 0.0f;
                 if (ok && r.inv_s != 0.0f) {
                     if (j == tok)
-                        d = a.inv_t * (rg.g * r.one_minus_p) +
-                            (rg.h != 0.0f ? logit_gradient<true>(GradCoef{0.0f, k.hp, k.off}, v[i], a.c, r.base) : 0.0f);
+                        d = rg.h != 0.0f ? taken_gradient<true>(a, rg, r, k, v[i]) : taken_gradient<false>(a, rg, r, k, v[i]);
                     else if (rg.h != 0.0f)
                         d = logit_gradient<true>(k, v[i], a.c, r.base);
                     else
@@ -323,7 +334,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
         const float f[1] = {xt};
         accumulate(st, f, a.c);
     }
-    const RowValues r = row_values(join_block<WAVES>(st, lds, a.c), xa, a.c, a.inv_t);
+    const RowValues r = row_values(join_block<WAVES>(st, lds, a.c), xa, a.c, a.inv_t, a.inv_lo);
     if (tid == 0) {
         if (a.logp) a.logp[at] = r.logp;
         if (a.lse) a.lse[at] = r.lse;
@@ -333,7 +344,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
         TokenLoss loss;
         const RowGrad rg = row_loss(p, rd, r.logp, &loss);
         if (few_rows && tid < kWave) finish_row(p, n, true, loss, rd.w, r.entropy);
-        const GradCoef k{-rg.g * a.inv_t * r.inv_s, -rg.h * a.inv_t * r.inv_s, r.entropy - kLn2 * r.log2_s};
+        const GradCoef k = grad_coef(a, rg, r);
         const bool empty = r.inv_s == 0.0f;
         auto write = [&](auto ent) {
             constexpr bool ENT = decltype(ent)::value;
@@ -354,9 +365,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
             // the taken token's own, by the lane that wrote its vector
             const uint32_t i = (uint32_t)tok / kPer;
             if (i < nv ? tid == i % NT : tid == (uint32_t)tok - nv * kPer) {
-                float d = a.inv_t * (rg.g * r.one_minus_p);
-                if constexpr (ENT) d += logit_gradient<true>(GradCoef{0.0f, k.hp, k.off}, xa, a.c, r.base);
-                dx[tok] = E::round(empty ? 0.0f : d);
+                dx[tok] = E::round(empty ? 0.0f : taken_gradient<ENT>(a, rg, r, k, xa));
             }
         };
         if (rg.h != 0.0f) write(std::true_type{});
@@ -437,7 +446,7 @@ __global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a, Polic
         o.u = __hip_atomic_load(q + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         all = join(all, o, a.c);
     }
-    const RowValues r = row_values(join_lanes<kWave>(all, a.c), xa, a.c, a.inv_t);
+    const RowValues r = row_values(join_lanes<kWave>(all, a.c), xa, a.c, a.inv_t, a.inv_lo);
     if (tid == 0) {
         if (a.logp) a.logp[at] = r.logp;
         if (a.lse) a.lse[at] = r.lse;
@@ -448,23 +457,61 @@ __global__ __launch_bounds__(kPartThreads) void k_rows_parts(LogitsArgs a, Polic
         TokenLoss loss;
         const RowGrad rg = row_loss(p, rd, r.logp, &loss);
         if (tid == 0) {
-            a.lse_n[n] = r.lse;
-            a.g_n[n] = rg.g;
-            a.h_n[n] = rg.h;
+            const GradCoef k = grad_coef(a, rg, r);
+            const float taken = rg.h != 0.0f ? taken_gradient<true>(a, rg, r, k, xa) : taken_gradient<false>(a, rg, r, k, xa);
+            a.split[n] = r.inv_s == 0.0f ? SplitRow{0.0f, 0.0f, 0.0f, 0.0f, 0.0f} : SplitRow{r.base, k.gp, k.hp, k.off, taken};
         }
         finish_row(p, n, true, loss, rd.w, r.entropy);
     }
 }
 
 // ---------------------------------------------------------------------------
-// the gradient of the logits from the row's saved log-normaliser: wavefronts
-// take parts of kGradK vectors a lane of a row.  HBM bounds it: 2,048 rows of
-// 50,001 fp32 with entropies 115 us, 5.0 TB/s, a large copy's rate (4.9).
+// the gradient of the logits from the row's saved log-normaliser, or, SPLIT, from
+// what the loss of split rows left for it: wavefronts take parts of kGradK
+// vectors a lane of a row.  HBM bounds it: 2,048 rows of 50,001 fp32 with
+// entropies 115 us, 5.0 TB/s, a large copy's rate (4.9).
 // ---------------------------------------------------------------------------
 constexpr int kGradThreads = 256;
 constexpr int kGradK = 4;
 
-template <bool BF16>
+// by the log-normaliser given
+struct FromLse {
+    float inv_t, inv_lo, lse, entropy;
+    RowGrad g;
+    // The scores are far from 0 where log p_j need not be, so a rounded 1 / temperature would cost |z_j| 2^-25 of p_j:
+    // its rest goes along (of the lowest finite value for a choice at -inf: the rest may be 0).
+    __device__ __forceinline__ float log_p(float f) const {
+        return fmaf(f, inv_t, fmaf(fmaxf(f, -3.4028235e38f), inv_lo, -lse));
+    }
+    __device__ __forceinline__ bool with_entropy() const { return g.h != 0.0f; }
+    template <bool ENT>
+    __device__ __forceinline__ float of(float f, float gj) const {
+        const float q = log_p(f), e = exp2_fast(q * kLog2e);  // log p_j, p_j
+        if constexpr (!ENT) return -gj * inv_t * e;
+        return -inv_t * e * fmaf(g.h, fmaxf(q, kFloor) + entropy, gj);
+    }
+    template <bool ENT>
+    __device__ __forceinline__ float other(float f) const { return of<ENT>(f, g.g); }
+    template <bool ENT>
+    __device__ __forceinline__ float taken(float f) const {
+        const float d = inv_t * (g.g * -expm1_fast(log_p(f)));
+        if constexpr (!ENT) return d;
+        return d + of<true>(f, 0.0f);
+    }
+};
+
+// by the row's statistics, as k_rows does
+struct FromStats {
+    float c;
+    SplitRow r;
+    __device__ __forceinline__ bool with_entropy() const { return r.hp != 0.0f; }
+    template <bool ENT>
+    __device__ __forceinline__ float other(float f) const { return logit_gradient<ENT>(GradCoef{r.gp, r.hp, r.off}, f, c, r.base); }
+    template <bool ENT>
+    __device__ __forceinline__ float taken(float) const { return r.taken; }
+};
+
+template <bool BF16, bool SPLIT>
 __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, uint32_t items, uint32_t per_row, Div31 by_row) {
     using E = Elem<BF16>;
     using T = typename E::T;
@@ -481,22 +528,21 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
     const bool ok = on && (lane != 0 || part != 0 ? tok >= 0 && tok < a.V : token_ok(a, tok));
     const uint32_t base = part * kGradK * kWave + lane;
     const bool mine = part == 0 && lane < tail;  // the elements after the last vector
-    float lse = 0.0f;
-    RowGrad rg;
-    float entropy = 0.0f;
-    if (ok) {
-        if (a.lse_n) {  // from the split loss
-            lse = a.lse_n[n];
-            rg.g = a.g_n[n];
-            rg.h = a.h_n[n];
-        } else {
-            lse = a.lse_in[at];
-            rg.g = a.g ? a.g[at] : 0.0f;
-            rg.h = a.h ? a.h[at] : 0.0f;
-        }
-        if (a.entropy_in) entropy = a.entropy_in[at];
+    typename std::conditional<SPLIT, FromStats, FromLse>::type grad;
+    bool weight = ok;
+    if constexpr (SPLIT) {
+        grad.c = a.c;
+        if (ok) grad.r = a.split[n];
+    } else {
+        grad.inv_t = a.inv_t;
+        grad.inv_lo = a.inv_lo;
+        grad.lse = ok ? a.lse_in[at] : 0.0f;
+        grad.g.g = ok && a.g ? a.g[at] : 0.0f;
+        grad.g.h = ok && a.h ? a.h[at] : 0.0f;
+        grad.entropy = ok && a.entropy_in ? a.entropy_in[at] : 0.0f;
+        weight = ok && grad.lse != kNone;
     }
-    if (!ok || lse == kNone) {  // nothing counts, or a row without weight
+    if (!weight) {  // nothing counts, or a row without weight
 #pragma unroll
         for (int k = 0; k < kGradK; ++k) {
             const uint32_t i = base + k * kWave;
@@ -512,41 +558,30 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
         v[k] = i < nv ? load16(x + (size_t)i * kPer) : u32x4{0, 0, 0, 0};
     }
     const float xt = mine ? E::one(x[nv * kPer + lane]) : 0.0f;
-    const float xa = E::one(x[tok]);
-    // The scores are far from 0 where log p_j need not be, so a rounded 1 / temperature would cost |z_j| 2^-25 of p_j:
-    // its rest goes along (of the lowest finite value for a choice at -inf: the rest may be 0).
-    auto log_p = [&](float f) { return fmaf(f, a.inv_t, fmaf(fmaxf(f, -3.4028235e38f), a.inv_lo, -lse)); };
-    auto one = [&](float f, float g, auto ent) {
-        const float q = log_p(f), e = exp2_fast(q * kLog2e);  // log p_j, p_j
-        if constexpr (!decltype(ent)::value) return -g * a.inv_t * e;
-        return -a.inv_t * e * fmaf(rg.h, fmaxf(q, kFloor) + entropy, g);
-    };
+    const float xa = SPLIT ? 0.0f : E::one(x[tok]);
     auto write = [&](auto ent) {
+        constexpr bool ENT = decltype(ent)::value;
 #pragma unroll
         for (int k = 0; k < kGradK; ++k) {
             const uint32_t i = base + k * kWave;
             float f[kPer];
             E::unpack(v[k], f);
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) f[j] = one(f[j], rg.g, ent);
+            for (int j = 0; j < kPer; ++j) f[j] = grad.template other<ENT>(f[j]);
             if (i < nv) store16(dx + (size_t)i * kPer, E::pack(f));
         }
-        if (mine) dx[nv * kPer + lane] = E::round(one(xt, rg.g, ent));
+        if (mine) dx[nv * kPer + lane] = E::round(grad.template other<ENT>(xt));
         // the taken token's own, by the lane that wrote its vector
         const uint32_t i = (uint32_t)tok / kPer;
         const bool holds = i < nv ? i / (kGradK * kWave) == part && i % kWave == lane
                                   : part == 0 && (uint32_t)tok - nv * kPer == lane;
-        if (holds) {
-            float d = a.inv_t * (rg.g * -expm1_fast(log_p(xa)));
-            if constexpr (decltype(ent)::value) d += one(xa, 0.0f, ent);
-            dx[tok] = E::round(d);
-        }
+        if (holds) dx[tok] = E::round(grad.template taken<ENT>(xa));
     };
-    if (rg.h != 0.0f) write(std::true_type{});
+    if (grad.with_entropy()) write(std::true_type{});
     else write(std::false_type{});
 }
 
-template <bool BF16>
+template <bool BF16, bool SPLIT>
 hipError_t launch_gradient(const LogitsArgs& a, hipStream_t s) {
     const int64_t nv = a.V / Elem<BF16>::kPer;
     const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
@@ -555,7 +590,7 @@ hipError_t launch_gradient(const LogitsArgs& a, hipStream_t s) {
     const int64_t items = rows * per_row;
     if (items >= 1ll << 31) return hipErrorInvalidValue;
     const unsigned grid = (unsigned)((items + kGradThreads / kWave - 1) / (kGradThreads / kWave));
-    hipLaunchKernelGGL((k_rows_gradient<BF16>), dim3(grid), dim3(kGradThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row,
+    hipLaunchKernelGGL((k_rows_gradient<BF16, SPLIT>), dim3(grid), dim3(kGradThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row,
                        make_div31((uint32_t)per_row));
     return hipGetLastError();
 }
@@ -622,7 +657,7 @@ hipError_t loss_logits(const LogitsArgs& a, const PolicyArgs& p, hipStream_t s) 
     if (a.V <= kShortWidth) return launch_short<BF16, LOSS>(a, p, p.mask != nullptr, s);
     if (a.parts > 1) {
         e = launch_parts<BF16, LOSS>(a, p, s);
-        if (e == hipSuccess) e = launch_gradient<BF16>(a, s);
+        if (e == hipSuccess) e = launch_gradient<BF16, true>(a, s);
         return e;
     }
     const bool few = a.shape.B * a.shape.T <= kPolicyBlocks;
@@ -649,7 +684,7 @@ hipError_t launch_token_logprobs(const LogitsArgs& a, bool bf16, hipStream_t s) 
 }
 
 hipError_t launch_token_logprobs_backward(const LogitsArgs& a, bool bf16, hipStream_t s) {
-    return bf16 ? launch_gradient<true>(a, s) : launch_gradient<false>(a, s);
+    return bf16 ? launch_gradient<true, false>(a, s) : launch_gradient<false, false>(a, s);
 }
 
 hipError_t launch_policy_loss_logits(const LogitsArgs& a, const PolicyArgs& p, bool bf16, hipStream_t s) {

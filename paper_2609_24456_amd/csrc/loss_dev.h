@@ -77,6 +77,13 @@ struct PolicyArgs {
     double* partial;      // [kPolicyBlocks][kPolicySums]
 };
 
+// What the gradient of a row split into parts needs from the join of its parts:
+// dx = e^(d) gp + ..., as GradCoef in k_logits.hip, at d = c (x - base), and the
+// taken token's own.  Nothing of it grows with the logits, as lse would.
+struct SplitRow {
+    float base, gp, hp, off, taken;
+};
+
 struct LogitsArgs {
     TokenShape shape;
     RowsView x, dx;
@@ -98,11 +105,7 @@ struct LogitsArgs {
     float* part;
     uint32_t* row_ticket;
     int32_t parts;
-    // by token number, from the split loss to its gradient launch: lse, and the
-    // gradients of logp and of the entropy
-    float* lse_n;
-    float* g_n;
-    float* h_n;
+    SplitRow* split;  // by token number, from the split loss to its gradient launch
 };
 
 hipError_t launch_token_count(const PolicyArgs& a, hipStream_t s);

@@ -144,10 +144,10 @@ Layout layout(int64_t B, uint64_t rest) {
 
 Layout policy_layout(int64_t B) { return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks); }
 
-// split rows: their parts' statistics, and the rows' log-normalisers and gradients, behind the partial sums
+// split rows: their parts' statistics, and what the rows' gradients need of them, behind the partial sums
 Layout logits_layout(int64_t B, int64_t T, const conduit_rows* x) {
     const int64_t rows = B * T, parts = logits_parts(rows, x->width, x->dtype == CONDUIT_BF16);
-    return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks + (parts > 1 ? 4 * (uint64_t)rows * (3 * parts + 3) : 0));
+    return layout(B, sizeof(double) * kPolicySums * kPolicyBlocks + (parts > 1 ? (uint64_t)rows * (12 * parts + sizeof(SplitRow)) : 0));
 }
 
 Layout preference_layout(int64_t P, int64_t T) {
@@ -166,9 +166,7 @@ void place_workspace(LogitsArgs& a, void* ws, const Layout& l) {
     const int64_t rows = a.shape.B * a.shape.T;
     a.row_ticket = reinterpret_cast<uint32_t*>(w + l.row_ticket);
     a.part = reinterpret_cast<float*>(w + l.rest + sizeof(double) * kPolicySums * kPolicyBlocks);
-    a.lse_n = a.part + 3 * rows * a.parts;
-    a.g_n = a.lse_n + rows;
-    a.h_n = a.g_n + rows;
+    a.split = reinterpret_cast<SplitRow*>(a.part + 3 * rows * a.parts);
 }
 
 conduit_status policy_terms(const conduit_policy_opts* o, PolicyTerms* t) {
@@ -367,7 +365,6 @@ conduit_status conduit_token_logprobs(const conduit_rows* logits, int64_t B, int
     a.entropy = entropy;
     a.parts = logits_parts(B * T, a.V, bf16);
     place_workspace(a, workspace, l);
-    a.lse_n = nullptr;
     return launched(launch_token_logprobs(a, bf16, static_cast<hipStream_t>(stream)), "token logprobs launch");
 }
 
@@ -475,7 +472,6 @@ conduit_status conduit_policy_loss_logits(const conduit_policy_opts* opts, const
     a.dx = view(dlogits);
     a.logp = logp;
     a.entropy = entropy;
-    a.entropy_in = entropy;
     a.parts = logits_parts(B * T, a.V, bf16);
     place_workspace(a, workspace, l);
     p.shape = a.shape;

@@ -84,7 +84,9 @@ struct RowValues {
     float lse, entropy, logp, one_minus_p;
 };
 
-__device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float c, float inv_t) {
+// inv_lo: what the rounding of 1 / temperature to inv_t left, which at a large
+// maximum is as much as the rounding of lse itself (0: not counted)
+__device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float c, float inv_t, float inv_lo) {
     RowValues r;
     if (st.s == 0.0f) {
         r.base = r.inv_s = r.log2_s = r.entropy = r.one_minus_p = 0.0f;
@@ -94,7 +96,7 @@ __device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float 
     r.base = st.m;
     r.inv_s = 1.0f / st.s;
     r.log2_s = log2_fast(st.s);
-    r.lse = fmaf(st.m, inv_t, r.log2_s * kLn2);
+    r.lse = fmaf(st.m, inv_t, fmaf(st.m, inv_lo, r.log2_s * kLn2));
     r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
     r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
     r.one_minus_p = -expm1_fast(r.logp);
