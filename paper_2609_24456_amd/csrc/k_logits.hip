@@ -156,7 +156,8 @@ __device__ __forceinline__ float taken_gradient(const LogitsArgs& a, const RowGr
 
 // what the loss of a row needs beside its log-probability, loaded ahead of it
 struct RowData {
-    float old, ref, adv, w;
+    float old, ref, adv;
+    double w;
     bool has_old, has_ref;
 };
 
@@ -181,7 +182,7 @@ __device__ __forceinline__ RowData row_data(const PolicyArgs& p, int64_t at, uin
 
 __device__ __forceinline__ RowGrad row_loss(const PolicyArgs& p, const RowData& d, float logp, TokenLoss* out) {
     const TokenLoss t = policy_token(p.o, logp, d.has_old ? d.old : logp, d.has_ref ? d.ref : logp, d.adv);
-    const float wf = (float)((double)d.w * p.o.scale);
+    const float wf = (float)(d.w * p.o.scale);
     if (out) *out = t;
     return RowGrad{wf * t.slope, -p.o.ent * wf};
 }

@@ -106,8 +106,8 @@ __device__ __forceinline__ ChunkData load_chunk_mask(const PolicyArgs& a, const 
     return d;
 }
 
-__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, const ChunkData& d, float w, PolicySums& sums) {
-    const float wf = (float)((double)w * a.o.scale), we = -a.o.ent * wf;
+__device__ __forceinline__ void policy_chunk(const PolicyArgs& a, const ChunkData& d, double w, PolicySums& sums) {
+    const float wf = (float)(w * a.o.scale), we = -a.o.ent * wf;
     float g[kChunk], h[kChunk];
     TokenSums few;
     int32_t tok[kChunk];
@@ -159,10 +159,10 @@ __global__ __launch_bounds__(NT) void k_policy_loss(PolicyArgs a, Chunks ch, boo
         rows = (uint32_t)(counts >> 32);
     }
     PolicySums sums;
-    const float flat = token_weight(a.o, tokens, rows, (uint32_t)a.shape.T);
+    const double flat = token_weight(a.o, tokens, rows, (uint32_t)a.shape.T);
     for (uint32_t c = first; c < ch.total; c += step) {
         if (c != first) d = load_chunk(a, ch, c);
-        float w = flat;
+        double w = flat;
         if (a.o.reduction == CONDUIT_SEQUENCE_MEAN && a.mask)
             w = token_weight(a.o, tokens, rows, SMALL ? s_count[d.row] : a.row_count[d.row]);
         policy_chunk(a, d, w, sums);

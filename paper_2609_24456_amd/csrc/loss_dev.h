@@ -217,15 +217,15 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyTerms& o, float lo
 
 // weight of a token: of the mean over tokens, of the mean over rows of each
 // row's mean, or 1
-__device__ __forceinline__ float token_weight(const PolicyTerms& o, uint32_t tokens, uint32_t rows, uint32_t row) {
-    if (o.reduction == CONDUIT_SUM) return 1.0f;
-    if (o.reduction == CONDUIT_TOKEN_MEAN) return 1.0f / (float)(tokens > 0 ? tokens : 1);
-    return 1.0f / ((float)(rows > 0 ? rows : 1) * (float)(row > 0 ? row : 1));
+__device__ __forceinline__ double token_weight(const PolicyTerms& o, uint32_t tokens, uint32_t rows, uint32_t row) {
+    if (o.reduction == CONDUIT_SUM) return 1.0;
+    if (o.reduction == CONDUIT_TOKEN_MEAN) return 1.0 / (double)(tokens > 0 ? tokens : 1);
+    return 1.0 / ((double)(rows > 0 ? rows : 1) * (double)(row > 0 ? row : 1));
 }
 
-// A lane's sums: a few tokens of one weight in 32 bits, then in 64.
+// A few tokens of one weight, and a lane's sums.
 struct TokenSums {
-    float v[kPolicySums] = {0, 0, 0, 0, 0, 0};
+    double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
     __device__ __forceinline__ void add(bool on, const TokenLoss& t, float entropy) {
         v[0] += on ? t.term : 0.0f;
         v[1] += on ? t.kl : 0.0f;
@@ -238,9 +238,9 @@ struct TokenSums {
 
 struct PolicySums {
     double v[kPolicySums] = {0, 0, 0, 0, 0, 0};
-    __device__ __forceinline__ void add(float w, const TokenSums& t) {
+    __device__ __forceinline__ void add(double w, const TokenSums& t) {
 #pragma unroll
-        for (int i = 0; i < kPolicySums; ++i) v[i] += i < 3 ? (double)w * (double)t.v[i] : (double)t.v[i];
+        for (int i = 0; i < kPolicySums; ++i) v[i] += i < 3 ? w * t.v[i] : t.v[i];
     }
 };
 
@@ -400,7 +400,7 @@ __device__ __forceinline__ void sum_slots(const double* slots, uint32_t first, u
 // wavefront leaves its sums in slot n, and the last row's first wavefront adds
 // the slots up, in a fixed order.  Called by that first wavefront of every row,
 // lane 0 holding the row's values (`on`: it counts).
-__device__ __forceinline__ void finish_row(const PolicyArgs& a, uint32_t n, bool on, const TokenLoss& t, float w, float entropy) {
+__device__ __forceinline__ void finish_row(const PolicyArgs& a, uint32_t n, bool on, const TokenLoss& t, double w, float entropy) {
     const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T);
     const uint32_t tokens = a.mask ? (uint32_t)a.head->counts : rows;
     const int lane = threadIdx.x % kWave;
@@ -425,18 +425,18 @@ __device__ __forceinline__ void finish_row(const PolicyArgs& a, uint32_t n, bool
     }
 }
 
-// A wavefront's lanes are added up in 32 bits (a tree of 64 values: six
-// roundings), everything above in 64: lane i of the first wavefront adds the
-// wavefronts' i-th sums and stores them in the workgroup's slot; the last
-// workgroup adds the slots up, in a fixed order, writes the statistics and
-// clears the counters.
+// All sums are in 64 bits (the partial sums of terms of both signs may be far
+// larger than their total, and past the largest float): lane i of the first
+// wavefront adds the wavefronts' i-th sums and stores them in the workgroup's
+// slot; the last workgroup adds the slots up, in a fixed order, writes the
+// statistics and clears the counters.
 template <int NT>
 __device__ __forceinline__ void finish_policy(const PolicyArgs& a, const PolicySums& s, uint32_t tokens, bool counted,
                                               double* lds) {
     constexpr int W = NT / kWave;
-    float v[kPolicySums];
+    double v[kPolicySums];
 #pragma unroll
-    for (int i = 0; i < kPolicySums; ++i) v[i] = lanes_sum<kWave>((float)s.v[i]);
+    for (int i = 0; i < kPolicySums; ++i) v[i] = wave_sum(s.v[i]);
     if (lane_id() == 0) {
 #pragma unroll
         for (int i = 0; i < kPolicySums; ++i) lds[i * W + threadIdx.x / kWave] = v[i];

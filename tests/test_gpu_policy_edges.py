@@ -48,3 +48,54 @@ def test_a_taken_choice_without_weight_has_an_infinite_divergence(T, V, dtype):
     s = host(stats)
     assert host(lp)[0, 2] == -np.inf and s[2] == np.inf and np.isfinite(s[[0, 1, 3, 4, 6, 7]]).all()
     assert torch.isfinite(dx.float()).all()
+
+
+def _sums(adv, reduction, mask=None):
+    """The statistics of a loss whose terms are -adv themselves (ratio 1), and its gradient."""
+    stats, g, lp = torch.empty(8, device="cuda"), torch.empty_like(adv), torch.zeros_like(adv)
+    cd.conduit_policy_loss(cd.policy_opts(reduction=reduction), lp, adv, stats, g, mask=mask)
+    assert torch.equal(g, (-adv).masked_fill(mask == 0, 0.0) if mask is not None else -adv) or reduction != "sum"
+    return host(stats).astype(np.float64)
+
+
+@pytest.mark.parametrize("n", [600, 20000, 300001])  # one workgroup, one chunk a lane, several
+def test_sums_of_terms_of_both_signs_are_in_64_bits(n):
+    """Terms up to 2^30 in steps of 2^-5 that nearly cancel: every partial sum fits 64 bits, whatever the order, so the total
+    is exact but for its last rounding, where sums in 32 bits would be off by 2^5 and more."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    a = torch.randint(-(1 << 23), 1 << 23, (n,), generator=g, device="cuda").double()
+    big = a * torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, 128.0, 2.0 ** -5)
+    half = big[: n // 2]
+    x = torch.cat([half, -half, torch.full((n - 2 * (n // 2),), 3.0, device="cuda", dtype=torch.float64)])
+    x = x[torch.randperm(n, generator=g, device="cuda")]
+    x[0] += 2.0 ** -5
+    adv = x.float()[None]
+    want = -float(adv.double().sum())
+    assert abs(want) <= 200.0
+    s = _sums(adv, "sum")
+    assert s[1] == s[0] == np.float32(want), (s[1], want)
+
+
+@pytest.mark.parametrize("n", [600, 20000])
+def test_partial_sums_beyond_the_largest_float(n):
+    """Partial sums may pass the largest float: the total is what counts."""
+    adv = torch.full((1, n), 3e38, device="cuda")
+    adv[0, n // 2:] = -3e38
+    s = _sums(adv, "sum")
+    assert s[0] == 0.0 and s[1] == 0.0
+
+
+@pytest.mark.parametrize("B,T", [(3, 200), (7, 3001), (1, 300001)])
+@pytest.mark.parametrize("reduction", ["token_mean", "sequence_mean"])
+@pytest.mark.parametrize("masked", [False, True])
+def test_means_are_rounded_once(B, T, reduction, masked):
+    """Positive terms that are whole numbers, so the 64-bit sum is exact: a mean is right to one rounding to 32 bits (and a
+    few of 64), the weights' included."""
+    g = torch.Generator(device="cuda").manual_seed(B + T)
+    adv = -torch.randint(1, 1 << 20, (B, T), generator=g, device="cuda").float()
+    mask = (torch.rand((B, T), generator=g, device="cuda") < 0.7).to(torch.uint8) if masked else None
+    on = mask.double() if masked else torch.ones((B, T), device="cuda", dtype=torch.float64)
+    x = -adv.double() * on
+    want = float(x.sum() / on.sum()) if reduction == "token_mean" else float((x.sum(1) / on.sum(1)).mean())
+    s = _sums(adv, reduction, mask)
+    assert abs(s[1] - want) <= 2.0 ** -24 * (1 + 1e-5) * want, (s[1] / want - 1) * 2 ** 24
