@@ -25,13 +25,21 @@ conduit_status launched(hipError_t e, const char* what) {
 
 constexpr int64_t kMaxTokens = (1ll << 31) - 1;
 constexpr int64_t kMaxWidth = 1ll << 28;
-constexpr int64_t kMaxStride = 1ll << 40;  // products of strides and indices stay below 2^63 in bytes
+constexpr int64_t kMaxStride = 1ll << 40;
+constexpr int64_t kMaxReach = 1ll << 56;  // elements from an array's first to past its last: every offset in bytes fits 64 bits
 constexpr int64_t kSplitRows = kPolicyBlocks;  // row tickets of a workspace (fewer rows than this are split)
+
+// rows (b, t) of `width` elements, b < B and t < T, end within kMaxReach (counts and strides of at most 2^63, not negative)
+bool within_reach(int64_t B, int64_t stride_b, int64_t T, int64_t stride_t, int64_t width) {
+    if (B <= 0 || T <= 0) return true;
+    return (__int128)(B - 1) * stride_b + (__int128)(T - 1) * stride_t + width <= kMaxReach;
+}
 
 conduit_status check_batch(int64_t B, int64_t T, int64_t stride) {
     if (B < 0 || T < 0) return bad("the number of sequences and of tokens must be >= 0");
     if (B > kMaxTokens || T > kMaxTokens || (B > 0 && T > kMaxTokens / B)) return bad("the batch must hold fewer than 2^31 tokens");
     if (stride < T || stride > kMaxStride) return bad("stride must be at least T (and at most 2^40)");
+    if (!within_reach(B, stride, 1, 0, T)) return bad("the per-token arrays must end within 2^56 elements of their start");
     return CONDUIT_OK;
 }
 
@@ -48,6 +56,8 @@ conduit_status check_rows(const conduit_rows* r, int64_t B, int64_t T, bool out,
     if (r->stride_b < 0 || r->stride_t < 0 || r->stride_b > kMaxStride || r->stride_t > kMaxStride)
         return bad((w + ": strides must be in [0, 2^40]").c_str());
     if (B == 0 || T == 0) return CONDUIT_OK;
+    if (!within_reach(B, r->stride_b, T, r->stride_t, r->width))
+        return bad((w + ": rows must end within 2^56 elements of their start").c_str());
     if (!r->data) return bad((w + ": NULL data").c_str());
     if (misaligned(r->data, elem_size(r->dtype))) return bad((w + ": data must be aligned to its elements").c_str());
     if (out) {
@@ -494,6 +504,7 @@ void conduit_preference_opts_default(conduit_preference_opts* opts) {
 
 conduit_status conduit_preference_loss_workspace(int64_t P, int64_t T, uint64_t* bytes) {
     if (!bytes) return bad("NULL size pointer");
+    if (P < 0) return bad("the number of pairs must be >= 0");
     if (P > kMaxTokens / 2) return bad("the batch must hold fewer than 2^31 tokens");
     CONDUIT_TRY(check_batch(2 * P, T, T));
     *bytes = preference_layout(P, T).bytes;
@@ -509,6 +520,7 @@ conduit_status conduit_preference_loss(const conduit_preference_opts* opts, int6
     if (!(opts->label_smoothing >= 0.0 && opts->label_smoothing < 1.0)) return bad("label_smoothing must be in [0, 1)");
     if (!std::isfinite(opts->scale)) return bad("scale must be finite");
     if (opts->loss < CONDUIT_PREFERENCE_SIGMOID || opts->loss > CONDUIT_PREFERENCE_SQUARED) return bad("unknown preference loss");
+    if (P < 0) return bad("the number of pairs must be >= 0");
     if (P > kMaxTokens / 2) return bad("the batch must hold fewer than 2^31 tokens");
     CONDUIT_TRY(check_batch(2 * P, T, stride));
     if (!stats || misaligned(stats, 4)) return bad("stats must not be NULL (and aligned)");
