@@ -101,13 +101,14 @@ bool tokens_apart(const void* a, const void* b, int64_t B, int64_t T, int64_t st
     return d >= T * 4 && stride * 4 - d >= T * 4;
 }
 
-// every output apart from the other outputs, and from every input that it is not itself
-conduit_status check_outputs(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins, int64_t B,
-                             int64_t T, int64_t stride) {
+// every output apart from the other outputs, from every input `ins` that it is not itself, and from the tokens
+conduit_status check_outputs(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins,
+                             const int32_t* tokens, int64_t B, int64_t T, int64_t stride) {
     for (const void* o : outs)
         if (o && misaligned(o, 4)) return bad("per-token arrays must be aligned to their elements");
     for (const void* i : ins)
         if (i && misaligned(i, 4)) return bad("per-token arrays must be aligned to their elements");
+    if (misaligned(tokens, 4)) return bad("per-token arrays must be aligned to their elements");
     if (B == 0 || T == 0) return CONDUIT_OK;
     for (auto o = outs.begin(); o != outs.end(); ++o) {
         if (!*o) continue;
@@ -115,6 +116,7 @@ conduit_status check_outputs(std::initializer_list<const void*> outs, std::initi
             if (*p && !tokens_apart(*o, *p, B, T, stride)) return bad("outputs overlap");
         for (const void* i : ins)
             if (i && i != *o && !tokens_apart(*o, i, B, T, stride)) return bad("an output overlaps an input");
+        if (tokens && !tokens_apart(*o, tokens, B, T, stride)) return bad("an output overlaps the tokens");
     }
     return CONDUIT_OK;
 }
@@ -363,7 +365,7 @@ conduit_status conduit_token_logprobs(const conduit_rows* logits, int64_t B, int
     CONDUIT_TRY(check_temperature(temperature));
     if (B == 0 || T == 0) return CONDUIT_OK;
     if (!tokens) return bad("tokens must not be NULL");
-    CONDUIT_TRY(check_outputs({logp, lse, entropy}, {tokens}, B, T, stride));
+    CONDUIT_TRY(check_outputs({logp, lse, entropy}, {}, tokens, B, T, stride));
     const Layout l = logits_layout(B, T, logits);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
     uint32_t* err = nullptr;
@@ -389,7 +391,7 @@ conduit_status conduit_token_logprobs_backward(const conduit_rows* logits, int64
     if (B == 0 || T == 0) return CONDUIT_OK;
     if (!tokens || !lse) return bad("tokens and lse must not be NULL");
     if (dentropy && !entropy) return bad("the gradient of the entropy needs the entropy");
-    CONDUIT_TRY(check_outputs({}, {tokens, lse, entropy, dlogp, dentropy}, B, T, stride));
+    CONDUIT_TRY(check_outputs({}, {lse, entropy, dlogp, dentropy}, tokens, B, T, stride));
     uint32_t* err = nullptr;
     CONDUIT_TRY(standalone_error_words(&err));
     LogitsArgs a = logits_args(logits, B, T, stride, tokens, mask, temperature, err);
@@ -422,7 +424,7 @@ conduit_status conduit_policy_loss(const conduit_policy_opts* opts, int64_t B, i
     CONDUIT_TRY(check_batch(B, T, stride));
     if (!stats || misaligned(stats, 4)) return bad("stats must not be NULL (and aligned)");
     if (B > 0 && T > 0 && (!logp || !adv)) return bad("logp and adv must not be NULL");
-    CONDUIT_TRY(check_outputs({dlogp, dentropy}, {logp, old_logp, ref_logp, adv, entropy}, B, T, stride));
+    CONDUIT_TRY(check_outputs({dlogp, dentropy}, {logp, old_logp, ref_logp, adv, entropy}, nullptr, B, T, stride));
     const Layout l = policy_layout(B);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
     uint32_t* err = nullptr;
@@ -465,7 +467,7 @@ conduit_status conduit_policy_loss_logits(const conduit_policy_opts* opts, const
     for (const float* o : {(const float*)logp, (const float*)entropy})
         for (const float* i : {old_logp, ref_logp, adv})
             if (!empty && o && o == i) return bad("logp and entropy must be apart from the inputs");
-    CONDUIT_TRY(check_outputs({logp, entropy}, {tokens, old_logp, ref_logp, adv}, B, T, stride));
+    CONDUIT_TRY(check_outputs({logp, entropy}, {old_logp, ref_logp, adv}, tokens, B, T, stride));
     const Layout l = logits_layout(B, T, logits);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
     uint32_t* err = nullptr;
@@ -527,7 +529,7 @@ conduit_status conduit_preference_loss(const conduit_preference_opts* opts, int6
     if (P > 0 && (!loss || (T > 0 && !logp))) return bad("logp and loss must not be NULL");
     for (const float* o : {loss, chosen, rejected})
         if (o && misaligned(o, 4)) return bad("loss, chosen and rejected must be aligned to their elements");
-    CONDUIT_TRY(check_outputs({dlogp}, {logp, ref_logp}, 2 * P, T, stride));
+    CONDUIT_TRY(check_outputs({dlogp}, {logp, ref_logp}, nullptr, 2 * P, T, stride));
     const Layout l = preference_layout(P, T);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -575,7 +577,7 @@ conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_r
     CONDUIT_TRY(check_temperature(temperature));
     if (B == 0 || T == 0) return CONDUIT_OK;
     if (!tokens) return bad("tokens must not be NULL");
-    CONDUIT_TRY(check_outputs({logp, lse, entropy}, {tokens}, B, T, stride));
+    CONDUIT_TRY(check_outputs({logp, lse, entropy}, {}, tokens, B, T, stride));
     const HeadLayout l = head_layout(B, T, hidden, weight, V, false);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.bytes));
     uint32_t* err = nullptr;
@@ -616,7 +618,7 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
     if (!empty) {
         if (!tokens || !lse) return bad("tokens and lse must not be NULL");
         if (dentropy && !entropy) return bad("the gradient of the entropy needs the entropy");
-        CONDUIT_TRY(check_outputs({}, {tokens, lse, entropy, dlogp, dentropy}, B, T, stride));
+        CONDUIT_TRY(check_outputs({}, {lse, entropy, dlogp, dentropy}, tokens, B, T, stride));
         if (!apart(dhidden->data, rows_extent(dhidden, B, T), hidden->data, rows_extent(hidden, B, T)) ||
             !apart(dhidden->data, rows_extent(dhidden, B, T), weight->data, rows_extent(weight, 1, V)) ||
             !apart(dweight->data, rows_extent(dweight, 1, V), hidden->data, rows_extent(hidden, B, T)) ||
