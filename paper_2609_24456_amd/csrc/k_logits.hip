@@ -288,11 +288,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
     constexpr int NT = WAVES * kWave;
     constexpr int kTile = NT * K;  // vectors
     __shared__ Stat lds[WAVES];
-    uint32_t n = blockIdx.x;
-    if constexpr (WAVES == 1) {
-        n = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
-    }
+    uint32_t n = block_number();
+    if constexpr (WAVES == 1) n = n * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
     const uint32_t tid = threadIdx.x % NT;
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
@@ -517,7 +515,7 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
-    const uint32_t item = blockIdx.x * (kGradThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t item = block_number() * (kGradThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     if (item >= items) return;
     const uint32_t n = div31(item, by_row), part = item - n * per_row, lane = lane_id();
     const int64_t at = a.shape.at(n);
@@ -590,8 +588,8 @@ hipError_t launch_gradient(const LogitsArgs& a, hipStream_t s) {
     // one launch takes fewer than 2^31 parts (the division's range)
     const int64_t items = rows * per_row;
     if (items >= 1ll << 31) return hipErrorInvalidValue;
-    const unsigned grid = (unsigned)((items + kGradThreads / kWave - 1) / (kGradThreads / kWave));
-    hipLaunchKernelGGL((k_rows_gradient<BF16, SPLIT>), dim3(grid), dim3(kGradThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row,
+    const dim3 grid = grid_of((items + kGradThreads / kWave - 1) / (kGradThreads / kWave), kGradThreads);
+    hipLaunchKernelGGL((k_rows_gradient<BF16, SPLIT>), grid, dim3(kGradThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row,
                        make_div31((uint32_t)per_row));
     return hipGetLastError();
 }
@@ -623,13 +621,13 @@ template <bool BF16, int MODE>
 hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, bool few_rows, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
     if (nv <= 8 * kWave)
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p, few_rows);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), grid_of((rows + 3) / 4, 256), dim3(256), 0, s, a, p, few_rows);
     else if (MODE == LOGPROBS)  // nothing stays: any width goes by in tiles of 8 vectors a lane
-        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), dim3((unsigned)rows), dim3(256), 0, s, a, p, few_rows);
+        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), grid_of(rows, 256), dim3(256), 0, s, a, p, few_rows);
     else if (nv <= 4096)
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), dim3((unsigned)rows), dim3(256), 0, s, a, p, few_rows);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), grid_of(rows, 256), dim3(256), 0, s, a, p, few_rows);
     else
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), dim3((unsigned)rows), dim3(1024), 0, s, a, p, few_rows);
+        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), grid_of(rows, 1024), dim3(1024), 0, s, a, p, few_rows);
     return hipGetLastError();
 }
 

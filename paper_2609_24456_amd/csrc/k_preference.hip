@@ -134,7 +134,8 @@ __device__ __forceinline__ void write_means(const PreferenceArgs& a, double* lds
 
 __global__ __launch_bounds__(kPairThreads) void k_preference(PreferenceArgs a) {
     __shared__ double lds[4 * kPairThreads / kWave];
-    const int64_t p = blockIdx.x;
+    const int64_t p = block_number();
+    if (p >= a.P) return;
     const RowSum c = row_sum(a, p, 0, a.T), r = row_sum(a, a.P + p, 0, a.T);
     double s[4] = {c.v[0], c.v[1], r.v[0], r.v[1]};
     block_sum<kPairThreads, 4>(s, lds);
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(kPairThreads) void k_preference(PreferenceArgs a) {
         write_gradient(a, p, 0, a.T, (float)x.q_chosen);
         write_gradient(a, a.P + p, 0, a.T, (float)x.q_rejected);
     }
-    if (last_block(a.head, blockIdx.x, gridDim.x)) write_means(a, lds);
+    if (last_block(a.head, (uint32_t)p, (uint32_t)a.P)) write_means(a, lds);
 }
 
 // parts of rows: grid (parts, 2 P)
@@ -193,7 +194,7 @@ int preference_parts(int64_t P, int64_t T) {
 
 hipError_t launch_preference_loss(const PreferenceArgs& a, hipStream_t s) {
     if (a.parts <= 1) {
-        hipLaunchKernelGGL(k_preference, dim3((unsigned)a.P), dim3(kPairThreads), 0, s, a);
+        hipLaunchKernelGGL(k_preference, grid_of(a.P, kPairThreads), dim3(kPairThreads), 0, s, a);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)a.parts, (unsigned)(2 * a.P));

@@ -137,6 +137,18 @@ hipError_t launch_preference_loss(const PreferenceArgs& a, hipStream_t s);
 int preference_parts(int64_t P, int64_t T);
 
 // ---------------------------------------------------------------------------
+// launches of a workgroup for each of many rows
+// ---------------------------------------------------------------------------
+// A launch takes fewer than 2^32 threads in a dimension, so many workgroups are
+// spread over two; the last of them may have nothing to do.
+inline dim3 grid_of(int64_t blocks, int threads) {
+    constexpr int64_t kAcross = 1 << 20;
+    if (blocks * threads < 1ll << 32) return dim3((unsigned)blocks);
+    return dim3((unsigned)kAcross, (unsigned)((blocks + kAcross - 1) / kAcross));
+}
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
+// ---------------------------------------------------------------------------
 // constants and small functions
 // ---------------------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f;
