@@ -620,14 +620,16 @@ constexpr int64_t kShortWidth = 64 * kShortElems;
 template <bool BF16, int MODE>
 hipError_t launch_long(const LogitsArgs& a, const PolicyArgs& p, bool few_rows, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
-    if (nv <= 8 * kWave)
+    const dim3 grid = grid_of(rows, 256);
+    if (nv <= 8 * kWave) {
         hipLaunchKernelGGL((k_rows<BF16, MODE, 1, 8>), grid_of((rows + 3) / 4, 256), dim3(256), 0, s, a, p, few_rows);
-    else if (MODE == LOGPROBS)  // nothing stays: any width goes by in tiles of 8 vectors a lane
-        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), grid_of(rows, 256), dim3(256), 0, s, a, p, few_rows);
-    else if (nv <= 4096)
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 4, 16>), grid_of(rows, 256), dim3(256), 0, s, a, p, few_rows);
-    else
-        hipLaunchKernelGGL((k_rows<BF16, MODE, 16, 16>), grid_of(rows, 1024), dim3(1024), 0, s, a, p, few_rows);
+    } else if constexpr (MODE == LOGPROBS) {  // nothing stays: any width goes by in tiles of 8 vectors a lane
+        hipLaunchKernelGGL((k_rows<BF16, LOGPROBS, 4, 8>), grid, dim3(256), 0, s, a, p, few_rows);
+    } else if (nv <= 4096) {
+        hipLaunchKernelGGL((k_rows<BF16, LOSS, 4, 16>), grid, dim3(256), 0, s, a, p, few_rows);
+    } else {
+        hipLaunchKernelGGL((k_rows<BF16, LOSS, 16, 16>), grid_of(rows, 1024), dim3(1024), 0, s, a, p, few_rows);
+    }
     return hipGetLastError();
 }
 
