@@ -5,6 +5,7 @@ import torch
 
 from gpu_util import host
 from oracle import losses as ref
+from test_gpu_losses import _mask, _policy_check, _policy_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +100,29 @@ def test_means_are_rounded_once(B, T, reduction, masked):
     want = float(x.sum() / on.sum()) if reduction == "token_mean" else float((x.sum(1) / on.sum(1)).mean())
     s = _sums(adv, reduction, mask)
     assert abs(s[1] - want) <= 2.0 ** -24 * (1 + 1e-5) * want, (s[1] / want - 1) * 2 ** 24
+
+
+# up to 2,048 chunks of 4 tokens of a row, and up to 2,048 rows with weights of their own, one workgroup takes by itself:
+# both sides of each edge
+@pytest.mark.parametrize("B,T", [(1, 8192), (1, 8193), (2048, 1), (2049, 1), (2048, 4), (2047, 5), (1024, 8), (1025, 8)])
+@pytest.mark.parametrize("reduction", ["token_mean", "sequence_mean", "sum"])
+@pytest.mark.parametrize("columns", [False, True])
+def test_both_sides_of_the_largest_batch_of_one_workgroup(B, T, reduction, columns):
+    """`columns`: columns [1, T + 1) of wider arrays, whose rows are never taken as one."""
+    rng = np.random.default_rng(B + T)
+    x, mask = _policy_inputs(rng, B, T), _mask(rng, B, T)
+
+    def dev(a):
+        if not columns:
+            return torch.from_numpy(a).cuda()
+        w = torch.zeros((B, T + 1), dtype=torch.from_numpy(a).dtype, device="cuda")
+        w[:, 1:] = torch.from_numpy(a).cuda()
+        return w[:, 1:]
+
+    kw = dict(clip_low=0.2, clip_high=0.2, dual_clip=3.0, kl_coef=0.05, entropy_coef=0.01, reduction=reduction)
+    for m in (None, mask):
+        nine = np.full((B, T), 9.0, np.float32)
+        stats, g, h = torch.full((8,), 9.0, device="cuda"), dev(nine), dev(nine)
+        cd.conduit_policy_loss(cd.policy_opts(**kw), dev(x["logp"]), dev(x["adv"]), stats, g, old_logp=dev(x["old"]),
+                               ref_logp=dev(x["ref"]), entropy=dev(x["entropy"]), dentropy=h, mask=None if m is None else dev(m))
+        _policy_check(x, m, kw, (host(stats), host(g.contiguous()), host(h.contiguous())))
