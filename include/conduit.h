@@ -570,12 +570,13 @@ conduit_status conduit_minibatch_gather(const void* src, int64_t row_bytes, int6
  * arrays and their columns [1, T) alike can be passed as they are.  mask is
  * uint8 (NULL: every token counts): at tokens where it is 0 nothing counts,
  * whatever stands there (a NaN, a token outside the vocabulary): per-token outputs
- * and gradients are written as 0, and no sum or mean sees them.  B * T < 2^31.  Sums over tokens run in
+ * and gradients are written as 0, and no sum or mean sees them.  B * T < 2^31, and every array
+ * ends within 2^56 elements of its start.  Sums over tokens run in
  * fp64 and are joined in a fixed order: results are the same on every run.
  * Tokens outside [0, V) that the mask counts are flagged, and are treated as
  * masked but for the token counts.
  * Per-token outputs may be one of the call's per-token float inputs (in place),
- * and overlap none otherwise.
+ * and overlap none otherwise, the tokens never.
  *
  * Workspaces: `workspace` is device memory of at least the size that the
  * call's _workspace function reports, 256-byte aligned, made ready once by
@@ -762,7 +763,11 @@ conduit_status conduit_head_logprobs(const conduit_rows* hidden, const conduit_r
  * are fp32.  dhidden: bf16 rows like hidden (0 at masked
  * tokens); dweight: V bf16 rows; both are overwritten and apart from every
  * input.  The workspace holds the logits' gradient of up to all choices, at
- * most 4 GiB of it; more tokens run in chunks of choices.
+ * most 4 GiB of it (more tokens run in chunks of choices), and up to 128 parts of
+ * the hidden states' gradient in fp32, at most 4 GiB: for 4,096 tokens, 2,048 units
+ * and 128,000 choices 5.0 GiB in all, against 1.0 of bf16 logits.  Without a mask
+ * the hidden row of a token outside [0, V) is read and multiplied by 0: a NaN in it
+ * reaches dweight.
  * Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_head_logprobs_backward_workspace(int64_t B, int64_t T, const conduit_rows* hidden,

@@ -195,7 +195,7 @@ __device__ __forceinline__ bool token_ok(const LogitsArgs& a, int32_t tok) {
 
 // ---------------------------------------------------------------------------
 // short rows: LANES lanes a row, up to E elements a lane.  Latency bounds it: 16,384
-// rows of 18 with the loss and its gradient 7.2 us (an empty launch is 2.3, the
+// rows of 18 with the loss and its gradient 7.45 us (an empty launch is 2.3, the
 // bytes 0.6).
 // ---------------------------------------------------------------------------
 constexpr int kShortThreads = 256;
@@ -277,7 +277,8 @@ __global__ __launch_bounds__(kShortThreads) void k_rows_short(LogitsArgs a, Poli
 // ---------------------------------------------------------------------------
 // HBM bounds it.  Log-probabilities only: 256 lanes a row, several rows a compute
 // unit, so that one row's join runs under another's loads (8,176 rows of 32,001
-// fp32: 76 us, 5.4 TB/s; 1,024 lanes a row: 111).  The loss holds a whole row of up
+// fp32: 77 us, 5.3 TB/s, where a reduction over 4 GiB reads 6.0 and a copy moves
+// 4.7; 1,024 lanes a row: 111).  The loss holds a whole row of up
 // to 256 KB in 1,024 lanes' registers and writes its gradient from there (8,192
 // rows of 128,000 bf16, 36% of them live: 545 us for 2.9 GB, 5.2 TB/s).
 template <bool BF16, int MODE, int WAVES, int K>
@@ -373,7 +374,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_rows(Logit
 }
 
 // ---------------------------------------------------------------------------
-// few long rows: parts of rows, joined by the last workgroup of each row
+// few long rows: parts of rows, joined by the last workgroup of each row.  Latency
+// bounds it: 64 rows of 128,000 bf16 8.4 us; with the loss and the gradient's launch
+// 18.4 (16.4 MB read once and written once would take 6.7), one row 10.6.
 // ---------------------------------------------------------------------------
 constexpr int kPartThreads = 256;
 constexpr int kPartK = 8;

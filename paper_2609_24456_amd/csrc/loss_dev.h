@@ -161,7 +161,7 @@ __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_lo
 // what the rounding of t (and of log2(e)) left out, so that the error does not
 // grow with x
 __device__ __forceinline__ float exp_fast(float x) {
-    const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.925963033500762e-8f;  // (the last: log2(e) - kLog2e)
+    const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.9259629911e-8f;  // (the last: log2(e) - kLog2e)
     const float e = exp2_fast(t);
     return fabsf(t) < 128.0f ? fmaf(e, r * kLn2, e) : e;  // (beyond: 0 or infinity, which times r may be no number)
 }

@@ -137,7 +137,8 @@ conduit_status check_workspace(const void* ws, uint64_t bytes, uint64_t need) {
 
 // ---------------------------------------------------------------------------
 // workspaces: [head][row tickets][row counts][what one call leaves for its own
-// next launch].  The first three are zero between calls.
+// next launch].  The head and the tickets are zero between calls; the counts are
+// written whole before they are read.
 // ---------------------------------------------------------------------------
 uint64_t up(uint64_t x) { return (x + 255) / 256 * 256; }
 
