@@ -1,0 +1,111 @@
+// Rows of float or bf16 scores in 16-byte vectors (k_logits.hip, k_top.hip,
+// k_listed.hip).
+#pragma once
+
+#include "softmax_dev.h"
+
+namespace conduit {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <bool BF16>
+struct Elem;
+template <>
+struct Elem<true> {
+    using T = uint16_t;
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float one(T x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+    static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[kPer]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __builtin_bit_cast(float, v[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ T round(float x) { return __builtin_bit_cast(T, (__bf16)x); }
+    static __device__ __forceinline__ u32x4 pack(const float (&x)[kPer]) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (uint32_t)round(x[2 * i]) | (uint32_t)round(x[2 * i + 1]) << 16;
+        return v;
+    }
+};
+template <>
+struct Elem<false> {
+    using T = float;
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ float one(T x) { return x; }
+    static __device__ __forceinline__ void unpack(u32x4 v, float (&x)[kPer]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = v[i];  // (a value: bit_cast of a vector's element as an lvalue reads element 0)
+            x[i] = __builtin_bit_cast(float, w);
+        }
+    }
+    static __device__ __forceinline__ T round(float x) { return x; }
+    static __device__ __forceinline__ u32x4 pack(const float (&x)[kPer]) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, x[i]);
+        return v;
+    }
+};
+
+// 16-byte accesses at the elements' own alignment (rows of any width start anywhere)
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* p) {
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, u32x4 v) {
+    __builtin_memcpy(p, &v, 16);
+}
+
+// keeps a vector packed: without it the unpacked halves of one use would be kept
+// in registers for the next
+__device__ __forceinline__ u32x4 again(u32x4 v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// K vectors of a lane
+template <bool BF16, int K>
+__device__ __forceinline__ void accumulate_tile(Stat& st, const u32x4 (&v)[K], float c) {
+    using E = Elem<BF16>;
+    float top = kNone;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(v[k], f);
+        top = top_of(f, top);
+    }
+    raise(st, top, c);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(again(v[k]), f);
+        add(st, f, c);
+    }
+}
+
+// joined over WAVES wavefronts of a workgroup, in every thread
+template <int WAVES>
+__device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
+    s = join_lanes<kWave>(s, c);
+    if constexpr (WAVES == 1) return s;
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = s;
+    __syncthreads();
+    Stat r = lds[lane_id() % WAVES];
+    return join_lanes<WAVES>(r, c);
+}
+
+// a vector of scores at -inf
+template <bool BF16>
+__device__ __forceinline__ u32x4 no_vector() {
+    constexpr uint32_t w = BF16 ? 0xff80ff80u : 0xff800000u;
+    return u32x4{w, w, w, w};
+}
+
+}  // namespace conduit
