@@ -589,7 +589,7 @@ conduit_status conduit_minibatch_gather(const void* src, int64_t row_bytes, int6
  * b * stride_b + t * stride_t of `data` (device). */
 typedef struct {
     void* data;
-    int32_t dtype;   /* CONDUIT_F32 or CONDUIT_BF16 */
+    int32_t dtype;   /* CONDUIT_F32 or CONDUIT_BF16 (rows of choices' numbers: CONDUIT_I32) */
     int32_t reserved;
     int64_t width;
     int64_t stride_b, stride_t;
@@ -780,6 +780,123 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
                                               void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Listed choices: a few choices of every token instead of all of them.  A
+ * listed array holds K numbers of choices (ids: I32) or K values (F32) a token,
+ * rows of 1 <= K <= 128 elements in the layout of the logits' rows.  Scores,
+ * workspaces, masks and errors as above.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * The K most probable choices of every token with their log-probabilities
+ * (a teacher's answer, the alternatives of a served token), in one pass over the
+ * logits with what conduit_token_logprobs gives.  ids and logps: the choices in
+ * falling order of their logits, the lowest number first among equal ones (-0
+ * and 0 are equal), choices at -inf among them; beyond V choices the number -1
+ * with log-probability -inf.  Masked tokens have 0 in both.  A row with a NaN or
+ * +inf has no ranking: its numbers are -1 and its log-probabilities NaN.  tokens
+ * may be NULL (then logp must be); logp, lse and entropy may be.  ids and logps
+ * are apart from each other and from every other array of the call.
+ * Rows of up to 2,048 choices take a wavefront, wider ones a workgroup; fewer
+ * rows than the GPU has compute units, and rows of more than 2^18 bf16 (2^17
+ * float) choices, are split into parts that the row's last workgroup joins, or,
+ * for more than 512 rows, a second launch.
+ * Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_token_alternatives_workspace(int64_t B, int64_t T, const conduit_rows* logits, int64_t K,
+                                                    uint64_t* bytes);
+conduit_status conduit_token_alternatives(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
+                                          const int32_t* tokens, const uint8_t* mask, double temperature,
+                                          const conduit_rows* ids, const conduit_rows* logps, float* logp, float* lse,
+                                          float* entropy, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * Log-probabilities of K given choices of every token, and of all other choices
+ * together:
+ *     logps_k = z_id - lse,   rest = log sum_{j not listed} exp(z_j - lse),
+ * z and lse as in conduit_token_logprobs.  A negative number is an entry without
+ * a choice: its log-probability is -inf.  A number >= V is flagged and taken
+ * likewise.  Equal numbers have equal log-probabilities, and count once outside
+ * the rest.  rest is summed over the others themselves (no difference of sums)
+ * and is -inf where they have no weight; a row of -inf alone gives -inf
+ * throughout.  rest and lse: float [B, T], each may be NULL.  logps is apart from
+ * every other array.  Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_listed_logprobs_workspace(int64_t B, int64_t T, const conduit_rows* logits, int64_t K, uint64_t* bytes);
+conduit_status conduit_listed_logprobs(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
+                                       const conduit_rows* ids, const uint8_t* mask, double temperature,
+                                       const conduit_rows* logps, float* rest, float* lse, void* workspace,
+                                       uint64_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of conduit_listed_logprobs: for gradients dlogps of the listed
+ * log-probabilities (of entries without a choice: not read into any sum) and
+ * drest of the rest (NULL: none), from the logits and the forward call's lse
+ * (and rest, with drest), with G the sum of a token's gradients:
+ *     dx_j = (sum_{id_k = j} dlogps_k + [j not listed] drest p_j / exp(rest) - p_j G) / temperature
+ * dlogits: rows of the logits' dtype and width, rounded once; it may be the
+ * logits themselves (in place), and is apart from every other array.  Masked
+ * rows are written as 0, and so are rows whose lse is -inf; a rest of -inf has no
+ * gradient.  Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_listed_logprobs_backward(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
+                                                const conduit_rows* ids, const uint8_t* mask, double temperature,
+                                                const float* lse, const float* rest, const conduit_rows* dlogps,
+                                                const float* drest, const conduit_rows* dlogits, void* stream);
+
+/* which divergence of student p and teacher q */
+typedef int32_t conduit_distill_kind;
+enum {
+    CONDUIT_DISTILL_FORWARD = 0, /* sum q log (q / p) */
+    CONDUIT_DISTILL_REVERSE = 1, /* sum p log (p / q) (needs the rest) */
+};
+
+typedef struct {
+    double teacher_temperature; /* without the rest: further softening of the teacher's values; default 1 */
+    double scale;               /* of the loss and its gradient; default 1 */
+    conduit_distill_kind loss;
+    conduit_reduction reduction;
+    int32_t rest;               /* 0 (default): the listed choices are all of the teacher's; 1: what they leave is one more */
+    int32_t reserved;
+} conduit_distill_opts;
+
+void conduit_distill_opts_default(conduit_distill_opts* opts);
+
+/*
+ * The divergence of a student from a teacher that is known at K listed choices,
+ * and its gradient, logits to their gradient in one call.  ids and teacher: the
+ * choices' numbers and the teacher's values y_k.  Entries whose number is
+ * negative, >= V (flagged) or in the list before, or whose value is -inf, are as
+ * if not there.  p is the student's probability at `temperature`.
+ *     rest = 0: q_k = exp(y_k / teacher_temperature) over the sum of these (y:
+ *         logits or log-probabilities); a token with no entries has divergence 0.
+ *     rest = 1: y are log-probabilities, q_k = exp(y_k), and all choices that are
+ *         not listed count as one with q_r = max(1 - sum q_k, 2^-23) and p_r the
+ *         sum of their probabilities; where these have no weight in the student's
+ *         row they add nothing.
+ * Per counted token KL = sum q log (q / p) or sum p log (p / q) over the listed
+ * choices (and the rest);
+ *     loss[t] = KL,  stats[0] = scale * sum w weight[t] KL,  w by `reduction`,
+ *     dx_j = scale w weight[t] (dKL / dz_j) / temperature.
+ * weight: float [B, T] or NULL (1).  loss: float [B, T], apart from the inputs (0
+ * where the mask is).  stats: float [3]: the loss; the mean of KL over the counted
+ * tokens; the counted tokens.  dlogits: as in conduit_listed_logprobs_backward,
+ * or NULL (no gradient).  A row of -inf alone, and a listed choice at -inf that
+ * the teacher gives weight (forward), have infinite divergence; the former's
+ * gradient is 0, and so is that of a token of weight 0.  A batch without counted
+ * tokens gives zeros.
+ * Rows of up to 256 KB cross memory once in each direction.  Up to four launches:
+ * the count of the tokens (with a mask), the rows, and where these are split the
+ * join of more than 512 and the gradient, or the sums of a batch of more than 512
+ * rows wider than 2,048.  Errors: EINVAL, EDEVICE, ESTATE.
+ */
+conduit_status conduit_distill_loss_workspace(int64_t B, int64_t T, const conduit_rows* logits, int64_t K, uint64_t* bytes);
+conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const conduit_rows* logits, int64_t B, int64_t T,
+                                    int64_t stride, const conduit_rows* ids, const conduit_rows* teacher,
+                                    const float* weight, const uint8_t* mask, double temperature, float* loss,
+                                    float* stats, const conduit_rows* dlogits, void* workspace,
+                                    uint64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * State, introspection, errors
  * ------------------------------------------------------------------------- */
 typedef struct {
@@ -928,7 +1045,7 @@ conduit_status conduit_buffer_restore(conduit_buffer* buf, const void* src, uint
  * Wait for `stream`, then report the sticky device-side error flag of `buf`
  * (NULL: the flag shared by the stand-alone calls conduit_gae,
  * conduit_gae_packed, conduit_minibatch_gather and those that take tokens
- * (conduit_token_logprobs to conduit_head_logprobs_backward), and then the words
+ * (conduit_token_logprobs to conduit_distill_loss), and then the words
  * conduit_gae_noalloc keeps in the current GPU's static table).  Returns OK or ESTATE (with
  * a description in conduit_last_error), or EDEVICE.
  */

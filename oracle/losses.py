@@ -117,3 +117,142 @@ def preference_loss(logp, ref=None, mask=None, beta=0.1, loss="sigmoid", label_s
     for b in range(2 * P):
         g[b][on[b]] = scale * (q[b] if b < P else -q[b - P]) / P / n[b]
     return out, beta * d[:P], beta * d[P:], np.array([scale * out.mean(), (u > 0).mean(), u.mean(), on.sum()]), g
+
+
+def _lists(ids, V, values=None):
+    """[(place, number)] of a token's entries that are choices (and, with values, not at -inf)."""
+    return [(k, int(j)) for k, j in enumerate(ids) if 0 <= j < V and (values is None or values[k] != -np.inf)]
+
+
+def alternatives(logits, K, mask=None, temperature=1.0):
+    """(numbers, log-probabilities) of the K largest logits of every row, the lowest number first among equal ones."""
+    x = np.asarray(logits, np.float64)
+    ids, logps = np.zeros(x.shape[:-1] + (K,), np.int64), np.zeros(x.shape[:-1] + (K,))
+    for at in np.ndindex(*x.shape[:-1]):
+        if mask is not None and not mask[at]:
+            continue
+        row = x[at]
+        if np.isnan(row).any() or np.isposinf(row).any():
+            ids[at], logps[at] = -1, np.nan
+            continue
+        best = np.argsort(-row, kind="stable")[:K]
+        ids[at], logps[at] = -1, -np.inf
+        ids[at][:len(best)] = best
+        if row.max() > -np.inf:
+            z = (row - row.max()) / temperature
+            logps[at][:len(best)] = z[best] - np.log(np.exp(z).sum())
+    return ids, logps
+
+
+def _row_of(row, listed, temperature):
+    """(log-probability of every choice, log-probability of those not in `listed`, log-normaliser) of a row."""
+    top = row.max()
+    if top == -np.inf:
+        return np.full(row.shape, -np.inf), -np.inf, -np.inf
+    z = (row - top) / temperature
+    log_sum = np.log(np.exp(z).sum())
+    rest = np.delete(z, sorted(set(listed)))
+    near = rest.max() if rest.size else -np.inf
+    logrest = near + np.log(np.exp(rest - near).sum()) - log_sum if near > -np.inf else -np.inf
+    return z - log_sum, logrest, top / temperature + log_sum
+
+
+def listed_logprobs(logits, ids, mask=None, temperature=1.0):
+    """(log-probabilities of ids, log-probability of all others, log-normaliser)."""
+    x = np.asarray(logits, np.float64)
+    logps, rest, lse = np.zeros(ids.shape), np.zeros(x.shape[:-1]), np.zeros(x.shape[:-1])
+    for at in np.ndindex(*x.shape[:-1]):
+        if mask is not None and not mask[at]:
+            continue
+        entries = _lists(ids[at], x.shape[-1])
+        logp, rest[at], lse[at] = _row_of(x[at], [j for _, j in entries], temperature)
+        logps[at] = -np.inf
+        for k, j in entries:
+            logps[at][k] = logp[j]
+    return logps, rest, lse
+
+
+def listed_gradient(logits, ids, g, h=None, mask=None, temperature=1.0):
+    """Gradient of sum(g logps + h rest) with respect to the logits."""
+    x = np.asarray(logits, np.float64)
+    d = np.zeros(x.shape)
+    for at in np.ndindex(*x.shape[:-1]):
+        entries = _lists(ids[at], x.shape[-1])
+        logp, rest, lse = _row_of(x[at], [j for _, j in entries], temperature)
+        if (mask is not None and not mask[at]) or lse == -np.inf:
+            continue
+        p = np.exp(logp)
+        for k, j in entries:
+            d[at] -= g[at][k] * p
+            d[at][j] += g[at][k]
+        if h is not None and rest > -np.inf:
+            share = np.exp(logp - rest)
+            share[[j for _, j in entries]] = 0
+            d[at] += h[at] * (share - p)
+    return d / temperature
+
+
+def distill_loss(logits, ids, teacher, loss="forward", rest=False, teacher_temperature=1.0, scale=1.0,
+                 reduction="token_mean", weight=None, mask=None, temperature=1.0, sizes=None):
+    """(loss per token, stats[3], gradient).  sizes: a list that receives, for every token, what its rounding errors go
+    by: the largest |log(q / p)| that counts, and exp(log(q / p)) of the rest."""
+    x = np.asarray(logits, np.float64)
+    B, T, V = x.shape
+    on = np.ones((B, T), bool) if mask is None else np.asarray(mask) != 0
+    n, rows = int(on.sum()), int(on.any(1).sum())
+    out, d, total = np.zeros((B, T)), np.zeros(x.shape), 0.0
+    for b, t in np.argwhere(on):
+        w = {"token_mean": 1 / n, "sequence_mean": 1 / (rows * max(1, on[b].sum())), "sum": 1.0}[reduction]
+        w *= 1.0 if weight is None else float(weight[b, t])
+        at = (b, t)
+        y, first = np.asarray(teacher[at], np.float64), {}
+        for k, j in _lists(ids[at], V, y):
+            first.setdefault(j, y[k])
+        js = np.array(sorted(first), int)
+        y = np.array([first[j] for j in js])
+        logp, logrest, lse = _row_of(x[at], js, temperature)
+        if not rest and not len(js):
+            continue
+        if lse == -np.inf:
+            out[at] = np.inf
+            total += w * np.inf if w else 0.0
+            continue
+        p = np.exp(logp)
+        if not rest:
+            y = y / teacher_temperature
+            y = y - y.max()
+            logq = y - np.log(np.exp(y).sum())
+            q, q_rest = np.exp(logq), 0.0
+            some = False
+        else:
+            logq, q = y, np.exp(y)
+            some = logrest > -np.inf
+            q_rest = max(1 - q.sum(), 2.0 ** -23) if some else 0.0
+        away = np.log(q_rest) - logrest if some else 0.0
+        others = np.ones(V, bool)
+        others[js] = False
+        g = np.zeros(V)
+        if loss == "forward":
+            terms = np.where(q > 0, q * (logq - logp[js]), 0.0)
+            out[at] = terms.sum() + q_rest * away
+            g = p * (q.sum() + q_rest)
+            g[js] -= q
+            if some:
+                g[others] -= np.exp(logp[others] - logrest) * q_rest
+            used = q > 0
+        else:
+            used = p[js] > 0
+            terms = p[js][used] * (logp[js][used] - logq[used])
+            out[at] = terms.sum() - (np.exp(logrest) * away if some else 0.0)
+            by = np.zeros(V)  # log(p / q) of every choice, of the rest as one
+            by[js[used]] = logp[js][used] - logq[used]
+            by[others] = -away
+            g = p * (by - out[at])
+        if w:
+            d[at] = scale * w * g / temperature
+            total += w * out[at]
+        if sizes is not None:
+            u = (logq - logp[js])[used & np.isfinite(logp[js])]
+            sizes.append((at, w, p, js, q, max(np.abs(u).max() if u.size else 0.0, abs(away)), np.exp(min(away, 80.0)) if some else 0.0))
+    stats = np.array([scale * total, out[on].sum() / n if n else 0.0, n])
+    return out, stats, d

@@ -141,6 +141,16 @@ class PreferenceOpts(C.Structure):
                 ("loss", C.c_int32), ("length_norm", C.c_int32)]
 
 
+DISTILL_FORWARD, DISTILL_REVERSE = 0, 1
+DIVERGENCES = {"forward": DISTILL_FORWARD, "reverse": DISTILL_REVERSE}
+MAX_LISTED = 128
+
+
+class DistillOpts(C.Structure):
+    _fields_ = [("teacher_temperature", C.c_double), ("scale", C.c_double), ("loss", C.c_int32),
+                ("reduction", C.c_int32), ("rest", C.c_int32), ("reserved", C.c_int32)]
+
+
 # every symbol include/conduit.h declares, with its ctypes signature
 P = C.c_void_p
 I64 = C.c_int64
@@ -201,6 +211,14 @@ SIGNATURES = {
     "conduit_head_logprobs": (ST, [P, P, I64, I64, I64, I64, P, P, F64, P, P, P, P, C.c_uint64, P]),
     "conduit_head_logprobs_backward_workspace": (ST, [I64, I64, P, P, I64, P]),
     "conduit_head_logprobs_backward": (ST, [P, P, I64, I64, I64, I64, P, P, F64, P, P, P, P, P, P, P, C.c_uint64, P]),
+    "conduit_token_alternatives_workspace": (ST, [I64, I64, P, I64, P]),
+    "conduit_token_alternatives": (ST, [P, I64, I64, I64, P, P, F64, P, P, P, P, P, P, C.c_uint64, P]),
+    "conduit_listed_logprobs_workspace": (ST, [I64, I64, P, I64, P]),
+    "conduit_listed_logprobs": (ST, [P, I64, I64, I64, P, P, F64, P, P, P, P, C.c_uint64, P]),
+    "conduit_listed_logprobs_backward": (ST, [P, I64, I64, I64, P, P, F64, P, P, P, P, P, P]),
+    "conduit_distill_opts_default": (None, [P]),
+    "conduit_distill_loss_workspace": (ST, [I64, I64, P, I64, P]),
+    "conduit_distill_loss": (ST, [P, P, I64, I64, I64, P, P, P, P, F64, P, P, P, P, C.c_uint64, P]),
     "conduit_run_offpolicy": (ST, [P, P, P, P, P, P, P]),
 }
 

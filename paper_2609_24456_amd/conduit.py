@@ -742,6 +742,141 @@ def conduit_head_logprobs_backward(hidden, weight, tokens, lse, dlogp, dhidden, 
                                                 en, g, h, C.byref(dx), C.byref(dw), wp, wn, _stream(stream)))
 
 
+# ---------------------------------------------------------------------------
+# listed choices: ids [B, T, K] int32 (or [T, K]) and values float32 of the same shape, elements next to each other
+# along K; per-token tensors as above
+# ---------------------------------------------------------------------------
+def _listed_ptr(t, dtypes, name, ids):
+    """conduit_rows of a tensor of one row for each of `ids`' rows; dtypes: what it may be."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    r = Rows()
+    if _native_rows is not None and _native_rows(C.addressof(r), t, ids, F32, BF16, I32):
+        return r
+    if t.dim() not in (2, 3) or t.dim() != ids.dim() or t.shape[:-1] != ids.shape[:-1]:
+        raise ValueError(f"{name} must be {tuple(ids.shape[:-1])} rows, got a tensor of shape {tuple(t.shape)}")
+    if t.shape[-1] > 1 and t.numel() > 0 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have its row's elements next to each other")
+    if not _on_device(t):
+        raise ValueError(f"{name} must be on a HIP device")
+    r.data, r.dtype, r.reserved, r.width, r.stride_t = t.data_ptr(), _TORCH_DTYPE[t.dtype], 0, t.shape[-1], t.stride(-2)
+    r.stride_b = t.stride(0) if t.dim() == 3 else 0
+    return r
+
+
+_FLOAT_ROWS = (torch.float32, torch.bfloat16)
+_VALUES = (torch.float32,)
+
+
+def _listed_ids(ids):
+    return _listed_ptr(ids, (torch.int32,), "ids", ids)
+
+
+def _listed_values(t, name, ids):
+    r = _listed_ptr(t, _VALUES, name, ids)
+    if t.shape[-1] != ids.shape[-1]:
+        raise ValueError(f"{name} must have the shape of ids, {tuple(ids.shape)}, got {tuple(t.shape)}")
+    return r
+
+
+def _listed_tokens(ids, *args):
+    """_token_ptrs of per-token tensors of which any may be None; they are shaped like `ids` without its last dimension."""
+    some = next((i for i in range(0, len(args), 3) if args[i] is not None), None)
+    if some is None:
+        B, T = ids.shape[:-1] if ids.dim() == 3 else (1, ids.shape[0])
+        return (B, T, T) + (None,) * (len(args) // 3)
+    if isinstance(args[some], torch.Tensor) and args[some].shape != ids.shape[:-1]:
+        raise ValueError(f"{args[some + 2]} must have shape {tuple(ids.shape[:-1])}, got {tuple(args[some].shape)}")
+    got = _token_ptrs(*args[some:])
+    return got[:3] + (None,) * (some // 3) + got[3:]
+
+
+def _listed_bytes(entry, logits, K):
+    n = C.c_uint64()
+    B, T = (logits.shape[0], logits.shape[1]) if logits.dim() == 3 else (1, logits.shape[0])
+    _check(entry(B, T, C.byref(_rows_struct(logits, "logits")), int(K), C.byref(n)))
+    return n.value
+
+
+def token_alternatives_workspace(logits, K):
+    """Bytes of workspace that conduit_token_alternatives needs for these logits and K choices a token."""
+    return _listed_bytes(lib().conduit_token_alternatives_workspace, logits, K)
+
+
+def conduit_token_alternatives(logits, ids, logps, tokens=None, logp=None, lse=None, entropy=None, mask=None,
+                               temperature=1.0, workspace=None, stream=None):
+    """The K most probable choices of every token of logits [B, T, V] into ids and logps [B, T, K], and with tokens what
+    conduit_token_logprobs gives."""
+    f = torch.float32
+    i, lps = _listed_ids(ids), _listed_values(logps, "logps", ids)
+    B, T, step, tok, lp, ls, en, mk = _listed_tokens(ids, tokens, torch.int32, "tokens", logp, f, "logp", lse, f, "lse",
+                                                     entropy, f, "entropy", mask, _U8, "mask")
+    x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
+    ws, wp, wn = _workspace(workspace, lambda: token_alternatives_workspace(logits, ids.shape[-1]), stream)
+    _check(lib().conduit_token_alternatives(C.byref(x), B, T, step, tok, mk, temperature, C.byref(i), C.byref(lps), lp, ls, en,
+                                            wp, wn, _stream(stream)))
+
+
+def listed_logprobs_workspace(logits, K):
+    """Bytes of workspace that conduit_listed_logprobs needs for these logits and K choices a token."""
+    return _listed_bytes(lib().conduit_listed_logprobs_workspace, logits, K)
+
+
+def conduit_listed_logprobs(logits, ids, logps, rest=None, lse=None, mask=None, temperature=1.0, workspace=None,
+                            stream=None):
+    """Log-probabilities of the choices ids [B, T, K] under logits [B, T, V], and of all others together (rest)."""
+    f = torch.float32
+    i, lps = _listed_ids(ids), _listed_values(logps, "logps", ids)
+    B, T, step, rs, ls, mk = _listed_tokens(ids, rest, f, "rest", lse, f, "lse", mask, _U8, "mask")
+    x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
+    ws, wp, wn = _workspace(workspace, lambda: listed_logprobs_workspace(logits, ids.shape[-1]), stream)
+    _check(lib().conduit_listed_logprobs(C.byref(x), B, T, step, C.byref(i), mk, temperature, C.byref(lps), rs, ls, wp, wn,
+                                         _stream(stream)))
+
+
+def conduit_listed_logprobs_backward(logits, ids, lse, dlogps, dlogits, rest=None, drest=None, mask=None, temperature=1.0,
+                                     stream=None):
+    """The gradient of conduit_listed_logprobs's logits, into dlogits (the logits themselves: in place)."""
+    f = torch.float32
+    i, g = _listed_ids(ids), _listed_values(dlogps, "dlogps", ids)
+    B, T, step, ls, rs, h, mk = _listed_tokens(ids, lse, f, "lse", rest, f, "rest", drest, f, "drest", mask, _U8, "mask")
+    x, dx = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids), _listed_ptr(dlogits, _FLOAT_ROWS, "dlogits", ids)
+    _check(lib().conduit_listed_logprobs_backward(C.byref(x), B, T, step, C.byref(i), mk, temperature, ls, rs, C.byref(g), h,
+                                                  C.byref(dx), _stream(stream)))
+
+
+def distill_opts(loss="forward", rest=False, teacher_temperature=1.0, scale=1.0, reduction="token_mean"):
+    """Options of the distillation loss."""
+    o = DistillOpts()
+    o.loss, o.rest, o.teacher_temperature = DIVERGENCES[loss], int(bool(rest)), float(teacher_temperature)
+    o.scale, o.reduction = float(scale), REDUCTIONS[reduction]
+    return o
+
+
+DISTILL_STATS = ("loss", "divergence", "tokens")
+
+
+def distill_loss_workspace(logits, K):
+    """Bytes of workspace that conduit_distill_loss needs for these logits and K choices a token."""
+    return _listed_bytes(lib().conduit_distill_loss_workspace, logits, K)
+
+
+def conduit_distill_loss(opts, logits, ids, teacher, loss, stats, dlogits=None, weight=None, mask=None, temperature=1.0,
+                         workspace=None, stream=None):
+    """The divergence of logits [B, T, V] from a teacher's values at the choices ids [B, T, K]: per token, stats
+    (DISTILL_STATS), and the gradient dlogits (the logits themselves: in place; None: no gradient)."""
+    f = torch.float32
+    i, y = _listed_ids(ids), _listed_values(teacher, "teacher", ids)
+    B, T, step, ls, w, mk = _listed_tokens(ids, loss, f, "loss", weight, f, "weight", mask, _U8, "mask")
+    x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
+    dx = None if dlogits is None else C.byref(_listed_ptr(dlogits, _FLOAT_ROWS, "dlogits", ids))
+    ws, wp, wn = _workspace(workspace, lambda: distill_loss_workspace(logits, ids.shape[-1]), stream)
+    _check(lib().conduit_distill_loss(C.byref(opts), C.byref(x), B, T, step, C.byref(i), C.byref(y), w, mk, temperature, ls,
+                                      _ptr(stats, f, "stats", numel=3), dx, wp, wn, _stream(stream)))
+
+
 def conduit_buffer_get_info(handle):
     return _info(handle)
 

@@ -1,0 +1,1010 @@
+// Log-probabilities of a few listed choices of every token and of all others
+// together, their gradient, and the divergence of a student from a teacher whose
+// probabilities are known at the listed choices, logits to their gradient in one
+// call (conduit_listed_logprobs, _backward, conduit_distill_loss).
+//
+// The pass over a row sums the others only: the listed choices are marked in a
+// bit map in LDS and count as -infinity there.  What is left to the others is
+// often far smaller than what the listed ones hold, and would be lost in the
+// difference of two sums.  With m, s the others' maximum and sum, and M, S the
+// whole row's, in powers of two as in k_logits.hip:
+//     log p_k = ln2 (c (x_k - M) - log2 S),   log p_rest = ln2 (log2 s + c (m - M) - log2 S).
+// The divergence goes by u = log q - log p of each listed choice, and of the rest
+// where it counts as one more:
+//     forward  sum q log (q / p) = sum q (exp(-u) - 1 + u) + sum q - sum p
+//     reverse  sum p log (p / q) = sum p (exp u - 1 - u) + sum p - sum q
+// whose terms have one sign, so that a small divergence is not a difference of
+// large sums.  The gradient of a listed choice goes by its own u, that of any
+// other is 2^(c (x - m)) times one number of the row.
+//
+// Duplicates of a choice are found by the bit map (a bit that is set already),
+// and only then looked for in the list.
+#include <type_traits>
+
+#include "listed_dev.h"
+#include "rows_dev.h"
+
+namespace conduit {
+
+namespace {
+
+enum ListedMode { SCORES, DISTILL };
+
+constexpr int kListedThreads = 256;
+
+// ---------------------------------------------------------------------------
+// sums over the choices that are not listed
+// ---------------------------------------------------------------------------
+struct Mass {
+    float m, s;
+};
+
+__device__ __forceinline__ Mass no_mass() { return Mass{kNone, 0.0f}; }
+
+template <int N>
+__device__ __forceinline__ void add_mass(Mass& t, const float (&x)[N], float c) {
+    const float base = t.m == kNone ? 0.0f : t.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) t.s += exp2_fast((x[i] - base) * c);
+}
+
+__device__ __forceinline__ void raise_mass(Mass& t, float top, float c) {
+    if (top > t.m) {
+        t.s *= exp2_fast((t.m - top) * c);
+        t.m = top;
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void accumulate_mass(Mass& t, const float (&x)[N], float c) {
+    raise_mass(t, top_of(x, kNone), c);
+    add_mass(t, x, c);
+}
+
+template <bool BF16, int K>
+__device__ __forceinline__ void accumulate_mass_tile(Mass& t, const u32x4 (&v)[K], float c) {
+    using E = Elem<BF16>;
+    float top = kNone;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(v[k], f);
+        top = top_of(f, top);
+    }
+    raise_mass(t, top, c);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[E::kPer];
+        E::unpack(again(v[k]), f);
+        add_mass(t, f, c);
+    }
+}
+
+// joined over groups of LANES lanes that are alike, or over all of them, in every lane
+template <int LANES>
+__device__ __forceinline__ Mass join_mass(const Mass& a, float c) {
+    Mass r;
+    r.m = lanes_reduce<LANES>(a.m, [](float x, float y) { return x > y ? x : y; });
+    r.s = lanes_sum<LANES>(a.s * exp2_fast(a.m == r.m ? 0.0f : (a.m - r.m) * c));
+    return Mass{uniform(r.m), uniform(r.s)};
+}
+
+// ---------------------------------------------------------------------------
+// the listed choices of a token: two a lane of a wavefront
+// ---------------------------------------------------------------------------
+constexpr int kLists = kMostListed / kWave;
+
+struct Listed {
+    int32_t id[kLists];
+    float y[kLists];     // the teacher's value, or the gradient
+    float x[kLists];     // the score
+    bool on[kLists];     // a choice of the row
+    bool first[kLists];  // the first of its number in the list
+};
+
+__device__ __forceinline__ void load_ids(const ListedArgs& a, uint32_t n, Listed& e) {
+    const int32_t* ids = static_cast<const int32_t*>(a.ids.data) + a.ids.at(n, a.shape);
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        const int32_t k = i * kWave + lane_id();
+        e.id[i] = k < a.K ? ids[k] : -1;
+    }
+}
+
+__device__ __forceinline__ void load_values(const ListedArgs& a, const RowsView& rows, uint32_t n, Listed& e) {
+    const float* y = static_cast<const float*>(rows.data) + rows.at(n, a.shape);
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        const int32_t k = i * kWave + lane_id();
+        e.y[i] = k < a.K ? y[k] : 0.0f;
+    }
+}
+
+// which of them are choices at all: a teacher's of value -infinity is as if not listed
+template <bool VALUES>
+__device__ __forceinline__ void check_ids(const ListedArgs& a, Listed& e, bool flags) {
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        e.on[i] = e.id[i] >= 0 && e.id[i] < a.V && !(VALUES && e.y[i] == kNone);
+        e.first[i] = e.on[i];
+        if (flags && e.id[i] >= a.V) flag_error(a.err, ERR_TOKEN);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load_scores(const typename Elem<BF16>::T* x, Listed& e) {
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) e.x[i] = e.on[i] ? Elem<BF16>::one(x[e.id[i]]) : kNone;
+}
+
+// Those of a number that the list has before are not the first.  sum: the values of
+// equal numbers are added up at the first, in the list's order.
+template <bool SUM>
+__device__ void find_first(Listed& e, int32_t K) {
+    float y[kLists];
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) y[i] = e.y[i];
+    for (int32_t j = 0; j < K; ++j) {
+        const int i = j / kWave, from = j % kWave;  // (uniform)
+        const int32_t id = __shfl(i == 0 ? e.id[0] : e.id[1], from, kWave);
+        const float v = __shfl(i == 0 ? y[0] : y[1], from, kWave);
+        if (!__shfl((int)(i == 0 ? e.on[0] : e.on[1]), from, kWave)) continue;
+#pragma unroll
+        for (int k = 0; k < kLists; ++k) {
+            const int32_t mine = k * kWave + lane_id();
+            if (!e.on[k] || e.id[k] != id || mine == j) continue;
+            if (mine > j) e.first[k] = false;
+            else if (SUM) e.y[k] += v;
+        }
+    }
+}
+
+// Marks the listed choices of one or more lanes' elements; true if a number is
+// there twice.  place(id, &word, &bit): false if the choice is not among them.
+template <typename Place>
+__device__ __forceinline__ bool mark(const Listed& e, Place place) {
+    bool twice = false;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        uint32_t* word;
+        uint32_t bit;
+        if (e.on[i] && place((uint32_t)e.id[i], &word, &bit)) twice |= (atomicOr(word, bit) & bit) != 0;
+    }
+    return __ballot(twice) != 0;
+}
+
+// elements of a vector whose bits are set, at -infinity
+template <bool BF16>
+__device__ __forceinline__ u32x4 without(u32x4 v, uint32_t bits) {
+    constexpr uint32_t kLow = BF16 ? 0xff80u : 0xff800000u;
+#pragma unroll
+    for (int j = 0; j < Elem<BF16>::kPer; ++j) {
+        if (!(bits >> j & 1)) continue;
+        if constexpr (BF16) v[j / 2] = j % 2 ? (v[j / 2] & 0xffffu) | kLow << 16 : (v[j / 2] & 0xffff0000u) | kLow;
+        else v[j] = kLow;
+    }
+    return v;
+}
+
+// the elements of a vector whose bits are not set
+template <bool BF16>
+__device__ __forceinline__ void store_others(typename Elem<BF16>::T* p, const float (&f)[Elem<BF16>::kPer], uint32_t bits) {
+    if (bits == 0) return store16(p, Elem<BF16>::pack(f));
+#pragma unroll
+    for (int j = 0; j < Elem<BF16>::kPer; ++j)
+        if (!(bits >> j & 1)) p[j] = Elem<BF16>::round(f[j]);
+}
+
+// ---------------------------------------------------------------------------
+// a row from the others' sum and its listed choices, by one wavefront
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float wave_top(float x) {
+    return lanes_reduce<kWave>(x, [](float p, float q) { return p > q ? p : q; });
+}
+
+// a (exp s - 1 - s) for s = log(b / a): b - a - a s, which at small s cancels
+__device__ __forceinline__ float curve(float a, float b, float s) {
+    float k, em1;
+    exp_remainder(s, &k, &em1);
+    if (fabsf(s) < 0.5f) return a * k;
+    return a == 0.0f ? b : (b - a) - a * s;
+}
+
+// b - a = a (exp s - 1)
+__device__ __forceinline__ float apart_by(float a, float b, float s) {
+    float k, em1;
+    exp_remainder(s, &k, &em1);
+    return fabsf(s) < 0.5f ? a * em1 : b - a;
+}
+
+// what a row's sums say
+struct RowMass {
+    float top, log2_s;   // M (0 in a row without weight), log2 S
+    float share, rest;   // 2^(c (m - M)) / S, log p_rest
+    bool weight, some;   // anything but -infinity in the row, among the others
+    __device__ __forceinline__ float logp(float x, float c) const { return ((x - top) * c - log2_s) * kLn2; }
+};
+
+__device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others, float c) {
+    RowMass r;
+    float top = kNone;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.x[i] : kNone);
+    top = wave_top(fmaxf(top, others.m));
+    r.weight = top != kNone;
+    r.top = r.weight ? top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.x[i] - r.top) * c) : 0.0f;
+    const float d = others.m == top ? 0.0f : (others.m - top) * c, k = exp2_fast(d);
+    const float S = fmaf(others.s, k, uniform(lanes_sum<kWave>(sum)));
+    r.log2_s = r.weight ? log2_fast(S) : 0.0f;
+    r.some = !(others.s == 0.0f);
+    r.share = r.weight ? k / S : 0.0f;
+    r.rest = r.some ? (log2_fast(others.s) + d - r.log2_s) * kLn2 : kNone;
+    return r;
+}
+
+// the teacher's side of a row
+struct Teacher {
+    float top, log;  // log q = (y / temperature - top) - log
+    double left;     // what its listed probabilities leave (with_rest)
+    bool any;
+};
+
+__device__ __forceinline__ Teacher teacher_row(const ListedArgs& a, const Listed& e) {
+    Teacher t{0.0f, 0.0f, 0.0, false};
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) any |= e.first[i];
+    t.any = __ballot(any) != 0;
+    if (a.with_rest) {
+        // in 64 bits: what is left of 1 may be far smaller than the sum's own rounding in 32
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp((double)e.y[i]) : 0.0;
+        t.left = 1.0 - wave_sum(sum);
+        return t;
+    }
+    float top = kNone;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.y[i] * a.q_inv_t : kNone);
+    t.top = t.any ? wave_top(top) : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.y[i] * a.q_inv_t - t.top) * kLog2e) : 0.0f;
+    t.log = t.any ? log2_fast(uniform(lanes_sum<kWave>(sum))) * kLn2 : 0.0f;
+    return t;
+}
+
+constexpr double kLeastRest = 1.0 / 8388608.0;  // 2^-23: what 32-bit log-probabilities say of a rest at best
+
+// The divergence of a row and what its gradient needs; w: the token's weight.
+__device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const Listed& e, const Mass& others, const RowMass& r,
+                                                 const Teacher& t, float w) {
+    ListedRow o{};
+    o.top = r.top;
+    o.log2_s = r.log2_s;
+    o.q_top = t.top;
+    o.q_log = t.log;
+    o.base = others.m == kNone ? 0.0f : others.m;
+    o.w = w * a.inv_t;
+    if (!a.with_rest && !t.any) {  // the teacher says nothing
+        o.w = 0.0f;
+        return o;
+    }
+    if (!r.weight) {
+        o.loss = INFINITY;
+        o.w = 0.0f;
+        return o;
+    }
+    float loss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        if (!e.first[i]) continue;
+        const float lq = (e.y[i] * a.q_inv_t - t.top) - t.log, lp = r.logp(e.x[i], a.c);
+        const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
+        loss += a.reverse ? curve(p, q, u) : curve(q, p, -u);
+    }
+    loss = uniform(lanes_sum<kWave>(loss));
+    const float p_rest = r.some ? exp_fast(r.rest) : 0.0f;
+    if (!a.with_rest) {
+        o.loss = loss + p_rest;
+        o.coef = r.some ? o.w * r.share : 0.0f;
+        return o;
+    }
+    const double kept = r.some ? (t.left > kLeastRest ? t.left : kLeastRest) : 0.0;
+    o.over = (float)(kept - t.left);
+    const float q_rest = (float)kept, away = r.some ? log2_fast(q_rest) * kLn2 - r.rest : 0.0f;
+    if (a.reverse) {
+        o.loss = loss + (r.some ? curve(p_rest, q_rest, away) : 0.0f) - o.over;
+        o.coef = r.some && o.w != 0.0f ? -o.w * (r.share * (away + o.loss)) : 0.0f;
+    } else {
+        o.loss = loss + (r.some ? curve(q_rest, p_rest, -away) : 0.0f) + o.over;
+        // (1 + over) share - q_rest / s
+        float k, em1;
+        exp_remainder(away, &k, &em1);
+        const float d = fabsf(away) < 0.5f ? r.share * (o.over - em1) : fmaf(1.0f + o.over, r.share, -q_rest / others.s);
+        o.coef = r.some && o.w != 0.0f ? o.w * d : 0.0f;
+    }
+    return o;
+}
+
+// the gradient of a listed choice of score x and teacher's value y
+__device__ __forceinline__ float listed_gradient(const ListedArgs& a, const ListedRow& o, float x, float y) {
+    if (o.w == 0.0f) return 0.0f;
+    const float lq = (y * a.q_inv_t - o.q_top) - o.q_log, lp = ((x - o.top) * a.c - o.log2_s) * kLn2;
+    const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
+    if (a.reverse) return p == 0.0f ? 0.0f : -o.w * p * (u + o.loss);
+    return o.w * fmaf(p, o.over, apart_by(q, p, -u));
+}
+
+__device__ __forceinline__ void write_scores(const ListedArgs& a, uint32_t n, int64_t at, const Listed& e, const Mass& others) {
+    const RowMass r = row_mass(e, others, a.c);
+    float* out = static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape);
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        const int32_t k = i * kWave + lane_id();
+        if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.c) : kNone;
+    }
+    if (lane_id() != 0) return;
+    if (a.rest) a.rest[at] = r.rest;
+    if (a.lse) a.lse[at] = r.weight ? fmaf(r.top, a.inv_t, fmaf(r.top, a.inv_lo, r.log2_s * kLn2)) : kNone;
+}
+
+// per-token outputs of a token that does not count, by a wavefront
+template <int MODE>
+__device__ __forceinline__ void write_nothing(const ListedArgs& a, uint32_t n, int64_t at) {
+    if constexpr (MODE == SCORES) {
+        float* out = static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape);
+        for (int32_t k = lane_id(); k < a.K; k += kWave) out[k] = 0.0f;
+        if (lane_id() == 0 && a.rest) a.rest[at] = 0.0f;
+        if (lane_id() == 0 && a.lse) a.lse[at] = 0.0f;
+    } else {
+        if (lane_id() == 0) a.loss[at] = 0.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the loss's sums
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double listed_weight(const ListedArgs& a, uint32_t b) {
+    uint32_t tokens = (uint32_t)(a.shape.B * a.shape.T), rows = (uint32_t)a.shape.B, row = (uint32_t)a.shape.T;
+    if (a.mask) {
+        const uint64_t counts = a.head->counts;
+        tokens = (uint32_t)counts;
+        rows = (uint32_t)(counts >> 32);
+        if (a.reduction == CONDUIT_SEQUENCE_MEAN) row = a.row_count[b];
+    }
+    PolicyTerms o{};
+    o.reduction = a.reduction;
+    return token_weight(o, tokens, rows, row);
+}
+
+// the token's part in the loss
+__device__ __forceinline__ double token_part(const ListedArgs& a, uint32_t n, int64_t at) {
+    const double w = listed_weight(a, div31(n, a.shape.by_T));
+    return a.weight ? w * (double)a.weight[at] : w;
+}
+
+__device__ __forceinline__ void write_distill_stats(const ListedArgs& a, const double (&v)[kDistillSums]) {
+    const uint32_t tokens = a.mask ? (uint32_t)a.head->counts : (uint32_t)(a.shape.B * a.shape.T);
+    a.stats[0] = (float)(a.scale * v[0]);
+    a.stats[1] = (float)(v[1] / (double)(tokens > 0 ? tokens : 1));
+    a.stats[2] = (float)tokens;
+    if (a.mask) a.head->counts = 0;  // for the next call
+}
+
+// `slots` contributions, each left by one wavefront (or workgroup), added up by
+// the wavefront of the last: as finish_row does for the policy loss
+__device__ __forceinline__ void finish_distill(const ListedArgs& a, uint32_t slot, uint32_t slots, double w_loss, double loss) {
+    bool last = false;
+    if (lane_id() == 0) {
+        store_agent(a.partial + (int64_t)slot * kDistillSums, w_loss);
+        store_agent(a.partial + (int64_t)slot * kDistillSums + 1, loss);
+        last = draw_ticket(a.head, slot, slots);
+    }
+    if (!__builtin_amdgcn_readfirstlane((int)last)) return;
+    double v[kDistillSums] = {0.0, 0.0};
+    for (uint32_t k = lane_id(); k < slots; k += kWave) {
+#pragma unroll
+        for (int i = 0; i < kDistillSums; ++i) v[i] += load_agent(a.partial + (int64_t)k * kDistillSums + i);
+    }
+#pragma unroll
+    for (int i = 0; i < kDistillSums; ++i) v[i] = wave_sum(v[i]);
+    if (lane_id() == 0) write_distill_stats(a, v);
+}
+
+// a row's contribution, by its first wavefront
+__device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, double part, float loss) {
+    if (a.sums) finish_distill(a, n, (uint32_t)(a.shape.B * a.shape.T), part == 0.0 ? 0.0 : part * (double)loss, (double)loss);
+}
+
+// sums over the tokens of a batch of many rows
+constexpr int kSumThreads = 256;
+
+__global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
+    __shared__ double lds[kDistillSums * kSumThreads / kWave];
+    double v[kDistillSums] = {0.0, 0.0};
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    for (uint32_t n = blockIdx.x * kSumThreads + threadIdx.x; n < n_rows; n += gridDim.x * kSumThreads) {
+        const int64_t at = a.shape.at(n);
+        if (a.mask && !a.mask[at]) continue;
+        const double part = token_part(a, n, at), loss = (double)a.loss[at];
+        v[0] += part == 0.0 ? 0.0 : part * loss;
+        v[1] += loss;
+    }
+    block_sum<kSumThreads, kDistillSums>(v, lds);
+    if (threadIdx.x < kWave) finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1]);
+}
+
+// ---------------------------------------------------------------------------
+// short rows: a wavefront each, E elements a lane
+// ---------------------------------------------------------------------------
+template <bool BF16, int MODE, int E>
+__global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
+    using T = typename Elem<BF16>::T;
+    constexpr int kRows = kListedThreads / kWave;
+    static_assert(E <= 32, "a word of bits a lane");
+    __shared__ uint32_t s_bits[kRows][kWave];
+    __shared__ double s_sum[kDistillSums * kRows];
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    uint32_t* bits = s_bits[w];
+    double sums[kDistillSums] = {0.0, 0.0};
+    for (uint32_t n = block_number() * kRows + w; n < n_rows; n += gridDim.x * gridDim.y * kRows) {
+        const int64_t at = a.shape.at(n);
+        const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+        T* dx = MODE == DISTILL && a.has_dx ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
+        if (a.mask && !a.mask[at]) {
+            write_nothing<MODE>(a, n, at);
+            if (MODE == DISTILL && a.has_dx) {
+                for (uint32_t j = l; j < (uint32_t)a.V; j += kWave) dx[j] = Elem<BF16>::round(0.0f);
+            }
+            continue;
+        }
+        float v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = l + i * kWave < a.V ? Elem<BF16>::one(x[l + i * kWave]) : kNone;
+        Listed e;
+        load_ids(a, n, e);
+        if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
+        check_ids<MODE == DISTILL>(a, e, true);
+        load_scores<BF16>(x, e);
+        wave_fence();  // (the last row's bits are read)
+        bits[l] = 0;
+        wave_fence();
+        const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+            *word = bits + id % kWave;
+            *bit = 1u << id / kWave;
+            return true;
+        });
+        if (twice) find_first<false>(e, a.K);
+        wave_fence();
+        const uint32_t marked = bits[l];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = marked >> i & 1 ? kNone : v[i];
+        Mass others = no_mass();
+        accumulate_mass(others, v, a.c);
+        others = join_mass<kWave>(others, a.c);
+        if constexpr (MODE == SCORES) {
+            write_scores(a, n, at, e, others);
+        } else {
+            const double part = token_part(a, n, at);
+            const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
+            if (l == 0) a.loss[at] = o.loss;
+            sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
+            sums[1] += (double)o.loss;
+            if (a.has_dx) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const uint32_t j = l + i * kWave;
+                    if (j < a.V && !(marked >> i & 1))
+                        dx[j] = Elem<BF16>::round(o.coef == 0.0f ? 0.0f : o.coef * exp2_fast((v[i] - o.base) * a.c));
+                }
+#pragma unroll
+                for (int i = 0; i < kLists; ++i)
+                    if (e.first[i]) dx[e.id[i]] = Elem<BF16>::round(listed_gradient(a, o, e.x[i], e.y[i]));
+            }
+        }
+    }
+    if constexpr (MODE == DISTILL) {
+        if (l == 0) {
+            s_sum[w] = sums[0];
+            s_sum[kRows + w] = sums[1];
+        }
+        __syncthreads();
+        if (threadIdx.x >= kWave) return;
+        double v[kDistillSums] = {0.0, 0.0};
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            v[0] += s_sum[i];
+            v[1] += s_sum[kRows + i];
+        }
+        finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// longer rows, or parts of them, whose gradient is not written here: a workgroup
+// each
+// ---------------------------------------------------------------------------
+constexpr int kScanVectors = 8;  // vectors a lane and tile
+
+// the row from its others' sum, by one wavefront
+template <bool BF16, int MODE>
+__device__ void finish_listed(const ListedArgs& a, uint32_t n, int64_t at, const Mass& others) {
+    using T = typename Elem<BF16>::T;
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    Listed e;
+    load_ids(a, n, e);
+    if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
+    check_ids<MODE == DISTILL>(a, e, true);
+    load_scores<BF16>(x, e);
+    find_first<false>(e, a.K);
+    if constexpr (MODE == SCORES) {
+        write_scores(a, n, at, e, others);
+    } else {
+        const double part = token_part(a, n, at);
+        const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
+        if (lane_id() == 0) a.loss[at] = o.loss;
+        if (lane_id() == 0 && a.has_dx) a.row[n] = o;
+        finish_token(a, n, part, o.loss);
+    }
+}
+
+// the join of a row's parts, by one wavefront
+template <bool BF16, int MODE>
+__device__ __forceinline__ void join_listed(const ListedArgs& a, uint32_t n, int64_t at) {
+    Mass all = no_mass();
+    for (int32_t p = lane_id(); p < a.parts; p += kWave) {
+        const float* q = a.part + 2 * ((int64_t)n * a.parts + p);
+        const float m = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float s = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float top = m > all.m ? m : all.m;
+        all.s = all.s * exp2_fast(all.m == top ? 0.0f : (all.m - top) * a.c) + s * exp2_fast(m == top ? 0.0f : (m - top) * a.c);
+        all.m = top;
+    }
+    finish_listed<BF16, MODE>(a, n, at, join_mass<kWave>(all, a.c));
+}
+
+template <bool BF16, int MODE>
+__global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    constexpr int kWords = kScanVectors * kPer / 32;  // of bits, a lane and tile
+    constexpr uint32_t kTile = kListedThreads * kScanVectors;
+    extern __shared__ uint32_t s_bits[];  // [tiles][kListedThreads][kWords]
+    __shared__ uint32_t s_tail;
+    __shared__ Mass s_mass[kListedThreads / kWave];
+    const uint32_t item = block_number(), tid = threadIdx.x;
+    if (item >= (uint32_t)(a.shape.B * a.shape.T) * (uint32_t)a.parts) return;
+    const uint32_t n = div31(item, a.by_parts), part = item - n * (uint32_t)a.parts;
+    const int64_t at = a.shape.at(n);
+    if (a.mask && !a.mask[at]) {
+        if (part == 0 && tid < kWave) {
+            write_nothing<MODE>(a, n, at);
+            if constexpr (MODE == DISTILL) finish_token(a, n, 0.0, 0.0f);
+        }
+        return;
+    }
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
+    u32x4 v[kScanVectors];
+    auto load = [&](uint32_t base) {
+#pragma unroll
+        for (int k = 0; k < kScanVectors; ++k) {
+            const uint32_t i = base + k * kListedThreads + tid;
+            v[k] = i < hi ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
+        }
+    };
+    load(lo);  // beside the list's
+    Listed e;
+    if (tid < kWave) {
+        load_ids(a, n, e);
+        if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
+        check_ids<MODE == DISTILL>(a, e, false);
+    }
+    const uint32_t tiles = (hi - lo + kTile - 1) / kTile;
+    for (uint32_t i = tid; i < tiles * kListedThreads * kWords; i += kListedThreads) s_bits[i] = 0;
+    if (tid == 0) s_tail = 0;
+    __syncthreads();
+    if (tid < kWave) {
+        mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+            const uint32_t i = id / kPer, j = id % kPer;
+            if (i >= nv) {
+                *word = &s_tail;
+                *bit = 1u << j;
+                return part == 0;
+            }
+            if (i < lo || i >= hi) return false;
+            const uint32_t r = i - lo, tile = r / kTile, slot = r % kTile / kListedThreads, at_bit = slot * kPer + j;
+            *word = s_bits + (tile * kListedThreads + r % kListedThreads) * kWords + at_bit / 32;
+            *bit = 1u << at_bit % 32;
+            return true;
+        });
+    }
+    __syncthreads();
+    Mass others = no_mass();
+    if (part == 0 && tid < tail) {
+        const float f[1] = {s_tail >> tid & 1 ? kNone : E::one(x[nv * kPer + tid])};
+        accumulate_mass(others, f, a.c);
+    }
+    for (uint32_t tile = 0; tile < tiles; ++tile) {
+        if (tile > 0) load(lo + tile * kTile);
+        uint32_t bits[kWords], any = 0;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) any |= bits[i] = s_bits[(tile * kListedThreads + tid) * kWords + i];
+        if (any) {
+#pragma unroll
+            for (int k = 0; k < kScanVectors; ++k) v[k] = without<BF16>(v[k], bits[k * kPer / 32] >> k * kPer % 32 & ((1u << kPer) - 1));
+        }
+        accumulate_mass_tile<BF16>(others, v, a.c);
+    }
+    others = join_mass<kWave>(others, a.c);
+    if (lane_id() == 0) s_mass[tid / kWave] = others;
+    __syncthreads();
+    if (tid >= kWave) return;
+    others = join_mass<kListedThreads / kWave>(s_mass[lane_id() % (kListedThreads / kWave)], a.c);
+    if (a.parts == 1) return finish_listed<BF16, MODE>(a, n, at, others);
+    bool last = false;
+    if (lane_id() == 0) {
+        float* mine = a.part + 2 * (int64_t)item;
+        __hip_atomic_store(mine, others.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 1, others.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // acknowledged before the ticket is drawn
+        if (a.row_ticket) last = draw_last(a.row_ticket + n * kTicketStep, (uint32_t)a.parts);
+    }
+    if (__builtin_amdgcn_readfirstlane((int)last)) join_listed<BF16, MODE>(a, n, at);
+}
+
+// the join of many split rows, by a launch of its own: a wavefront a row
+template <bool BF16, int MODE>
+__global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
+    const uint32_t n = block_number() * (kListedThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    const int64_t at = a.shape.at(n);
+    if (!a.mask || a.mask[at]) join_listed<BF16, MODE>(a, n, at);
+}
+
+// ---------------------------------------------------------------------------
+// distillation of rows that fit a workgroup's registers, K vectors a lane
+// ---------------------------------------------------------------------------
+constexpr int kRowVectors = 16 * 1024;  // of a workgroup of 1,024
+
+template <bool BF16, int WAVES, int K>
+__global__ __launch_bounds__(WAVES * kWave) void k_distill_rows(ListedArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    constexpr int NT = WAVES * kWave;
+    constexpr int kWords = K * kPer / 32;
+    __shared__ uint32_t s_bits[NT][kWords];
+    __shared__ uint32_t s_tail;
+    __shared__ Mass s_mass[WAVES];
+    __shared__ ListedRow s_row;
+    const uint32_t n = block_number(), tid = threadIdx.x;
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    const int64_t at = a.shape.at(n);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    if (a.mask && !a.mask[at]) {
+        for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+        if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
+        if (tid < kWave) {
+            write_nothing<DISTILL>(a, n, at);
+            finish_token(a, n, 0.0, 0.0f);
+        }
+        return;
+    }
+    u32x4 v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = k * NT + tid;
+        v[k] = i < nv ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
+    }
+    float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
+    Listed e;
+    double part = 0.0;
+    if (tid < kWave) {
+        load_ids(a, n, e);
+        load_values(a, a.teacher, n, e);
+        check_ids<true>(a, e, true);
+        load_scores<BF16>(x, e);
+        part = token_part(a, n, at);
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) s_bits[tid][i] = 0;
+    if (tid == 0) s_tail = 0;
+    __syncthreads();
+    Teacher t{};
+    if (tid < kWave) {
+        const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+            const uint32_t i = id / kPer, j = id % kPer, at_bit = i / NT * kPer + j;
+            *word = i < nv ? &s_bits[i % NT][at_bit / 32] : &s_tail;
+            *bit = 1u << (i < nv ? at_bit % 32 : j);
+            return true;
+        });
+        if (twice) find_first<false>(e, a.K);
+    }
+    __syncthreads();
+    if (tid < kWave) t = teacher_row(a, e);
+    uint32_t bits[kWords], any = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) any |= bits[i] = s_bits[tid][i];
+    auto listed = [&](int k) { return bits[k * kPer / 32] >> k * kPer % 32 & ((1u << kPer) - 1); };
+    if (any) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = without<BF16>(v[k], listed(k));
+    }
+    const bool listed_tail = tid < tail && (s_tail >> tid & 1);
+    if (listed_tail) xt = kNone;
+    Mass others = no_mass();
+    accumulate_mass_tile<BF16>(others, v, a.c);
+    {
+        const float f[1] = {xt};
+        accumulate_mass(others, f, a.c);
+    }
+    others = join_mass<kWave>(others, a.c);
+    if (lane_id() == 0) s_mass[tid / kWave] = others;
+    __syncthreads();
+    others = join_mass<WAVES>(s_mass[lane_id() % WAVES], a.c);
+    if (tid < kWave) {
+        const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), t, (float)(part * a.scale));
+        if (tid == 0) {
+            s_row = o;
+            a.loss[at] = o.loss;
+        }
+#pragma unroll
+        for (int i = 0; i < kLists; ++i)
+            if (e.first[i]) dx[e.id[i]] = E::round(listed_gradient(a, o, e.x[i], e.y[i]));
+    }
+    __syncthreads();
+    const float coef = s_row.coef, base = s_row.base;
+    const bool none = coef == 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = k * NT + tid;
+        if (i >= nv) continue;
+        float f[kPer];
+        E::unpack(again(v[k]), f);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) f[j] = none ? 0.0f : coef * exp2_fast((f[j] - base) * a.c);
+        store_others<BF16>(dx + (size_t)i * kPer, f, listed(k));
+    }
+    if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(none ? 0.0f : coef * exp2_fast((xt - base) * a.c));
+    if (tid < kWave) finish_token(a, n, part, s_row.loss);
+}
+
+// ---------------------------------------------------------------------------
+// the gradient of given gradients of the log-probabilities, or, SPLIT, of the
+// divergence of split rows from what their join left: wavefronts take parts of
+// kGradK vectors a lane of a row
+// ---------------------------------------------------------------------------
+constexpr int kGradK = 4;
+
+template <bool BF16, bool SPLIT>
+__global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a, uint32_t items, uint32_t per_row, Div31 by_row) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    constexpr uint32_t kWindow = kGradK * kWave;
+    static_assert(kGradK * kPer <= 32, "a word of bits a lane");
+    __shared__ uint32_t s_bits[kListedThreads / kWave][kWave + 1];
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+    const uint32_t item = block_number() * (kListedThreads / kWave) + w;
+    if (item >= items) return;
+    const uint32_t n = div31(item, by_row), part = item - n * per_row;
+    const int64_t at = a.shape.at(n);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const uint32_t first = part * kWindow, base = first + lane;
+    const bool mine = part == 0 && lane < tail;  // the elements after the last vector
+    bool weight = !a.mask || a.mask[at];
+    float lse = 0.0f;
+    if constexpr (!SPLIT) {
+        lse = weight ? a.lse_in[at] : 0.0f;
+        weight = weight && lse != kNone;
+    }
+    if (!weight) {  // nothing counts, or a row without weight
+#pragma unroll
+        for (int k = 0; k < kGradK; ++k) {
+            const uint32_t i = base + k * kWave;
+            if (i < nv) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+        }
+        if (mine) dx[nv * kPer + lane] = E::round(0.0f);
+        return;
+    }
+    u32x4 v[kGradK];
+#pragma unroll
+    for (int k = 0; k < kGradK; ++k) {
+        const uint32_t i = base + k * kWave;
+        v[k] = i < nv ? load16(x + (size_t)i * kPer) : u32x4{0, 0, 0, 0};
+    }
+    const float xt = mine ? E::one(x[nv * kPer + lane]) : 0.0f;
+    Listed e;
+    load_ids(a, n, e);
+    load_values(a, SPLIT ? a.teacher : a.g, n, e);
+    check_ids<SPLIT>(a, e, !SPLIT && part == 0);
+    ListedRow o{};
+    float sum = 0.0f, h = 0.0f, rest = 0.0f;  // of the gradients; of log p_rest; log p_rest
+    if constexpr (SPLIT) {
+        o = a.row[n];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) sum += e.on[i] ? e.y[i] : 0.0f;
+        sum = uniform(lanes_sum<kWave>(sum));
+        if (a.h) {
+            rest = a.rest_in[at];
+            h = rest == kNone ? 0.0f : a.h[at];  // (no others: their log-probability stays -infinity)
+        }
+    }
+    // the listed choices of this part of the row
+    uint32_t* bits = s_bits[w];
+    bits[lane] = 0;
+    if (lane == 0) bits[kWave] = 0;
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        const uint32_t k = (uint32_t)e.id[i] / kPer;
+        e.on[i] = e.on[i] && (k < nv ? k - first < kWindow : part == 0);
+        e.first[i] = e.on[i];
+    }
+    load_scores<BF16>(x, e);
+    const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+        const uint32_t k = id / kPer, j = id % kPer;
+        *word = k < nv ? bits + k % kWave : bits + kWave;
+        *bit = 1u << (k < nv ? (k - first) / kWave * kPer + j : j);
+        return true;
+    });
+    if (twice) find_first<!SPLIT>(e, a.K);
+    wave_fence();
+    const uint32_t marked = bits[lane], marked_tail = bits[kWave];
+    auto log_p = [&](float f) {  // as FromLse in k_logits.hip, for what may be far from 0
+        return fmaf(f, a.inv_t, fmaf(fmaxf(f, -3.4028235e38f), a.inv_lo, -lse));
+    };
+    // of any other choice: coef times its share of the rest (with h), or its probability
+    float coef, shift = 0.0f;
+    if constexpr (SPLIT) {
+        coef = o.coef;
+    } else if (h == 0.0f) {
+        coef = -sum * a.inv_t;
+    } else {
+        shift = rest;
+        coef = -fmaf(sum, exp_fast(rest), h * expm1_fast(rest)) * a.inv_t;
+    }
+    auto other = [&](float f) {
+        if (coef == 0.0f) return 0.0f;
+        if constexpr (SPLIT) return coef * exp2_fast((f - o.base) * a.c);
+        return coef * exp2_fast((log_p(f) - shift) * kLog2e);
+    };
+#pragma unroll
+    for (int k = 0; k < kGradK; ++k) {
+        const uint32_t i = base + k * kWave;
+        float f[kPer];
+        E::unpack(v[k], f);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) f[j] = other(f[j]);
+        if (i < nv) store_others<BF16>(dx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
+    }
+    if (mine && !(marked_tail >> lane & 1)) dx[nv * kPer + lane] = E::round(other(xt));
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        if (!e.first[i]) continue;
+        float d;
+        if constexpr (SPLIT) d = listed_gradient(a, o, e.x[i], e.y[i]);
+        else d = (e.y[i] - (sum + h) * exp_fast(log_p(e.x[i]))) * a.inv_t;
+        dx[e.id[i]] = E::round(d);
+    }
+}
+
+template <bool BF16, bool SPLIT>
+hipError_t launch_gradient(const ListedArgs& a, hipStream_t s) {
+    const int64_t nv = a.V / Elem<BF16>::kPer;
+    const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
+    const int64_t items = a.shape.B * a.shape.T * per_row;
+    if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
+    hipLaunchKernelGGL((k_listed_gradient<BF16, SPLIT>), grid_of((items + kListedThreads / kWave - 1) / (kListedThreads / kWave), kListedThreads),
+                       dim3(kListedThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row, make_div31((uint32_t)per_row));
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// which kernel a row's width takes
+// ---------------------------------------------------------------------------
+template <bool BF16, int MODE>
+hipError_t launch_short(const ListedArgs& a, hipStream_t s) {
+    constexpr int kRows = kListedThreads / kWave;
+    const int64_t want = (a.shape.B * a.shape.T + kRows - 1) / kRows;
+    // (the loss's workgroups each leave a sum)
+    const dim3 grid = MODE == DISTILL ? dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)) : grid_of(want, kListedThreads);
+    if (a.V <= 8 * kWave) hipLaunchKernelGGL((k_listed_short<BF16, MODE, 8>), grid, dim3(kListedThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_listed_short<BF16, MODE, kShortRow / kWave>), grid, dim3(kListedThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <bool BF16, int MODE>
+hipError_t launch_scan(const ListedArgs& a, hipStream_t s) {
+    constexpr int kPer = Elem<BF16>::kPer;
+    const int64_t rows = a.shape.B * a.shape.T, items = rows * a.parts;
+    if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
+    constexpr int kTile = kListedThreads * kScanVectors;
+    const unsigned lds = (a.per + kTile - 1) / kTile * (kTile * kPer / 8);
+    hipLaunchKernelGGL((k_listed_scan<BF16, MODE>), grid_of(items, kListedThreads), dim3(kListedThreads), lds, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 1 || a.row_ticket) return e;
+    constexpr int kRows = kListedThreads / kWave;
+    hipLaunchKernelGGL((k_listed_join<BF16, MODE>), grid_of((rows + kRows - 1) / kRows, kListedThreads), dim3(kListedThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t listed_logprobs(const ListedArgs& a, hipStream_t s) {
+    return a.V <= kShortRow ? launch_short<BF16, SCORES>(a, s) : launch_scan<BF16, SCORES>(a, s);
+}
+
+template <bool BF16>
+hipError_t distill(const ListedArgs& a, hipStream_t s) {
+    const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
+    hipError_t e = hipSuccess;
+    if (a.mask) {  // the tokens' weight needs their number
+        PolicyArgs p{};
+        p.shape = a.shape;
+        p.o.reduction = a.reduction;
+        p.mask = a.mask;
+        p.head = a.head;
+        p.row_count = a.row_count;
+        e = launch_token_count(p, s);
+        if (e != hipSuccess) return e;
+    }
+    if (a.V <= kShortRow) return launch_short<BF16, DISTILL>(a, s);
+    if (a.parts > 1 || !a.has_dx) {
+        e = launch_scan<BF16, DISTILL>(a, s);
+        if (e == hipSuccess && a.has_dx) e = launch_gradient<BF16, true>(a, s);
+    } else if (nv <= 4096) {
+        hipLaunchKernelGGL((k_distill_rows<BF16, 4, 16>), grid_of(rows, 256), dim3(256), 0, s, a);
+        e = hipGetLastError();
+    } else {
+        hipLaunchKernelGGL((k_distill_rows<BF16, 16, 16>), grid_of(rows, 1024), dim3(1024), 0, s, a);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || a.sums) return e;
+    const int64_t want = (rows + kSumThreads - 1) / kSumThreads;
+    hipLaunchKernelGGL(k_distill_sum, dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)), dim3(kSumThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Parts of a row: rows are split where the rows alone would leave compute units
+// without a workgroup, into parts of at least four vectors a lane, or where a row
+// is wider than one workgroup takes (whole_rows: than its registers hold).
+RowParts listed_parts(int64_t rows, int64_t V, bool bf16, bool whole_rows) {
+    const int64_t cus = device_cus(), nv = V / (bf16 ? 8 : 4), least = whole_rows && nv > kRowVectors ? kListedThreads * kScanVectors : kPartVectors;
+    if (V <= kShortRow || rows <= 0) return RowParts{1, (int32_t)nv};
+    int64_t parts = (nv + least - 1) / least;
+    if (rows < cus) {
+        const int64_t want = (2 * cus + rows - 1) / rows, most = nv / (4 * kListedThreads);
+        const int64_t split = want < most ? want : most;
+        if (split > parts) parts = split;
+    }
+    return RowParts{(int32_t)parts, (int32_t)((nv + parts - 1) / parts)};
+}
+
+hipError_t launch_listed_logprobs(const ListedArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? listed_logprobs<true>(a, s) : listed_logprobs<false>(a, s);
+}
+
+hipError_t launch_listed_logprobs_backward(const ListedArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? launch_gradient<true, false>(a, s) : launch_gradient<false, false>(a, s);
+}
+
+hipError_t launch_distill_loss(const ListedArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? distill<true>(a, s) : distill<false>(a, s);
+}
+
+}  // namespace conduit

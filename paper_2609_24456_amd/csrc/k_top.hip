@@ -1,0 +1,497 @@
+// The K most probable choices of every token with their log-probabilities,
+// beside the taken token's, the log-normaliser and the entropy
+// (conduit_token_alternatives).
+//
+// A choice's rank goes by its key: the score's bits in the order of the numbers
+// (-0 as 0), then its number counted from the end, so that no two keys are equal
+// and the lowest number comes first among equal scores.  Of a row cut into any
+// pieces the K-th largest of the pieces' maxima is at most the K-th largest
+// score: at least K scores reach it.  With the lanes' running maxima as the
+// pieces, which the softmax keeps anyway, few more than K do (256 lanes, K = 64:
+// 74 of scores in random places), and these are ranked by counting, each, the
+// larger ones.
+//
+// Where the row does not fit the registers of a wavefront, the pass also leaves
+// the maximum of every group of 8 vectors (128 bytes, a cache line) in LDS: only
+// groups that reach the bound are read again.
+//
+// Rows whose scores are equal in many places, or that hold their largest ones in
+// few lanes, may have more candidates than the lists take.  Then the K-th
+// largest maximum of a group is found exactly.  Fewer than K groups are above
+// it, and of those that reach it the first K are enough; among their elements
+// the K-th largest key is found bit by bit.
+#include "listed_dev.h"
+#include "rows_dev.h"
+
+namespace conduit {
+
+namespace {
+
+constexpr int kTopThreads = 256;
+constexpr int kTopVectors = 8;   // vectors a lane and tile
+constexpr int kGroup = 8;        // vectors a group
+constexpr int kMostCandidates = 512;
+constexpr int kMostGroups = 512;
+constexpr int kShortCandidates = 256;
+static_assert(2 * kMostListed <= kMostGroups && kMostListed <= kShortCandidates, "the exact selection fits the lists");
+static_assert(kPartVectors % kGroup == 0, "whole groups");
+
+// a score's place among the numbers, at least that of -infinity: 0x007fffff
+__device__ __forceinline__ uint32_t order_key(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // (-0 becomes 0)
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_score(uint32_t k) {
+    return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+__device__ __forceinline__ uint64_t choice_key(float x, uint32_t j) { return (uint64_t)order_key(x) << 32 | (uint32_t)~j; }
+
+// The largest bound that at least `need` of a wavefront's keys reach, or, found
+// sooner, one that exactly `need` reach; 0 if there are fewer.
+template <int N>
+__device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[N], uint32_t need) {
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t trial = t | 1u << bit;
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __builtin_popcountll(__ballot(key[i] >= trial));
+        if (n < need) continue;
+        t = trial;
+        if (n == need) break;
+    }
+    return t;
+}
+
+// a row whose log-normaliser is no number (a NaN or +infinity among its scores) has no ranking
+__device__ __forceinline__ bool no_ranking(const Stat& s) { return !(s.s == s.s); }
+
+struct TopRow {
+    int32_t* ids;
+    float* logps;
+    __device__ __forceinline__ TopRow(const TopArgs& a, uint32_t n)
+        : ids(static_cast<int32_t*>(a.ids.data) + a.ids.at(n, a.shape)),
+          logps(static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape)) {}
+};
+
+__device__ __forceinline__ void write_values(const TopArgs& a, int64_t at, float logp, float lse, float entropy) {
+    if (a.logp) a.logp[at] = logp;
+    if (a.lse) a.lse[at] = lse;
+    if (a.entropy) a.entropy[at] = entropy;
+}
+
+// K entries of one kind, by NT threads
+template <int NT>
+__device__ __forceinline__ void fill_row(const TopArgs& a, const TopRow& o, uint32_t tid, int32_t from, int32_t id, float logp) {
+    for (int32_t k = from + (int32_t)tid; k < a.K; k += NT) {
+        o.ids[k] = id;
+        o.logps[k] = logp;
+    }
+}
+
+// a token that does not count
+template <int NT>
+__device__ __forceinline__ void write_nothing(const TopArgs& a, uint32_t n, int64_t at, uint32_t tid) {
+    if (tid == 0) write_values(a, at, 0.0f, 0.0f, 0.0f);
+    fill_row<NT>(a, TopRow(a, n), tid, 0, 0, 0.0f);
+}
+
+// the candidates' ranks, f(rank, key) for the first K of them
+template <int NT, typename F>
+__device__ __forceinline__ void rank(const uint64_t* cand, uint32_t n, int32_t K, uint32_t tid, F f) {
+    for (uint32_t c = tid; c < n; c += NT) {
+        const uint64_t key = cand[c];
+        uint32_t r = 0;
+#pragma unroll 8
+        for (uint32_t j = 0; j < n; ++j) r += cand[j] > key;
+        if (r < (uint32_t)K) f(r, key);
+    }
+}
+
+// the row's K choices from its candidates, by NT threads
+template <int NT>
+__device__ __forceinline__ void write_ranked(const TopArgs& a, uint32_t row, const uint64_t* cand, uint32_t n, const RowValues& r,
+                                             uint32_t tid) {
+    const TopRow o(a, row);
+    const bool weight = r.inv_s != 0.0f;
+    const float base = uniform(r.base), log2_s = uniform(r.log2_s);
+    rank<NT>(cand, n, a.K, tid, [&](uint32_t k, uint64_t key) {
+        o.ids[k] = (int32_t)~(uint32_t)key;
+        o.logps[k] = weight ? ((key_score((uint32_t)(key >> 32)) - base) * a.c - log2_s) * kLn2 : kNone;
+    });
+    if (n < (uint32_t)a.K) fill_row<NT>(a, o, tid, (int32_t)n, -1, kNone);  // fewer choices than K
+}
+
+// does the token count, with its taken token (flagged where that is outside the vocabulary)
+__device__ __forceinline__ bool counts(const TopArgs& a, int64_t at, bool flags, int32_t* tok) {
+    *tok = 0;
+    if (a.mask && !a.mask[at]) return false;
+    if (!a.tokens) return true;
+    *tok = a.tokens[at];
+    if (*tok >= 0 && *tok < a.V) return true;
+    if (flags) flag_error(a.err, ERR_TOKEN);
+    return false;
+}
+
+// ---------------------------------------------------------------------------
+// short rows: a wavefront each, E elements a lane
+// ---------------------------------------------------------------------------
+template <bool BF16, int E>
+__global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
+    using T = typename Elem<BF16>::T;
+    __shared__ uint64_t s_cand[kTopThreads / kWave][kShortCandidates];
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
+    const uint32_t n = block_number() * (kTopThreads / kWave) + w;
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    uint64_t* cand = s_cand[w];
+    const int64_t at = a.shape.at(n);
+    int32_t tok;
+    if (!counts(a, at, l == 0, &tok)) return write_nothing<kWave>(a, n, at, l);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    float v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = l + i * kWave < a.V ? Elem<BF16>::one(x[l + i * kWave]) : kNone;
+    const float xa = Elem<BF16>::one(x[tok]);
+    Stat st = no_stat();
+    accumulate(st, v, a.c);
+    const float mine = st.m;
+    st = join_lanes<kWave>(st, a.c);
+    const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
+    if (l == 0) write_values(a, at, r.logp, r.lse, r.entropy);
+    if (no_ranking(st)) return fill_row<kWave>(a, TopRow(a, n), l, 0, -1, __builtin_nanf(""));
+    uint32_t key[E];  // 0 beyond the row
+#pragma unroll
+    for (int i = 0; i < E; ++i) key[i] = l + i * kWave < a.V ? order_key(v[i]) : 0;
+    uint32_t bound = 1;
+    if (a.K < kWave && a.V > kShortCandidates / 2) {
+        const uint32_t top[1] = {order_key(mine)};
+        bound = key_bound(top, (uint32_t)a.K);
+    }
+    uint32_t some = 0, ties = kShortCandidates;  // (all that reach the bound)
+#pragma unroll
+    for (int i = 0; i < E; ++i) some += __builtin_popcountll(__ballot(key[i] >= bound));
+    if (some > kShortCandidates) {
+        bound = key_bound(key, (uint32_t)a.K);
+        uint32_t above = 0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) above += __builtin_popcountll(__ballot(key[i] > bound));
+        ties = (uint32_t)a.K - above;  // (exactly K reach it, or the K-th largest is it)
+    }
+    // an element's number grows with i and then with the lane: ties are met in order
+    uint32_t found = 0, equal = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const uint64_t same = __ballot(key[i] == bound);
+        const bool take = key[i] > bound || (key[i] == bound && equal + __builtin_popcountll(same & below_lane()) < ties);
+        const uint64_t taken = __ballot(take);
+        if (take) cand[found + __builtin_popcountll(taken & below_lane())] = (uint64_t)key[i] << 32 | (uint32_t)~(l + i * kWave);
+        found += __builtin_popcountll(taken);
+        equal += __builtin_popcountll(same);
+    }
+    wave_fence();
+    write_ranked<kWave>(a, n, cand, found, r, l);
+}
+
+// ---------------------------------------------------------------------------
+// longer rows, or parts of them: a workgroup each
+// ---------------------------------------------------------------------------
+struct TopShared {
+    uint64_t cand[kMostCandidates];
+    uint32_t list[kMostGroups];
+    uint32_t top[kTopThreads];
+    Stat stat[kTopThreads / kWave];
+    uint32_t sum[2][kTopThreads / kWave];
+    uint32_t bound, groups, found;
+    bool last;
+};
+
+// sum over the workgroup, in every thread; `turn` alternates from call to call
+__device__ __forceinline__ uint32_t block_count(TopShared& s, uint32_t mine, int turn) {
+    mine = lanes_sum<kWave>(mine);
+    if (lane_id() == 0) s.sum[turn][threadIdx.x / kWave] = mine;
+    __syncthreads();
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < kTopThreads / kWave; ++i) r += s.sum[turn][i];
+    return r;
+}
+
+// The K-th largest of all keys, which `each(f)` gives f one after the other, is
+// found bit by bit, and those that reach it become the candidates: K of them, or
+// all if there are fewer.  Every thread takes part.
+template <typename Each>
+__device__ __forceinline__ uint32_t exact_candidates(TopShared& s, int32_t K, Each each) {
+    uint64_t t = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t trial = t | 1ull << bit;
+        uint32_t mine = 0;
+        each([&](uint64_t key) { mine += key >= trial; });
+        if (block_count(s, mine, bit & 1) >= (uint32_t)K) t = trial;
+    }
+    if (threadIdx.x == 0) s.found = 0;
+    __syncthreads();
+    each([&](uint64_t key) {
+        if (key != 0 && key >= t) s.cand[atomicAdd(&s.found, 1u)] = key;
+    });
+    __syncthreads();
+    return s.found;
+}
+
+// the bound that K of the lanes' largest keys reach, in every thread
+__device__ __forceinline__ uint32_t block_bound(TopShared& s, uint32_t mine, int32_t K) {
+    s.top[threadIdx.x] = mine;
+    if (threadIdx.x == 0) s.groups = s.found = 0;
+    __syncthreads();
+    if (threadIdx.x < kWave) {
+        uint32_t top[kTopThreads / kWave];
+#pragma unroll
+        for (int i = 0; i < kTopThreads / kWave; ++i) top[i] = s.top[i * kWave + threadIdx.x];
+        const uint32_t t = key_bound(top, (uint32_t)K);
+        if (threadIdx.x == 0) s.bound = t;
+    }
+    __syncthreads();
+    return s.bound;
+}
+
+// Joins a row's parts: their statistics, and the K largest of their K keys each.
+// By a whole workgroup.
+template <bool BF16>
+__device__ void join_top(const TopArgs& a, uint32_t n, int64_t at, int32_t tok, TopShared& s) {
+    using T = typename Elem<BF16>::T;
+    const uint32_t tid = threadIdx.x;
+    const float xa = Elem<BF16>::one((static_cast<const T*>(a.x.data) + a.x.at(n, a.shape))[tok]);
+    Stat st = no_stat();
+    for (int32_t p = tid; p < a.parts; p += kTopThreads) {
+        const float* q = a.part + 3 * ((int64_t)n * a.parts + p);
+        Stat o;
+        o.m = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        o.s = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        o.u = __hip_atomic_load(q + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        st = join(st, o, a.c);
+    }
+    // the best of every part come first, then the second best, ...: the lanes' largest are spread over the first ranks
+    const uint64_t* keys = a.key + (int64_t)n * a.parts * a.K;
+    const uint32_t total = (uint32_t)a.parts * (uint32_t)a.K;
+    auto each = [&](auto f) {
+        for (uint32_t e = tid; e < total; e += kTopThreads) {
+            const uint32_t r = e / (uint32_t)a.parts, p = e - r * (uint32_t)a.parts;
+            f(__hip_atomic_load(keys + (int64_t)p * a.K + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        }
+    };
+    uint32_t mine = 0;
+    each([&](uint64_t key) {
+        const uint32_t k = (uint32_t)(key >> 32);
+        mine = k > mine ? k : mine;
+    });
+    st = join_block<kTopThreads / kWave>(st, s.stat, a.c);
+    const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
+    if (tid == 0) write_values(a, at, r.logp, r.lse, r.entropy);
+    if (no_ranking(st)) return fill_row<kTopThreads>(a, TopRow(a, n), tid, 0, -1, __builtin_nanf(""));
+    const uint32_t bound = block_bound(s, mine, a.K);
+    each([&](uint64_t key) {
+        if (key == 0 || (uint32_t)(key >> 32) < bound) return;
+        const uint32_t k = atomicAdd(&s.found, 1u);
+        if (k < kMostCandidates) s.cand[k] = key;
+    });
+    __syncthreads();
+    uint32_t found = s.found;
+    if (found > kMostCandidates) found = exact_candidates(s, a.K, each);
+    write_ranked<kTopThreads>(a, n, s.cand, found, r, tid);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kTopThreads) void k_top_rows(TopArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer;
+    extern __shared__ float s_group[];  // the groups' maxima
+    __shared__ TopShared s;
+    const uint32_t item = block_number(), tid = threadIdx.x;
+    if (item >= (uint32_t)(a.shape.B * a.shape.T) * (uint32_t)a.parts) return;
+    const uint32_t n = div31(item, a.by_parts), part = item - n * (uint32_t)a.parts;
+    const int64_t at = a.shape.at(n);
+    int32_t tok;
+    if (!counts(a, at, part == 0 && tid == 0, &tok)) {
+        if (part == 0) write_nothing<kTopThreads>(a, n, at, tid);
+        return;
+    }
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
+    const uint32_t groups = (hi - lo + kGroup - 1) / kGroup;
+    const bool last_one = part == 0 && tid < tail;  // the elements after the last vector
+    const float xt = last_one ? E::one(x[nv * kPer + tid]) : kNone;
+    const float xa = a.parts == 1 ? E::one(x[tok]) : 0.0f;
+    Stat st = no_stat();
+    for (uint32_t base = lo; base < hi; base += kTopThreads * kTopVectors) {
+        u32x4 v[kTopVectors];
+#pragma unroll
+        for (int k = 0; k < kTopVectors; ++k) {
+            const uint32_t i = base + k * kTopThreads + tid;
+            v[k] = i < hi ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
+        }
+        float top = kNone;
+#pragma unroll
+        for (int k = 0; k < kTopVectors; ++k) {
+            const uint32_t i = base + k * kTopThreads + tid;
+            float f[kPer];
+            E::unpack(v[k], f);
+            const float mine = top_of(f, kNone);
+            top = fmaxf(top, mine);
+            const float group = lanes_reduce<kGroup>(mine, [](float p, float q) { return fmaxf(p, q); });
+            if (tid % kGroup == 0 && i < hi) s_group[(i - lo) / kGroup] = group;
+        }
+        raise(st, top, a.c);
+#pragma unroll
+        for (int k = 0; k < kTopVectors; ++k) {
+            float f[kPer];
+            E::unpack(again(v[k]), f);
+            add(st, f, a.c);
+        }
+    }
+    {
+        const float f[1] = {xt};
+        accumulate(st, f, a.c);
+    }
+    const float mine = st.m;
+    st = join_block<kTopThreads / kWave>(st, s.stat, a.c);
+    const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
+    uint32_t found = 0;
+    if (!no_ranking(st)) {
+        const uint32_t bound = block_bound(s, order_key(mine), a.K);
+        for (uint32_t g = tid; g < groups; g += kTopThreads) {
+            if (order_key(s_group[g]) < bound) continue;
+            const uint32_t k = atomicAdd(&s.groups, 1u);
+            if (k < kMostGroups) s.list[k] = g;
+        }
+        __syncthreads();
+        uint32_t listed = s.groups;
+        auto each = [&](auto f) {
+            for (uint32_t q = tid / kGroup; q < listed; q += kTopThreads / kGroup) {
+                const uint32_t i = lo + s.list[q] * kGroup + tid % kGroup;
+                if (i >= hi) continue;
+                float e[kPer];
+                E::unpack(load16(x + (size_t)i * kPer), e);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) f(choice_key(e[j], i * kPer + j));
+            }
+            if (last_one) f(choice_key(xt, nv * kPer + tid));
+        };
+        if (listed <= kMostGroups) {
+            each([&](uint64_t key) {
+                if ((uint32_t)(key >> 32) < bound) return;
+                const uint32_t k = atomicAdd(&s.found, 1u);
+                if (k < kMostCandidates) s.cand[k] = key;
+            });
+            __syncthreads();
+            found = s.found;
+        }
+        if (listed > kMostGroups || found > kMostCandidates) {
+            uint32_t t = 0;  // the K-th largest maximum (0: fewer groups)
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t trial = t | 1u << bit;
+                uint32_t k = 0;
+                for (uint32_t g = tid; g < groups; g += kTopThreads) k += order_key(s_group[g]) >= trial;
+                if (block_count(s, k, bit & 1) >= (uint32_t)a.K) t = trial;
+            }
+            __syncthreads();
+            if (tid < kWave) {
+                uint32_t k = 0, equal = 0;
+                for (uint32_t base = 0; base < groups; base += kWave) {
+                    const uint32_t g = base + tid, key = g < groups ? order_key(s_group[g]) : 0;
+                    const uint64_t same = __ballot(g < groups && key == t);
+                    const bool take = g < groups && (key > t || (key == t && equal + __builtin_popcountll(same & below_lane()) < (uint32_t)a.K));
+                    const uint64_t taken = __ballot(take);
+                    if (take) s.list[k + __builtin_popcountll(taken & below_lane())] = g;
+                    k += __builtin_popcountll(taken);
+                    equal += __builtin_popcountll(same);
+                }
+                if (tid == 0) s.groups = k;
+            }
+            __syncthreads();
+            listed = s.groups;
+            found = exact_candidates(s, a.K, each);
+        }
+    }
+    if (a.parts == 1) {
+        if (tid == 0) write_values(a, at, r.logp, r.lse, r.entropy);
+        if (no_ranking(st)) return fill_row<kTopThreads>(a, TopRow(a, n), tid, 0, -1, __builtin_nanf(""));
+        return write_ranked<kTopThreads>(a, n, s.cand, found, r, tid);
+    }
+    // a part: its K keys in order (0: there are fewer) and its statistics, for the join
+    uint64_t* key = a.key + (int64_t)item * a.K;
+    rank<kTopThreads>(s.cand, found, a.K, tid, [&](uint32_t k, uint64_t v) {
+        __hip_atomic_store(key + k, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+    for (uint32_t k = found + tid; k < (uint32_t)a.K; k += kTopThreads) __hip_atomic_store(key + k, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) {
+        float* mine = a.part + 3 * (int64_t)item;
+        __hip_atomic_store(mine, st.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 1, st.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 2, st.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (!a.row_ticket) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // every wavefront's stores are acknowledged before the ticket is drawn
+    __syncthreads();
+    if (tid == 0) s.last = draw_last(a.row_ticket + n * kTicketStep, (uint32_t)a.parts);
+    __syncthreads();
+    if (s.last) join_top<BF16>(a, n, at, tok, s);
+}
+
+// the join of many split rows, by a launch of its own
+template <bool BF16>
+__global__ __launch_bounds__(kTopThreads) void k_top_join(TopArgs a) {
+    __shared__ TopShared s;
+    const uint32_t n = block_number();
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    const int64_t at = a.shape.at(n);
+    int32_t tok;
+    if (!counts(a, at, false, &tok)) return;
+    join_top<BF16>(a, n, at, tok, s);
+}
+
+template <bool BF16>
+hipError_t alternatives(const TopArgs& a, hipStream_t s) {
+    const int64_t rows = a.shape.B * a.shape.T;
+    constexpr int kRows = kTopThreads / kWave;
+    if (a.V <= 8 * kWave) {
+        hipLaunchKernelGGL((k_top_short<BF16, 8>), grid_of((rows + kRows - 1) / kRows, kTopThreads), dim3(kTopThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    if (a.V <= kShortRow) {
+        hipLaunchKernelGGL((k_top_short<BF16, kShortRow / kWave>), grid_of((rows + kRows - 1) / kRows, kTopThreads), dim3(kTopThreads),
+                           0, s, a);
+        return hipGetLastError();
+    }
+    // one launch takes fewer than 2^31 parts (the division's range)
+    const int64_t items = rows * a.parts;
+    if (items >= 1ll << 31) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_top_rows<BF16>), grid_of(items, kTopThreads), dim3(kTopThreads), sizeof(float) * (a.per / kGroup), s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 1 || a.row_ticket) return e;
+    hipLaunchKernelGGL((k_top_join<BF16>), grid_of(rows, kTopThreads), dim3(kTopThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Parts of a row: as in k_logits.hip, or where a row is wider than the groups'
+// maxima of one workgroup; whole groups each.
+RowParts top_parts(int64_t rows, int64_t V, bool bf16) {
+    const int64_t cus = device_cus(), nv = V / (bf16 ? 8 : 4);
+    if (V <= kShortRow || rows <= 0) return RowParts{1, (int32_t)nv};
+    int64_t parts = (nv + kPartVectors - 1) / kPartVectors;
+    if (rows < cus) {
+        const int64_t want = (2 * cus + rows - 1) / rows, most = nv / (4 * kTopThreads);
+        const int64_t split = want < most ? want : most;
+        if (split > parts) parts = split;
+    }
+    const int64_t per = ((nv + parts - 1) / parts + kGroup - 1) / kGroup * kGroup;
+    return RowParts{(int32_t)((nv + per - 1) / per), (int32_t)per};
+}
+
+hipError_t launch_token_alternatives(const TopArgs& a, bool bf16, hipStream_t s) {
+    return bf16 ? alternatives<true>(a, s) : alternatives<false>(a, s);
+}
+
+}  // namespace conduit

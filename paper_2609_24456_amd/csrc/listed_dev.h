@@ -1,0 +1,120 @@
+// Launch arguments of the kernels on listed choices (k_top.hip, k_listed.hip).
+#pragma once
+
+#include "softmax_dev.h"
+
+namespace conduit {
+
+constexpr int kMostListed = 128;      // choices a token
+constexpr int64_t kShortRow = 2048;   // choices that one wavefront takes
+constexpr int kPartVectors = 32768;   // most vectors of a part of a row: its LDS grows with them
+
+// how a call's rows are split: parts of `per` vectors
+struct RowParts {
+    int32_t parts, per;
+};
+RowParts top_parts(int64_t rows, int64_t V, bool bf16);
+RowParts listed_parts(int64_t rows, int64_t V, bool bf16, bool whole_rows);
+
+// The K most probable choices of every token.
+struct TopArgs {
+    TokenShape shape;
+    RowsView x;
+    int64_t V;
+    float c, inv_t, inv_lo;  // as in LogitsArgs
+    const int32_t* tokens;   // NULL: no taken token
+    const uint8_t* mask;
+    RowsView ids, logps;
+    int32_t K;
+    float* logp;
+    float* lse;
+    float* entropy;
+    uint32_t* err;
+    // split rows: statistics and K keys of each part of a row
+    int32_t parts;
+    int32_t per;  // vectors a part, a multiple of 8
+    Div31 by_parts;
+    float* part;
+    uint64_t* key;
+    uint32_t* row_ticket;  // NULL: a second launch joins the parts
+};
+
+hipError_t launch_token_alternatives(const TopArgs& a, bool bf16, hipStream_t s);
+
+// The row of a token as its listed choices and the others make it, for the
+// gradient: dx_j = coef 2^(c (x_j - base)) for the others, and of a listed one
+// by its own and the teacher's probability.
+struct ListedRow {
+    float base, coef;
+    float top, log2_s;  // log p = ln2 (c (x - top) - log2_s)
+    float q_top, q_log; // log q = (y / teacher's temperature - q_top) - q_log
+    float loss, over, w;
+};
+
+struct ListedArgs {
+    TokenShape shape;
+    RowsView x, dx;
+    int64_t V;
+    float c, inv_t, inv_lo;
+    const uint8_t* mask;
+    RowsView ids;
+    int32_t K;
+    uint32_t* err;
+    // log-probabilities
+    RowsView logps;
+    float* rest;
+    float* lse;
+    // their gradient
+    const float* lse_in;
+    const float* rest_in;
+    RowsView g;
+    const float* h;
+    // distillation
+    RowsView teacher;
+    float q_inv_t;
+    bool reverse, with_rest, has_dx;
+    int32_t reduction;
+    double scale;
+    const float* weight;
+    float* loss;
+    float* stats;
+    WorkspaceHead* head;
+    uint32_t* row_count;
+    double* partial;  // [kPolicyBlocks][2]
+    bool sums;        // the statistics are summed up as the rows go
+    // split rows
+    int32_t parts, per;
+    Div31 by_parts;
+    float* part;           // [rows][parts][2]
+    ListedRow* row;        // [rows]
+    uint32_t* row_ticket;  // NULL: a second launch joins the parts
+};
+
+constexpr int kDistillSums = 2;  // weighted and plain divergence
+
+hipError_t launch_listed_logprobs(const ListedArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_listed_logprobs_backward(const ListedArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_distill_loss(const ListedArgs& a, bool bf16, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// device code of both
+// ---------------------------------------------------------------------------
+// Orders LDS accesses of a wavefront's lanes: what they wrote before is what
+// they read after.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The first lane's value, in every lane.  Sums over lanes of products may be
+// contracted to one's own product and the rounded other, and then differ from lane
+// to lane in the last place: who writes a value must not depend on which lane it
+// fell to.
+__device__ __forceinline__ float uniform(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
+__device__ __forceinline__ uint64_t below_lane() { return (1ull << lane_id()) - 1; }
+
+}  // namespace conduit

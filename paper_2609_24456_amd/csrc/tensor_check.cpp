@@ -129,28 +129,31 @@ struct Rows {
     int64_t width, stride_b, stride_t;
 };
 
-// rows(address of a Rows, t, tokens, f32, bf16): fills it in for a float32 or
-// bfloat16 tensor on a HIP device of one row for each element of `tokens`, and
-// says whether it did.  f32 and bf16 are the library's numbers of the dtypes.
+// rows(address of a Rows, t, tokens, f32, bf16, i32 = -1): fills it in for a
+// float32 or bfloat16 tensor on a HIP device of one row for each element of
+// `tokens`, and says whether it did.  f32, bf16 and i32 are the library's numbers
+// of the dtypes.  With i32 the tensor may be an int32 one too, and `tokens` is
+// itself a tensor of rows, one for each of t's.
 PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 5) {
-        PyErr_SetString(PyExc_TypeError, "rows takes (address, tensor, tokens, f32, bf16)");
+    if (nargs != 5 && nargs != 6) {
+        PyErr_SetString(PyExc_TypeError, "rows takes (address, tensor, tokens, f32, bf16[, i32])");
         return nullptr;
     }
     if (!THPVariable_CheckExact(args[1]) || !THPVariable_CheckExact(args[2])) Py_RETURN_FALSE;
     Rows* r = static_cast<Rows*>(PyLong_AsVoidPtr(args[0]));
-    const long f32 = PyLong_AsLong(args[3]), bf16 = PyLong_AsLong(args[4]);
+    const long f32 = PyLong_AsLong(args[3]), bf16 = PyLong_AsLong(args[4]), i32 = nargs == 6 ? PyLong_AsLong(args[5]) : -1;
     if (PyErr_Occurred()) return nullptr;
     try {
         const at::Tensor& t = THPVariable_Unpack(args[1]);
         const at::Tensor& n = THPVariable_Unpack(args[2]);
-        const int64_t d = n.dim();
-        if (!t.is_cuda() || (d != 1 && d != 2) || t.dim() != d + 1) Py_RETURN_FALSE;
-        if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) Py_RETURN_FALSE;
+        const int64_t d = t.dim() - 1;
+        if (!t.is_cuda() || (d != 1 && d != 2) || n.dim() != (nargs == 6 ? d + 1 : d)) Py_RETURN_FALSE;
+        const bool whole = nargs == 6 && t.scalar_type() == at::kInt;
+        if (!whole && t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) Py_RETURN_FALSE;
         for (int64_t i = 0; i < d; ++i)
             if (t.size(i) != n.size(i)) Py_RETURN_FALSE;
         if (t.size(d) > 1 && t.stride(d) != 1) Py_RETURN_FALSE;
-        *r = Rows{t.data_ptr(), (int32_t)(t.scalar_type() == at::kFloat ? f32 : bf16), 0, t.size(d),
+        *r = Rows{t.data_ptr(), (int32_t)(whole ? i32 : t.scalar_type() == at::kFloat ? f32 : bf16), 0, t.size(d),
                   d == 2 ? t.stride(0) : 0, t.stride(d - 1)};
     } catch (...) {
         Py_RETURN_FALSE;
