@@ -291,7 +291,7 @@ def test_binding_checks(monkeypatch):
     with pytest.raises(ValueError, match="dlogits must be"):
         cd.conduit_distill_loss(cd.distill_opts(), x, i, y, t, stats, dlogits=x[:1])
     with pytest.raises(ValueError):
-        cd.conduit_distill_loss(cd.distill_opts(), x, i, y, t, torch.zeros(4), workspace=torch.zeros(1 << 16, dtype=torch.uint8))
+        cd.conduit_distill_loss(cd.distill_opts(), x, i, y, t, torch.zeros(2), workspace=torch.zeros(1 << 16, dtype=torch.uint8))
     monkeypatch.setattr(cd, "_on_device", lambda t: False)
     with pytest.raises(ValueError, match="on a HIP device"):
         cd.conduit_listed_logprobs(x, i, y)
