@@ -247,7 +247,7 @@ __device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others,
 
 // the teacher's side of a row
 struct Teacher {
-    float top, log;  // log q = (y / temperature - top) - log
+    float top, log;  // log q = (y - top) / temperature - log: the largest goes first, as for the scores
     double left;     // what its listed probabilities leave (with_rest)
     bool any;
 };
@@ -268,11 +268,11 @@ __device__ __forceinline__ Teacher teacher_row(const ListedArgs& a, const Listed
     }
     float top = kNone;
 #pragma unroll
-    for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.y[i] * a.q_inv_t : kNone);
+    for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.y[i] : kNone);
     t.top = t.any ? wave_top(top) : 0.0f;
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.y[i] * a.q_inv_t - t.top) * kLog2e) : 0.0f;
+    for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.y[i] - t.top) * (a.q_inv_t * kLog2e)) : 0.0f;
     t.log = t.any ? log2_fast(uniform(lanes_sum<kWave>(sum))) * kLn2 : 0.0f;
     return t;
 }
@@ -302,7 +302,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         if (!e.first[i]) continue;
-        const float lq = (e.y[i] * a.q_inv_t - t.top) - t.log, lp = r.logp(e.x[i], a.c);
+        const float lq = (e.y[i] - t.top) * a.q_inv_t - t.log, lp = r.logp(e.x[i], a.c);
         const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
         loss += a.reverse ? curve(p, q, u) : curve(q, p, -u);
     }
@@ -333,7 +333,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
 // the gradient of a listed choice of score x and teacher's value y
 __device__ __forceinline__ float listed_gradient(const ListedArgs& a, const ListedRow& o, float x, float y) {
     if (o.w == 0.0f) return 0.0f;
-    const float lq = (y * a.q_inv_t - o.q_top) - o.q_log, lp = ((x - o.top) * a.c - o.log2_s) * kLn2;
+    const float lq = (y - o.q_top) * a.q_inv_t - o.q_log, lp = ((x - o.top) * a.c - o.log2_s) * kLn2;
     const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
     if (a.reverse) return p == 0.0f ? 0.0f : -o.w * p * (u + o.loss);
     return o.w * fmaf(p, o.over, apart_by(q, p, -u));
@@ -670,22 +670,41 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// distillation of rows that fit a workgroup's registers, K vectors a lane
+// distillation of rows that fit the registers of WAVES wavefronts, K vectors a lane
 // ---------------------------------------------------------------------------
+// A row crosses memory once in each direction.  HBM bounds it where the rows are
+// wide or fp32 (4,088 rows of 32,001 fp32, 37% of them live: 147 us, 4.9 TB/s, a
+// large copy's rate; 8,192 of 128,000 bf16: 600, 4.8), the steps of a row one after
+// the other where they are not: load, sum, join, the list's part, store.  A lane
+// takes up to 16 vectors, so that a row has few wavefronts to join and a compute
+// unit several rows at different steps, and what a lane's vectors have beyond the
+// row is left out (unmasked, read and written, V x rows bf16: 5,001 x 16,384 on one
+// wavefront 91 us, on four 166-235; 10,001 x 8,192 on two 90, on four 109; 50,001 x
+// 2,048 on eight 110, on sixteen 137; fp32, with half the work in a vector, is
+// better on sixteen of 8 vectors: 32,001 x 4,088 masked 147, on eight of 16 156).
+// The list is loaded ahead of the row and its scores behind it.
 constexpr int kRowVectors = 16 * 1024;  // of a workgroup of 1,024
 
+template <int WAVES>
+__device__ __forceinline__ void row_sync() {
+    if constexpr (WAVES == 1) wave_fence();
+    else __syncthreads();
+}
+
 template <bool BF16, int WAVES, int K>
-__global__ __launch_bounds__(WAVES * kWave) void k_distill_rows(ListedArgs a) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_rows(ListedArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
     constexpr int NT = WAVES * kWave;
     constexpr int kWords = K * kPer / 32;
-    __shared__ uint32_t s_bits[NT][kWords];
-    __shared__ uint32_t s_tail;
+    constexpr int kRows = WAVES == 1 ? 256 / kWave : 1;  // of a workgroup
+    __shared__ uint32_t s_bits[kRows][NT][kWords];
+    __shared__ uint32_t s_tail[kRows];
     __shared__ Mass s_mass[WAVES];
     __shared__ ListedRow s_row;
-    const uint32_t n = block_number(), tid = threadIdx.x;
+    const uint32_t w = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0;
+    const uint32_t n = block_number() * kRows + w, tid = threadIdx.x % NT;
     if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
@@ -700,83 +719,117 @@ __global__ __launch_bounds__(WAVES * kWave) void k_distill_rows(ListedArgs a) {
         }
         return;
     }
-    u32x4 v[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = k * NT + tid;
-        v[k] = i < nv ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
-    }
-    float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
+    // the list first: its scores' addresses wait for it under the row's loads
     Listed e;
     double part = 0.0;
     if (tid < kWave) {
         load_ids(a, n, e);
         load_values(a, a.teacher, n, e);
-        check_ids<true>(a, e, true);
-        load_scores<BF16>(x, e);
         part = token_part(a, n, at);
     }
+    // vectors k of all lanes are beyond the row from some k on: nothing is done for them
+    u32x4 v[K];
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) s_bits[tid][i] = 0;
-    if (tid == 0) s_tail = 0;
-    __syncthreads();
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = k * NT + tid;
+        v[k] = no_vector<BF16>();
+        if (k * NT < nv && i < nv) v[k] = load16(x + (size_t)i * kPer);
+    }
+    float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
+    if (tid < kWave) {
+        check_ids<true>(a, e, true);
+        load_scores<BF16>(x, e);
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) s_bits[w][tid][i] = 0;
+    if (tid == 0) s_tail[w] = 0;
+    row_sync<WAVES>();
     Teacher t{};
     if (tid < kWave) {
         const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
             const uint32_t i = id / kPer, j = id % kPer, at_bit = i / NT * kPer + j;
-            *word = i < nv ? &s_bits[i % NT][at_bit / 32] : &s_tail;
+            *word = i < nv ? &s_bits[w][i % NT][at_bit / 32] : &s_tail[w];
             *bit = 1u << (i < nv ? at_bit % 32 : j);
             return true;
         });
         if (twice) find_first<false>(e, a.K);
     }
-    __syncthreads();
+    row_sync<WAVES>();
     if (tid < kWave) t = teacher_row(a, e);
     uint32_t bits[kWords], any = 0;
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) any |= bits[i] = s_bits[tid][i];
+    for (int i = 0; i < kWords; ++i) any |= bits[i] = s_bits[w][tid][i];
     auto listed = [&](int k) { return bits[k * kPer / 32] >> k * kPer % 32 & ((1u << kPer) - 1); };
     if (any) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = without<BF16>(v[k], listed(k));
+        for (int k = 0; k < K; ++k)
+            if (listed(k)) v[k] = without<BF16>(v[k], listed(k));
     }
-    const bool listed_tail = tid < tail && (s_tail >> tid & 1);
+    const bool listed_tail = tid < tail && (s_tail[w] >> tid & 1);
     if (listed_tail) xt = kNone;
     Mass others = no_mass();
-    accumulate_mass_tile<BF16>(others, v, a.c);
     {
+        float top = xt;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (k * NT < nv) {
+                float f[kPer];
+                E::unpack(v[k], f);
+                top = top_of(f, top);
+            }
+        }
+        others.m = top;
         const float f[1] = {xt};
-        accumulate_mass(others, f, a.c);
+        add_mass(others, f, a.c);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (k * NT < nv) {
+                float f[kPer];
+                E::unpack(again(v[k]), f);
+                add_mass(others, f, a.c);
+            }
+        }
     }
     others = join_mass<kWave>(others, a.c);
-    if (lane_id() == 0) s_mass[tid / kWave] = others;
-    __syncthreads();
-    others = join_mass<WAVES>(s_mass[lane_id() % WAVES], a.c);
+    if constexpr (WAVES > 1) {
+        if (lane_id() == 0) s_mass[tid / kWave] = others;
+        __syncthreads();
+        others = join_mass<WAVES>(s_mass[lane_id() % WAVES], a.c);
+    }
+    ListedRow o{};
     if (tid < kWave) {
-        const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), t, (float)(part * a.scale));
+        o = distill_row(a, e, others, row_mass(e, others, a.c), t, (float)(part * a.scale));
         if (tid == 0) {
-            s_row = o;
+            if constexpr (WAVES > 1) s_row = o;
             a.loss[at] = o.loss;
         }
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
             if (e.first[i]) dx[e.id[i]] = E::round(listed_gradient(a, o, e.x[i], e.y[i]));
     }
-    __syncthreads();
-    const float coef = s_row.coef, base = s_row.base;
-    const bool none = coef == 0.0f;
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        o.coef = s_row.coef;
+        o.base = s_row.base;
+    }
+    const float coef = uniform(o.coef), base = uniform(o.base);
+    if (coef == 0.0f) {  // whatever the scores are
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = no_vector<BF16>();
+        xt = kNone;
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const uint32_t i = k * NT + tid;
-        if (i >= nv) continue;
+        if (k * NT >= nv || i >= nv) continue;
         float f[kPer];
         E::unpack(again(v[k]), f);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) f[j] = none ? 0.0f : coef * exp2_fast((f[j] - base) * a.c);
+        for (int j = 0; j < kPer; ++j) f[j] = coef * exp2_fast((f[j] - base) * a.c);
         store_others<BF16>(dx + (size_t)i * kPer, f, listed(k));
     }
-    if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(none ? 0.0f : coef * exp2_fast((xt - base) * a.c));
-    if (tid < kWave) finish_token(a, n, part, s_row.loss);
+    if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(coef * exp2_fast((xt - base) * a.c));
+    if (tid < kWave) finish_token(a, n, part, o.loss);
 }
 
 // ---------------------------------------------------------------------------
@@ -965,12 +1018,18 @@ hipError_t distill(const ListedArgs& a, hipStream_t s) {
     if (a.parts > 1 || !a.has_dx) {
         e = launch_scan<BF16, DISTILL>(a, s);
         if (e == hipSuccess && a.has_dx) e = launch_gradient<BF16, true>(a, s);
-    } else if (nv <= 4096) {
-        hipLaunchKernelGGL((k_distill_rows<BF16, 4, 16>), grid_of(rows, 256), dim3(256), 0, s, a);
-        e = hipGetLastError();
     } else {
-        hipLaunchKernelGGL((k_distill_rows<BF16, 16, 16>), grid_of(rows, 1024), dim3(1024), 0, s, a);
-        e = hipGetLastError();
+        auto go = [&](auto waves, auto vectors) {
+            constexpr int WAVES = decltype(waves)::value, K = decltype(vectors)::value;
+            constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = WAVES * kRows * kWave;
+            hipLaunchKernelGGL((k_distill_rows<BF16, WAVES, K>), grid_of((rows + kRows - 1) / kRows, kThreads), dim3(kThreads), 0, s, a);
+            return hipGetLastError();
+        };
+        if (nv <= 16 * 64) e = go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
+        else if (nv <= 16 * 128) e = go(std::integral_constant<int, 2>{}, std::integral_constant<int, 16>{});
+        else if (nv <= 16 * 256) e = go(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
+        else if (nv <= 16 * 512) e = go(std::integral_constant<int, BF16 ? 8 : 16>{}, std::integral_constant<int, BF16 ? 16 : 8>{});
+        else e = go(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
     }
     if (e != hipSuccess || a.sums) return e;
     const int64_t want = (rows + kSumThreads - 1) / kSumThreads;

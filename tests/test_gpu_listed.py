@@ -370,9 +370,24 @@ def test_distill_of_near_and_far_students():
                 _check_distill(x, z, ids, y, None, None, 1.0, F32, dict(opts, teacher_temperature=1.0))
 
 
-@pytest.mark.parametrize("B,T,V,dtype", [(1, 530, 70001, F32), (3, 2, 140003, BF16), (2, 300, 9001, BF16), (700, 1, 2049, F32)])
+@pytest.mark.parametrize("V", [30, 300, 3000, 30000])
+def test_distill_from_logits_far_from_zero(V):
+    """A teacher's values may be logits of any offset: their differences count, not their size."""
+    rng = np.random.default_rng(V)
+    x, z = _logits(rng, 2, 10, V, F32)
+    ids, y = _teacher(rng, z, 20)
+    for offset, tau in ((3e4, 2.0), (-1e5, 0.7)):
+        _check_distill(x, z, ids, (y + np.float32(offset)).astype(np.float32), None, None, 1.0, F32,
+                       dict(loss="forward", teacher_temperature=tau))
+
+
+@pytest.mark.parametrize("B,T,V,dtype", [(1, 530, 70001, F32), (3, 2, 140003, BF16), (2, 300, 9001, BF16), (700, 1, 2049, F32),
+                                         (1, 300, 4096, F32), (1, 300, 8001, F32), (2, 150, 8203, BF16), (1, 300, 16385, F32),
+                                         (1, 300, 20001, BF16), (3, 100, 30003, F32), (1, 300, 50001, BF16), (1, 300, 40005, F32),
+                                         (1, 300, 100007, BF16), (1, 520, 131072, BF16)])
 def test_distill_of_many_and_wide_rows(B, T, V, dtype):
-    """Rows wider than a workgroup's registers (more than 512 of them joined by a launch of its own), sums of many rows."""
+    """Rows of every number of wavefronts and wider than a workgroup's registers (more than 512 of these joined by a launch
+    of its own), sums of many rows."""
     g = torch.Generator(device="cuda").manual_seed(V)
     x = torch.randn((B, T, V), generator=g, device="cuda").mul_(3).to(dtype)
     mask = (torch.rand((B, T), generator=g, device="cuda") < 0.3).to(torch.uint8)
