@@ -46,19 +46,31 @@ __device__ __forceinline__ float key_score(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t choice_key(float x, uint32_t j) { return (uint64_t)order_key(x) << 32 | (uint32_t)~j; }
 
-// The largest bound that at least `need` of a wavefront's keys reach, or, found
-// sooner, one that exactly `need` reach; 0 if there are fewer.
+// A bound that at least `need` of a wavefront's N keys a lane reach, and at most
+// `spare` more unless keys are equal: bit by bit from the highest in which the keys
+// differ.  (need: at most 64 N.)
 template <int N>
-__device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[N], uint32_t need) {
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+__device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[N], uint32_t need, uint32_t spare) {
+    uint32_t hi = key[0], lo = key[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+        hi = key[i] > hi ? key[i] : hi;
+        lo = key[i] < lo ? key[i] : lo;
+    }
+    hi = __builtin_amdgcn_readfirstlane(lanes_reduce<kWave>(hi, [](uint32_t p, uint32_t q) { return p > q ? p : q; }));
+    lo = __builtin_amdgcn_readfirstlane(lanes_reduce<kWave>(lo, [](uint32_t p, uint32_t q) { return p < q ? p : q; }));
+    uint32_t t = lo;
+    if (hi == lo) return t;
+    int bit = 31 - __builtin_clz(hi ^ lo);
+    t = hi >> bit >> 1 << bit << 1;  // what they have in common: all reach it
+    for (; bit >= 0; --bit) {
         const uint32_t trial = t | 1u << bit;
         uint32_t n = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) n += __builtin_popcountll(__ballot(key[i] >= trial));
         if (n < need) continue;
         t = trial;
-        if (n == need) break;
+        if (n <= need + spare) break;
     }
     return t;
 }
@@ -165,13 +177,13 @@ __global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
     uint32_t bound = 1;
     if (a.K < kWave && a.V > kShortCandidates / 2) {
         const uint32_t top[1] = {order_key(mine)};
-        bound = key_bound(top, (uint32_t)a.K);
+        bound = key_bound(top, (uint32_t)a.K, (uint32_t)a.K / 4);
     }
     uint32_t some = 0, ties = kShortCandidates;  // (all that reach the bound)
 #pragma unroll
     for (int i = 0; i < E; ++i) some += __builtin_popcountll(__ballot(key[i] >= bound));
     if (some > kShortCandidates) {
-        bound = key_bound(key, (uint32_t)a.K);
+        bound = key_bound(key, (uint32_t)a.K, 0);
         uint32_t above = 0;
 #pragma unroll
         for (int i = 0; i < E; ++i) above += __builtin_popcountll(__ballot(key[i] > bound));
@@ -193,15 +205,96 @@ __global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// a lane's statistics over tiles of vectors
+// ---------------------------------------------------------------------------
+// The sums go by d' = c x - B in one rounding, with B the rounded c max x: what it
+// is off by is a factor of the whole sum, which stat() takes out.  (That leaves 7.5
+// cycles of a fp32 element and 9.5 of a bf16 one, 4 of them of the exponential, of
+// 9.5 and 11.5.)  A choice at -infinity would give 0 times -infinity: a tile whose
+// weighted sum is no number is summed again with the exponents held, and so are
+// those after it.  Where c x is beyond the floats' range, or nearly, they are as in
+// softmax_dev.h.
+struct TileStat {
+    Stat st = no_stat();
+    float B = 0.0f;
+    bool held = false, far = false;  // uniform
+
+    // as Stat has them, which go by c (x - max x)
+    __device__ __forceinline__ Stat stat(float c) const {
+        if (far || st.m == kNone) return st;
+        const float d = fmaf(st.m, c, -B), e = exp2_fast(-d);
+        return Stat{st.m, st.s * e, fmaf(-d, st.s, st.u) * e};
+    }
+
+    template <bool BF16, bool HELD, int N>
+    __device__ __forceinline__ void sum(const u32x4 (&v)[N], float c) {
+        using E = Elem<BF16>;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float f[E::kPer];
+            E::unpack(again(v[k]), f);
+#pragma unroll
+            for (int j = 0; j < E::kPer; ++j) {
+                const float d = fmaf(f[j], c, -B), e = exp2_fast(d);
+                st.s += e;
+                st.u = fmaf(e, HELD ? fmaxf(d, kFloor) : d, st.u);
+            }
+        }
+    }
+
+    // top: the largest of the lane's vectors; whole: none of them is beyond the row
+    template <bool BF16, int N>
+    __device__ __forceinline__ void add_tile(const u32x4 (&v)[N], float top, float c, bool whole) {
+        const float b = top * c;
+        if (!far && __ballot(top > st.m && !(fabsf(b) < 0x1p100f)) != 0) {
+            st = stat(c);
+            far = true;
+        }
+        if (far) {
+            raise(st, top, c);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                float f[Elem<BF16>::kPer];
+                Elem<BF16>::unpack(again(v[k]), f);
+                conduit::add(st, f, c);
+            }
+            return;
+        }
+        if (top > st.m) {
+            const float d = fminf(B - b, 0.0f), e = exp2_fast(d);
+            st.u = fmaf(st.s, fmaxf(d, kFloor), st.u) * e;
+            st.s *= e;
+            st.m = top;
+            B = b;
+        }
+        if (whole && !held) {
+            const Stat before = st;
+            sum<BF16, false>(v, c);
+            if (__ballot(!(st.u == st.u)) == 0) return;
+            st = before;
+            held = true;
+        }
+        sum<BF16, true>(v, c);
+    }
+};
+
+// ---------------------------------------------------------------------------
 // longer rows, or parts of them: a workgroup each
 // ---------------------------------------------------------------------------
+// HBM bounds it, and the exponentials nearly as much in bf16 (4,096 rows of 128,000
+// bf16, K = 64: 202 us, 5.2 TB/s, where a reduction that only reads reaches 6.0; by
+// the sums of softmax_dev.h 219).  Few rows are bound by latency: 64 rows of
+// 128,000 bf16 in parts, K = 20: 14 us, of which the loads take 3, the part's
+// selection 3 and the join's 4.  Five or six workgroups a compute unit (80
+// registers) cover each other's loads; eight cost spills, workgroups of 512 lanes
+// have their selections at the same time (masked rows: 98 against 115).
 struct TopShared {
     uint64_t cand[kMostCandidates];
     uint32_t list[kMostGroups];
     uint32_t top[kTopThreads];
     Stat stat[kTopThreads / kWave];
     uint32_t sum[2][kTopThreads / kWave];
-    uint32_t bound, groups, found;
+    uint32_t groups, found;
     bool last;
 };
 
@@ -237,29 +330,42 @@ __device__ __forceinline__ uint32_t exact_candidates(TopShared& s, int32_t K, Ea
     return s.found;
 }
 
-// the bound that K of the lanes' largest keys reach, in every thread
-__device__ __forceinline__ uint32_t block_bound(TopShared& s, uint32_t mine, int32_t K) {
-    s.top[threadIdx.x] = mine;
-    if (threadIdx.x == 0) s.groups = s.found = 0;
+// The statistics joined over the workgroup, and the bound that K of the lanes' largest
+// keys reach, in every thread; the lists are empty.
+__device__ __forceinline__ Stat block_stat(TopShared& s, Stat st, uint32_t key, float c, int32_t K, uint32_t* bound) {
+    const uint32_t tid = threadIdx.x, lane = lane_id();
+    s.top[tid] = key;
+    if (tid == 0) s.groups = s.found = 0;
+    st = join_lanes<kWave>(st, c);
+    if (lane == 0) s.stat[tid / kWave] = st;
     __syncthreads();
-    if (threadIdx.x < kWave) {
-        uint32_t top[kTopThreads / kWave];
+    uint32_t top[kTopThreads / kWave];
 #pragma unroll
-        for (int i = 0; i < kTopThreads / kWave; ++i) top[i] = s.top[i * kWave + threadIdx.x];
-        const uint32_t t = key_bound(top, (uint32_t)K);
-        if (threadIdx.x == 0) s.bound = t;
-    }
-    __syncthreads();
-    return s.bound;
+    for (int i = 0; i < kTopThreads / kWave; ++i) top[i] = s.top[i * kWave + lane];
+    *bound = key_bound(top, (uint32_t)K, (uint32_t)K / 4);
+    return join_lanes<kTopThreads / kWave>(s.stat[lane % (kTopThreads / kWave)], c);
 }
 
 // Joins a row's parts: their statistics, and the K largest of their K keys each.
 // By a whole workgroup.
-template <bool BF16>
-__device__ void join_top(const TopArgs& a, uint32_t n, int64_t at, int32_t tok, TopShared& s) {
-    using T = typename Elem<BF16>::T;
+__device__ void join_top(const TopArgs& a, uint32_t n, int64_t at, float xa, TopShared& s) {
     const uint32_t tid = threadIdx.x;
-    const float xa = Elem<BF16>::one((static_cast<const T*>(a.x.data) + a.x.at(n, a.shape))[tok]);
+    // the best of every part come first, then the second best, ...: the lanes' largest are spread over the first ranks
+    const uint64_t* keys = a.key + (int64_t)n * a.parts * a.K;
+    const uint32_t total = (uint32_t)a.parts * (uint32_t)a.K;
+    auto each = [&](auto f) {
+        for (uint32_t e = tid; e < total; e += kTopThreads) {
+            const uint32_t r = div31(e, a.by_parts), p = e - r * (uint32_t)a.parts;
+            f(__hip_atomic_load(keys + (int64_t)p * a.K + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        }
+    };
+    uint32_t mine = 0;
+    uint64_t first = 0;
+    each([&](uint64_t key) {
+        const uint32_t k = (uint32_t)(key >> 32);
+        mine = k > mine ? k : mine;
+        first = key;
+    });
     Stat st = no_stat();
     for (int32_t p = tid; p < a.parts; p += kTopThreads) {
         const float* q = a.part + 3 * ((int64_t)n * a.parts + p);
@@ -269,38 +375,34 @@ __device__ void join_top(const TopArgs& a, uint32_t n, int64_t at, int32_t tok, 
         o.u = __hip_atomic_load(q + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         st = join(st, o, a.c);
     }
-    // the best of every part come first, then the second best, ...: the lanes' largest are spread over the first ranks
-    const uint64_t* keys = a.key + (int64_t)n * a.parts * a.K;
-    const uint32_t total = (uint32_t)a.parts * (uint32_t)a.K;
-    auto each = [&](auto f) {
-        for (uint32_t e = tid; e < total; e += kTopThreads) {
-            const uint32_t r = e / (uint32_t)a.parts, p = e - r * (uint32_t)a.parts;
-            f(__hip_atomic_load(keys + (int64_t)p * a.K + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        }
-    };
-    uint32_t mine = 0;
-    each([&](uint64_t key) {
-        const uint32_t k = (uint32_t)(key >> 32);
-        mine = k > mine ? k : mine;
-    });
-    st = join_block<kTopThreads / kWave>(st, s.stat, a.c);
+    uint32_t bound = 0, found = total;
+    if (total <= kTopThreads) {  // all are candidates
+        st = join_lanes<kWave>(st, a.c);
+        if (lane_id() == 0) s.stat[tid / kWave] = st;
+        s.cand[tid] = first;
+        __syncthreads();
+        st = join_lanes<kTopThreads / kWave>(s.stat[lane_id() % (kTopThreads / kWave)], a.c);
+    } else {
+        st = block_stat(s, st, mine, a.c, a.K, &bound);
+    }
     const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
     if (tid == 0) write_values(a, at, r.logp, r.lse, r.entropy);
     if (no_ranking(st)) return fill_row<kTopThreads>(a, TopRow(a, n), tid, 0, -1, __builtin_nanf(""));
-    const uint32_t bound = block_bound(s, mine, a.K);
-    each([&](uint64_t key) {
-        if (key == 0 || (uint32_t)(key >> 32) < bound) return;
-        const uint32_t k = atomicAdd(&s.found, 1u);
-        if (k < kMostCandidates) s.cand[k] = key;
-    });
-    __syncthreads();
-    uint32_t found = s.found;
-    if (found > kMostCandidates) found = exact_candidates(s, a.K, each);
+    if (total > kTopThreads) {
+        each([&](uint64_t key) {
+            if (key == 0 || (uint32_t)(key >> 32) < bound) return;
+            const uint32_t k = atomicAdd(&s.found, 1u);
+            if (k < kMostCandidates) s.cand[k] = key;
+        });
+        __syncthreads();
+        found = s.found;
+        if (found > kMostCandidates) found = exact_candidates(s, a.K, each);
+    }
     write_ranked<kTopThreads>(a, n, s.cand, found, r, tid);
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kTopThreads) void k_top_rows(TopArgs a) {
+__global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
@@ -321,8 +423,8 @@ __global__ __launch_bounds__(kTopThreads) void k_top_rows(TopArgs a) {
     const uint32_t groups = (hi - lo + kGroup - 1) / kGroup;
     const bool last_one = part == 0 && tid < tail;  // the elements after the last vector
     const float xt = last_one ? E::one(x[nv * kPer + tid]) : kNone;
-    const float xa = a.parts == 1 ? E::one(x[tok]) : 0.0f;
-    Stat st = no_stat();
+    const float xa = E::one(x[tok]);
+    TileStat ts;
     for (uint32_t base = lo; base < hi; base += kTopThreads * kTopVectors) {
         u32x4 v[kTopVectors];
 #pragma unroll
@@ -341,24 +443,18 @@ __global__ __launch_bounds__(kTopThreads) void k_top_rows(TopArgs a) {
             const float group = lanes_reduce<kGroup>(mine, [](float p, float q) { return fmaxf(p, q); });
             if (tid % kGroup == 0 && i < hi) s_group[(i - lo) / kGroup] = group;
         }
-        raise(st, top, a.c);
-#pragma unroll
-        for (int k = 0; k < kTopVectors; ++k) {
-            float f[kPer];
-            E::unpack(again(v[k]), f);
-            add(st, f, a.c);
-        }
+        ts.add_tile<BF16>(v, top, a.c, base + kTopThreads * kTopVectors <= hi);
     }
+    Stat st = ts.stat(a.c);
     {
         const float f[1] = {xt};
         accumulate(st, f, a.c);
     }
-    const float mine = st.m;
-    st = join_block<kTopThreads / kWave>(st, s.stat, a.c);
+    uint32_t bound;
+    st = block_stat(s, st, order_key(st.m), a.c, a.K, &bound);
     const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
     uint32_t found = 0;
     if (!no_ranking(st)) {
-        const uint32_t bound = block_bound(s, order_key(mine), a.K);
         for (uint32_t g = tid; g < groups; g += kTopThreads) {
             if (order_key(s_group[g]) < bound) continue;
             const uint32_t k = atomicAdd(&s.groups, 1u);
@@ -435,7 +531,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_rows(TopArgs a) {
     __syncthreads();
     if (tid == 0) s.last = draw_last(a.row_ticket + n * kTicketStep, (uint32_t)a.parts);
     __syncthreads();
-    if (s.last) join_top<BF16>(a, n, at, tok, s);
+    if (s.last) join_top(a, n, at, xa, s);
 }
 
 // the join of many split rows, by a launch of its own
@@ -447,7 +543,8 @@ __global__ __launch_bounds__(kTopThreads) void k_top_join(TopArgs a) {
     const int64_t at = a.shape.at(n);
     int32_t tok;
     if (!counts(a, at, false, &tok)) return;
-    join_top<BF16>(a, n, at, tok, s);
+    using E = Elem<BF16>;
+    join_top(a, n, at, E::one((static_cast<const typename E::T*>(a.x.data) + a.x.at(n, a.shape))[tok]), s);
 }
 
 template <bool BF16>
