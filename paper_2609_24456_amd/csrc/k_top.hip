@@ -20,6 +20,8 @@
 // largest maximum of a group is found exactly.  Fewer than K groups are above
 // it, and of those that reach it the first K are enough; among their elements
 // the K-th largest key is found bit by bit.
+#include <type_traits>
+
 #include "listed_dev.h"
 #include "rows_dev.h"
 
@@ -146,6 +148,63 @@ __device__ __forceinline__ bool counts(const TopArgs& a, int64_t at, bool flags,
 }
 
 // ---------------------------------------------------------------------------
+// the shortest rows: LANES lanes each, up to kFewElems elements a lane
+// ---------------------------------------------------------------------------
+// Every choice is ranked against all others, with the row's keys in LDS.  Latency
+// bounds it (16,384 rows of 18 fp32, K = 5: 4.7 us; on a wavefront a row 13.3; of 64: 9.9
+// against 15.8, but of 100 on 32 lanes 19.7 against 16.1).
+constexpr int kFewElems = 4;
+
+template <bool BF16, int LANES>
+__global__ __launch_bounds__(kTopThreads) void k_top_few(TopArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kRows = kTopThreads / LANES, kMost = LANES * kFewElems;
+    __shared__ __align__(16) uint64_t s_key[kRows][kMost + 2];  // (2: rows' banks apart)
+    const uint32_t l = threadIdx.x % LANES, g = threadIdx.x / LANES, n = block_number() * kRows + g;
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    const int64_t at = a.shape.at(n);
+    int32_t tok;
+    if (!counts(a, at, l == 0, &tok)) return write_nothing<LANES>(a, n, at, l);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    float v[kFewElems], xa = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kFewElems; ++i) {
+        const int32_t j = l + i * LANES;
+        v[i] = j < a.V ? E::one(x[j]) : kNone;
+        if (j == tok) xa = v[i];  // (the others hold 0)
+    }
+    uint64_t key[kFewElems];  // 0 beyond the row
+#pragma unroll
+    for (int i = 0; i < kFewElems; ++i) {
+        const uint32_t j = l + i * LANES;
+        key[i] = j < a.V ? choice_key(v[i], j) : 0;
+        s_key[g][j] = key[i];
+    }
+    Stat st = no_stat();
+    accumulate(st, v, a.c);
+    st = join_lanes<LANES>(st, a.c);
+    const RowValues r = row_values(st, lanes_sum<LANES>(xa), a.c, a.inv_t, a.inv_lo);
+    if (l == 0) write_values(a, at, r.logp, r.lse, r.entropy);
+    const TopRow o(a, n);
+    if (no_ranking(st)) return fill_row<LANES>(a, o, l, 0, -1, __builtin_nanf(""));
+    wave_fence();
+    uint32_t rank[kFewElems] = {};
+    for (uint32_t m = 0; m < a.V; m += 2) {
+        const uint64_t p = s_key[g][m], q = s_key[g][m + 1];
+#pragma unroll
+        for (int i = 0; i < kFewElems; ++i) rank[i] += (uint32_t)(p > key[i]) + (uint32_t)(q > key[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewElems; ++i) {
+        if (key[i] == 0 || rank[i] >= (uint32_t)a.K) continue;
+        o.ids[rank[i]] = l + i * LANES;
+        o.logps[rank[i]] = r.inv_s != 0.0f ? ((v[i] - r.base) * a.c - r.log2_s) * kLn2 : kNone;
+    }
+    if (a.V < a.K) fill_row<LANES>(a, o, l, (int32_t)a.V, -1, kNone);
+}
+
+// ---------------------------------------------------------------------------
 // short rows: a wavefront each, E elements a lane
 // ---------------------------------------------------------------------------
 template <bool BF16, int E>
@@ -175,19 +234,24 @@ __global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
 #pragma unroll
     for (int i = 0; i < E; ++i) key[i] = l + i * kWave < a.V ? order_key(v[i]) : 0;
     uint32_t bound = 1;
-    if (a.K < kWave && a.V > kShortCandidates / 2) {
+    if (a.K < kWave && a.V > kWave) {
         const uint32_t top[1] = {order_key(mine)};
         bound = key_bound(top, (uint32_t)a.K, (uint32_t)a.K / 4);
     }
-    uint32_t some = 0, ties = kShortCandidates;  // (all that reach the bound)
+    auto reach = [&](uint32_t least) {
+        uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) some += __builtin_popcountll(__ballot(key[i] >= bound));
+        for (int i = 0; i < E; ++i) n += __builtin_popcountll(__ballot(key[i] >= least));
+        return n;
+    };
+    uint32_t some = reach(bound), ties = kShortCandidates;  // (all that reach the bound)
+    if (some > (uint32_t)a.K + (uint32_t)a.K / 2 + 16) {  // ranking takes the square of their number
+        bound = key_bound(key, (uint32_t)a.K, (uint32_t)a.K / 4);
+        some = reach(bound);
+    }
     if (some > kShortCandidates) {
         bound = key_bound(key, (uint32_t)a.K, 0);
-        uint32_t above = 0;
-#pragma unroll
-        for (int i = 0; i < E; ++i) above += __builtin_popcountll(__ballot(key[i] > bound));
-        ties = (uint32_t)a.K - above;  // (exactly K reach it, or the K-th largest is it)
+        ties = (uint32_t)a.K - reach(bound + 1);  // (exactly K reach it, or the K-th largest is it)
     }
     // an element's number grows with i and then with the lane: ties are met in order
     uint32_t found = 0, equal = 0;
@@ -227,10 +291,11 @@ struct TileStat {
     }
 
     template <bool BF16, bool HELD, int N>
-    __device__ __forceinline__ void sum(const u32x4 (&v)[N], float c) {
+    __device__ __forceinline__ void sum(const u32x4 (&v)[N], float c, uint32_t left) {
         using E = Elem<BF16>;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
+            if (HELD && k * kTopThreads >= left) continue;  // nothing but padding
             float f[E::kPer];
             E::unpack(again(v[k]), f);
 #pragma unroll
@@ -242,9 +307,9 @@ struct TileStat {
         }
     }
 
-    // top: the largest of the lane's vectors; whole: none of them is beyond the row
+    // top: the largest of the lane's vectors; left: the row's vectors from the tile on
     template <bool BF16, int N>
-    __device__ __forceinline__ void add_tile(const u32x4 (&v)[N], float top, float c, bool whole) {
+    __device__ __forceinline__ void add_tile(const u32x4 (&v)[N], float top, float c, uint32_t left) {
         const float b = top * c;
         if (!far && __ballot(top > st.m && !(fabsf(b) < 0x1p100f)) != 0) {
             st = stat(c);
@@ -267,14 +332,14 @@ struct TileStat {
             st.m = top;
             B = b;
         }
-        if (whole && !held) {
+        if (left >= N * kTopThreads && !held) {
             const Stat before = st;
-            sum<BF16, false>(v, c);
+            sum<BF16, false>(v, c, left);
             if (__ballot(!(st.u == st.u)) == 0) return;
             st = before;
             held = true;
         }
-        sum<BF16, true>(v, c);
+        sum<BF16, true>(v, c, left);
     }
 };
 
@@ -437,13 +502,14 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
         for (int k = 0; k < kTopVectors; ++k) {
             const uint32_t i = base + k * kTopThreads + tid;
             float f[kPer];
+            if (base + k * kTopThreads >= hi) continue;
             E::unpack(v[k], f);
             const float mine = top_of(f, kNone);
             top = fmaxf(top, mine);
             const float group = lanes_reduce<kGroup>(mine, [](float p, float q) { return fmaxf(p, q); });
             if (tid % kGroup == 0 && i < hi) s_group[(i - lo) / kGroup] = group;
         }
-        ts.add_tile<BF16>(v, top, a.c, base + kTopThreads * kTopVectors <= hi);
+        ts.add_tile<BF16>(v, top, a.c, hi - base);
     }
     Stat st = ts.stat(a.c);
     {
@@ -551,6 +617,14 @@ template <bool BF16>
 hipError_t alternatives(const TopArgs& a, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T;
     constexpr int kRows = kTopThreads / kWave;
+    auto few = [&](auto lanes) {
+        constexpr int LANES = decltype(lanes)::value, kFewRows = kTopThreads / LANES;
+        hipLaunchKernelGGL((k_top_few<BF16, LANES>), grid_of((rows + kFewRows - 1) / kFewRows, kTopThreads), dim3(kTopThreads), 0, s, a);
+        return hipGetLastError();
+    };
+    if (a.V <= 4 * kFewElems) return few(std::integral_constant<int, 4>{});
+    if (a.V <= 8 * kFewElems) return few(std::integral_constant<int, 8>{});
+    if (a.V <= 16 * kFewElems) return few(std::integral_constant<int, 16>{});
     if (a.V <= 8 * kWave) {
         hipLaunchKernelGGL((k_top_short<BF16, 8>), grid_of((rows + kRows - 1) / kRows, kTopThreads), dim3(kTopThreads), 0, s, a);
         return hipGetLastError();

@@ -69,7 +69,7 @@ def _step(dtype, want):
 
 # one choice, rows of a wavefront (8 and 32 elements a lane) and their edges, of a workgroup with and without elements
 # after the last vector, wide enough to be split where there are few of them
-WIDTHS = [1, 2, 3, 18, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 2047, 2048, 2049, 4097, 5001, 16385, 33001]
+WIDTHS = [1, 2, 3, 16, 17, 18, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 2047, 2048, 2049, 4097, 5001, 16385, 33001]
 
 
 def _shape(V):
