@@ -417,7 +417,25 @@ __device__ __forceinline__ void finish_distill(const ListedArgs& a, uint32_t slo
 
 // a row's contribution, by its first wavefront
 __device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, double part, float loss) {
-    if (a.sums) finish_distill(a, n, (uint32_t)(a.shape.B * a.shape.T), part == 0.0 ? 0.0 : part * (double)loss, (double)loss);
+    const double w_loss = part == 0.0 ? 0.0 : part * (double)loss;
+    if (a.sums == SUM_ROWS) finish_distill(a, n, (uint32_t)(a.shape.B * a.shape.T), w_loss, (double)loss);
+    if (a.sums == SUM_NEXT && lane_id() == 0) {  // (nothing waits for it here: no tickets)
+        a.partial[(int64_t)n * kDistillSums] = w_loss;
+        a.partial[(int64_t)n * kDistillSums + 1] = (double)loss;
+    }
+}
+
+// what SUM_NEXT left, by one wavefront of the next launch
+__device__ __forceinline__ void sum_rows(const ListedArgs& a) {
+    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T);
+    double v[kDistillSums] = {0.0, 0.0};
+    for (uint32_t k = lane_id(); k < rows; k += kWave) {
+#pragma unroll
+        for (int i = 0; i < kDistillSums; ++i) v[i] += a.partial[(int64_t)k * kDistillSums + i];
+    }
+#pragma unroll
+    for (int i = 0; i < kDistillSums; ++i) v[i] = wave_sum(v[i]);
+    if (lane_id() == 0) write_distill_stats(a, v);
 }
 
 // sums over the tokens of a batch of many rows
@@ -531,41 +549,62 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kScanVectors = 8;  // vectors a lane and tile
 
+// a row's list with its scores, and the teacher's side of it, by one wavefront
+struct RowList {
+    Listed e;
+    Teacher t;
+    double part;  // the token's weight
+    bool twice;   // a number may be there more than once
+};
+
+// what does not wait for the row; check: entries that are no choices are flagged
+template <int MODE>
+__device__ __forceinline__ void load_list(const ListedArgs& a, uint32_t n, int64_t at, bool check, RowList& r) {
+    load_ids(a, n, r.e);
+    if constexpr (MODE == DISTILL) {
+        load_values(a, a.teacher, n, r.e);
+        r.part = token_part(a, n, at);
+    }
+    check_ids<MODE == DISTILL>(a, r.e, check);
+}
+
 // the row from its others' sum, by one wavefront
 template <bool BF16, int MODE>
-__device__ void finish_listed(const ListedArgs& a, uint32_t n, int64_t at, const Mass& others) {
-    using T = typename Elem<BF16>::T;
-    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    Listed e;
-    load_ids(a, n, e);
-    if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
-    check_ids<MODE == DISTILL>(a, e, true);
-    load_scores<BF16>(x, e);
-    find_first<false>(e, a.K);
+__device__ __forceinline__ void finish_listed(const ListedArgs& a, uint32_t n, int64_t at, const Mass& others, RowList& r) {
+    if (r.twice) {
+        find_first<false>(r.e, a.K);
+        if constexpr (MODE == DISTILL) r.t = teacher_row(a, r.e);
+    }
     if constexpr (MODE == SCORES) {
-        write_scores(a, n, at, e, others);
+        write_scores(a, n, at, r.e, others);
     } else {
-        const double part = token_part(a, n, at);
-        const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
+        const ListedRow o = distill_row(a, r.e, others, row_mass(r.e, others, a.c), r.t, (float)(r.part * a.scale));
         if (lane_id() == 0) a.loss[at] = o.loss;
         if (lane_id() == 0 && a.has_dx) a.row[n] = o;
-        finish_token(a, n, part, o.loss);
+        finish_token(a, n, r.part, o.loss);
     }
 }
 
+// A row's parts leave their others' maximum and sum, and whether they met a number
+// twice (0 or 1: a choice is in one part alone).
+constexpr int kPartWords = 3;
+
 // the join of a row's parts, by one wavefront
 template <bool BF16, int MODE>
-__device__ __forceinline__ void join_listed(const ListedArgs& a, uint32_t n, int64_t at) {
+__device__ __forceinline__ void join_listed(const ListedArgs& a, uint32_t n, int64_t at, RowList& r) {
     Mass all = no_mass();
+    bool twice = false;
     for (int32_t p = lane_id(); p < a.parts; p += kWave) {
-        const float* q = a.part + 2 * ((int64_t)n * a.parts + p);
+        const float* q = a.part + kPartWords * ((int64_t)n * a.parts + p);
         const float m = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const float s = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        twice |= __hip_atomic_load(q + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0.0f;
         const float top = m > all.m ? m : all.m;
         all.s = all.s * exp2_fast(all.m == top ? 0.0f : (all.m - top) * a.c) + s * exp2_fast(m == top ? 0.0f : (m - top) * a.c);
         all.m = top;
     }
-    finish_listed<BF16, MODE>(a, n, at, join_mass<kWave>(all, a.c));
+    r.twice = __ballot(twice) != 0;
+    finish_listed<BF16, MODE>(a, n, at, join_mass<kWave>(all, a.c), r);
 }
 
 template <bool BF16, int MODE>
@@ -592,6 +631,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
+    RowList r{};
+    if (tid < kWave) load_list<MODE>(a, n, at, part == 0, r);  // (ahead of the row's loads)
     u32x4 v[kScanVectors];
     auto load = [&](uint32_t base) {
 #pragma unroll
@@ -600,19 +641,14 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
             v[k] = i < hi ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
         }
     };
-    load(lo);  // beside the list's
-    Listed e;
-    if (tid < kWave) {
-        load_ids(a, n, e);
-        if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
-        check_ids<MODE == DISTILL>(a, e, false);
-    }
+    load(lo);
     const uint32_t tiles = (hi - lo + kTile - 1) / kTile;
     for (uint32_t i = tid; i < tiles * kListedThreads * kWords; i += kListedThreads) s_bits[i] = 0;
     if (tid == 0) s_tail = 0;
     __syncthreads();
     if (tid < kWave) {
-        mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+        load_scores<BF16>(x, r.e);
+        r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
             const uint32_t i = id / kPer, j = id % kPer;
             if (i >= nv) {
                 *word = &s_tail;
@@ -620,11 +656,12 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
                 return part == 0;
             }
             if (i < lo || i >= hi) return false;
-            const uint32_t r = i - lo, tile = r / kTile, slot = r % kTile / kListedThreads, at_bit = slot * kPer + j;
-            *word = s_bits + (tile * kListedThreads + r % kListedThreads) * kWords + at_bit / 32;
+            const uint32_t q = i - lo, tile = q / kTile, slot = q % kTile / kListedThreads, at_bit = slot * kPer + j;
+            *word = s_bits + (tile * kListedThreads + q % kListedThreads) * kWords + at_bit / 32;
             *bit = 1u << at_bit % 32;
             return true;
         });
+        if constexpr (MODE == DISTILL) r.t = teacher_row(a, r.e);
     }
     __syncthreads();
     Mass others = no_mass();
@@ -648,16 +685,17 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     __syncthreads();
     if (tid >= kWave) return;
     others = join_mass<kListedThreads / kWave>(s_mass[lane_id() % (kListedThreads / kWave)], a.c);
-    if (a.parts == 1) return finish_listed<BF16, MODE>(a, n, at, others);
+    if (a.parts == 1) return finish_listed<BF16, MODE>(a, n, at, others, r);
     bool last = false;
     if (lane_id() == 0) {
-        float* mine = a.part + 2 * (int64_t)item;
+        float* mine = a.part + kPartWords * (int64_t)item;
         __hip_atomic_store(mine, others.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __hip_atomic_store(mine + 1, others.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 2, r.twice ? 1.0f : 0.0f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // acknowledged before the ticket is drawn
         if (a.row_ticket) last = draw_last(a.row_ticket + n * kTicketStep, (uint32_t)a.parts);
     }
-    if (__builtin_amdgcn_readfirstlane((int)last)) join_listed<BF16, MODE>(a, n, at);
+    if (__builtin_amdgcn_readfirstlane((int)last)) join_listed<BF16, MODE>(a, n, at, r);
 }
 
 // the join of many split rows, by a launch of its own: a wavefront a row
@@ -666,7 +704,12 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
     const uint32_t n = block_number() * (kListedThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
     const int64_t at = a.shape.at(n);
-    if (!a.mask || a.mask[at]) join_listed<BF16, MODE>(a, n, at);
+    if (a.mask && !a.mask[at]) return;
+    RowList r{};
+    load_list<MODE>(a, n, at, false, r);
+    load_scores<BF16>(static_cast<const typename Elem<BF16>::T*>(a.x.data) + a.x.at(n, a.shape), r.e);
+    if constexpr (MODE == DISTILL) r.t = teacher_row(a, r.e);
+    join_listed<BF16, MODE>(a, n, at, r);
 }
 
 // ---------------------------------------------------------------------------
@@ -849,6 +892,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     __shared__ uint32_t s_bits[kListedThreads / kWave][kWave + 1];
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
     const uint32_t item = block_number() * (kListedThreads / kWave) + w;
+    if (SPLIT && a.sums == SUM_NEXT && item == 0) sum_rows(a);
     if (item >= items) return;
     const uint32_t n = div31(item, by_row), part = item - n * per_row;
     const int64_t at = a.shape.at(n);
@@ -1031,7 +1075,7 @@ hipError_t distill(const ListedArgs& a, hipStream_t s) {
         else if (nv <= 16 * 512) e = go(std::integral_constant<int, BF16 ? 8 : 16>{}, std::integral_constant<int, BF16 ? 16 : 8>{});
         else e = go(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
     }
-    if (e != hipSuccess || a.sums) return e;
+    if (e != hipSuccess || a.sums != SUM_LAUNCH) return e;
     const int64_t want = (rows + kSumThreads - 1) / kSumThreads;
     hipLaunchKernelGGL(k_distill_sum, dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)), dim3(kSumThreads), 0, s, a);
     return hipGetLastError();

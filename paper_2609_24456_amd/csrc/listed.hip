@@ -76,9 +76,9 @@ ListedLayout listed_layout(int64_t B, int64_t T, const conduit_rows* x, bool who
     const int64_t rows = B * T;
     o.split = listed_parts(rows, x->width, x->dtype == CONDUIT_BF16, whole_rows);
     const uint64_t n = o.split.parts > 1 ? (uint64_t)rows * o.split.parts : 0, sums = up(sizeof(double) * kDistillSums * kPolicyBlocks);
-    o.l = layout(B, sums + up(8 * n) + (n > 0 ? sizeof(ListedRow) * (uint64_t)rows : 0));
+    o.l = layout(B, sums + up(12 * n) + (n > 0 ? sizeof(ListedRow) * (uint64_t)rows : 0));
     o.part = o.l.rest + sums;
-    o.more = o.part + up(8 * n);
+    o.more = o.part + up(12 * n);
     return o;
 }
 
@@ -285,8 +285,8 @@ conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const cond
     a.head = reinterpret_cast<WorkspaceHead*>(w);
     a.row_count = reinterpret_cast<uint32_t*>(w + l.l.row_count);
     a.partial = reinterpret_cast<double*>(w + l.l.rest);
-    a.sums = B * T <= kPolicyBlocks;
     place_parts(a, w, l);
+    a.sums = B * T > kPolicyBlocks ? SUM_LAUNCH : a.parts > 1 && a.has_dx ? SUM_NEXT : SUM_ROWS;
     a.row = reinterpret_cast<ListedRow*>(w + l.more);
     return launched(launch_distill_loss(a, logits->dtype == CONDUIT_BF16, s), "distillation launch");
 }

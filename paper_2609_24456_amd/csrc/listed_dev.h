@@ -51,6 +51,10 @@ struct ListedRow {
     float loss, over, w;
 };
 
+// who adds up the rows' parts in the loss: a launch over the tokens, the rows themselves (the last one's wavefront), or,
+// of split rows, the gradient's launch
+enum ListedSums : int32_t { SUM_LAUNCH, SUM_ROWS, SUM_NEXT };
+
 struct ListedArgs {
     TokenShape shape;
     RowsView x, dx;
@@ -81,11 +85,11 @@ struct ListedArgs {
     WorkspaceHead* head;
     uint32_t* row_count;
     double* partial;  // [kPolicyBlocks][2]
-    bool sums;        // the statistics are summed up as the rows go
+    int32_t sums;     // SUM_...
     // split rows
     int32_t parts, per;
     Div31 by_parts;
-    float* part;           // [rows][parts][2]
+    float* part;           // [rows][parts][3]
     ListedRow* row;        // [rows]
     uint32_t* row_ticket;  // NULL: a second launch joins the parts
 };
