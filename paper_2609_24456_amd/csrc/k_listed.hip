@@ -368,36 +368,47 @@ __device__ __forceinline__ void write_nothing(const ListedArgs& a, uint32_t n, i
 // ---------------------------------------------------------------------------
 // the loss's sums
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ double listed_weight(const ListedArgs& a, uint32_t b) {
-    uint32_t tokens = (uint32_t)(a.shape.B * a.shape.T), rows = (uint32_t)a.shape.B, row = (uint32_t)a.shape.T;
-    if (a.mask) {
-        const uint64_t counts = a.head->counts;
-        tokens = (uint32_t)counts;
-        rows = (uint32_t)(counts >> 32);
-        if (a.reduction == CONDUIT_SEQUENCE_MEAN) row = a.row_count[b];
+// Tokens that count, by a wavefront: of a small batch from the mask itself (16 loads of
+// a byte a lane at most, under the row's; a launch for it takes 4.5 us), else from the
+// launch before.
+__device__ __forceinline__ uint32_t counted_tokens(const ListedArgs& a) {
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    if (!a.mask) return n_rows;
+    if (a.counted) return (uint32_t)a.head->counts;
+    uint32_t tokens = 0;
+    for (uint32_t base = 0; base < n_rows; base += 8 * kWave) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t n = base + i * kWave + lane_id();
+            tokens += __builtin_popcountll(__ballot(n < n_rows && a.mask[a.shape.at(n)]));
+        }
     }
-    PolicyTerms o{};
-    o.reduction = a.reduction;
-    return token_weight(o, tokens, rows, row);
+    return tokens;
 }
 
 // the token's part in the loss
-__device__ __forceinline__ double token_part(const ListedArgs& a, uint32_t n, int64_t at) {
-    const double w = listed_weight(a, div31(n, a.shape.by_T));
+__device__ __forceinline__ double token_part(const ListedArgs& a, uint32_t n, int64_t at, uint32_t tokens) {
+    uint32_t rows = (uint32_t)a.shape.B, row = (uint32_t)a.shape.T;
+    if (a.counted && a.reduction == CONDUIT_SEQUENCE_MEAN) {
+        rows = (uint32_t)(a.head->counts >> 32);
+        row = a.row_count[div31(n, a.shape.by_T)];
+    }
+    PolicyTerms o{};
+    o.reduction = a.reduction;
+    const double w = token_weight(o, tokens, rows, row);
     return a.weight ? w * (double)a.weight[at] : w;
 }
 
-__device__ __forceinline__ void write_distill_stats(const ListedArgs& a, const double (&v)[kDistillSums]) {
-    const uint32_t tokens = a.mask ? (uint32_t)a.head->counts : (uint32_t)(a.shape.B * a.shape.T);
+__device__ __forceinline__ void write_distill_stats(const ListedArgs& a, const double (&v)[kDistillSums], uint32_t tokens) {
     a.stats[0] = (float)(a.scale * v[0]);
     a.stats[1] = (float)(v[1] / (double)(tokens > 0 ? tokens : 1));
     a.stats[2] = (float)tokens;
-    if (a.mask) a.head->counts = 0;  // for the next call
+    if (a.counted) a.head->counts = 0;  // for the next call
 }
 
 // `slots` contributions, each left by one wavefront (or workgroup), added up by
 // the wavefront of the last: as finish_row does for the policy loss
-__device__ __forceinline__ void finish_distill(const ListedArgs& a, uint32_t slot, uint32_t slots, double w_loss, double loss) {
+__device__ __forceinline__ void finish_distill(const ListedArgs& a, uint32_t slot, uint32_t slots, double w_loss, double loss, uint32_t tokens) {
     bool last = false;
     if (lane_id() == 0) {
         store_agent(a.partial + (int64_t)slot * kDistillSums, w_loss);
@@ -412,13 +423,13 @@ __device__ __forceinline__ void finish_distill(const ListedArgs& a, uint32_t slo
     }
 #pragma unroll
     for (int i = 0; i < kDistillSums; ++i) v[i] = wave_sum(v[i]);
-    if (lane_id() == 0) write_distill_stats(a, v);
+    if (lane_id() == 0) write_distill_stats(a, v, tokens);
 }
 
 // a row's contribution, by its first wavefront
-__device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, double part, float loss) {
+__device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, double part, float loss, uint32_t tokens) {
     const double w_loss = part == 0.0 ? 0.0 : part * (double)loss;
-    if (a.sums == SUM_ROWS) finish_distill(a, n, (uint32_t)(a.shape.B * a.shape.T), w_loss, (double)loss);
+    if (a.sums == SUM_ROWS) finish_distill(a, n, (uint32_t)(a.shape.B * a.shape.T), w_loss, (double)loss, tokens);
     if (a.sums == SUM_NEXT && lane_id() == 0) {  // (nothing waits for it here: no tickets)
         a.partial[(int64_t)n * kDistillSums] = w_loss;
         a.partial[(int64_t)n * kDistillSums + 1] = (double)loss;
@@ -427,7 +438,7 @@ __device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, do
 
 // what SUM_NEXT left, by one wavefront of the next launch
 __device__ __forceinline__ void sum_rows(const ListedArgs& a) {
-    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T);
+    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T), tokens = counted_tokens(a);
     double v[kDistillSums] = {0.0, 0.0};
     for (uint32_t k = lane_id(); k < rows; k += kWave) {
 #pragma unroll
@@ -435,7 +446,7 @@ __device__ __forceinline__ void sum_rows(const ListedArgs& a) {
     }
 #pragma unroll
     for (int i = 0; i < kDistillSums; ++i) v[i] = wave_sum(v[i]);
-    if (lane_id() == 0) write_distill_stats(a, v);
+    if (lane_id() == 0) write_distill_stats(a, v, tokens);
 }
 
 // sums over the tokens of a batch of many rows
@@ -444,16 +455,16 @@ constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
     __shared__ double lds[kDistillSums * kSumThreads / kWave];
     double v[kDistillSums] = {0.0, 0.0};
-    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T), tokens = counted_tokens(a);
     for (uint32_t n = blockIdx.x * kSumThreads + threadIdx.x; n < n_rows; n += gridDim.x * kSumThreads) {
         const int64_t at = a.shape.at(n);
         if (a.mask && !a.mask[at]) continue;
-        const double part = token_part(a, n, at), loss = (double)a.loss[at];
+        const double part = token_part(a, n, at, tokens), loss = (double)a.loss[at];
         v[0] += part == 0.0 ? 0.0 : part * loss;
         v[1] += loss;
     }
     block_sum<kSumThreads, kDistillSums>(v, lds);
-    if (threadIdx.x < kWave) finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1]);
+    if (threadIdx.x < kWave) finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1], tokens);
 }
 
 // ---------------------------------------------------------------------------
@@ -470,6 +481,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
     const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
     uint32_t* bits = s_bits[w];
     double sums[kDistillSums] = {0.0, 0.0};
+    const uint32_t tokens = MODE == DISTILL ? counted_tokens(a) : 0;
     for (uint32_t n = block_number() * kRows + w; n < n_rows; n += gridDim.x * gridDim.y * kRows) {
         const int64_t at = a.shape.at(n);
         const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
         if constexpr (MODE == SCORES) {
             write_scores(a, n, at, e, others);
         } else {
-            const double part = token_part(a, n, at);
+            const double part = token_part(a, n, at, tokens);
             const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
             if (l == 0) a.loss[at] = o.loss;
             sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
@@ -539,7 +551,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
             v[0] += s_sum[i];
             v[1] += s_sum[kRows + i];
         }
-        finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1]);
+        finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1], tokens);
     }
 }
 
@@ -553,7 +565,8 @@ constexpr int kScanVectors = 8;  // vectors a lane and tile
 struct RowList {
     Listed e;
     Teacher t;
-    double part;  // the token's weight
+    double part;      // the token's weight
+    uint32_t tokens;  // that count
     bool twice;   // a number may be there more than once
 };
 
@@ -563,7 +576,8 @@ __device__ __forceinline__ void load_list(const ListedArgs& a, uint32_t n, int64
     load_ids(a, n, r.e);
     if constexpr (MODE == DISTILL) {
         load_values(a, a.teacher, n, r.e);
-        r.part = token_part(a, n, at);
+        r.tokens = counted_tokens(a);
+        r.part = token_part(a, n, at, r.tokens);
     }
     check_ids<MODE == DISTILL>(a, r.e, check);
 }
@@ -581,7 +595,7 @@ __device__ __forceinline__ void finish_listed(const ListedArgs& a, uint32_t n, i
         const ListedRow o = distill_row(a, r.e, others, row_mass(r.e, others, a.c), r.t, (float)(r.part * a.scale));
         if (lane_id() == 0) a.loss[at] = o.loss;
         if (lane_id() == 0 && a.has_dx) a.row[n] = o;
-        finish_token(a, n, r.part, o.loss);
+        finish_token(a, n, r.part, o.loss, r.tokens);
     }
 }
 
@@ -624,7 +638,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     if (a.mask && !a.mask[at]) {
         if (part == 0 && tid < kWave) {
             write_nothing<MODE>(a, n, at);
-            if constexpr (MODE == DISTILL) finish_token(a, n, 0.0, 0.0f);
+            if constexpr (MODE == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
         }
         return;
     }
@@ -758,17 +772,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
         if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
         if (tid < kWave) {
             write_nothing<DISTILL>(a, n, at);
-            finish_token(a, n, 0.0, 0.0f);
+            finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
         }
         return;
     }
     // the list first: its scores' addresses wait for it under the row's loads
     Listed e;
     double part = 0.0;
+    uint32_t tokens = 0;
     if (tid < kWave) {
         load_ids(a, n, e);
         load_values(a, a.teacher, n, e);
-        part = token_part(a, n, at);
+        tokens = counted_tokens(a);
+        part = token_part(a, n, at, tokens);
     }
     // vectors k of all lanes are beyond the row from some k on: nothing is done for them
     u32x4 v[K];
@@ -872,7 +888,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
         store_others<BF16>(dx + (size_t)i * kPer, f, listed(k));
     }
     if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(coef * exp2_fast((xt - base) * a.c));
-    if (tid < kWave) finish_token(a, n, part, o.loss);
+    if (tid < kWave) finish_token(a, n, part, o.loss, tokens);
 }
 
 // ---------------------------------------------------------------------------
@@ -1048,7 +1064,7 @@ template <bool BF16>
 hipError_t distill(const ListedArgs& a, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T, nv = a.V / Elem<BF16>::kPer;
     hipError_t e = hipSuccess;
-    if (a.mask) {  // the tokens' weight needs their number
+    if (a.counted) {  // the tokens' weight needs their number
         PolicyArgs p{};
         p.shape = a.shape;
         p.o.reduction = a.reduction;

@@ -86,6 +86,7 @@ struct ListedArgs {
     uint32_t* row_count;
     double* partial;  // [kPolicyBlocks][2]
     int32_t sums;     // SUM_...
+    bool counted;     // a launch before counts the tokens
     // split rows
     int32_t parts, per;
     Div31 by_parts;
@@ -94,7 +95,8 @@ struct ListedArgs {
     uint32_t* row_ticket;  // NULL: a second launch joins the parts
 };
 
-constexpr int kDistillSums = 2;  // weighted and plain divergence
+constexpr int64_t kCountedHere = 1024;  // most tokens that each row counts for itself
+constexpr int kDistillSums = 2;         // weighted and plain divergence
 
 hipError_t launch_listed_logprobs(const ListedArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_listed_logprobs_backward(const ListedArgs& a, bool bf16, hipStream_t s);
