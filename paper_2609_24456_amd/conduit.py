@@ -774,23 +774,27 @@ def _listed_ids(ids):
     return _listed_ptr(ids, (torch.int32,), "ids", ids)
 
 
-def _listed_values(t, name, ids):
+def _listed_values(t, name, ids, i):
+    """conduit_rows of values beside the choices' numbers `ids`, whose conduit_rows `i` is."""
     r = _listed_ptr(t, _VALUES, name, ids)
-    if t.shape[-1] != ids.shape[-1]:
+    if r.width != i.width:
         raise ValueError(f"{name} must have the shape of ids, {tuple(ids.shape)}, got {tuple(t.shape)}")
     return r
 
 
 def _listed_tokens(ids, *args):
     """_token_ptrs of per-token tensors of which any may be None; they are shaped like `ids` without its last dimension."""
-    some = next((i for i in range(0, len(args), 3) if args[i] is not None), None)
-    if some is None:
-        B, T = ids.shape[:-1] if ids.dim() == 3 else (1, ids.shape[0])
-        return (B, T, T) + (None,) * (len(args) // 3)
-    if isinstance(args[some], torch.Tensor) and args[some].shape != ids.shape[:-1]:
-        raise ValueError(f"{args[some + 2]} must have shape {tuple(ids.shape[:-1])}, got {tuple(args[some].shape)}")
-    got = _token_ptrs(*args[some:])
-    return got[:3] + (None,) * (some // 3) + got[3:]
+    some = 0
+    while some < len(args) and args[some] is None:
+        some += 3
+    shape = ids.shape
+    B, T = (shape[0], shape[1]) if len(shape) == 3 else (1, shape[0])
+    if some == len(args):
+        return (B, T, T) + (None,) * (some // 3)
+    got = _token_ptrs(*args[some:]) if some else _token_ptrs(*args)
+    if got[0] != B or got[1] != T or args[some].dim() != len(shape) - 1:
+        raise ValueError(f"{args[some + 2]} must have shape {tuple(shape[:-1])}, got {tuple(args[some].shape)}")
+    return got[:3] + (None,) * (some // 3) + got[3:] if some else got
 
 
 def _listed_bytes(entry, logits, K):
@@ -810,7 +814,8 @@ def conduit_token_alternatives(logits, ids, logps, tokens=None, logp=None, lse=N
     """The K most probable choices of every token of logits [B, T, V] into ids and logps [B, T, K], and with tokens what
     conduit_token_logprobs gives."""
     f = torch.float32
-    i, lps = _listed_ids(ids), _listed_values(logps, "logps", ids)
+    i = _listed_ids(ids)
+    lps = _listed_values(logps, "logps", ids, i)
     B, T, step, tok, lp, ls, en, mk = _listed_tokens(ids, tokens, torch.int32, "tokens", logp, f, "logp", lse, f, "lse",
                                                      entropy, f, "entropy", mask, _U8, "mask")
     x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
@@ -828,7 +833,8 @@ def conduit_listed_logprobs(logits, ids, logps, rest=None, lse=None, mask=None, 
                             stream=None):
     """Log-probabilities of the choices ids [B, T, K] under logits [B, T, V], and of all others together (rest)."""
     f = torch.float32
-    i, lps = _listed_ids(ids), _listed_values(logps, "logps", ids)
+    i = _listed_ids(ids)
+    lps = _listed_values(logps, "logps", ids, i)
     B, T, step, rs, ls, mk = _listed_tokens(ids, rest, f, "rest", lse, f, "lse", mask, _U8, "mask")
     x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
     ws, wp, wn = _workspace(workspace, lambda: listed_logprobs_workspace(logits, ids.shape[-1]), stream)
@@ -840,7 +846,8 @@ def conduit_listed_logprobs_backward(logits, ids, lse, dlogps, dlogits, rest=Non
                                      stream=None):
     """The gradient of conduit_listed_logprobs's logits, into dlogits (the logits themselves: in place)."""
     f = torch.float32
-    i, g = _listed_ids(ids), _listed_values(dlogps, "dlogps", ids)
+    i = _listed_ids(ids)
+    g = _listed_values(dlogps, "dlogps", ids, i)
     B, T, step, ls, rs, h, mk = _listed_tokens(ids, lse, f, "lse", rest, f, "rest", drest, f, "drest", mask, _U8, "mask")
     x, dx = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids), _listed_ptr(dlogits, _FLOAT_ROWS, "dlogits", ids)
     _check(lib().conduit_listed_logprobs_backward(C.byref(x), B, T, step, C.byref(i), mk, temperature, ls, rs, C.byref(g), h,
@@ -868,7 +875,8 @@ def conduit_distill_loss(opts, logits, ids, teacher, loss, stats, dlogits=None, 
     """The divergence of logits [B, T, V] from a teacher's values at the choices ids [B, T, K]: per token, stats
     (DISTILL_STATS), and the gradient dlogits (the logits themselves: in place; None: no gradient)."""
     f = torch.float32
-    i, y = _listed_ids(ids), _listed_values(teacher, "teacher", ids)
+    i = _listed_ids(ids)
+    y = _listed_values(teacher, "teacher", ids, i)
     B, T, step, ls, w, mk = _listed_tokens(ids, loss, f, "loss", weight, f, "weight", mask, _U8, "mask")
     x = _listed_ptr(logits, _FLOAT_ROWS, "logits", ids)
     dx = None if dlogits is None else C.byref(_listed_ptr(dlogits, _FLOAT_ROWS, "dlogits", ids))
