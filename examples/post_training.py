@@ -11,7 +11,8 @@ parameter of each sequence) and the output projection.  An iteration
   5. hands the sequences' new priorities back (ReplayBuffer.update).
 
 With --logits the same through logits that a model returned (conduit_policy_loss_logits), and with --preference a
-step of the preference loss over pairs of the batch's sequences.
+step of the preference loss over pairs of the batch's sequences.  With --distill the start's scores are kept as a few
+choices a position (conduit_token_alternatives), and the gradient back towards them is taken (conduit_distill_loss).
 
 Position t predicts token t + 1, so what is scored are the columns [:, 1:] of the delivered arrays against the hidden
 states [:, :-1]: views, nothing is copied.
@@ -101,6 +102,24 @@ def preference_step(batch, logits, ref_logp):
     return stats, grad
 
 
+def teacher_choices(batch, logits, choices):
+    """What is kept of a teacher: its best choices of every position and their log-probabilities."""
+    shape = tuple(batch.tokens[:, 1:].shape) + (choices,)
+    ids, logps = torch.empty(shape, dtype=torch.int32, device="cuda"), torch.empty(shape, device="cuda")
+    cd.conduit_token_alternatives(logits[:, :-1], ids, logps, mask=batch.mask[:, 1:])
+    return ids, logps
+
+
+def distill_step(batch, logits, ids, logps, opts):
+    """The divergence from a teacher's choices, and its gradient in the logits' place; how likely the student finds the
+    teacher's choices, and all others together."""
+    view, mask = logits[:, :-1], batch.mask[:, 1:]
+    scores, rest, loss, stats = torch.empty_like(logps), per_token(batch), per_token(batch), torch.empty(3, device="cuda")
+    cd.conduit_listed_logprobs(view, ids, scores, rest=rest, mask=mask)
+    cd.conduit_distill_loss(opts, view, ids, logps, loss, stats, dlogits=view, mask=mask)
+    return stats, scores, rest, logits
+
+
 def main(argv=None):
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     p.add_argument("--sequences", type=int, default=16)
@@ -111,6 +130,8 @@ def main(argv=None):
     p.add_argument("--lr", type=float, default=0.003, help="step, relative to each parameter's norm")
     p.add_argument("--logits", action="store_true", help="also the loss from logits")
     p.add_argument("--preference", action="store_true", help="also the preference loss")
+    p.add_argument("--distill", action="store_true", help="also the divergence from the start's best choices")
+    p.add_argument("--choices", type=int, default=16, help="choices a position that --distill keeps")
     a = p.parse_args(argv)
     n, T, V, H = a.sequences, a.max_len, a.vocab, a.hidden
     buf = record(4 * n, T, V, seed=0)
@@ -130,6 +151,9 @@ def main(argv=None):
     cd.conduit_head_logprobs(hidden[:, :-1], weight, batch.tokens[:, 1:], ref, mask=batch.mask[:, 1:],
                              workspace=workspaces[0])
     batch.old[:, 1:].copy_(ref)
+    scores = lambda: (hidden.float().reshape(-1, H) @ weight.float().t()).reshape(n, T, V).to(torch.bfloat16)  # noqa: E731
+    if a.distill:
+        kept = teacher_choices(batch, scores(), a.choices)
     losses = []
     for step in range(a.steps):
         stats = policy_step(batch, hidden, weight, ref, opts, a.lr, workspaces)
@@ -138,8 +162,12 @@ def main(argv=None):
         print(f"step {step}: " + "  ".join(f"{k} {v:.4g}" for k, v in named.items()), flush=True)
     buf.update(idx, (batch.adv.abs().sum(1) * 1000).to(torch.int32) + 1)
     out = {"losses": losses}
+    if a.distill:
+        stats = distill_step(batch, scores(), *kept, cd.distill_opts(rest=True))[0]
+        out["distill"] = stats.tolist()
+        print("distill: " + "  ".join(f"{k} {v:.4g}" for k, v in zip(cd.DISTILL_STATS, out["distill"])), flush=True)
     if a.logits or a.preference:
-        logits = (hidden.float().reshape(-1, H) @ weight.float().t()).reshape(n, T, V).to(torch.bfloat16)
+        logits = scores()
     if a.preference:
         stats, grad = preference_step(batch, logits, ref)
         out["preference"] = stats.tolist()
