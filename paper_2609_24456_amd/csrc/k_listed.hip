@@ -28,9 +28,11 @@ namespace conduit {
 
 namespace {
 
-enum ListedMode { SCORES, DISTILL };
+enum ListedMode { SCORES, DISTILL, DIVERGENCE };  // (DIVERGENCE: distillation without the gradient)
 
 constexpr int kListedThreads = 256;
+constexpr int kShortElems = 8;                        // elements a lane of a short row
+constexpr int64_t kShortRow = kShortElems * kWave;
 
 // ---------------------------------------------------------------------------
 // sums over the choices that are not listed
@@ -468,17 +470,21 @@ __global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// short rows: a wavefront each, E elements a lane
+// short rows: a wavefront each, up to E elements a lane
 // ---------------------------------------------------------------------------
-template <bool BF16, int MODE, int E>
-__global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
+// The list's part of a row bounds it, not the row (fp32, K = 8 of 300, distillation:
+// 65,536 rows 82 us; 244 rows of 257, 43% of them live: 8.0, of which a launch is 2.3).
+// The loss's workgroups are few, since each draws a ticket; a large batch has them of
+// 1,024 (65,536 rows of 18: 103 to 77 us).
+template <bool BF16, int MODE, int NT>
+__global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
     using T = typename Elem<BF16>::T;
-    constexpr int kRows = kListedThreads / kWave;
+    constexpr int kRows = NT / kWave, E = kShortElems;
     static_assert(E <= 32, "a word of bits a lane");
     __shared__ uint32_t s_bits[kRows][kWave];
-    __shared__ double s_sum[kDistillSums * kRows];
+    __shared__ double s_sum[kDistillSums][kRows];
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
-    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T), V = (uint32_t)a.V;
     uint32_t* bits = s_bits[w];
     double sums[kDistillSums] = {0.0, 0.0};
     const uint32_t tokens = MODE == DISTILL ? counted_tokens(a) : 0;
@@ -489,16 +495,16 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
         if (a.mask && !a.mask[at]) {
             write_nothing<MODE>(a, n, at);
             if (MODE == DISTILL && a.has_dx) {
-                for (uint32_t j = l; j < (uint32_t)a.V; j += kWave) dx[j] = Elem<BF16>::round(0.0f);
+                for (uint32_t j = l; j < V; j += kWave) dx[j] = Elem<BF16>::round(0.0f);
             }
             continue;
         }
-        float v[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = l + i * kWave < a.V ? Elem<BF16>::one(x[l + i * kWave]) : kNone;
         Listed e;
         load_ids(a, n, e);
         if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
+        float v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = l + i * kWave < V ? Elem<BF16>::one(x[l + i * kWave]) : kNone;
         check_ids<MODE == DISTILL>(a, e, true);
         load_scores<BF16>(x, e);
         wave_fence();  // (the last row's bits are read)
@@ -526,11 +532,12 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
             sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
             sums[1] += (double)o.loss;
             if (a.has_dx) {
+                const bool none = o.coef == 0.0f;  // whatever the scores are
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const uint32_t j = l + i * kWave;
-                    if (j < a.V && !(marked >> i & 1))
-                        dx[j] = Elem<BF16>::round(o.coef == 0.0f ? 0.0f : o.coef * exp2_fast((v[i] - o.base) * a.c));
+                    if (j < V && !(marked >> i & 1))
+                        dx[j] = Elem<BF16>::round(none ? 0.0f : o.coef * exp2_fast((v[i] - o.base) * a.c));
                 }
 #pragma unroll
                 for (int i = 0; i < kLists; ++i)
@@ -540,18 +547,13 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_short(ListedArgs a) {
     }
     if constexpr (MODE == DISTILL) {
         if (l == 0) {
-            s_sum[w] = sums[0];
-            s_sum[kRows + w] = sums[1];
+            s_sum[0][w] = sums[0];
+            s_sum[1][w] = sums[1];
         }
         __syncthreads();
         if (threadIdx.x >= kWave) return;
-        double v[kDistillSums] = {0.0, 0.0};
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            v[0] += s_sum[i];
-            v[1] += s_sum[kRows + i];
-        }
-        finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1], tokens);
+        const double v0 = lanes_sum<kRows>(s_sum[0][l % kRows]), v1 = lanes_sum<kRows>(s_sum[1][l % kRows]);
+        finish_distill(a, blockIdx.x, gridDim.x, v0, v1, tokens);
     }
 }
 
@@ -727,7 +729,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// distillation of rows that fit the registers of WAVES wavefronts, K vectors a lane
+// rows that fit the registers of WAVES wavefronts, K vectors a lane
 // ---------------------------------------------------------------------------
 // A row crosses memory once in each direction.  HBM bounds it where the rows are
 // wide or fp32 (4,088 rows of 32,001 fp32, 37% of them live: 147 us, 4.9 TB/s, a
@@ -739,7 +741,11 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
 // wavefront 91 us, on four 166-235; 10,001 x 8,192 on two 90, on four 109; 50,001 x
 // 2,048 on eight 110, on sixteen 137; fp32, with half the work in a vector, is
 // better on sixteen of 8 vectors: 32,001 x 4,088 masked 147, on eight of 16 156).
-// The list is loaded ahead of the row and its scores behind it.
+// The list is loaded ahead of the row and its scores behind it.  Up to 1,024 vectors
+// the scores alone go this way too: a row's steps hide under those of three others
+// (65,536 rows of 2,100 bf16, K = 5: 79 us, a workgroup a row 327), and rows from 513
+// choices on are better loaded in vectors (2,000 bf16: 70, by elements 198; distilled
+// 194 against 608).
 constexpr int kRowVectors = 16 * 1024;  // of a workgroup of 1,024
 
 template <int WAVES>
@@ -748,8 +754,8 @@ __device__ __forceinline__ void row_sync() {
     else __syncthreads();
 }
 
-template <bool BF16, int WAVES, int K>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_rows(ListedArgs a) {
+template <bool BF16, int MODE, int WAVES, int K>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_rows(ListedArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
@@ -760,32 +766,29 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
     __shared__ uint32_t s_tail[kRows];
     __shared__ Mass s_mass[WAVES];
     __shared__ ListedRow s_row;
+    static_assert(MODE == DISTILL || WAVES == 1);
+    constexpr int LIST = MODE == SCORES ? SCORES : DISTILL;
     const uint32_t w = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0;
     const uint32_t n = block_number() * kRows + w, tid = threadIdx.x % NT;
     if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
+    T* dx = MODE == DISTILL ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
     const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
     if (a.mask && !a.mask[at]) {
-        for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
-        if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
+        if constexpr (MODE == DISTILL) {
+            for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
+        }
         if (tid < kWave) {
-            write_nothing<DISTILL>(a, n, at);
-            finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
+            write_nothing<LIST>(a, n, at);
+            if constexpr (LIST == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
         }
         return;
     }
     // the list first: its scores' addresses wait for it under the row's loads
-    Listed e;
-    double part = 0.0;
-    uint32_t tokens = 0;
-    if (tid < kWave) {
-        load_ids(a, n, e);
-        load_values(a, a.teacher, n, e);
-        tokens = counted_tokens(a);
-        part = token_part(a, n, at, tokens);
-    }
+    RowList r{};
+    if (tid < kWave) load_list<LIST>(a, n, at, true, r);
     // vectors k of all lanes are beyond the row from some k on: nothing is done for them
     u32x4 v[K];
 #pragma unroll
@@ -795,26 +798,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
         if (k * NT < nv && i < nv) v[k] = load16(x + (size_t)i * kPer);
     }
     float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
-    if (tid < kWave) {
-        check_ids<true>(a, e, true);
-        load_scores<BF16>(x, e);
-    }
+    if (tid < kWave) load_scores<BF16>(x, r.e);
 #pragma unroll
     for (int i = 0; i < kWords; ++i) s_bits[w][tid][i] = 0;
     if (tid == 0) s_tail[w] = 0;
     row_sync<WAVES>();
-    Teacher t{};
     if (tid < kWave) {
-        const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+        r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
             const uint32_t i = id / kPer, j = id % kPer, at_bit = i / NT * kPer + j;
             *word = i < nv ? &s_bits[w][i % NT][at_bit / 32] : &s_tail[w];
             *bit = 1u << (i < nv ? at_bit % 32 : j);
             return true;
         });
-        if (twice) find_first<false>(e, a.K);
+        if (r.twice) find_first<false>(r.e, a.K);
     }
     row_sync<WAVES>();
-    if (tid < kWave) t = teacher_row(a, e);
+    if (LIST == DISTILL && tid < kWave) r.t = teacher_row(a, r.e);
     uint32_t bits[kWords], any = 0;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) any |= bits[i] = s_bits[w][tid][i];
@@ -855,17 +854,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
         __syncthreads();
         others = join_mass<WAVES>(s_mass[lane_id() % WAVES], a.c);
     }
+    if constexpr (MODE == SCORES) {
+        write_scores(a, n, at, r.e, others);
+        return;
+    }
     ListedRow o{};
     if (tid < kWave) {
-        o = distill_row(a, e, others, row_mass(e, others, a.c), t, (float)(part * a.scale));
+        o = distill_row(a, r.e, others, row_mass(r.e, others, a.c), r.t, (float)(r.part * a.scale));
         if (tid == 0) {
             if constexpr (WAVES > 1) s_row = o;
             a.loss[at] = o.loss;
         }
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
-            if (e.first[i]) dx[e.id[i]] = E::round(listed_gradient(a, o, e.x[i], e.y[i]));
+            if (MODE == DISTILL && r.e.first[i]) dx[r.e.id[i]] = E::round(listed_gradient(a, o, r.e.x[i], r.e.y[i]));
     }
+    if constexpr (MODE == DIVERGENCE) return finish_token(a, n, r.part, o.loss, r.tokens);
     if constexpr (WAVES > 1) {
         __syncthreads();
         o.coef = s_row.coef;
@@ -888,7 +892,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_distill_ro
         store_others<BF16>(dx + (size_t)i * kPer, f, listed(k));
     }
     if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(coef * exp2_fast((xt - base) * a.c));
-    if (tid < kWave) finish_token(a, n, part, o.loss, tokens);
+    if (tid < kWave) finish_token(a, n, r.part, o.loss, r.tokens);
 }
 
 // ---------------------------------------------------------------------------
@@ -1031,13 +1035,17 @@ hipError_t launch_gradient(const ListedArgs& a, hipStream_t s) {
 // ---------------------------------------------------------------------------
 template <bool BF16, int MODE>
 hipError_t launch_short(const ListedArgs& a, hipStream_t s) {
-    constexpr int kRows = kListedThreads / kWave;
-    const int64_t want = (a.shape.B * a.shape.T + kRows - 1) / kRows;
-    // (the loss's workgroups each leave a sum)
-    const dim3 grid = MODE == DISTILL ? dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)) : grid_of(want, kListedThreads);
-    if (a.V <= 8 * kWave) hipLaunchKernelGGL((k_listed_short<BF16, MODE, 8>), grid, dim3(kListedThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_listed_short<BF16, MODE, kShortRow / kWave>), grid, dim3(kListedThreads), 0, s, a);
-    return hipGetLastError();
+    const int64_t rows = a.shape.B * a.shape.T;
+    auto go = [&](auto threads) {
+        constexpr int NT = decltype(threads)::value, kRows = NT / kWave;
+        const int64_t want = (rows + kRows - 1) / kRows;
+        // (the loss's workgroups each leave a sum)
+        const dim3 grid = MODE == DISTILL ? dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)) : grid_of(want, NT);
+        hipLaunchKernelGGL((k_listed_short<BF16, MODE, NT>), grid, dim3(NT), 0, s, a);
+        return hipGetLastError();
+    };
+    if (MODE == DISTILL && rows > 8 * kPolicyBlocks) return go(std::integral_constant<int, 1024>{});
+    return go(std::integral_constant<int, kListedThreads>{});
 }
 
 template <bool BF16, int MODE>
@@ -1055,9 +1063,19 @@ hipError_t launch_scan(const ListedArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <bool BF16, int MODE, int WAVES, int K>
+hipError_t launch_rows(const ListedArgs& a, hipStream_t s) {
+    constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = WAVES * kRows * kWave;
+    hipLaunchKernelGGL((k_listed_rows<BF16, MODE, WAVES, K>), grid_of((a.shape.B * a.shape.T + kRows - 1) / kRows, kThreads),
+                       dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 template <bool BF16>
 hipError_t listed_logprobs(const ListedArgs& a, hipStream_t s) {
-    return a.V <= kShortRow ? launch_short<BF16, SCORES>(a, s) : launch_scan<BF16, SCORES>(a, s);
+    if (a.V <= kShortRow) return launch_short<BF16, SCORES>(a, s);
+    if (a.V / Elem<BF16>::kPer <= 16 * kWave) return launch_rows<BF16, SCORES, 1, 16>(a, s);
+    return launch_scan<BF16, SCORES>(a, s);
 }
 
 template <bool BF16>
@@ -1075,21 +1093,19 @@ hipError_t distill(const ListedArgs& a, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (a.V <= kShortRow) return launch_short<BF16, DISTILL>(a, s);
-    if (a.parts > 1 || !a.has_dx) {
+    if (a.parts == 1 && nv <= 16 * kWave) {
+        e = a.has_dx ? launch_rows<BF16, DISTILL, 1, 16>(a, s) : launch_rows<BF16, DIVERGENCE, 1, 16>(a, s);
+    } else if (a.parts > 1 || !a.has_dx) {
         e = launch_scan<BF16, DISTILL>(a, s);
         if (e == hipSuccess && a.has_dx) e = launch_gradient<BF16, true>(a, s);
+    } else if (nv <= 16 * 2 * kWave) {
+        e = launch_rows<BF16, DISTILL, 2, 16>(a, s);
+    } else if (nv <= 16 * 4 * kWave) {
+        e = launch_rows<BF16, DISTILL, 4, 16>(a, s);
+    } else if (nv <= 16 * 8 * kWave) {
+        e = launch_rows<BF16, DISTILL, BF16 ? 8 : 16, BF16 ? 16 : 8>(a, s);
     } else {
-        auto go = [&](auto waves, auto vectors) {
-            constexpr int WAVES = decltype(waves)::value, K = decltype(vectors)::value;
-            constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = WAVES * kRows * kWave;
-            hipLaunchKernelGGL((k_distill_rows<BF16, WAVES, K>), grid_of((rows + kRows - 1) / kRows, kThreads), dim3(kThreads), 0, s, a);
-            return hipGetLastError();
-        };
-        if (nv <= 16 * 64) e = go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
-        else if (nv <= 16 * 128) e = go(std::integral_constant<int, 2>{}, std::integral_constant<int, 16>{});
-        else if (nv <= 16 * 256) e = go(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
-        else if (nv <= 16 * 512) e = go(std::integral_constant<int, BF16 ? 8 : 16>{}, std::integral_constant<int, BF16 ? 16 : 8>{});
-        else e = go(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
+        e = launch_rows<BF16, DISTILL, 16, 16>(a, s);
     }
     if (e != hipSuccess || a.sums != SUM_LAUNCH) return e;
     const int64_t want = (rows + kSumThreads - 1) / kSumThreads;

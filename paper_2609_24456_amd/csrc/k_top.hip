@@ -35,6 +35,7 @@ constexpr int kGroup = 8;        // vectors a group
 constexpr int kMostCandidates = 512;
 constexpr int kMostGroups = 512;
 constexpr int kShortCandidates = 256;
+constexpr int64_t kShortRow = 2048;  // choices that one wavefront takes
 static_assert(2 * kMostListed <= kMostGroups && kMostListed <= kShortCandidates, "the exact selection fits the lists");
 static_assert(kPartVectors % kGroup == 0, "whole groups");
 

@@ -6,7 +6,6 @@
 namespace conduit {
 
 constexpr int kMostListed = 128;      // choices a token
-constexpr int64_t kShortRow = 2048;   // choices that one wavefront takes
 constexpr int kPartVectors = 32768;   // most vectors of a part of a row: its LDS grows with them
 
 // how a call's rows are split: parts of `per` vectors
