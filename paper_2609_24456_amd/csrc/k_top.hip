@@ -35,7 +35,8 @@ constexpr int kGroup = 8;        // vectors a group
 constexpr int kMostCandidates = 512;
 constexpr int kMostGroups = 512;
 constexpr int kShortCandidates = 256;
-constexpr int64_t kShortRow = 2048;  // choices that one wavefront takes
+constexpr int kShortElems = 8;       // elements a lane of a short row
+constexpr int64_t kShortRow = kShortElems * kWave;
 static_assert(2 * kMostListed <= kMostGroups && kMostListed <= kShortCandidates, "the exact selection fits the lists");
 static_assert(kPartVectors % kGroup == 0, "whole groups");
 
@@ -49,9 +50,28 @@ __device__ __forceinline__ float key_score(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t choice_key(float x, uint32_t j) { return (uint64_t)order_key(x) << 32 | (uint32_t)~j; }
 
-// A bound that at least `need` of a wavefront's N keys a lane reach, and at most
-// `spare` more unless keys are equal: bit by bit from the highest in which the keys
-// differ.  (need: at most 64 N.)
+// A bound that at least `need` keys reach, and at most `spare` more unless keys are
+// equal: bit by bit from the highest in which the largest key `hi` and the least `lo`
+// differ.  reach(t): how many reach t (uniform); at least `need` reach lo.
+template <typename Reach>
+__device__ __forceinline__ uint32_t bound_between(uint32_t hi, uint32_t lo, uint32_t need, uint32_t spare, Reach reach) {
+    if (hi == lo) return lo;
+    int bit = 31 - __builtin_clz(hi ^ lo);
+    uint32_t t = hi >> bit >> 1 << bit << 1;  // what they have in common: all reach it
+    for (; bit >= 0; --bit) {
+        const uint32_t trial = t | 1u << bit, n = reach(trial);
+        if (n < need) continue;
+        t = trial;
+        if (n <= need + spare) break;
+    }
+    return t;
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    return __builtin_amdgcn_readfirstlane(lanes_reduce<kWave>(x, [](uint32_t p, uint32_t q) { return p > q ? p : q; }));
+}
+
+// of a wavefront's N keys a lane (need: at most 64 N)
 template <int N>
 __device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[N], uint32_t need, uint32_t spare) {
     uint32_t hi = key[0], lo = key[0];
@@ -60,22 +80,12 @@ __device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[N], uint32_t
         hi = key[i] > hi ? key[i] : hi;
         lo = key[i] < lo ? key[i] : lo;
     }
-    hi = __builtin_amdgcn_readfirstlane(lanes_reduce<kWave>(hi, [](uint32_t p, uint32_t q) { return p > q ? p : q; }));
-    lo = __builtin_amdgcn_readfirstlane(lanes_reduce<kWave>(lo, [](uint32_t p, uint32_t q) { return p < q ? p : q; }));
-    uint32_t t = lo;
-    if (hi == lo) return t;
-    int bit = 31 - __builtin_clz(hi ^ lo);
-    t = hi >> bit >> 1 << bit << 1;  // what they have in common: all reach it
-    for (; bit >= 0; --bit) {
-        const uint32_t trial = t | 1u << bit;
+    return bound_between(wave_max(hi), ~wave_max(~lo), need, spare, [&](uint32_t least) {
         uint32_t n = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) n += __builtin_popcountll(__ballot(key[i] >= trial));
-        if (n < need) continue;
-        t = trial;
-        if (n <= need + spare) break;
-    }
-    return t;
+        for (int i = 0; i < N; ++i) n += __builtin_popcountll(__ballot(key[i] >= least));
+        return n;
+    });
 }
 
 // a row whose log-normaliser is no number (a NaN or +infinity among its scores) has no ranking
@@ -149,6 +159,81 @@ __device__ __forceinline__ bool counts(const TopArgs& a, int64_t at, bool flags,
 }
 
 // ---------------------------------------------------------------------------
+// a lane's statistics over tiles of vectors
+// ---------------------------------------------------------------------------
+// The sums go by d' = c x - B in one rounding, with B the rounded c max x: what it
+// is off by is a factor of the whole sum, which stat() takes out.  (That leaves 7.5
+// cycles of a fp32 element and 9.5 of a bf16 one, 4 of them of the exponential, of
+// 9.5 and 11.5.)  A choice at -infinity would give 0 times -infinity: a tile whose
+// weighted sum is no number is summed again with the exponents held, and so are
+// those after it.  Where c x is beyond the floats' range, or nearly, they are as in
+// softmax_dev.h.
+struct TileStat {
+    Stat st = no_stat();
+    float B = 0.0f;
+    bool held = false, far = false;  // uniform
+
+    // as Stat has them, which go by c (x - max x)
+    __device__ __forceinline__ Stat stat(float c) const {
+        if (far || st.m == kNone) return st;
+        const float d = fmaf(st.m, c, -B), e = exp2_fast(-d);
+        return Stat{st.m, st.s * e, fmaf(-d, st.s, st.u) * e};
+    }
+
+    template <bool BF16, bool HELD, int STRIDE, int N>
+    __device__ __forceinline__ void sum(const u32x4 (&v)[N], float c, uint32_t left) {
+        using E = Elem<BF16>;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (HELD && k * STRIDE >= left) continue;  // nothing but padding
+            float f[E::kPer];
+            E::unpack(again(v[k]), f);
+#pragma unroll
+            for (int j = 0; j < E::kPer; ++j) {
+                const float d = fmaf(f[j], c, -B), e = exp2_fast(d);
+                st.s += e;
+                st.u = fmaf(e, HELD ? fmaxf(d, kFloor) : d, st.u);
+            }
+        }
+    }
+
+    // top: the largest of the lane's vectors, STRIDE apart; left: the row's vectors from the tile on
+    template <bool BF16, int STRIDE, int N>
+    __device__ __forceinline__ void add_tile(const u32x4 (&v)[N], float top, float c, uint32_t left) {
+        const float b = top * c;
+        if (!far && __ballot(top > st.m && !(fabsf(b) < 0x1p100f)) != 0) {
+            st = stat(c);
+            far = true;
+        }
+        if (far) {
+            raise(st, top, c);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                float f[Elem<BF16>::kPer];
+                Elem<BF16>::unpack(again(v[k]), f);
+                conduit::add(st, f, c);
+            }
+            return;
+        }
+        if (top > st.m) {
+            const float d = fminf(B - b, 0.0f), e = exp2_fast(d);
+            st.u = fmaf(st.s, fmaxf(d, kFloor), st.u) * e;
+            st.s *= e;
+            st.m = top;
+            B = b;
+        }
+        if (left >= N * STRIDE && !held) {
+            const Stat before = st;
+            sum<BF16, false, STRIDE>(v, c, left);
+            if (__ballot(!(st.u == st.u)) == 0) return;
+            st = before;
+            held = true;
+        }
+        sum<BF16, true, STRIDE>(v, c, left);
+    }
+};
+
+// ---------------------------------------------------------------------------
 // the shortest rows: LANES lanes each, up to kFewElems elements a lane
 // ---------------------------------------------------------------------------
 // Every choice is ranked against all others, with the row's keys in LDS.  Latency
@@ -208,9 +293,10 @@ __global__ __launch_bounds__(kTopThreads) void k_top_few(TopArgs a) {
 // ---------------------------------------------------------------------------
 // short rows: a wavefront each, E elements a lane
 // ---------------------------------------------------------------------------
-template <bool BF16, int E>
+template <bool BF16>
 __global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
     using T = typename Elem<BF16>::T;
+    constexpr int E = kShortElems;
     __shared__ uint64_t s_cand[kTopThreads / kWave][kShortCandidates];
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
     const uint32_t n = block_number() * (kTopThreads / kWave) + w;
@@ -270,79 +356,141 @@ __global__ __launch_bounds__(kTopThreads) void k_top_short(TopArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// a lane's statistics over tiles of vectors
+// rows of up to kWaveElems elements a lane, in vectors: a wavefront each
 // ---------------------------------------------------------------------------
-// The sums go by d' = c x - B in one rounding, with B the rounded c max x: what it
-// is off by is a factor of the whole sum, which stat() takes out.  (That leaves 7.5
-// cycles of a fp32 element and 9.5 of a bf16 one, 4 of them of the exponential, of
-// 9.5 and 11.5.)  A choice at -infinity would give 0 times -infinity: a tile whose
-// weighted sum is no number is summed again with the exponents held, and so are
-// those after it.  Where c x is beyond the floats' range, or nearly, they are as in
-// softmax_dev.h.
-struct TileStat {
-    Stat st = no_stat();
-    float B = 0.0f;
-    bool held = false, far = false;  // uniform
+// Four pieces a lane give the bound; where few pieces hold the largest scores, so
+// that too many reach it, it is found among the scores themselves.  Equal ones beyond
+// the list's room are counted from the row's start.  The counting bounds it, not the
+// memory (16,384 rows, K = 20: 1,000 bf16 25 us, by elements in the order of the
+// lanes 43; 2,100 fp32 41, a workgroup a row 70; 4,000 bf16 47 against 73; K = 100
+// of 4,000 fp32 100).
+constexpr int kWaveElems = 64;  // a lane
+constexpr uint32_t kLeastKey = 0x007fffffu;  // -infinity's
 
-    // as Stat has them, which go by c (x - max x)
-    __device__ __forceinline__ Stat stat(float c) const {
-        if (far || st.m == kNone) return st;
-        const float d = fmaf(st.m, c, -B), e = exp2_fast(-d);
-        return Stat{st.m, st.s * e, fmaf(-d, st.s, st.u) * e};
+template <bool BF16>
+__global__ __launch_bounds__(kTopThreads) void k_top_wave(TopArgs a) {
+    using E = Elem<BF16>;
+    using T = typename E::T;
+    constexpr int kPer = E::kPer, kWaveVectors = kWaveElems / kPer;
+    __shared__ uint64_t s_cand[kTopThreads / kWave][kShortCandidates];
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
+    const uint32_t n = block_number() * (kTopThreads / kWave) + w;
+    if (n >= (uint32_t)(a.shape.B * a.shape.T)) return;
+    uint64_t* cand = s_cand[w];
+    const int64_t at = a.shape.at(n);
+    int32_t tok;
+    if (!counts(a, at, l == 0, &tok)) return write_nothing<kWave>(a, n, at, l);
+    const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
+    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer, K = (uint32_t)a.K;
+    u32x4 v[kWaveVectors];
+#pragma unroll
+    for (int k = 0; k < kWaveVectors; ++k) {
+        v[k] = no_vector<BF16>();
+        if (k * kWave < nv && k * kWave + l < nv) v[k] = load16(x + (size_t)(k * kWave + l) * kPer);
     }
-
-    template <bool BF16, bool HELD, int N>
-    __device__ __forceinline__ void sum(const u32x4 (&v)[N], float c, uint32_t left) {
-        using E = Elem<BF16>;
+    const float xt = l < tail ? E::one(x[nv * kPer + l]) : kNone, xa = E::one(x[tok]);
+    // four pieces of the row a lane, by their largest
+    float top[4] = {xt, kNone, kNone, kNone}, most = kNone;
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            if (HELD && k * kTopThreads >= left) continue;  // nothing but padding
-            float f[E::kPer];
-            E::unpack(again(v[k]), f);
+    for (int k = 0; k < kWaveVectors; ++k) {
+        if (k * kWave < nv) {
+            float f[kPer];
+            E::unpack(v[k], f);
+            const float mine = top_of(f, kNone);
+            top[k % 4] = fmaxf(top[k % 4], mine);
+            most = fmaxf(most, mine);
+        }
+    }
+    TileStat ts;
+    ts.add_tile<BF16, kWave>(v, most, a.c, nv);
+    Stat st = ts.stat(a.c);
+    {
+        const float f[1] = {xt};
+        accumulate(st, f, a.c);
+    }
+    st = join_lanes<kWave>(st, a.c);
+    const RowValues r = row_values(st, xa, a.c, a.inv_t, a.inv_lo);
+    if (l == 0) write_values(a, at, r.logp, r.lse, r.entropy);
+    if (no_ranking(st)) return fill_row<kWave>(a, TopRow(a, n), l, 0, -1, __builtin_nanf(""));
+    // f(k, j, score) for the lane's elements, j of vector k (and j = 0 of the tail, k = kWaveVectors); all lanes together
+    auto each = [&](auto f) {
 #pragma unroll
-            for (int j = 0; j < E::kPer; ++j) {
-                const float d = fmaf(f[j], c, -B), e = exp2_fast(d);
-                st.s += e;
-                st.u = fmaf(e, HELD ? fmaxf(d, kFloor) : d, st.u);
+        for (int k = 0; k < kWaveVectors; ++k) {
+            if (k * kWave < nv) {
+                float e[kPer];
+                E::unpack(again(v[k]), e);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) f(k, j, e[j]);
             }
         }
-    }
-
-    // top: the largest of the lane's vectors; left: the row's vectors from the tile on
-    template <bool BF16, int N>
-    __device__ __forceinline__ void add_tile(const u32x4 (&v)[N], float top, float c, uint32_t left) {
-        const float b = top * c;
-        if (!far && __ballot(top > st.m && !(fabsf(b) < 0x1p100f)) != 0) {
-            st = stat(c);
-            far = true;
-        }
-        if (far) {
-            raise(st, top, c);
+        f(kWaveVectors, 0, xt);
+    };
+    auto reach = [&](uint32_t least) {  // (padding is at -infinity, which all reach)
+        const float score = key_score(least > kLeastKey ? least : kLeastKey);
+        uint32_t some = 0;
+        each([&](int, int, float e) { some += __builtin_popcountll(__ballot(e >= score)); });
+        return some;
+    };
+    uint32_t key[4];
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                float f[Elem<BF16>::kPer];
-                Elem<BF16>::unpack(again(v[k]), f);
-                conduit::add(st, f, c);
-            }
-            return;
-        }
-        if (top > st.m) {
-            const float d = fminf(B - b, 0.0f), e = exp2_fast(d);
-            st.u = fmaf(st.s, fmaxf(d, kFloor), st.u) * e;
-            st.s *= e;
-            st.m = top;
-            B = b;
-        }
-        if (left >= N * kTopThreads && !held) {
-            const Stat before = st;
-            sum<BF16, false>(v, c, left);
-            if (__ballot(!(st.u == st.u)) == 0) return;
-            st = before;
-            held = true;
-        }
-        sum<BF16, true>(v, c, left);
+    for (int i = 0; i < 4; ++i) key[i] = order_key(top[i]);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(order_key(st.m));
+    uint32_t bound = key_bound(key, K, K / 4), ties = ~0u;  // (all that reach the bound)
+#pragma unroll 1
+    for (int round = 0;; ++round) {
+        if (round > 0) bound = bound_between(hi, kLeastKey, K, round == 1 ? K / 4 : 0, reach);
+        // (ranking takes the square of their number)
+        if (reach(bound) <= (round == 0 ? K + K / 2 + 32 : kShortCandidates)) break;
+        if (round < 2) continue;
+        if (bound < kLeastKey) bound = kLeastKey;
+        ties = K - reach(bound + 1);  // (the K-th largest is it)
+        break;
     }
-};
+    const float score = key_score(bound > kLeastKey ? bound : kLeastKey);
+    auto place = [&](int k, int j) { return k < kWaveVectors ? (k * kWave + l) * kPer + j : nv * kPer + l; };
+    uint32_t found = 0;
+    auto take = [&](bool mine, uint32_t number, float e) {
+        const uint64_t taken = __ballot(mine);
+        if (mine) cand[found + __builtin_popcountll(taken & below_lane())] = choice_key(e, number);
+        found += __builtin_popcountll(taken);
+    };
+    if (ties == ~0u) {
+        each([&](int k, int j, float e) {
+            const bool mine = e >= score && (k < kWaveVectors ? k * kWave + l < nv : l < tail);
+            if (__ballot(mine) != 0) take(mine, place(k, j), e);
+        });
+    } else {
+        // of the equal ones the first: by vector, then lane, then element
+        uint32_t equal = 0;
+#pragma unroll 1
+        for (uint32_t k = 0; k * kWave < nv + kWave; ++k) {
+            const bool last = k * kWave >= nv;  // the tail
+            const uint32_t base = last ? nv * kPer + l : (k * kWave + l) * kPer, many = last ? 1 : kPer;
+            const bool here = last ? l < tail : k * kWave + l < nv;
+            float e[kPer];
+            uint32_t same = 0;
+            for (uint32_t j = 0; j < kPer; ++j) {
+                e[j] = here && j < many ? E::one(x[base + j]) : kNone;
+                same += here && j < many && e[j] == score;
+            }
+            uint32_t upto = same;
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) {
+                const uint32_t o = __shfl_up(upto, d, kWave);
+                upto += l >= (uint32_t)d ? o : 0;
+            }
+            uint32_t before = equal + upto - same;
+            for (uint32_t j = 0; j < kPer; ++j) {
+                const bool valid = here && j < many, is = valid && e[j] == score;
+                take(valid && (e[j] > score || (is && before < ties)), base + j, e[j]);
+                before += is;
+            }
+            equal += __shfl(upto, kWave - 1, kWave);
+        }
+    }
+    wave_fence();
+    write_ranked<kWave>(a, n, cand, found, r, l);
+}
 
 // ---------------------------------------------------------------------------
 // longer rows, or parts of them: a workgroup each
@@ -510,7 +658,7 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
             const float group = lanes_reduce<kGroup>(mine, [](float p, float q) { return fmaxf(p, q); });
             if (tid % kGroup == 0 && i < hi) s_group[(i - lo) / kGroup] = group;
         }
-        ts.add_tile<BF16>(v, top, a.c, hi - base);
+        ts.add_tile<BF16, kTopThreads>(v, top, a.c, hi - base);
     }
     Stat st = ts.stat(a.c);
     {
@@ -626,13 +774,13 @@ hipError_t alternatives(const TopArgs& a, hipStream_t s) {
     if (a.V <= 4 * kFewElems) return few(std::integral_constant<int, 4>{});
     if (a.V <= 8 * kFewElems) return few(std::integral_constant<int, 8>{});
     if (a.V <= 16 * kFewElems) return few(std::integral_constant<int, 16>{});
-    if (a.V <= 8 * kWave) {
-        hipLaunchKernelGGL((k_top_short<BF16, 8>), grid_of((rows + kRows - 1) / kRows, kTopThreads), dim3(kTopThreads), 0, s, a);
+    const dim3 each = grid_of((rows + kRows - 1) / kRows, kTopThreads);
+    if (a.V <= kShortRow) {
+        hipLaunchKernelGGL((k_top_short<BF16>), each, dim3(kTopThreads), 0, s, a);
         return hipGetLastError();
     }
-    if (a.V <= kShortRow) {
-        hipLaunchKernelGGL((k_top_short<BF16, kShortRow / kWave>), grid_of((rows + kRows - 1) / kRows, kTopThreads), dim3(kTopThreads),
-                           0, s, a);
+    if (a.V / Elem<BF16>::kPer * Elem<BF16>::kPer <= kWaveElems * kWave) {
+        hipLaunchKernelGGL((k_top_wave<BF16>), each, dim3(kTopThreads), 0, s, a);
         return hipGetLastError();
     }
     // one launch takes fewer than 2^31 parts (the division's range)

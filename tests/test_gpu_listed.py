@@ -69,7 +69,7 @@ def _step(dtype, want):
 
 # one choice, rows of a wavefront (8 and 32 elements a lane) and their edges, of a workgroup with and without elements
 # after the last vector, wide enough to be split where there are few of them
-WIDTHS = [1, 2, 3, 16, 17, 18, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 2047, 2048, 2049, 4097, 5001, 16385, 33001]
+WIDTHS = [1, 2, 3, 16, 17, 18, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 2047, 2048, 2049, 4095, 4097, 4103, 5001, 16385, 33001]
 
 
 def _shape(V):
@@ -129,7 +129,7 @@ def _hard_rows(rng, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("V", [3, 18, 130, 300, 513, 2048, 2049, 5000, 40000])
+@pytest.mark.parametrize("V", [3, 18, 130, 300, 513, 700, 2048, 2049, 4103, 5000, 40000])
 @pytest.mark.parametrize("rows", ["few", "many"])
 def test_alternatives_of_equal_and_ordered_scores(rows, V, dtype):
     rng = np.random.default_rng(V)
