@@ -796,7 +796,7 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * +inf has no ranking: its numbers are -1 and its log-probabilities NaN.  tokens
  * may be NULL (then logp must be); logp, lse and entropy may be.  ids and logps
  * are apart from each other and from every other array of the call.
- * Rows of up to 2,048 choices share a wavefront or take one, wider ones a workgroup; fewer
+ * Rows of up to 4,096 choices share a wavefront or take one, wider ones a workgroup; fewer
  * rows than the GPU has compute units, and rows of more than 2^18 bf16 (2^17
  * float) choices, are split into parts that the row's last workgroup joins, or,
  * for more than 512 rows, a second launch.

@@ -233,13 +233,13 @@ __device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others,
 #pragma unroll
     for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.x[i] : kNone);
     top = wave_top(fmaxf(top, others.m));
-    r.weight = top != kNone;
-    r.top = r.weight ? top : 0.0f;
+    r.top = top != kNone ? top : 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.x[i] - r.top) * c) : 0.0f;
     const float d = others.m == top ? 0.0f : (others.m - top) * c, k = exp2_fast(d);
     const float S = fmaf(others.s, k, uniform(lanes_sum<kWave>(sum)));
+    r.weight = !(S == 0.0f);  // (a row of NaN alone has no largest score either)
     r.log2_s = r.weight ? log2_fast(S) : 0.0f;
     r.some = !(others.s == 0.0f);
     r.share = r.weight ? k / S : 0.0f;

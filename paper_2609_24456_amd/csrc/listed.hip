@@ -36,13 +36,16 @@ conduit_status check_apart(const conduit_rows* o, const char* what, std::initial
     return CONDUIT_OK;
 }
 
-// per-token outputs apart from rows that are read
-conduit_status check_outputs_apart(std::initializer_list<const void*> outs, std::initializer_list<const conduit_rows*> rows, int64_t B,
-                                   int64_t T, int64_t stride) {
-    const int64_t each = 4 * ((B - 1) * stride + T);
-    for (const void* o : outs)
+// per-token outputs apart from rows that are read and from the mask
+conduit_status check_outputs_apart(std::initializer_list<const void*> outs, std::initializer_list<const conduit_rows*> rows,
+                                   const uint8_t* mask, int64_t B, int64_t T, int64_t stride) {
+    const int64_t each = (B - 1) * stride + T;
+    for (const void* o : outs) {
+        if (!o) continue;
         for (const conduit_rows* r : rows)
-            if (o && r && !apart(o, each, r->data, rows_extent(r, B, T))) return bad("an output overlaps an input");
+            if (!apart(o, 4 * each, r->data, rows_extent(r, B, T))) return bad("an output overlaps an input");
+        if (mask && !apart(o, 4 * each, mask, each)) return bad("an output overlaps the mask");
+    }
     return CONDUIT_OK;
 }
 
@@ -146,7 +149,7 @@ conduit_status conduit_token_alternatives(const conduit_rows* logits, int64_t B,
     CONDUIT_TRY(check_outputs({logp, lse, entropy}, {}, tokens, B, T, stride));
     CONDUIT_TRY(check_apart(ids, "ids", {logits, logps}, {tokens, logp, lse, entropy}, mask, B, T, stride));
     CONDUIT_TRY(check_apart(logps, "logps", {logits}, {tokens, logp, lse, entropy}, mask, B, T, stride));
-    CONDUIT_TRY(check_outputs_apart({logp, lse, entropy}, {logits}, B, T, stride));
+    CONDUIT_TRY(check_outputs_apart({logp, lse, entropy}, {logits}, mask, B, T, stride));
     const ListedLayout l = top_layout(B, T, logits, ids->width);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));
     uint32_t* err = nullptr;
@@ -182,7 +185,7 @@ conduit_status conduit_listed_logprobs(const conduit_rows* logits, int64_t B, in
     if (B == 0 || T == 0) return CONDUIT_OK;
     CONDUIT_TRY(check_outputs({rest, lse}, {}, nullptr, B, T, stride));
     CONDUIT_TRY(check_apart(logps, "logps", {logits, ids}, {rest, lse}, mask, B, T, stride));
-    CONDUIT_TRY(check_outputs_apart({rest, lse}, {logits, ids}, B, T, stride));
+    CONDUIT_TRY(check_outputs_apart({rest, lse}, {logits, ids}, mask, B, T, stride));
     const ListedLayout l = listed_layout(B, T, logits, false);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));
     uint32_t* err = nullptr;
@@ -259,8 +262,15 @@ conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const cond
         if (!loss) return bad("loss must not be NULL");
         CONDUIT_TRY(check_outputs({loss}, {weight}, nullptr, B, T, stride));
         if (loss == weight) return bad("loss must be apart from the inputs");  // (the statistics are summed up after it is written)
-        CONDUIT_TRY(check_outputs_apart({loss}, {logits, ids, teacher}, B, T, stride));
+        CONDUIT_TRY(check_outputs_apart({loss}, {logits, ids, teacher}, mask, B, T, stride));
         if (dlogits) CONDUIT_TRY(check_apart(dlogits, "dlogits", {ids, teacher}, {weight, loss}, mask, B, T, stride));
+        // (the statistics are three values on their own)
+        const int64_t each = (B - 1) * stride + T;
+        for (const conduit_rows* r : {logits, ids, teacher, dlogits})
+            if (r && !apart(stats, 12, r->data, rows_extent(r, B, T))) return bad("stats must be apart from the call's other arrays");
+        for (const void* t : {static_cast<const void*>(weight), static_cast<const void*>(loss)})
+            if (t && !apart(stats, 12, t, 4 * each)) return bad("stats must be apart from the call's other arrays");
+        if (mask && !apart(stats, 12, mask, each)) return bad("stats must be apart from the call's other arrays");
     }
     const ListedLayout l = distill_layout(B, T, logits, dlogits != nullptr);
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));

@@ -240,6 +240,32 @@ def test_listed_logprobs_and_gradient(V, dtype):
             _close(host(dx.float()), w, 4 * tol * size / tau + _step(dtype, w))
 
 
+def test_rows_with_a_nan_or_infinity():
+    """NaN in every output of the row, whether the list holds it or not or the row is nothing else; the others as ever."""
+    rng = np.random.default_rng(8)
+    for V, B, T in ((18, 1, 9), (300, 1, 9), (2100, 1, 9), (9000, 1, 300), (40000, 1, 9)):
+        for dtype in (F32, BF16):
+            x, _ = _logits(rng, B, T, V, dtype)
+            ids, y = _teacher(rng, x.double().cpu().numpy(), 5)
+            inside, outside = int(ids[0, 1, 2]), next(j for j in range(V) if j not in ids[0, 2])
+            x[0, 1, inside], x[0, 2, outside], x[0, 3, int(ids[0, 3, 0])], x[0, 4], x[0, 5, V - 1] = NAN, NAN, float("inf"), NAN, float("inf")
+            bad = np.zeros((B, T), bool)
+            bad[0, 1:6] = True
+            out = [torch.zeros(s, device="cuda") for s in ((B, T, 5), (B, T), (B, T))]
+            cd.conduit_listed_logprobs(x, _gpu(ids), out[0], rest=out[1], lse=out[2])
+            assert (np.isnan(host(out[0])).all(-1) == bad).all() and (np.isnan(host(out[0])).any(-1) == bad).all()
+            assert (np.isnan(host(out[2])) == bad).all()
+            dx = torch.zeros_like(x)
+            cd.conduit_listed_logprobs_backward(x, _gpu(ids), out[2], _gpu(y), dx)
+            assert (np.isnan(host(dx.float())).all(-1) == bad).all() and (np.isnan(host(dx.float())).any(-1) == bad).all()
+            for opts in FORMS:
+                dx.zero_()
+                loss, stats = _distill(cd.distill_opts(**opts), x, ids, y, dx)
+                assert (np.isnan(loss) == bad).all() and np.isnan(stats[:2]).all() and stats[2] == B * T
+                assert (np.isnan(host(dx.float())).all(-1) == bad).all() and (np.isnan(host(dx.float())).any(-1) == bad).all()
+                assert (np.isnan(_distill(cd.distill_opts(**opts), x, ids, y)[0]) == bad).all()
+
+
 def test_rest_far_below_the_listed():
     """A rest of 1e-8 to 1e-30 of the row keeps its digits, in every kernel; nothing left is -infinity."""
     for V in (40, 700, 5000, 40000):

@@ -185,7 +185,7 @@ ON = 4 * (T * K * B - 1)  # the last element of a listed array
     (dict(logp=at(6, 2)), "aligned"), (dict(lps=vals(at(2))), "ids must be apart"), (dict(lps=vals(at(2, ON))), "ids must be apart"),
     (dict(i=ids(at(1, 8))), "ids must be apart"), (dict(lps=vals(at(1))), "logps must be apart"),
     (dict(i=ids(at(5))), "ids must be apart"), (dict(lps=vals(at(7))), "logps must be apart"), (dict(lse=at(1)), "overlaps an input"),
-    (dict(mask=at(2, ON)), "ids must be apart"), (dict(mask=at(3)), "logps must be apart"),
+    (dict(mask=at(2, ON)), "ids must be apart"), (dict(mask=at(3)), "logps must be apart"), (dict(mask=at(8)), "overlaps the mask"),
 ])
 def test_alternatives_refusals(kw, msg):
     assert alternatives(**kw) == cd.EINVAL and msg in cd.last_error(), cd.last_error()
@@ -195,6 +195,7 @@ def test_alternatives_refusals(kw, msg):
     (dict(lps=vals(**LAP)), "rows must not overlap"), (dict(lse=at(6)), "overlap"), (dict(lps=vals(at(2, ON))), "logps must be apart"),
     (dict(lps=vals(at(1))), "logps must be apart"), (dict(lps=vals(at(6))), "logps must be apart"), (dict(rest=at(2)), "overlaps an input"),
     (dict(lse=at(1, 12)), "overlaps an input"), (dict(rest=at(6, 1)), "aligned"), (dict(mask=at(3)), "logps must be apart"),
+    (dict(mask=at(7, 40)), "overlaps the mask"),
 ])
 def test_listed_refusals(kw, msg):
     assert listed(**kw) == cd.EINVAL and msg in cd.last_error(), cd.last_error()
@@ -216,6 +217,9 @@ def test_listed_gradient_refusals(kw, msg):
     (dict(loss=at(6, 4)), "overlaps an input"), (dict(loss=at(3)), "overlaps an input"), (dict(loss=at(1)), "overlaps an input"),
     (dict(dx=rows(at(4), dtype=cd.BF16)), "dtype and width"), (dict(dx=rows(at(1, 4))), "apart from them"),
     (dict(dx=rows(at(7))), "dlogits must be apart"), (dict(dx=rows(at(2))), "dlogits must be apart"), (dict(mask=at(4)), "dlogits must be apart"),
+    (dict(stats=at(1, 4)), "stats must be apart"), (dict(stats=at(2)), "stats must be apart"), (dict(stats=at(3)), "stats must be apart"),
+    (dict(stats=at(4)), "stats must be apart"), (dict(stats=at(6)), "stats must be apart"), (dict(stats=at(7)), "stats must be apart"),
+    (dict(mask=at(8)), "stats must be apart"), (dict(mask=at(7)), "overlaps the mask"),
     (dict(reduction=3), "reduction"), (dict(reduction=-1), "reduction"), (dict(scale=float("inf")), "scale"),
     (dict(scale=float("nan")), "scale"), (dict(teacher_temperature=0.0), "temperature"), (dict(teacher_temperature=float("nan")), "temperature"),
     (dict(rest=1, teacher_temperature=2.0), "teacher_temperature 1"),
