@@ -645,7 +645,9 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
         return;
     }
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const T* vx = x + row.head;  // the vectors
+    const uint32_t nv = row.count;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
     RowList r{};
     if (tid < kWave) load_list<MODE>(a, n, at, part == 0, r);  // (ahead of the row's loads)
@@ -654,7 +656,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
 #pragma unroll
         for (int k = 0; k < kScanVectors; ++k) {
             const uint32_t i = base + k * kListedThreads + tid;
-            v[k] = i < hi ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
+            v[k] = i < hi ? load16(vx + (size_t)i * kPer) : no_vector<BF16>();
         }
     };
     load(lo);
@@ -665,7 +667,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     if (tid < kWave) {
         load_scores<BF16>(x, r.e);
         r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
-            const uint32_t i = id / kPer, j = id % kPer;
+            uint32_t i, j;
+            row.find(id, &i, &j);
             if (i >= nv) {
                 *word = &s_tail;
                 *bit = 1u << j;
@@ -681,8 +684,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     }
     __syncthreads();
     Mass others = no_mass();
-    if (part == 0 && tid < tail) {
-        const float f[1] = {s_tail >> tid & 1 ? kNone : E::one(x[nv * kPer + tid])};
+    if (part == 0 && tid < row.beside()) {
+        const float f[1] = {s_tail >> tid & 1 ? kNone : E::one(x[row.beside_at(tid)])};
         accumulate_mass(others, f, a.c);
     }
     for (uint32_t tile = 0; tile < tiles; ++tile) {
@@ -774,11 +777,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     T* dx = MODE == DISTILL ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
-    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const T* vx = x + row.head;  // the vectors
+    T* vdx = MODE == DISTILL ? dx + row.head : nullptr;
+    const uint32_t nv = row.count, tail = row.beside();
     if (a.mask && !a.mask[at]) {
         if constexpr (MODE == DISTILL) {
-            for (uint32_t i = tid; i < nv; i += NT) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
-            if (tid < tail) dx[nv * kPer + tid] = E::round(0.0f);
+            for (uint32_t i = tid; i < nv; i += NT) store16(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (tid < tail) dx[row.beside_at(tid)] = E::round(0.0f);
         }
         if (tid < kWave) {
             write_nothing<LIST>(a, n, at);
@@ -795,9 +801,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     for (int k = 0; k < K; ++k) {
         const uint32_t i = k * NT + tid;
         v[k] = no_vector<BF16>();
-        if (k * NT < nv && i < nv) v[k] = load16(x + (size_t)i * kPer);
+        if (k * NT < nv && i < nv) v[k] = load16(vx + (size_t)i * kPer);
     }
-    float xt = tid < tail ? E::one(x[nv * kPer + tid]) : kNone;
+    float xt = tid < tail ? E::one(x[row.beside_at(tid)]) : kNone;
     if (tid < kWave) load_scores<BF16>(x, r.e);
 #pragma unroll
     for (int i = 0; i < kWords; ++i) s_bits[w][tid][i] = 0;
@@ -805,7 +811,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     row_sync<WAVES>();
     if (tid < kWave) {
         r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
-            const uint32_t i = id / kPer, j = id % kPer, at_bit = i / NT * kPer + j;
+            uint32_t i, j;
+            row.find(id, &i, &j);
+            const uint32_t at_bit = i / NT * kPer + j;
             *word = i < nv ? &s_bits[w][i % NT][at_bit / 32] : &s_tail[w];
             *bit = 1u << (i < nv ? at_bit % 32 : j);
             return true;
@@ -889,9 +897,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         E::unpack(again(v[k]), f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) f[j] = coef * exp2_fast((f[j] - base) * a.c);
-        store_others<BF16>(dx + (size_t)i * kPer, f, listed(k));
+        store_others<BF16>(vdx + (size_t)i * kPer, f, listed(k));
     }
-    if (tid < tail && !listed_tail) dx[nv * kPer + tid] = E::round(coef * exp2_fast((xt - base) * a.c));
+    if (tid < tail && !listed_tail) dx[row.beside_at(tid)] = E::round(coef * exp2_fast((xt - base) * a.c));
     if (tid < kWave) finish_token(a, n, r.part, o.loss, r.tokens);
 }
 
@@ -918,9 +926,12 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
-    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const T* vx = x + row.head;  // the vectors
+    T* vdx = dx + row.head;
+    const uint32_t nv = row.count;
     const uint32_t first = part * kWindow, base = first + lane;
-    const bool mine = part == 0 && lane < tail;  // the elements after the last vector
+    const bool mine = part == 0 && lane < row.beside();  // the elements beside the vectors
     bool weight = !a.mask || a.mask[at];
     float lse = 0.0f;
     if constexpr (!SPLIT) {
@@ -931,18 +942,18 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
 #pragma unroll
         for (int k = 0; k < kGradK; ++k) {
             const uint32_t i = base + k * kWave;
-            if (i < nv) store16(dx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (i < nv) store16(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
         }
-        if (mine) dx[nv * kPer + lane] = E::round(0.0f);
+        if (mine) dx[row.beside_at(lane)] = E::round(0.0f);
         return;
     }
     u32x4 v[kGradK];
 #pragma unroll
     for (int k = 0; k < kGradK; ++k) {
         const uint32_t i = base + k * kWave;
-        v[k] = i < nv ? load16(x + (size_t)i * kPer) : u32x4{0, 0, 0, 0};
+        v[k] = i < nv ? load16(vx + (size_t)i * kPer) : u32x4{0, 0, 0, 0};
     }
-    const float xt = mine ? E::one(x[nv * kPer + lane]) : 0.0f;
+    const float xt = mine ? E::one(x[row.beside_at(lane)]) : 0.0f;
     Listed e;
     load_ids(a, n, e);
     load_values(a, SPLIT ? a.teacher : a.g, n, e);
@@ -967,13 +978,15 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     wave_fence();
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
-        const uint32_t k = (uint32_t)e.id[i] / kPer;
+        uint32_t k, j;
+        row.find((uint32_t)e.id[i], &k, &j);
         e.on[i] = e.on[i] && (k < nv ? k - first < kWindow : part == 0);
         e.first[i] = e.on[i];
     }
     load_scores<BF16>(x, e);
     const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
-        const uint32_t k = id / kPer, j = id % kPer;
+        uint32_t k, j;
+        row.find(id, &k, &j);
         *word = k < nv ? bits + k % kWave : bits + kWave;
         *bit = 1u << (k < nv ? (k - first) / kWave * kPer + j : j);
         return true;
@@ -1006,9 +1019,9 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
         E::unpack(v[k], f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) f[j] = other(f[j]);
-        if (i < nv) store_others<BF16>(dx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
+        if (i < nv) store_others<BF16>(vdx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
     }
-    if (mine && !(marked_tail >> lane & 1)) dx[nv * kPer + lane] = E::round(other(xt));
+    if (mine && !(marked_tail >> lane & 1)) dx[row.beside_at(lane)] = E::round(other(xt));
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         if (!e.first[i]) continue;

@@ -632,11 +632,13 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
         return;
     }
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    const uint32_t V = (uint32_t)a.V, nv = V / kPer, tail = V % kPer;
+    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const T* vx = x + row.head;  // the vectors
+    const uint32_t nv = row.count;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
     const uint32_t groups = (hi - lo + kGroup - 1) / kGroup;
-    const bool last_one = part == 0 && tid < tail;  // the elements after the last vector
-    const float xt = last_one ? E::one(x[nv * kPer + tid]) : kNone;
+    const bool last_one = part == 0 && tid < row.beside();  // the elements beside the vectors
+    const float xt = last_one ? E::one(x[row.beside_at(tid)]) : kNone;
     const float xa = E::one(x[tok]);
     TileStat ts;
     for (uint32_t base = lo; base < hi; base += kTopThreads * kTopVectors) {
@@ -644,7 +646,7 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
 #pragma unroll
         for (int k = 0; k < kTopVectors; ++k) {
             const uint32_t i = base + k * kTopThreads + tid;
-            v[k] = i < hi ? load16(x + (size_t)i * kPer) : no_vector<BF16>();
+            v[k] = i < hi ? load16(vx + (size_t)i * kPer) : no_vector<BF16>();
         }
         float top = kNone;
 #pragma unroll
@@ -682,11 +684,11 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
                 const uint32_t i = lo + s.list[q] * kGroup + tid % kGroup;
                 if (i >= hi) continue;
                 float e[kPer];
-                E::unpack(load16(x + (size_t)i * kPer), e);
+                E::unpack(load16(vx + (size_t)i * kPer), e);
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) f(choice_key(e[j], i * kPer + j));
+                for (int j = 0; j < kPer; ++j) f(choice_key(e[j], row.head + i * kPer + j));
             }
-            if (last_one) f(choice_key(xt, nv * kPer + tid));
+            if (last_one) f(choice_key(xt, row.beside_at(tid)));
         };
         if (listed <= kMostGroups) {
             each([&](uint64_t key) {

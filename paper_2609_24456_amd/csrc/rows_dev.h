@@ -101,6 +101,29 @@ __device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
     return join_lanes<WAVES>(r, c);
 }
 
+// A row of V elements as vectors from a 4-byte boundary on, and up to kPer elements
+// beside them.  16-byte accesses that start at an odd bf16 element take longer (864 of
+// 2,048 rows of 50,001 with their gradients 74 us, from the boundary on 57; the best 64
+// of 1,488 rows of 127,999: 106 and 83); rows of odd widths start at one every other time.
+template <bool BF16>
+struct RowVectors {
+    static constexpr int kPer = Elem<BF16>::kPer;
+    uint32_t head;   // elements before the vectors: 0 or 1
+    uint32_t count;  // vectors
+    uint32_t rest;   // elements after them
+    __device__ __forceinline__ RowVectors(const void* x, uint32_t V)
+        : head(BF16 ? (uint32_t)(reinterpret_cast<uintptr_t>(x) / 2 % 2) : 0), count((V - head) / kPer), rest((V - head) % kPer) {}
+    // the elements beside the vectors: those after them, then the one before
+    __device__ __forceinline__ uint32_t beside() const { return rest + head; }
+    __device__ __forceinline__ uint32_t beside_at(uint32_t t) const { return t < rest ? head + count * kPer + t : 0; }
+    // where element `id` is: vector i (count: beside them) and its place j
+    __device__ __forceinline__ void find(uint32_t id, uint32_t* i, uint32_t* j) const {
+        const uint32_t k = id - head;
+        *i = id < head ? count : k / kPer;
+        *j = id < head ? rest : k % kPer;
+    }
+};
+
 // a vector of scores at -inf
 template <bool BF16>
 __device__ __forceinline__ u32x4 no_vector() {
