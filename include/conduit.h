@@ -796,10 +796,10 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * +inf has no ranking: its numbers are -1 and its log-probabilities NaN.  tokens
  * may be NULL (then logp must be); logp, lse and entropy may be.  ids and logps
  * are apart from each other and from every other array of the call.
- * Rows of up to 4,096 choices share a wavefront or take one, wider ones a workgroup; fewer
- * rows than the GPU has compute units, and rows of more than 2^18 bf16 (2^17
- * float) choices, are split into parts that the row's last workgroup joins, or,
- * for more than 512 rows, a second launch.
+ * Rows of up to 4,096 choices share a wavefront or take one, wider ones a
+ * workgroup; fewer rows than the GPU has compute units, and rows of more than 2^18
+ * bf16 (2^17 float) choices, are split into parts that the row's last workgroup
+ * joins, or, for more than 512 rows, a second launch.
  * Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_token_alternatives_workspace(int64_t B, int64_t T, const conduit_rows* logits, int64_t K,
@@ -885,10 +885,10 @@ void conduit_distill_opts_default(conduit_distill_opts* opts);
  * gradient is 0, and so is that of a token of weight 0.  A batch without counted
  * tokens gives zeros.
  * Rows of up to 256 KB cross memory once in each direction.  Up to five launches:
- * the count of the tokens (with a mask, of more than 1,024 tokens or for the mean
- * over sequences), the rows, where these are split the join of more than 512 and
- * the gradient, and the sums of a batch of more than 512 rows wider than 512.
- * Errors: EINVAL, EDEVICE, ESTATE.
+ * the count of the tokens (with a mask, of more than 1,024 tokens, 2,048 if it is
+ * in one piece, or for the mean over sequences), the rows, where these are split
+ * the join of more than 512 and the gradient, and the sums of a batch of more than
+ * 512 rows wider than 512.  Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_distill_loss_workspace(int64_t B, int64_t T, const conduit_rows* logits, int64_t K, uint64_t* bytes);
 conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const conduit_rows* logits, int64_t B, int64_t T,

@@ -370,14 +370,39 @@ __device__ __forceinline__ void write_nothing(const ListedArgs& a, uint32_t n, i
 // ---------------------------------------------------------------------------
 // the loss's sums
 // ---------------------------------------------------------------------------
-// Tokens that count, by a wavefront: of a small batch from the mask itself (16 loads of
-// a byte a lane at most, under the row's; a launch for it takes 4.5 us), else from the
-// launch before.
+// Tokens that count, by a wavefront: of a small batch from the mask itself, else from
+// the launch before.  A mask in one piece goes by in 16 bytes a lane, one round of
+// loads for 2,048 tokens, any other by bytes.  (The launch takes 4.6 us and a gap; 2,048
+// rows of 50,001 bf16 59.8 us with the counting, 57 without; of 8,192 tokens it costs
+// the rows more than the launch.)
 __device__ __forceinline__ uint32_t counted_tokens(const ListedArgs& a) {
     const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
     if (!a.mask) return n_rows;
     if (a.counted) return (uint32_t)a.head->counts;
     uint32_t tokens = 0;
+    if (a.flat_mask) {
+        constexpr uint32_t kAtOnce = 2;
+        const uint32_t whole = n_rows / 16, rest = n_rows % 16;
+        uint32_t mine = lane_id() < rest && a.mask[whole * 16 + lane_id()] ? 1 : 0;
+#pragma unroll 1
+        for (uint32_t base = 0; base < whole; base += kAtOnce * kWave) {
+            u32x4 m[kAtOnce];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t k = base + i * kWave + lane_id();
+                m[i] = k < whole ? load16(a.mask + (size_t)k * 16) : u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t x = m[i][q];
+                    mine += __builtin_popcount((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);  // bytes that are not 0
+                }
+            }
+        }
+        return __builtin_amdgcn_readfirstlane(lanes_sum<kWave>(mine));
+    }
     for (uint32_t base = 0; base < n_rows; base += 8 * kWave) {
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
@@ -574,14 +599,19 @@ struct RowList {
 
 // what does not wait for the row; check: entries that are no choices are flagged
 template <int MODE>
-__device__ __forceinline__ void load_list(const ListedArgs& a, uint32_t n, int64_t at, bool check, RowList& r) {
+__device__ __forceinline__ void load_list(const ListedArgs& a, uint32_t n, bool check, RowList& r) {
     load_ids(a, n, r.e);
+    if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, r.e);
+    check_ids<MODE == DISTILL>(a, r.e, check);
+}
+
+// the token's weight, behind the row's loads
+template <int MODE>
+__device__ __forceinline__ void load_weight(const ListedArgs& a, uint32_t n, int64_t at, RowList& r) {
     if constexpr (MODE == DISTILL) {
-        load_values(a, a.teacher, n, r.e);
         r.tokens = counted_tokens(a);
         r.part = token_part(a, n, at, r.tokens);
     }
-    check_ids<MODE == DISTILL>(a, r.e, check);
 }
 
 // the row from its others' sum, by one wavefront
@@ -650,7 +680,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     const uint32_t nv = row.count;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
     RowList r{};
-    if (tid < kWave) load_list<MODE>(a, n, at, part == 0, r);  // (ahead of the row's loads)
+    if (tid < kWave) load_list<MODE>(a, n, part == 0, r);  // (ahead of the row's loads)
     u32x4 v[kScanVectors];
     auto load = [&](uint32_t base) {
 #pragma unroll
@@ -666,6 +696,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     __syncthreads();
     if (tid < kWave) {
         load_scores<BF16>(x, r.e);
+        load_weight<MODE>(a, n, at, r);
         r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
             uint32_t i, j;
             row.find(id, &i, &j);
@@ -725,7 +756,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
     const int64_t at = a.shape.at(n);
     if (a.mask && !a.mask[at]) return;
     RowList r{};
-    load_list<MODE>(a, n, at, false, r);
+    load_list<MODE>(a, n, false, r);
+    load_weight<MODE>(a, n, at, r);
     load_scores<BF16>(static_cast<const typename Elem<BF16>::T*>(a.x.data) + a.x.at(n, a.shape), r.e);
     if constexpr (MODE == DISTILL) r.t = teacher_row(a, r.e);
     join_listed<BF16, MODE>(a, n, at, r);
@@ -794,7 +826,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     }
     // the list first: its scores' addresses wait for it under the row's loads
     RowList r{};
-    if (tid < kWave) load_list<LIST>(a, n, at, true, r);
+    if (tid < kWave) load_list<LIST>(a, n, true, r);
     // vectors k of all lanes are beyond the row from some k on: nothing is done for them
     u32x4 v[K];
 #pragma unroll
@@ -804,7 +836,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         if (k * NT < nv && i < nv) v[k] = load16(vx + (size_t)i * kPer);
     }
     float xt = tid < tail ? E::one(x[row.beside_at(tid)]) : kNone;
-    if (tid < kWave) load_scores<BF16>(x, r.e);
+    if (tid < kWave) {
+        load_scores<BF16>(x, r.e);
+        load_weight<LIST>(a, n, at, r);
+    }
 #pragma unroll
     for (int i = 0; i < kWords; ++i) s_bits[w][tid][i] = 0;
     if (tid == 0) s_tail[w] = 0;

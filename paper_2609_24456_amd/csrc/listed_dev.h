@@ -86,6 +86,7 @@ struct ListedArgs {
     double* partial;  // [kPolicyBlocks][2]
     int32_t sums;     // SUM_...
     bool counted;     // a launch before counts the tokens
+    bool flat_mask;   // in one piece, at a multiple of 16 bytes
     // split rows
     int32_t parts, per;
     Div31 by_parts;
@@ -95,6 +96,7 @@ struct ListedArgs {
 };
 
 constexpr int64_t kCountedHere = 1024;  // most tokens that each row counts for itself
+constexpr int64_t kCountedFlat = 2048;  // of a mask in one piece
 constexpr int kDistillSums = 2;         // weighted and plain divergence
 
 hipError_t launch_listed_logprobs(const ListedArgs& a, bool bf16, hipStream_t s);

@@ -408,7 +408,7 @@ def test_distill_from_logits_far_from_zero(V):
 
 
 @pytest.mark.parametrize("B,T,V,dtype", [(1, 530, 70001, F32), (3, 2, 140003, BF16), (2, 300, 9001, BF16), (700, 1, 2049, F32),
-                                         (1, 300, 4096, F32), (1, 300, 8001, F32), (2, 150, 8203, BF16), (1, 300, 16385, F32),
+                                         (1, 300, 4096, F32), (1, 300, 8001, F32), (2, 150, 8203, BF16), (7, 171, 2050, BF16), (4, 512, 700, F32), (1, 2049, 700, F32), (1, 300, 16385, F32),
                                          (1, 300, 20001, BF16), (3, 100, 30003, F32), (1, 300, 50001, BF16), (1, 300, 40005, F32),
                                          (1, 300, 100007, BF16), (1, 520, 131072, BF16)])
 def test_distill_of_many_and_wide_rows(B, T, V, dtype):
