@@ -189,9 +189,9 @@ __device__ __forceinline__ u32x4 without(u32x4 v, uint32_t bits) {
 }
 
 // the elements of a vector whose bits are not set
-template <bool BF16>
+template <bool BF16, bool PAST>
 __device__ __forceinline__ void store_others(typename Elem<BF16>::T* p, const float (&f)[Elem<BF16>::kPer], uint32_t bits) {
-    if (bits == 0) return store16(p, Elem<BF16>::pack(f));
+    if (bits == 0) return put16<PAST>(p, Elem<BF16>::pack(f));
 #pragma unroll
     for (int j = 0; j < Elem<BF16>::kPer; ++j)
         if (!(bits >> j & 1)) p[j] = Elem<BF16>::round(f[j]);
@@ -675,7 +675,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
         return;
     }
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const RowVectors<BF16, 4> row(x, (uint32_t)a.V);
     const T* vx = x + row.head;  // the vectors
     const uint32_t nv = row.count;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;
@@ -789,7 +789,7 @@ __device__ __forceinline__ void row_sync() {
     else __syncthreads();
 }
 
-template <bool BF16, int MODE, int WAVES, int K>
+template <bool BF16, int MODE, int WAVES, int K, bool PAST>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_rows(ListedArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
@@ -798,7 +798,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     constexpr int kWords = K * kPer / 32;
     constexpr int kRows = WAVES == 1 ? 256 / kWave : 1;  // of a workgroup
     __shared__ uint32_t s_bits[kRows][NT][kWords];
-    __shared__ uint32_t s_tail[kRows];
+    __shared__ uint32_t s_beside[kRows][2];
     __shared__ Mass s_mass[WAVES];
     __shared__ ListedRow s_row;
     static_assert(MODE == DISTILL || WAVES == 1);
@@ -809,14 +809,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     T* dx = MODE == DISTILL ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
-    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    using Vectors = RowVectors<BF16, MODE == DISTILL ? 64 : 4>;
+    static_assert(Vectors::kMostBeside <= kWave);
+    const Vectors row(MODE == DISTILL ? dx : x, (uint32_t)a.V);
     const T* vx = x + row.head;  // the vectors
     T* vdx = MODE == DISTILL ? dx + row.head : nullptr;
-    const uint32_t nv = row.count, tail = row.beside();
+    const uint32_t nv = row.count, beside = row.beside();
     if (a.mask && !a.mask[at]) {
         if constexpr (MODE == DISTILL) {
-            for (uint32_t i = tid; i < nv; i += NT) store16(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
-            if (tid < tail) dx[row.beside_at(tid)] = E::round(0.0f);
+            for (uint32_t i = tid; i < nv; i += NT) put16<PAST>(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (tid < beside) dx[row.beside_at(tid)] = E::round(0.0f);
         }
         if (tid < kWave) {
             write_nothing<LIST>(a, n, at);
@@ -835,22 +837,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         v[k] = no_vector<BF16>();
         if (k * NT < nv && i < nv) v[k] = load16(vx + (size_t)i * kPer);
     }
-    float xt = tid < tail ? E::one(x[row.beside_at(tid)]) : kNone;
+    float xt = tid < beside ? E::one(x[row.beside_at(tid)]) : kNone;
     if (tid < kWave) {
         load_scores<BF16>(x, r.e);
         load_weight<LIST>(a, n, at, r);
     }
 #pragma unroll
     for (int i = 0; i < kWords; ++i) s_bits[w][tid][i] = 0;
-    if (tid == 0) s_tail[w] = 0;
+    if (tid < 2) s_beside[w][tid] = 0;
     row_sync<WAVES>();
     if (tid < kWave) {
         r.twice = mark(r.e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
             uint32_t i, j;
             row.find(id, &i, &j);
             const uint32_t at_bit = i / NT * kPer + j;
-            *word = i < nv ? &s_bits[w][i % NT][at_bit / 32] : &s_tail[w];
-            *bit = 1u << (i < nv ? at_bit % 32 : j);
+            *word = i < nv ? &s_bits[w][i % NT][at_bit / 32] : &s_beside[w][j / 32];
+            *bit = 1u << (i < nv ? at_bit : j) % 32;
             return true;
         });
         if (r.twice) find_first<false>(r.e, a.K);
@@ -866,8 +868,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         for (int k = 0; k < K; ++k)
             if (listed(k)) v[k] = without<BF16>(v[k], listed(k));
     }
-    const bool listed_tail = tid < tail && (s_tail[w] >> tid & 1);
-    if (listed_tail) xt = kNone;
+    const bool listed_beside = tid < beside && (s_beside[w][tid / 32] >> tid % 32 & 1);
+    if (listed_beside) xt = kNone;
     Mass others = no_mass();
     {
         float top = xt;
@@ -932,9 +934,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         E::unpack(again(v[k]), f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) f[j] = coef * exp2_fast((f[j] - base) * a.c);
-        store_others<BF16>(vdx + (size_t)i * kPer, f, listed(k));
+        store_others<BF16, PAST>(vdx + (size_t)i * kPer, f, listed(k));
     }
-    if (tid < tail && !listed_tail) dx[row.beside_at(tid)] = E::round(coef * exp2_fast((xt - base) * a.c));
+    if (tid < beside && !listed_beside) dx[row.beside_at(tid)] = E::round(coef * exp2_fast((xt - base) * a.c));
     if (tid < kWave) finish_token(a, n, r.part, o.loss, r.tokens);
 }
 
@@ -945,14 +947,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
 // ---------------------------------------------------------------------------
 constexpr int kGradK = 4;
 
-template <bool BF16, bool SPLIT>
+template <bool BF16, bool SPLIT, bool PAST>
 __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a, uint32_t items, uint32_t per_row, Div31 by_row) {
     using E = Elem<BF16>;
     using T = typename E::T;
     constexpr int kPer = E::kPer;
     constexpr uint32_t kWindow = kGradK * kWave;
     static_assert(kGradK * kPer <= 32, "a word of bits a lane");
-    __shared__ uint32_t s_bits[kListedThreads / kWave][kWave + 1];
+    __shared__ uint32_t s_bits[kListedThreads / kWave][kWave + 2];  // (the last two: beside the vectors)
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
     const uint32_t item = block_number() * (kListedThreads / kWave) + w;
     if (SPLIT && a.sums == SUM_NEXT && item == 0) sum_rows(a);
@@ -961,7 +963,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     const int64_t at = a.shape.at(n);
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
     T* dx = static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape);
-    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const RowVectors<BF16, 64> row(dx, (uint32_t)a.V);
     const T* vx = x + row.head;  // the vectors
     T* vdx = dx + row.head;
     const uint32_t nv = row.count;
@@ -977,7 +979,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
 #pragma unroll
         for (int k = 0; k < kGradK; ++k) {
             const uint32_t i = base + k * kWave;
-            if (i < nv) store16(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
+            if (i < nv) put16<PAST>(vdx + (size_t)i * kPer, u32x4{0, 0, 0, 0});
         }
         if (mine) dx[row.beside_at(lane)] = E::round(0.0f);
         return;
@@ -1009,7 +1011,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     // the listed choices of this part of the row
     uint32_t* bits = s_bits[w];
     bits[lane] = 0;
-    if (lane == 0) bits[kWave] = 0;
+    if (lane < 2) bits[kWave + lane] = 0;
     wave_fence();
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
@@ -1022,13 +1024,13 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
         uint32_t k, j;
         row.find(id, &k, &j);
-        *word = k < nv ? bits + k % kWave : bits + kWave;
-        *bit = 1u << (k < nv ? (k - first) / kWave * kPer + j : j);
+        *word = bits + (k < nv ? k % kWave : kWave + j / 32);
+        *bit = 1u << (k < nv ? (k - first) / kWave * kPer + j : j % 32);
         return true;
     });
     if (twice) find_first<!SPLIT>(e, a.K);
     wave_fence();
-    const uint32_t marked = bits[lane], marked_tail = bits[kWave];
+    const uint32_t marked = bits[lane], marked_beside = bits[kWave + lane / 32] >> lane % 32 & 1;
     auto log_p = [&](float f) {  // as FromLse in k_logits.hip, for what may be far from 0
         return fmaf(f, a.inv_t, fmaf(fmaxf(f, -3.4028235e38f), a.inv_lo, -lse));
     };
@@ -1054,9 +1056,9 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
         E::unpack(v[k], f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) f[j] = other(f[j]);
-        if (i < nv) store_others<BF16>(vdx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
+        if (i < nv) store_others<BF16, PAST>(vdx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
     }
-    if (mine && !(marked_tail >> lane & 1)) dx[row.beside_at(lane)] = E::round(other(xt));
+    if (mine && !marked_beside) dx[row.beside_at(lane)] = E::round(other(xt));
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         if (!e.first[i]) continue;
@@ -1073,8 +1075,13 @@ hipError_t launch_gradient(const ListedArgs& a, hipStream_t s) {
     const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
     const int64_t items = a.shape.B * a.shape.T * per_row;
     if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
-    hipLaunchKernelGGL((k_listed_gradient<BF16, SPLIT>), grid_of((items + kListedThreads / kWave - 1) / (kListedThreads / kWave), kListedThreads),
-                       dim3(kListedThreads), 0, s, a, (uint32_t)items, (uint32_t)per_row, make_div31((uint32_t)per_row));
+    auto go = [&](auto past) {
+        hipLaunchKernelGGL((k_listed_gradient<BF16, SPLIT, decltype(past)::value>),
+                           grid_of((items + kListedThreads / kWave - 1) / (kListedThreads / kWave), kListedThreads), dim3(kListedThreads), 0,
+                           s, a, (uint32_t)items, (uint32_t)per_row, make_div31((uint32_t)per_row));
+    };
+    if (a.past) go(std::true_type{});
+    else go(std::false_type{});
     return hipGetLastError();
 }
 
@@ -1114,8 +1121,9 @@ hipError_t launch_scan(const ListedArgs& a, hipStream_t s) {
 template <bool BF16, int MODE, int WAVES, int K>
 hipError_t launch_rows(const ListedArgs& a, hipStream_t s) {
     constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = WAVES * kRows * kWave;
-    hipLaunchKernelGGL((k_listed_rows<BF16, MODE, WAVES, K>), grid_of((a.shape.B * a.shape.T + kRows - 1) / kRows, kThreads),
-                       dim3(kThreads), 0, s, a);
+    const dim3 grid = grid_of((a.shape.B * a.shape.T + kRows - 1) / kRows, kThreads);
+    if (MODE == DISTILL && a.past) hipLaunchKernelGGL((k_listed_rows<BF16, MODE, WAVES, K, MODE == DISTILL>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_listed_rows<BF16, MODE, WAVES, K, false>), grid, dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

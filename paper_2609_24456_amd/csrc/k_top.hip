@@ -632,7 +632,7 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
         return;
     }
     const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
-    const RowVectors<BF16> row(x, (uint32_t)a.V);
+    const RowVectors<BF16, 4> row(x, (uint32_t)a.V);
     const T* vx = x + row.head;  // the vectors
     const uint32_t nv = row.count;
     const uint32_t lo = part * (uint32_t)a.per < nv ? part * (uint32_t)a.per : nv, hi = lo + a.per < nv ? lo + a.per : nv;

@@ -108,6 +108,13 @@ void common_args(Args& a, const conduit_rows* x, int64_t B, int64_t T, int64_t s
     a.err = err;
 }
 
+// (in bytes that are written, whatever lies between the rows)
+void set_gradient(ListedArgs& a, const conduit_rows* dx) {
+    a.dx = view(dx);
+    a.has_dx = true;
+    a.past = (double)(a.shape.B * a.shape.T) * (double)a.V * elem_size(dx->dtype) > (double)kPastBytes;
+}
+
 template <typename Args>
 void place_parts(Args& a, uint8_t* w, const ListedLayout& o) {
     a.parts = o.split.parts;
@@ -222,8 +229,7 @@ conduit_status conduit_listed_logprobs_backward(const conduit_rows* logits, int6
     a.rest_in = rest;
     a.g = view(dlogps);
     a.h = drest;
-    a.dx = view(dlogits);
-    a.has_dx = true;
+    set_gradient(a, dlogits);
     return launched(launch_listed_logprobs_backward(a, logits->dtype == CONDUIT_BF16, static_cast<hipStream_t>(stream)),
                     "listed logprobs gradient launch");
 }
@@ -289,8 +295,7 @@ conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const cond
     a.weight = weight;
     a.loss = loss;
     a.stats = stats;
-    a.has_dx = dlogits != nullptr;
-    if (dlogits) a.dx = view(dlogits);
+    if (dlogits) set_gradient(a, dlogits);
     uint8_t* w = static_cast<uint8_t*>(workspace);
     a.head = reinterpret_cast<WorkspaceHead*>(w);
     a.row_count = reinterpret_cast<uint32_t*>(w + l.l.row_count);

@@ -5,6 +5,9 @@
 
 namespace conduit {
 
+// Gradients of more bytes are written past the caches: half as much again as the last
+// level holds (256 MB), since up to there a reader finds part of them.
+constexpr int64_t kPastBytes = 384 << 20;
 constexpr int kMostListed = 128;      // choices a token
 constexpr int kPartVectors = 32768;   // most vectors of a part of a row: its LDS grows with them
 
@@ -76,6 +79,7 @@ struct ListedArgs {
     RowsView teacher;
     float q_inv_t;
     bool reverse, with_rest, has_dx;
+    bool past;  // the gradient is written past the caches (rows_dev.h)
     int32_t reduction;
     double scale;
     const float* weight;

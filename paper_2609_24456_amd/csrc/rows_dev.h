@@ -101,28 +101,47 @@ __device__ __forceinline__ Stat join_block(Stat s, Stat* lds, float c) {
     return join_lanes<WAVES>(r, c);
 }
 
-// A row of V elements as vectors from a 4-byte boundary on, and up to kPer elements
-// beside them.  16-byte accesses that start at an odd bf16 element take longer (864 of
-// 2,048 rows of 50,001 with their gradients 74 us, from the boundary on 57; the best 64
-// of 1,488 rows of 127,999: 106 and 83); rows of odd widths start at one every other time.
-template <bool BF16>
+// A row of V elements as vectors from an ALIGN-byte boundary on, and the elements beside
+// them: fewer than ALIGN bytes of them before, fewer than kPer after.
+//   4, to be read: 16-byte accesses that start at an odd bf16 element take longer (the
+// best 64 of 1,488 rows of 127,999: 106 us, from the boundary on 83; rows of odd widths
+// start at one every other time).
+//   64, to be written: see put16.
+template <bool BF16, int ALIGN>
 struct RowVectors {
-    static constexpr int kPer = Elem<BF16>::kPer;
-    uint32_t head;   // elements before the vectors: 0 or 1
+    static constexpr int kPer = Elem<BF16>::kPer, kSize = 16 / kPer;
+    static constexpr int kMostBeside = ALIGN / kSize - 1 + kPer - 1;
+    uint32_t head;   // elements before the vectors
     uint32_t count;  // vectors
     uint32_t rest;   // elements after them
-    __device__ __forceinline__ RowVectors(const void* x, uint32_t V)
-        : head(BF16 ? (uint32_t)(reinterpret_cast<uintptr_t>(x) / 2 % 2) : 0), count((V - head) / kPer), rest((V - head) % kPer) {}
-    // the elements beside the vectors: those after them, then the one before
+    __device__ __forceinline__ RowVectors(const void* row, uint32_t V) {
+        head = (uint32_t)(-reinterpret_cast<uintptr_t>(row) % ALIGN) / kSize;
+        head = head < V ? head : V;
+        count = (V - head) / kPer;
+        rest = (V - head) % kPer;
+    }
+    // the elements beside the vectors: those after them, then those before
     __device__ __forceinline__ uint32_t beside() const { return rest + head; }
-    __device__ __forceinline__ uint32_t beside_at(uint32_t t) const { return t < rest ? head + count * kPer + t : 0; }
+    __device__ __forceinline__ uint32_t beside_at(uint32_t t) const { return t < rest ? head + count * kPer + t : t - rest; }
     // where element `id` is: vector i (count: beside them) and its place j
     __device__ __forceinline__ void find(uint32_t id, uint32_t* i, uint32_t* j) const {
         const uint32_t k = id - head;
         *i = id < head ? count : k / kPer;
-        *j = id < head ? rest : k % kPer;
+        *j = id < head ? rest + id : k % kPer;
     }
 };
+
+// A vector of a gradient, at a multiple of 16 bytes.  PAST: past the caches, at a higher
+// rate, for gradients that these do not hold until they are read: 8,192 x 128,000 bf16,
+// 36% of them live, 557 us, else 594; then read and written once more 1,280 and 1,337;
+// but 2,048 x 50,001, which the caches hold, 148 and 126.  Rows that do not start at a
+// 64-byte boundary lose by it (4,088 x 32,001 fp32, 36% live: from a boundary on 135, from
+// the first element on 149, in the caches' order 141).
+template <bool PAST, typename T>
+__device__ __forceinline__ void put16(T* p, u32x4 v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = v;
+}
 
 // a vector of scores at -inf
 template <bool BF16>
