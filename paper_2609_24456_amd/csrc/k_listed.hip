@@ -653,7 +653,7 @@ __device__ __forceinline__ void join_listed(const ListedArgs& a, uint32_t n, int
     finish_listed<BF16, MODE>(a, n, at, join_mass<kWave>(all, a.c), r);
 }
 
-template <bool BF16, int MODE>
+template <bool BF16, int MODE, bool ONCE>
 __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
 #pragma unroll
         for (int k = 0; k < kScanVectors; ++k) {
             const uint32_t i = base + k * kListedThreads + tid;
-            v[k] = i < hi ? load16(vx + (size_t)i * kPer) : no_vector<BF16>();
+            v[k] = i < hi ? read16<ONCE>(vx + (size_t)i * kPer) : no_vector<BF16>();
         }
     };
     load(lo);
@@ -1110,7 +1110,9 @@ hipError_t launch_scan(const ListedArgs& a, hipStream_t s) {
     if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
     constexpr int kTile = kListedThreads * kScanVectors;
     const unsigned lds = (a.per + kTile - 1) / kTile * (kTile * kPer / 8);
-    hipLaunchKernelGGL((k_listed_scan<BF16, MODE>), grid_of(items, kListedThreads), dim3(kListedThreads), lds, s, a);
+    // (with a gradient to come the rows are read again)
+    if (a.once && !a.has_dx) hipLaunchKernelGGL((k_listed_scan<BF16, MODE, true>), grid_of(items, kListedThreads), dim3(kListedThreads), lds, s, a);
+    else hipLaunchKernelGGL((k_listed_scan<BF16, MODE, false>), grid_of(items, kListedThreads), dim3(kListedThreads), lds, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1 || a.row_ticket) return e;
     constexpr int kRows = kListedThreads / kWave;

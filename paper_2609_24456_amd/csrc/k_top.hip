@@ -615,7 +615,7 @@ __device__ void join_top(const TopArgs& a, uint32_t n, int64_t at, float xa, Top
     write_ranked<kTopThreads>(a, n, s.cand, found, r, tid);
 }
 
-template <bool BF16>
+template <bool BF16, bool ONCE>
 __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
     using E = Elem<BF16>;
     using T = typename E::T;
@@ -646,7 +646,7 @@ __global__ __launch_bounds__(kTopThreads, 6) void k_top_rows(TopArgs a) {
 #pragma unroll
         for (int k = 0; k < kTopVectors; ++k) {
             const uint32_t i = base + k * kTopThreads + tid;
-            v[k] = i < hi ? load16(vx + (size_t)i * kPer) : no_vector<BF16>();
+            v[k] = i < hi ? read16<ONCE>(vx + (size_t)i * kPer) : no_vector<BF16>();
         }
         float top = kNone;
 #pragma unroll
@@ -788,7 +788,12 @@ hipError_t alternatives(const TopArgs& a, hipStream_t s) {
     // one launch takes fewer than 2^31 parts (the division's range)
     const int64_t items = rows * a.parts;
     if (items >= 1ll << 31) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_top_rows<BF16>), grid_of(items, kTopThreads), dim3(kTopThreads), sizeof(float) * (a.per / kGroup), s, a);
+    auto go = [&](auto once) {
+        hipLaunchKernelGGL((k_top_rows<BF16, decltype(once)::value>), grid_of(items, kTopThreads), dim3(kTopThreads),
+                           sizeof(float) * (a.per / kGroup), s, a);
+    };
+    if (a.once) go(std::true_type{});
+    else go(std::false_type{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1 || a.row_ticket) return e;
     hipLaunchKernelGGL((k_top_join<BF16>), grid_of(rows, kTopThreads), dim3(kTopThreads), 0, s, a);

@@ -99,6 +99,8 @@ void common_args(Args& a, const conduit_rows* x, int64_t B, int64_t T, int64_t s
     a.shape = make_shape(B, T, stride);
     a.x = view(x);
     a.V = x->width;
+    // (by the rows' bytes, whatever lies between them)
+    a.once = (double)(B * T) * (double)x->width * elem_size(x->dtype) > (double)kPastBytes;
     a.c = (float)((double)1.4426950408889634074 / temperature);
     a.inv_t = (float)(1.0 / temperature);
     a.inv_lo = (float)(1.0 / temperature - (double)a.inv_t);
@@ -108,11 +110,10 @@ void common_args(Args& a, const conduit_rows* x, int64_t B, int64_t T, int64_t s
     a.err = err;
 }
 
-// (in bytes that are written, whatever lies between the rows)
 void set_gradient(ListedArgs& a, const conduit_rows* dx) {
     a.dx = view(dx);
     a.has_dx = true;
-    a.past = (double)(a.shape.B * a.shape.T) * (double)a.V * elem_size(dx->dtype) > (double)kPastBytes;
+    a.past = a.once;
 }
 
 template <typename Args>

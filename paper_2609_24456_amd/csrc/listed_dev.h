@@ -5,8 +5,8 @@
 
 namespace conduit {
 
-// Gradients of more bytes are written past the caches: half as much again as the last
-// level holds (256 MB), since up to there a reader finds part of them.
+// Logits of more bytes are read and gradients written past the caches: half as much
+// again as the last level holds (256 MB), since up to there the next reader finds part.
 constexpr int64_t kPastBytes = 384 << 20;
 constexpr int kMostListed = 128;      // choices a token
 constexpr int kPartVectors = 32768;   // most vectors of a part of a row: its LDS grows with them
@@ -24,6 +24,7 @@ struct TopArgs {
     RowsView x;
     int64_t V;
     float c, inv_t, inv_lo;  // as in LogitsArgs
+    bool once;               // the logits are read past the caches (rows_dev.h)
     const int32_t* tokens;   // NULL: no taken token
     const uint8_t* mask;
     RowsView ids, logps;
@@ -62,6 +63,7 @@ struct ListedArgs {
     RowsView x, dx;
     int64_t V;
     float c, inv_t, inv_lo;
+    bool once;  // as in TopArgs
     const uint8_t* mask;
     RowsView ids;
     int32_t K;

@@ -450,8 +450,8 @@ def test_distill_of_many_and_wide_rows(B, T, V, dtype):
 
 
 @pytest.mark.parametrize("V,dtype", [(700, F32), (2101, BF16), (9001, BF16), (20001, BF16), (30001, F32), (50001, BF16), (50001, F32), (100001, BF16), (140003, F32)])
-def test_gradients_larger_than_the_caches(V, dtype):
-    """They are written another way: the same bits as from two calls of half the rows."""
+def test_batches_larger_than_the_caches(V, dtype):
+    """Their logits are read and gradients written another way: the same bits as from two calls of half the rows."""
     size = 4 if dtype == F32 else 2
     rows = (410 << 20) // (V * size) // 2 * 2
     g = torch.Generator(device="cuda").manual_seed(V)
@@ -461,9 +461,15 @@ def test_gradients_larger_than_the_caches(V, dtype):
     mask = (torch.rand((1, rows), generator=g, device="cuda") < 0.6).to(torch.uint8)
     one, two = torch.full_like(x, NAN), torch.full_like(x, NAN)
     loss, stats, lse = torch.empty((1, rows), device="cuda"), torch.empty(3, device="cuda"), torch.empty((1, rows), device="cuda")
-    logps = torch.empty_like(y)
-    cd.conduit_listed_logprobs(x, ids, logps, lse=lse)
     halves = [slice(0, rows // 2), slice(rows // 2, rows)]
+    outs = [[torch.full_like(t, 9) for t in (ids, y, lse, lse, y, lse)] for _ in range(2)]
+    for parts, (top, lp, entropy, rest, logps, z) in zip(([slice(0, rows)], halves), outs):
+        for h in parts:
+            cd.conduit_token_alternatives(x[:, h], top[:, h], lp[:, h], entropy=entropy[:, h], mask=mask[:, h])
+            cd.conduit_listed_logprobs(x[:, h], ids[:, h], logps[:, h], rest=rest[:, h], lse=z[:, h])
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    lse = z
     opts = cd.distill_opts(rest=True, reduction="sum")
     cd.conduit_distill_loss(opts, x, ids, y, loss, stats, dlogits=one, mask=mask)
     for h in halves:
