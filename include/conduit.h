@@ -886,7 +886,7 @@ void conduit_distill_opts_default(conduit_distill_opts* opts);
  * tokens gives zeros.
  * Rows of up to 256 KB cross memory once in each direction.  Up to five launches:
  * the count of the tokens (with a mask, of more than 1,024 tokens, 2,048 if it is
- * in one piece, or for the mean over sequences), the rows, where these are split
+ * in one piece, 512 for the mean over sequences), the rows, where these are split
  * the join of more than 512 and the gradient, and the sums of a batch of more than
  * 512 rows wider than 512.  Errors: EINVAL, EDEVICE, ESTATE.
  */

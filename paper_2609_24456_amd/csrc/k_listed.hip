@@ -375,11 +375,14 @@ __device__ __forceinline__ void write_nothing(const ListedArgs& a, uint32_t n, i
 // loads for 2,048 tokens, any other by bytes.  (The launch takes 4.6 us and a gap; 2,048
 // rows of 50,001 bf16 59.8 us with the counting, 57 without; of 8,192 tokens it costs
 // the rows more than the launch.)
-__device__ __forceinline__ uint32_t counted_tokens(const ListedArgs& a) {
+struct Counts {
+    uint32_t tokens, rows;  // that count, and sequences with one (for the mean over these)
+};
+
+__device__ __forceinline__ Counts counted_tokens(const ListedArgs& a) {
     const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
-    if (!a.mask) return n_rows;
-    if (a.counted) return (uint32_t)a.head->counts;
-    uint32_t tokens = 0;
+    if (!a.mask) return Counts{n_rows, (uint32_t)a.shape.B};
+    if (a.counted) return Counts{(uint32_t)a.head->counts, (uint32_t)(a.head->counts >> 32)};
     if (a.flat_mask) {
         constexpr uint32_t kAtOnce = 2;
         const uint32_t whole = n_rows / 16, rest = n_rows % 16;
@@ -401,28 +404,50 @@ __device__ __forceinline__ uint32_t counted_tokens(const ListedArgs& a) {
                 }
             }
         }
-        return __builtin_amdgcn_readfirstlane(lanes_sum<kWave>(mine));
+        return Counts{(uint32_t)__builtin_amdgcn_readfirstlane(lanes_sum<kWave>(mine)), 0};
     }
+    Counts c{0, 0};
+    uint32_t last = ~0u;  // the sequence of the last token that counts
     for (uint32_t base = 0; base < n_rows; base += 8 * kWave) {
+        uint8_t on[8];
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
             const uint32_t n = base + i * kWave + lane_id();
-            tokens += __builtin_popcountll(__ballot(n < n_rows && a.mask[a.shape.at(n)]));
+            on[i] = n < n_rows ? a.mask[a.shape.at(n)] : 0;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint64_t m = __ballot(on[i] != 0);
+            c.tokens += __builtin_popcountll(m);
+            if (a.reduction != CONDUIT_SEQUENCE_MEAN || m == 0) continue;
+            // the first of its sequence: the one before it that counts is of another
+            const uint32_t b = div31(base + i * kWave + lane_id(), a.shape.by_T);
+            const uint64_t before = m & below_lane();
+            const uint32_t other = __shfl(b, before ? 63 - __builtin_clzll(before) : 0, kWave);
+            c.rows += __builtin_popcountll(__ballot(on[i] && b != (before ? other : last)));
+            last = __shfl(b, 63 - __builtin_clzll(m), kWave);
         }
     }
+    return c;
+}
+
+// Tokens of a sequence that count, by a wavefront.
+__device__ __forceinline__ uint32_t sequence_tokens(const ListedArgs& a, uint32_t b) {
+    if (!a.mask) return (uint32_t)a.shape.T;
+    if (a.counted) return a.row_count[b];
+    const uint8_t* mask = a.mask + (int64_t)b * a.shape.stride;
+    uint32_t tokens = 0;
+    for (uint32_t t = 0; t < (uint32_t)a.shape.T; t += kWave)
+        tokens += __builtin_popcountll(__ballot(t + lane_id() < (uint32_t)a.shape.T && mask[t + lane_id()]));
     return tokens;
 }
 
-// the token's part in the loss
-__device__ __forceinline__ double token_part(const ListedArgs& a, uint32_t n, int64_t at, uint32_t tokens) {
-    uint32_t rows = (uint32_t)a.shape.B, row = (uint32_t)a.shape.T;
-    if (a.counted && a.reduction == CONDUIT_SEQUENCE_MEAN) {
-        rows = (uint32_t)(a.head->counts >> 32);
-        row = a.row_count[div31(n, a.shape.by_T)];
-    }
+// The token's part in the loss.  (a.counted or by a whole wavefront: see the two above)
+__device__ __forceinline__ double token_part(const ListedArgs& a, uint32_t n, int64_t at, const Counts& c) {
     PolicyTerms o{};
     o.reduction = a.reduction;
-    const double w = token_weight(o, tokens, rows, row);
+    const uint32_t row = a.reduction == CONDUIT_SEQUENCE_MEAN ? sequence_tokens(a, div31(n, a.shape.by_T)) : 1;
+    const double w = token_weight(o, c.tokens, c.rows, row);
     return a.weight ? w * (double)a.weight[at] : w;
 }
 
@@ -465,7 +490,7 @@ __device__ __forceinline__ void finish_token(const ListedArgs& a, uint32_t n, do
 
 // what SUM_NEXT left, by one wavefront of the next launch
 __device__ __forceinline__ void sum_rows(const ListedArgs& a) {
-    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T), tokens = counted_tokens(a);
+    const uint32_t rows = (uint32_t)(a.shape.B * a.shape.T), tokens = counted_tokens(a).tokens;
     double v[kDistillSums] = {0.0, 0.0};
     for (uint32_t k = lane_id(); k < rows; k += kWave) {
 #pragma unroll
@@ -482,16 +507,17 @@ constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
     __shared__ double lds[kDistillSums * kSumThreads / kWave];
     double v[kDistillSums] = {0.0, 0.0};
-    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T), tokens = counted_tokens(a);
+    const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T);
+    const Counts counts = counted_tokens(a);
     for (uint32_t n = blockIdx.x * kSumThreads + threadIdx.x; n < n_rows; n += gridDim.x * kSumThreads) {
         const int64_t at = a.shape.at(n);
         if (a.mask && !a.mask[at]) continue;
-        const double part = token_part(a, n, at, tokens), loss = (double)a.loss[at];
+        const double part = token_part(a, n, at, counts), loss = (double)a.loss[at];
         v[0] += part == 0.0 ? 0.0 : part * loss;
         v[1] += loss;
     }
     block_sum<kSumThreads, kDistillSums>(v, lds);
-    if (threadIdx.x < kWave) finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1], tokens);
+    if (threadIdx.x < kWave) finish_distill(a, blockIdx.x, gridDim.x, v[0], v[1], counts.tokens);
 }
 
 // ---------------------------------------------------------------------------
@@ -512,7 +538,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
     const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T), V = (uint32_t)a.V;
     uint32_t* bits = s_bits[w];
     double sums[kDistillSums] = {0.0, 0.0};
-    const uint32_t tokens = MODE == DISTILL ? counted_tokens(a) : 0;
+    const Counts counts = MODE == DISTILL ? counted_tokens(a) : Counts{};
     for (uint32_t n = block_number() * kRows + w; n < n_rows; n += gridDim.x * gridDim.y * kRows) {
         const int64_t at = a.shape.at(n);
         const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
@@ -551,7 +577,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
         if constexpr (MODE == SCORES) {
             write_scores(a, n, at, e, others);
         } else {
-            const double part = token_part(a, n, at, tokens);
+            const double part = token_part(a, n, at, counts);
             const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
             if (l == 0) a.loss[at] = o.loss;
             sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
@@ -578,7 +604,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
         __syncthreads();
         if (threadIdx.x >= kWave) return;
         const double v0 = lanes_sum<kRows>(s_sum[0][l % kRows]), v1 = lanes_sum<kRows>(s_sum[1][l % kRows]);
-        finish_distill(a, blockIdx.x, gridDim.x, v0, v1, tokens);
+        finish_distill(a, blockIdx.x, gridDim.x, v0, v1, counts.tokens);
     }
 }
 
@@ -609,8 +635,9 @@ __device__ __forceinline__ void load_list(const ListedArgs& a, uint32_t n, bool 
 template <int MODE>
 __device__ __forceinline__ void load_weight(const ListedArgs& a, uint32_t n, int64_t at, RowList& r) {
     if constexpr (MODE == DISTILL) {
-        r.tokens = counted_tokens(a);
-        r.part = token_part(a, n, at, r.tokens);
+        const Counts counts = counted_tokens(a);
+        r.tokens = counts.tokens;
+        r.part = token_part(a, n, at, counts);
     }
 }
 
@@ -670,7 +697,7 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_scan(ListedArgs a) {
     if (a.mask && !a.mask[at]) {
         if (part == 0 && tid < kWave) {
             write_nothing<MODE>(a, n, at);
-            if constexpr (MODE == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
+            if constexpr (MODE == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a).tokens);
         }
         return;
     }
@@ -822,7 +849,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
         }
         if (tid < kWave) {
             write_nothing<LIST>(a, n, at);
-            if constexpr (LIST == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a));
+            if constexpr (LIST == DISTILL) finish_token(a, n, 0.0, 0.0f, counted_tokens(a).tokens);
         }
         return;
     }

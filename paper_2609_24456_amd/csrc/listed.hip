@@ -302,8 +302,10 @@ conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const cond
     a.row_count = reinterpret_cast<uint32_t*>(w + l.l.row_count);
     a.partial = reinterpret_cast<double*>(w + l.l.rest);
     place_parts(a, w, l);
-    a.flat_mask = mask && (stride == T || B == 1) && !misaligned(mask, 16);
-    a.counted = mask && (opts->reduction == CONDUIT_SEQUENCE_MEAN || B * T > (a.flat_mask ? kCountedFlat : kCountedHere));
+    // (the mean over sequences needs each one's tokens, which a launch over the tokens does not count)
+    const bool sequences = opts->reduction == CONDUIT_SEQUENCE_MEAN;
+    a.flat_mask = mask && !sequences && (stride == T || B == 1) && !misaligned(mask, 16);
+    a.counted = mask && B * T > (sequences ? kPolicyBlocks : a.flat_mask ? kCountedFlat : kCountedHere);
     a.sums = B * T > kPolicyBlocks ? SUM_LAUNCH : a.parts > 1 && a.has_dx ? SUM_NEXT : SUM_ROWS;
     a.row = reinterpret_cast<ListedRow*>(w + l.more);
     return launched(launch_distill_loss(a, logits->dtype == CONDUIT_BF16, s), "distillation launch");
