@@ -612,6 +612,12 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
 // longer rows, or parts of them, whose gradient is not written here: a workgroup
 // each
 // ---------------------------------------------------------------------------
+// HBM bounds it (4,088 rows of 50,001 fp32, K = 32: 131 us, 6.2 TB/s; 36% of them live
+// 56, 5.3), few rows are bound by latency (64 of 128,000 bf16 in parts, K = 5: 8.0 us on
+// logits in the caches, of which a launch is 2.3 and the loads 2).  The list, the
+// token's weight and the teacher's side are the first wavefront's, under the row's
+// loads; a number met twice is noted with a part's sums, so that the join looks for
+// duplicates (110 ns an entry) only then.
 constexpr int kScanVectors = 8;  // vectors a lane and tile
 
 // a row's list with its scores, and the teacher's side of it, by one wavefront
@@ -794,15 +800,15 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_join(ListedArgs a) {
 // rows that fit the registers of WAVES wavefronts, K vectors a lane
 // ---------------------------------------------------------------------------
 // A row crosses memory once in each direction.  HBM bounds it where the rows are
-// wide or fp32 (4,088 rows of 32,001 fp32, 37% of them live: 147 us, 4.9 TB/s, a
-// large copy's rate; 8,192 of 128,000 bf16: 600, 4.8), the steps of a row one after
-// the other where they are not: load, sum, join, the list's part, store.  A lane
-// takes up to 16 vectors, so that a row has few wavefronts to join and a compute
-// unit several rows at different steps, and what a lane's vectors have beyond the
-// row is left out (unmasked, read and written, V x rows bf16: 5,001 x 16,384 on one
-// wavefront 91 us, on four 166-235; 10,001 x 8,192 on two 90, on four 109; 50,001 x
-// 2,048 on eight 110, on sixteen 137; fp32, with half the work in a vector, is
-// better on sixteen of 8 vectors: 32,001 x 4,088 masked 147, on eight of 16 156).
+// wide or fp32 (4,088 rows of 32,001 fp32, 36% of them live: 134 us, 5.3 TB/s; 8,192 of
+// 128,000 bf16: 557, 5.1; a large copy reaches 4.7-4.9, a fill 6.9), the steps of a row
+// one after the other where they are not: load, sum, join, the list's part, store.  A
+// lane takes up to 16 vectors, so that a row has few wavefronts to join and a compute
+// unit several rows at different steps, and what a lane's vectors have beyond the row
+// is left out (read and written, V x rows bf16, before rows started at boundaries:
+// 5,001 x 16,384 on one wavefront 91 us, on four 166-235; 10,001 x 8,192 on two 90, on
+// four 109; 50,001 x 2,048 on eight 110, on sixteen 137; fp32, with half the work in a
+// vector, is better on sixteen of 8 vectors: 32,001 x 4,088 147, on eight of 16 156).
 // The list is loaded ahead of the row and its scores behind it.  Up to 1,024 vectors
 // the scores alone go this way too: a row's steps hide under those of three others
 // (65,536 rows of 2,100 bf16, K = 5: 79 us, a workgroup a row 327), and rows from 513
@@ -972,6 +978,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
 // divergence of split rows from what their join left: wavefronts take parts of
 // kGradK vectors a lane of a row
 // ---------------------------------------------------------------------------
+// HBM bounds it (2,048 rows of 50,001 fp32, 42% of them live, K = 32: 116 us, 4.8 TB/s).
+// Each wavefront loads the list again and marks what is in its part of the row, in 1 KB
+// of LDS a workgroup: no barrier.
 constexpr int kGradK = 4;
 
 template <bool BF16, bool SPLIT, bool PAST>

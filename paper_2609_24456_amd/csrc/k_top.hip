@@ -496,8 +496,8 @@ __global__ __launch_bounds__(kTopThreads) void k_top_wave(TopArgs a) {
 // longer rows, or parts of them: a workgroup each
 // ---------------------------------------------------------------------------
 // HBM bounds it, and the exponentials nearly as much in bf16 (4,096 rows of 128,000
-// bf16, K = 64: 202 us, 5.2 TB/s, where a reduction that only reads reaches 6.0; by
-// the sums of softmax_dev.h 219).  Few rows are bound by latency: 64 rows of
+// bf16, K = 64: 195 us, 5.4 TB/s, where a reduction that only reads reaches 6.0; in the
+// caches' order 202, by the sums of softmax_dev.h 219).  Few rows are bound by latency: 64 rows of
 // 128,000 bf16 in parts, K = 20: 14 us, of which the loads take 3, the part's
 // selection 3 and the join's 4.  Five or six workgroups a compute unit (80
 // registers) cover each other's loads; eight cost spills, workgroups of 512 lanes
