@@ -437,8 +437,13 @@ __device__ __forceinline__ uint32_t sequence_tokens(const ListedArgs& a, uint32_
     if (a.counted) return a.row_count[b];
     const uint8_t* mask = a.mask + (int64_t)b * a.shape.stride;
     uint32_t tokens = 0;
-    for (uint32_t t = 0; t < (uint32_t)a.shape.T; t += kWave)
-        tokens += __builtin_popcountll(__ballot(t + lane_id() < (uint32_t)a.shape.T && mask[t + lane_id()]));
+    for (uint32_t base = 0; base < (uint32_t)a.shape.T; base += 8 * kWave) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t t = base + i * kWave + lane_id();
+            tokens += __builtin_popcountll(__ballot(t < (uint32_t)a.shape.T && mask[t]));
+        }
+    }
     return tokens;
 }
 
