@@ -64,7 +64,7 @@ def build_tensor_check(verbose: bool = False) -> str:
     inc = ext.include_paths() + [sysconfig.get_paths()["include"], "/opt/rocm/include"]
     cmd = (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__=1",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DTORCH_VERSION_BUILT="{torch.__version__}"']
-           + [x for i in inc for x in ("-isystem", i)]
+           + [x for i in inc for x in ("-isystem", i)] + ["-I", INCLUDE]
            + [os.path.join(CSRC, "tensor_check.cpp"), "-o", TENSOR_CHECK + ".tmp", "-L" + lib, "-ltorch_python", "-ltorch",
               "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib])
     if verbose:

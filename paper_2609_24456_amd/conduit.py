@@ -20,8 +20,9 @@ try:  # built beside libconduit.so; without it, or for another torch, every chec
     _address = _tensor_check.address
     _native_batch = getattr(_tensor_check, "token_batch", None)
     _native_rows = getattr(_tensor_check, "rows", None)
+    _native_listed = getattr(_tensor_check, "listed", None)
 except ImportError:
-    _native_batch = _native_rows = None
+    _native_batch = _native_rows = _native_listed = None
 
     def _address(t, dtype, nbytes, numel):
         return None
@@ -770,6 +771,25 @@ _FLOAT_ROWS = (torch.float32, torch.bfloat16)
 _VALUES = (torch.float32,)
 
 
+_LISTED = ("conduit_token_alternatives", "conduit_listed_logprobs", "conduit_listed_logprobs_backward", "conduit_distill_loss")
+_listed_entries = None
+
+
+def _listed_call(which, opts, temperature, stream, *tensors):
+    """The call, checked and made natively where all of its arguments are plain ones (_tensor_check); whether it was."""
+    global _listed_entries
+    if _native_listed is None or not getattr(tensors[2], "is_cuda", False):  # (the logits)
+        return False
+    if _listed_entries is None:
+        _listed_entries = [C.cast(getattr(lib(), n), C.c_void_p).value for n in _LISTED]
+    s = _stream(stream)
+    status = _native_listed(which, _listed_entries[which], opts, temperature, s if isinstance(s, int) else s.value or 0, *tensors)
+    if status is None:
+        return False
+    _check(status)
+    return True
+
+
 def _listed_ids(ids):
     return _listed_ptr(ids, (torch.int32,), "ids", ids)
 
@@ -813,6 +833,9 @@ def conduit_token_alternatives(logits, ids, logps, tokens=None, logp=None, lse=N
                                temperature=1.0, workspace=None, stream=None):
     """The K most probable choices of every token of logits [B, T, V] into ids and logps [B, T, K], and with tokens what
     conduit_token_logprobs gives."""
+    if workspace is not None and _listed_call(0, None, temperature, stream, workspace, None, logits, ids, logps, None, tokens, logp,
+                                              lse, entropy, mask):
+        return
     f = torch.float32
     i = _listed_ids(ids)
     lps = _listed_values(logps, "logps", ids, i)
@@ -832,6 +855,9 @@ def listed_logprobs_workspace(logits, K):
 def conduit_listed_logprobs(logits, ids, logps, rest=None, lse=None, mask=None, temperature=1.0, workspace=None,
                             stream=None):
     """Log-probabilities of the choices ids [B, T, K] under logits [B, T, V], and of all others together (rest)."""
+    if workspace is not None and _listed_call(1, None, temperature, stream, workspace, None, logits, ids, logps, None, rest, lse, None,
+                                              None, mask):
+        return
     f = torch.float32
     i = _listed_ids(ids)
     lps = _listed_values(logps, "logps", ids, i)
@@ -845,6 +871,8 @@ def conduit_listed_logprobs(logits, ids, logps, rest=None, lse=None, mask=None, 
 def conduit_listed_logprobs_backward(logits, ids, lse, dlogps, dlogits, rest=None, drest=None, mask=None, temperature=1.0,
                                      stream=None):
     """The gradient of conduit_listed_logprobs's logits, into dlogits (the logits themselves: in place)."""
+    if _listed_call(2, None, temperature, stream, None, None, logits, ids, dlogps, dlogits, lse, rest, drest, None, mask):
+        return
     f = torch.float32
     i = _listed_ids(ids)
     g = _listed_values(dlogps, "dlogps", ids, i)
@@ -874,6 +902,9 @@ def conduit_distill_loss(opts, logits, ids, teacher, loss, stats, dlogits=None, 
                          workspace=None, stream=None):
     """The divergence of logits [B, T, V] from a teacher's values at the choices ids [B, T, K]: per token, stats
     (DISTILL_STATS), and the gradient dlogits (the logits themselves: in place; None: no gradient)."""
+    if workspace is not None and isinstance(opts, DistillOpts) and _listed_call(
+            3, C.addressof(opts), temperature, stream, workspace, stats, logits, ids, teacher, dlogits, loss, weight, None, None, mask):
+        return
     f = torch.float32
     i = _listed_ids(ids)
     y = _listed_values(teacher, "teacher", ids, i)

@@ -10,6 +10,8 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "conduit.h"
+
 namespace {
 
 bool dtype_is(PyObject* want, at::ScalarType have) {
@@ -122,12 +124,7 @@ PyObject* token_batch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return out;
 }
 
-// the members of conduit_rows
-struct Rows {
-    void* data;
-    int32_t dtype, reserved;
-    int64_t width, stride_b, stride_t;
-};
+using Rows = conduit_rows;
 
 // rows(address of a Rows, t, tokens, f32, bf16, i32 = -1): fills it in for a
 // float32 or bfloat16 tensor on a HIP device of one row for each element of
@@ -161,7 +158,124 @@ PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Py_RETURN_TRUE;
 }
 
+// A tensor on a HIP device, exactly of class Tensor; null: not one
+const at::Tensor* device_tensor(PyObject* o) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.is_cuda() ? &t : nullptr;
+}
+
+// conduit_rows of a tensor of rows, one for each row of `ids`
+bool rows_like(PyObject* o, const at::Tensor& ids, Rows* r) {
+    const at::Tensor* t = device_tensor(o);
+    const int64_t d = ids.dim() - 1;
+    if (!t || t->dim() != d + 1) return false;
+    for (int64_t i = 0; i < d; ++i)
+        if (t->size(i) != ids.size(i)) return false;
+    if (t->size(d) > 1 && t->stride(d) != 1) return false;
+    const at::ScalarType type = t->scalar_type();
+    const int32_t dtype = type == at::kFloat ? CONDUIT_F32 : type == at::kBFloat16 ? CONDUIT_BF16 : type == at::kInt ? CONDUIT_I32 : -1;
+    if (dtype < 0) return false;
+    *r = Rows{t->data_ptr(), dtype, 0, t->size(d), d == 2 ? t->stride(0) : 0, t->stride(d - 1)};
+    return true;
+}
+
+// listed(which, entry point's address, options' address or None, temperature, stream,
+// workspace, stats, logits, ids, values, dlogits, four per-token tensors, mask): a
+// call on listed choices (0 alternatives: tokens, logp, lse, entropy; 1
+// log-probabilities: rest, lse; 2 their gradient: lse, rest, drest; 3 distillation:
+// loss, weight) whose arguments are all plain ones, and its status; None, and no
+// call, if anything is otherwise.  (Argument by argument through ctypes a call takes
+// 7.4 us on the host, this way 4.9, most of it the launch.)
+PyObject* listed(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 16) {
+        PyErr_SetString(PyExc_TypeError, "listed takes 16 arguments");
+        return nullptr;
+    }
+    const long which = PyLong_AsLong(args[0]);
+    void* const entry = PyLong_AsVoidPtr(args[1]);
+    void* const opts = args[2] == Py_None ? nullptr : PyLong_AsVoidPtr(args[2]);
+    const double temperature = PyFloat_AsDouble(args[3]);
+    void* const stream = PyLong_AsVoidPtr(args[4]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (!entry || which < 0 || which > 3) Py_RETURN_NONE;
+    Rows x, ids, values, dx;
+    Batch batch{};
+    void* at[5] = {nullptr, nullptr, nullptr, nullptr, nullptr};
+    void* workspace = nullptr;
+    float* stats = nullptr;
+    uint64_t bytes = 0;
+    try {
+        const at::Tensor* i = device_tensor(args[8]);
+        if (!i || (i->dim() != 2 && i->dim() != 3) || !rows_like(args[8], *i, &ids) || ids.dtype != CONDUIT_I32) Py_RETURN_NONE;
+        if (!rows_like(args[7], *i, &x) || x.dtype == CONDUIT_I32) Py_RETURN_NONE;
+        if (!rows_like(args[9], *i, &values) || values.dtype != CONDUIT_F32 || values.width != ids.width) Py_RETURN_NONE;
+        if (args[10] != Py_None && (!rows_like(args[10], *i, &dx) || dx.dtype == CONDUIT_I32)) Py_RETURN_NONE;
+        batch.dim = i->dim() - 1;
+        batch.B = batch.dim == 2 ? i->size(0) : 1;
+        batch.T = i->size(batch.dim - 1);
+        batch.stride = batch.T;
+        bool first = true;
+        for (int k = 0; k < 5; ++k) {
+            if (args[11 + k] == Py_None) continue;
+            const at::Tensor* t = device_tensor(args[11 + k]);
+            Batch b;
+            if (!t || !read_batch(*t, &b) || b.dim != batch.dim || b.B != batch.B || b.T != batch.T) Py_RETURN_NONE;
+            if (!first && b.stride != batch.stride) Py_RETURN_NONE;
+            const at::ScalarType type = t->scalar_type();
+            if (k == 4 ? type != at::kByte && type != at::kBool : type != (which == 0 && k == 0 ? at::kInt : at::kFloat)) Py_RETURN_NONE;
+            batch.stride = b.stride;
+            first = false;
+            at[k] = t->data_ptr();
+        }
+        if (args[5] != Py_None) {
+            const at::Tensor* t = device_tensor(args[5]);
+            if (!t || t->scalar_type() != at::kByte || !t->is_contiguous()) Py_RETURN_NONE;
+            workspace = t->data_ptr();
+            bytes = (uint64_t)t->numel();
+        }
+        if (args[6] != Py_None) {
+            const at::Tensor* t = device_tensor(args[6]);
+            if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->numel() < 3) Py_RETURN_NONE;
+            stats = static_cast<float*>(t->data_ptr());
+        }
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    Rows* const gradient = args[10] == Py_None ? nullptr : &dx;
+    float* const f[4] = {static_cast<float*>(at[0]), static_cast<float*>(at[1]), static_cast<float*>(at[2]), static_cast<float*>(at[3])};
+    const uint8_t* const mask = static_cast<const uint8_t*>(at[4]);
+    const int64_t B = batch.B, T = batch.T, step = batch.stride;
+    conduit_status status;
+    Py_BEGIN_ALLOW_THREADS;
+    switch (which) {
+    case 0:
+        status = reinterpret_cast<decltype(&conduit_token_alternatives)>(entry)(
+            &x, B, T, step, static_cast<const int32_t*>(at[0]), mask, temperature, &ids, &values, f[1], f[2], f[3], workspace, bytes, stream);
+        break;
+    case 1:
+        status = reinterpret_cast<decltype(&conduit_listed_logprobs)>(entry)(&x, B, T, step, &ids, mask, temperature, &values, f[0], f[1],
+                                                                             workspace, bytes, stream);
+        break;
+    case 2:
+        status = reinterpret_cast<decltype(&conduit_listed_logprobs_backward)>(entry)(&x, B, T, step, &ids, mask, temperature, f[0], f[1],
+                                                                                      &values, f[2], gradient, stream);
+        break;
+    default:
+        status = reinterpret_cast<decltype(&conduit_distill_loss)>(entry)(static_cast<const conduit_distill_opts*>(opts), &x, B, T, step, &ids,
+                                                                          &values, f[1], mask, temperature, f[0], stats, gradient, workspace,
+                                                                          bytes, stream);
+    }
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong((long)status);
+}
+
 PyMethodDef methods[] = {
+    {"listed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(listed)), METH_FASTCALL,
+     "a call on listed choices with checked tensors: its status, or None"},
     {"token_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(token_batch)), METH_FASTCALL,
      "layout and device addresses of checked per-token tensors, or None"},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rows)), METH_FASTCALL,

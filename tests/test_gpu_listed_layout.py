@@ -1,5 +1,7 @@
 """The calls on listed choices: both ways of checking arguments give the same calls, offsets past 32 bits reach the right
 elements, other streams have workspaces of their own, and more rows than one dimension of a launch takes."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -45,12 +47,39 @@ def test_both_ways_of_checking_arguments_are_the_same(monkeypatch):
         if one:
             args = [t[1] for t in args]
         a = _calls(*args)
-        with monkeypatch.context() as m:
-            m.setattr(cd, "_native_batch", None)
-            m.setattr(cd, "_native_rows", None)
-            b = _calls(*args)
-        for i, (p, q) in enumerate(zip(a, b)):
-            assert torch.equal(p, q), i
+        ws = cd.workspace(1 << 20)
+        for gone in ((), ("_native_listed",), ("_native_listed", "_native_batch", "_native_rows")):
+            with monkeypatch.context() as m:
+                for name in gone:
+                    m.setattr(cd, name, None)
+                for kw in (dict(), dict(workspace=ws), dict(workspace=ws, stream=torch.cuda.current_stream()),
+                           dict(workspace=ws, stream=torch.cuda.current_stream().cuda_stream)):
+                    for mask in (args[4], args[4].bool()):
+                        for i, (p, q) in enumerate(zip(a, _calls(*args[:4], mask, **kw))):
+                            assert torch.equal(p, q), i
+
+
+def test_native_calls_raise_the_library_s_errors():
+    x, tok, ids, y, mask = _inputs(2, 5, 50, 4, F32, 1)
+    ws, t, stats = cd.workspace(1 << 20), torch.empty((2, 5), device="cuda"), torch.empty(3, device="cuda")
+    for call in (lambda: cd.conduit_listed_logprobs(x, ids, torch.empty_like(y), mask=mask, temperature=-1, workspace=ws),
+                 lambda: cd.conduit_listed_logprobs(x, ids, torch.empty_like(y), workspace=ws[:256]),
+                 lambda: cd.conduit_listed_logprobs_backward(x, ids, None, y, torch.empty_like(x)),
+                 lambda: cd.conduit_token_alternatives(x, ids, y, logp=t, workspace=ws),
+                 lambda: cd.conduit_distill_loss(cd.distill_opts(loss="reverse"), x, ids, y, t, stats, workspace=ws),
+                 lambda: cd.conduit_distill_loss(cd.distill_opts(), x, ids, y, t, None, workspace=ws)):
+        with pytest.raises(cd.ConduitError):
+            call()
+    with pytest.raises((TypeError, C.ArgumentError)):
+        cd.conduit_listed_logprobs(x, ids, torch.empty_like(y), temperature="1", workspace=ws)
+    with pytest.raises(ValueError, match="stats"):
+        cd.conduit_distill_loss(cd.distill_opts(), x, ids, y, t, stats[:2], workspace=ws)
+    with pytest.raises(ValueError, match="must have shape"):
+        cd.conduit_listed_logprobs(x, ids, torch.empty_like(y), lse=t[:1], workspace=ws)
+    with pytest.raises(ValueError):  # another step between rows
+        cd.conduit_listed_logprobs(x, ids, torch.empty_like(y), lse=t, rest=torch.empty((2, 6), device="cuda")[:, 1:], workspace=ws)
+    with pytest.raises(TypeError):
+        cd.conduit_token_alternatives(x, ids, y, tokens=tok.long(), workspace=ws)
 
 
 def test_shapes_that_do_not_fit_reach_nothing():
