@@ -299,3 +299,14 @@ def test_binding_checks(monkeypatch):
     monkeypatch.setattr(cd, "_on_device", lambda t: False)
     with pytest.raises(ValueError, match="on a HIP device"):
         cd.conduit_listed_logprobs(x, i, y)
+
+
+def test_native_calls_leave_everything_else_to_python():
+    from paper_2609_24456_amd import _tensor_check
+    x, i, y = torch.zeros(2, 5, 16), torch.zeros(2, 5, 3, dtype=torch.int32), torch.zeros(2, 5, 3)
+    args = [1, 16, None, 1.0, 0, torch.zeros(256, dtype=torch.uint8), None, x, i, y, None, None, None, None, None, None]
+    assert _tensor_check.listed(*args) is None  # (host tensors: no call)
+    for at_, bad in ((0, 7), (0, "1"), (1, None), (3, "warm"), (4, "s"), (7, None), (8, 3), (9, [1])):
+        assert _tensor_check.listed(*(args[:at_] + [bad] + args[at_ + 1:])) is None
+    with pytest.raises(TypeError):
+        _tensor_check.listed(*args[:15])
