@@ -33,6 +33,7 @@ enum ListedMode { SCORES, DISTILL, DIVERGENCE };  // (DIVERGENCE: distillation w
 constexpr int kListedThreads = 256;
 constexpr int kShortElems = 8;                        // elements a lane of a short row
 constexpr int64_t kShortRow = kShortElems * kWave;
+constexpr int kFewLanes = 16, kFewElems = 4;          // of rows that share a wavefront
 
 // ---------------------------------------------------------------------------
 // sums over the choices that are not listed
@@ -92,7 +93,36 @@ __device__ __forceinline__ Mass join_mass(const Mass& a, float c) {
 }
 
 // ---------------------------------------------------------------------------
-// the listed choices of a token: two a lane of a wavefront
+// A row's list is worked on by LANES lanes: a wavefront, or a part of one, whose
+// other parts have rows of their own.
+// ---------------------------------------------------------------------------
+template <int LANES>
+__device__ __forceinline__ uint32_t group_lane() { return lane_id() % LANES; }
+
+// the first lane's value, in every lane
+template <int LANES>
+__device__ __forceinline__ float group_first(float x) {
+    if constexpr (LANES == kWave) return uniform(x);
+    else return __shfl(x, 0, LANES);
+}
+
+template <int LANES>
+__device__ __forceinline__ bool group_any(bool x) {
+    const uint64_t all = __ballot(x);
+    if constexpr (LANES == kWave) return all != 0;
+    else return (all >> lane_id() / LANES * LANES & ((1ull << LANES) - 1)) != 0;
+}
+
+template <int LANES>
+__device__ __forceinline__ Mass join_group(const Mass& a, float c) {
+    Mass r;
+    r.m = lanes_reduce<LANES>(a.m, [](float x, float y) { return x > y ? x : y; });
+    r.s = lanes_sum<LANES>(a.s * exp2_fast(a.m == r.m ? 0.0f : (a.m - r.m) * c));
+    return Mass{group_first<LANES>(r.m), group_first<LANES>(r.s)};
+}
+
+// ---------------------------------------------------------------------------
+// the listed choices of a token: two a lane
 // ---------------------------------------------------------------------------
 constexpr int kLists = kMostListed / kWave;
 
@@ -104,20 +134,22 @@ struct Listed {
     bool first[kLists];  // the first of its number in the list
 };
 
+template <int LANES = kWave>
 __device__ __forceinline__ void load_ids(const ListedArgs& a, uint32_t n, Listed& e) {
     const int32_t* ids = static_cast<const int32_t*>(a.ids.data) + a.ids.at(n, a.shape);
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
-        const int32_t k = i * kWave + lane_id();
+        const int32_t k = i * LANES + group_lane<LANES>();
         e.id[i] = k < a.K ? ids[k] : -1;
     }
 }
 
+template <int LANES = kWave>
 __device__ __forceinline__ void load_values(const ListedArgs& a, const RowsView& rows, uint32_t n, Listed& e) {
     const float* y = static_cast<const float*>(rows.data) + rows.at(n, a.shape);
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
-        const int32_t k = i * kWave + lane_id();
+        const int32_t k = i * LANES + group_lane<LANES>();
         e.y[i] = k < a.K ? y[k] : 0.0f;
     }
 }
@@ -141,19 +173,19 @@ __device__ __forceinline__ void load_scores(const typename Elem<BF16>::T* x, Lis
 
 // Those of a number that the list has before are not the first.  sum: the values of
 // equal numbers are added up at the first, in the list's order.
-template <bool SUM>
+template <bool SUM, int LANES = kWave>
 __device__ void find_first(Listed& e, int32_t K) {
     float y[kLists];
 #pragma unroll
     for (int i = 0; i < kLists; ++i) y[i] = e.y[i];
     for (int32_t j = 0; j < K; ++j) {
-        const int i = j / kWave, from = j % kWave;  // (uniform)
-        const int32_t id = __shfl(i == 0 ? e.id[0] : e.id[1], from, kWave);
-        const float v = __shfl(i == 0 ? y[0] : y[1], from, kWave);
-        if (!__shfl((int)(i == 0 ? e.on[0] : e.on[1]), from, kWave)) continue;
+        const int i = j / LANES, from = j % LANES;
+        const int32_t id = __shfl(i == 0 ? e.id[0] : e.id[1], from, LANES);
+        const float v = __shfl(i == 0 ? y[0] : y[1], from, LANES);
+        if (!__shfl((int)(i == 0 ? e.on[0] : e.on[1]), from, LANES)) continue;
 #pragma unroll
         for (int k = 0; k < kLists; ++k) {
-            const int32_t mine = k * kWave + lane_id();
+            const int32_t mine = k * LANES + group_lane<LANES>();
             if (!e.on[k] || e.id[k] != id || mine == j) continue;
             if (mine > j) e.first[k] = false;
             else if (SUM) e.y[k] += v;
@@ -163,7 +195,7 @@ __device__ void find_first(Listed& e, int32_t K) {
 
 // Marks the listed choices of one or more lanes' elements; true if a number is
 // there twice.  place(id, &word, &bit): false if the choice is not among them.
-template <typename Place>
+template <int LANES = kWave, typename Place>
 __device__ __forceinline__ bool mark(const Listed& e, Place place) {
     bool twice = false;
 #pragma unroll
@@ -172,7 +204,7 @@ __device__ __forceinline__ bool mark(const Listed& e, Place place) {
         uint32_t bit;
         if (e.on[i] && place((uint32_t)e.id[i], &word, &bit)) twice |= (atomicOr(word, bit) & bit) != 0;
     }
-    return __ballot(twice) != 0;
+    return group_any<LANES>(twice);
 }
 
 // elements of a vector whose bits are set, at -infinity
@@ -198,10 +230,11 @@ __device__ __forceinline__ void store_others(typename Elem<BF16>::T* p, const fl
 }
 
 // ---------------------------------------------------------------------------
-// a row from the others' sum and its listed choices, by one wavefront
+// a row from the others' sum and its listed choices, by LANES lanes
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float wave_top(float x) {
-    return lanes_reduce<kWave>(x, [](float p, float q) { return p > q ? p : q; });
+template <int LANES>
+__device__ __forceinline__ float top_of_lanes(float x) {
+    return lanes_reduce<LANES>(x, [](float p, float q) { return p > q ? p : q; });
 }
 
 // a (exp s - 1 - s) for s = log(b / a): b - a - a s, which at small s cancels
@@ -227,18 +260,19 @@ struct RowMass {
     __device__ __forceinline__ float logp(float x, float c) const { return ((x - top) * c - log2_s) * kLn2; }
 };
 
+template <int LANES = kWave>
 __device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others, float c) {
     RowMass r;
     float top = kNone;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.x[i] : kNone);
-    top = wave_top(fmaxf(top, others.m));
+    top = top_of_lanes<LANES>(fmaxf(top, others.m));
     r.top = top != kNone ? top : 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.x[i] - r.top) * c) : 0.0f;
     const float d = others.m == top ? 0.0f : (others.m - top) * c, k = exp2_fast(d);
-    const float S = fmaf(others.s, k, uniform(lanes_sum<kWave>(sum)));
+    const float S = fmaf(others.s, k, group_first<LANES>(lanes_sum<LANES>(sum)));
     r.weight = !(S == 0.0f);  // (a row of NaN alone has no largest score either)
     r.log2_s = r.weight ? log2_fast(S) : 0.0f;
     r.some = !(others.s == 0.0f);
@@ -254,34 +288,36 @@ struct Teacher {
     bool any;
 };
 
+template <int LANES = kWave>
 __device__ __forceinline__ Teacher teacher_row(const ListedArgs& a, const Listed& e) {
     Teacher t{0.0f, 0.0f, 0.0, false};
     bool any = false;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) any |= e.first[i];
-    t.any = __ballot(any) != 0;
+    t.any = group_any<LANES>(any);
     if (a.with_rest) {
         // in 64 bits: what is left of 1 may be far smaller than the sum's own rounding in 32
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp((double)e.y[i]) : 0.0;
-        t.left = 1.0 - wave_sum(sum);
+        t.left = 1.0 - lanes_sum<LANES>(sum);
         return t;
     }
     float top = kNone;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) top = fmaxf(top, e.first[i] ? e.y[i] : kNone);
-    t.top = t.any ? wave_top(top) : 0.0f;
+    t.top = t.any ? top_of_lanes<LANES>(top) : 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.y[i] - t.top) * (a.q_inv_t * kLog2e)) : 0.0f;
-    t.log = t.any ? log2_fast(uniform(lanes_sum<kWave>(sum))) * kLn2 : 0.0f;
+    t.log = t.any ? log2_fast(group_first<LANES>(lanes_sum<LANES>(sum))) * kLn2 : 0.0f;
     return t;
 }
 
 constexpr double kLeastRest = 1.0 / 8388608.0;  // 2^-23: what 32-bit log-probabilities say of a rest at best
 
 // The divergence of a row and what its gradient needs; w: the token's weight.
+template <int LANES = kWave>
 __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const Listed& e, const Mass& others, const RowMass& r,
                                                  const Teacher& t, float w) {
     ListedRow o{};
@@ -308,7 +344,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
         const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
         loss += a.reverse ? curve(p, q, u) : curve(q, p, -u);
     }
-    loss = uniform(lanes_sum<kWave>(loss));
+    loss = group_first<LANES>(lanes_sum<LANES>(loss));
     const float p_rest = r.some ? exp_fast(r.rest) : 0.0f;
     if (!a.with_rest) {
         o.loss = loss + p_rest;
@@ -341,29 +377,30 @@ __device__ __forceinline__ float listed_gradient(const ListedArgs& a, const List
     return o.w * fmaf(p, o.over, apart_by(q, p, -u));
 }
 
+template <int LANES = kWave>
 __device__ __forceinline__ void write_scores(const ListedArgs& a, uint32_t n, int64_t at, const Listed& e, const Mass& others) {
-    const RowMass r = row_mass(e, others, a.c);
+    const RowMass r = row_mass<LANES>(e, others, a.c);
     float* out = static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape);
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
-        const int32_t k = i * kWave + lane_id();
+        const int32_t k = i * LANES + group_lane<LANES>();
         if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.c) : kNone;
     }
-    if (lane_id() != 0) return;
+    if (group_lane<LANES>() != 0) return;
     if (a.rest) a.rest[at] = r.rest;
     if (a.lse) a.lse[at] = r.weight ? fmaf(r.top, a.inv_t, fmaf(r.top, a.inv_lo, r.log2_s * kLn2)) : kNone;
 }
 
-// per-token outputs of a token that does not count, by a wavefront
-template <int MODE>
+// per-token outputs of a token that does not count, by LANES lanes
+template <int MODE, int LANES = kWave>
 __device__ __forceinline__ void write_nothing(const ListedArgs& a, uint32_t n, int64_t at) {
     if constexpr (MODE == SCORES) {
         float* out = static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape);
-        for (int32_t k = lane_id(); k < a.K; k += kWave) out[k] = 0.0f;
-        if (lane_id() == 0 && a.rest) a.rest[at] = 0.0f;
-        if (lane_id() == 0 && a.lse) a.lse[at] = 0.0f;
+        for (int32_t k = group_lane<LANES>(); k < a.K; k += LANES) out[k] = 0.0f;
+        if (group_lane<LANES>() == 0 && a.rest) a.rest[at] = 0.0f;
+        if (group_lane<LANES>() == 0 && a.lse) a.lse[at] = 0.0f;
     } else {
-        if (lane_id() == 0) a.loss[at] = 0.0f;
+        if (group_lane<LANES>() == 0) a.loss[at] = 0.0f;
     }
 }
 
@@ -526,20 +563,22 @@ __global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// short rows: a wavefront each, up to E elements a lane
+// short rows: LANES lanes each, up to E elements a lane
 // ---------------------------------------------------------------------------
 // The list's part of a row bounds it, not the row (fp32, K = 8 of 300, distillation:
-// 65,536 rows 82 us; 244 rows of 257, 43% of them live: 8.0, of which a launch is 2.3).
-// The loss's workgroups are few, since each draws a ticket; a large batch has them of
-// 1,024 (65,536 rows of 18: 103 to 77 us).
-template <bool BF16, int MODE, int NT>
+// 65,536 rows 82 us; 244 rows of 257, 43% of them live: 7.8, of which a launch is 2.3).
+// So many rows of up to 64 choices with short lists share a wavefront, 16 lanes each
+// (65,536 rows of 18, K = 8: 23 us, a wavefront each 77; scores of 5 choices 8.6 against
+// 29).  The loss's workgroups are few, since each draws a ticket; a large batch has
+// them of 1,024 threads (256: 103 us for the 77).
+template <bool BF16, int MODE, int NT, int LANES, int E>
 __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
     using T = typename Elem<BF16>::T;
-    constexpr int kRows = NT / kWave, E = kShortElems;
-    static_assert(E <= 32, "a word of bits a lane");
-    __shared__ uint32_t s_bits[kRows][kWave];
+    constexpr int kRows = NT / LANES;
+    static_assert(E <= 32 && kRows <= kWave, "a word of bits a lane");
+    __shared__ uint32_t s_bits[kRows][LANES];
     __shared__ double s_sum[kDistillSums][kRows];
-    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane_id();
+    const uint32_t w = LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : threadIdx.x / LANES, l = group_lane<LANES>();
     const uint32_t n_rows = (uint32_t)(a.shape.B * a.shape.T), V = (uint32_t)a.V;
     uint32_t* bits = s_bits[w];
     double sums[kDistillSums] = {0.0, 0.0};
@@ -549,41 +588,41 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
         const T* x = static_cast<const T*>(a.x.data) + a.x.at(n, a.shape);
         T* dx = MODE == DISTILL && a.has_dx ? static_cast<T*>(a.dx.data) + a.dx.at(n, a.shape) : nullptr;
         if (a.mask && !a.mask[at]) {
-            write_nothing<MODE>(a, n, at);
+            write_nothing<MODE, LANES>(a, n, at);
             if (MODE == DISTILL && a.has_dx) {
-                for (uint32_t j = l; j < V; j += kWave) dx[j] = Elem<BF16>::round(0.0f);
+                for (uint32_t j = l; j < V; j += LANES) dx[j] = Elem<BF16>::round(0.0f);
             }
             continue;
         }
         Listed e;
-        load_ids(a, n, e);
-        if constexpr (MODE == DISTILL) load_values(a, a.teacher, n, e);
+        load_ids<LANES>(a, n, e);
+        if constexpr (MODE == DISTILL) load_values<LANES>(a, a.teacher, n, e);
         float v[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = l + i * kWave < V ? Elem<BF16>::one(x[l + i * kWave]) : kNone;
+        for (int i = 0; i < E; ++i) v[i] = l + i * LANES < V ? Elem<BF16>::one(x[l + i * LANES]) : kNone;
         check_ids<MODE == DISTILL>(a, e, true);
         load_scores<BF16>(x, e);
         wave_fence();  // (the last row's bits are read)
         bits[l] = 0;
         wave_fence();
-        const bool twice = mark(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
-            *word = bits + id % kWave;
-            *bit = 1u << id / kWave;
+        const bool twice = mark<LANES>(e, [&](uint32_t id, uint32_t** word, uint32_t* bit) {
+            *word = bits + id % LANES;
+            *bit = 1u << id / LANES;
             return true;
         });
-        if (twice) find_first<false>(e, a.K);
+        if (twice) find_first<false, LANES>(e, a.K);
         wave_fence();
         const uint32_t marked = bits[l];
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = marked >> i & 1 ? kNone : v[i];
         Mass others = no_mass();
         accumulate_mass(others, v, a.c);
-        others = join_mass<kWave>(others, a.c);
+        others = join_group<LANES>(others, a.c);
         if constexpr (MODE == SCORES) {
-            write_scores(a, n, at, e, others);
+            write_scores<LANES>(a, n, at, e, others);
         } else {
             const double part = token_part(a, n, at, counts);
-            const ListedRow o = distill_row(a, e, others, row_mass(e, others, a.c), teacher_row(a, e), (float)(part * a.scale));
+            const ListedRow o = distill_row<LANES>(a, e, others, row_mass<LANES>(e, others, a.c), teacher_row<LANES>(a, e), (float)(part * a.scale));
             if (l == 0) a.loss[at] = o.loss;
             sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
             sums[1] += (double)o.loss;
@@ -591,7 +630,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
                 const bool none = o.coef == 0.0f;  // whatever the scores are
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const uint32_t j = l + i * kWave;
+                    const uint32_t j = l + i * LANES;
                     if (j < V && !(marked >> i & 1))
                         dx[j] = Elem<BF16>::round(none ? 0.0f : o.coef * exp2_fast((v[i] - o.base) * a.c));
                 }
@@ -608,7 +647,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
         }
         __syncthreads();
         if (threadIdx.x >= kWave) return;
-        const double v0 = lanes_sum<kRows>(s_sum[0][l % kRows]), v1 = lanes_sum<kRows>(s_sum[1][l % kRows]);
+        const double v0 = lanes_sum<kRows>(s_sum[0][lane_id() % kRows]), v1 = lanes_sum<kRows>(s_sum[1][lane_id() % kRows]);
         finish_distill(a, blockIdx.x, gridDim.x, v0, v1, counts.tokens);
     }
 }
@@ -1132,16 +1171,24 @@ hipError_t launch_gradient(const ListedArgs& a, hipStream_t s) {
 template <bool BF16, int MODE>
 hipError_t launch_short(const ListedArgs& a, hipStream_t s) {
     const int64_t rows = a.shape.B * a.shape.T;
-    auto go = [&](auto threads) {
-        constexpr int NT = decltype(threads)::value, kRows = NT / kWave;
+    auto go = [&](auto threads, auto lanes, auto elems) {
+        constexpr int NT = decltype(threads)::value, LANES = decltype(lanes)::value, E = decltype(elems)::value, kRows = NT / LANES;
         const int64_t want = (rows + kRows - 1) / kRows;
         // (the loss's workgroups each leave a sum)
         const dim3 grid = MODE == DISTILL ? dim3((unsigned)(want < kPolicyBlocks ? want : kPolicyBlocks)) : grid_of(want, NT);
-        hipLaunchKernelGGL((k_listed_short<BF16, MODE, NT>), grid, dim3(NT), 0, s, a);
+        hipLaunchKernelGGL((k_listed_short<BF16, MODE, NT, LANES, E>), grid, dim3(NT), 0, s, a);
         return hipGetLastError();
     };
-    if (MODE == DISTILL && rows > 8 * kPolicyBlocks) return go(std::integral_constant<int, 1024>{});
-    return go(std::integral_constant<int, kListedThreads>{});
+    using Small = std::integral_constant<int, kListedThreads>;
+    using Large = std::integral_constant<int, 1024>;
+    using Part = std::integral_constant<int, kFewLanes>;
+    using Wave = std::integral_constant<int, kWave>;
+    using Few = std::integral_constant<int, kFewElems>;
+    using Elems = std::integral_constant<int, kShortElems>;
+    // (a sequence's tokens are counted by whole wavefronts where no launch has counted them, up to kPolicyBlocks rows)
+    const bool few = rows > kPolicyBlocks && a.V <= kFewElems * kFewLanes && a.K <= kLists * kFewLanes;
+    if (MODE == DISTILL && rows > (few ? 32 : 8) * kPolicyBlocks) return few ? go(Large{}, Part{}, Few{}) : go(Large{}, Wave{}, Elems{});
+    return few ? go(Small{}, Part{}, Few{}) : go(Small{}, Wave{}, Elems{});
 }
 
 template <bool BF16, int MODE>

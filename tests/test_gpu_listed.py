@@ -357,6 +357,61 @@ def test_distill_loss(V, dtype):
         _close(again[0], loss, 8 * _bound(z, tau) * (1 + np.abs(loss)) + 8 * _bound(z, tau) * 20)  # without the gradient
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [1, 2, 5, 16, 17, 33, 63, 64])
+def test_rows_that_share_a_wavefront(V, dtype):
+    """Many rows of few choices: a part of a wavefront each, some of them masked, empty, with numbers twice or not finite."""
+    rng = np.random.default_rng(V)
+    B, T, tau = 6, 119, 0.8
+    x, _ = _logits(rng, B, T, V, dtype)
+    x[1, 5], x[1, 6, V // 2], x[2, 7] = -np.inf, -np.inf, -np.inf
+    z = x.double().cpu().numpy()
+    mask = _mask(rng, B, T)
+    for K in (1, 16, 17, 32, 33):
+        ids = _ids(rng, B, T, V, K)
+        want = ref.listed_logprobs(z, ids, mask, tau)
+        out = [torch.full(s, NAN, device="cuda") for s in ((B, T, K), (B, T), (B, T))]
+        cd.conduit_listed_logprobs(x, _gpu(ids), out[0], rest=out[1], lse=out[2], mask=_gpu(mask), temperature=tau)
+        for g, w in zip(out, want):
+            _close(host(g), w, _bound(z, tau))
+    weight = rng.random((B, T)).astype(np.float32)
+    weight[mask == 0] = NAN
+    for i, opts in enumerate(FORMS):
+        ids, y = _teacher(rng, np.where(np.isfinite(z), z, -20.0), (3, 20, 32)[i])
+        ids[0, ::3] = np.where(rng.random(ids[0, ::3].shape) < 0.3, ids[0, ::3, :1], ids[0, ::3])
+        y[3, ::4, 0] = -np.inf
+        ids[4, ::5] = -1
+        if opts["loss"] == "reverse":  # (a teacher's choice at -inf of the student's would be infinite only forward)
+            ids[1, 6] = -1
+        for m in (mask, None):
+            loss, stats = _check_distill(x, z, ids, y, m, np.nan_to_num(weight, nan=0.5) if m is None else weight, tau, dtype, opts,
+                                         in_place=i == 1)
+
+
+def test_many_rows_that_share_a_wavefront():
+    """The same bits from one large batch as from its halves."""
+    rows, V, K = 36000, 18, 7
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for dtype in (F32, BF16):
+        x = torch.randn((1, rows, V), generator=g, device="cuda").mul_(2).to(dtype)
+        ids = torch.randint(-1, V, (1, rows, K), generator=g, device="cuda", dtype=torch.int32)
+        y = torch.log_softmax(torch.randn((1, rows, K), generator=g, device="cuda"), -1) - 0.1
+        mask = (torch.rand((1, rows), generator=g, device="cuda") < 0.6).to(torch.uint8)
+        outs = [[torch.full_like(t, 9) for t in (x, y[..., 0], y, y[..., 0])] for _ in range(2)]
+        stats = torch.empty((3, 3), device="cuda")
+        opts = cd.distill_opts(rest=True, reduction="sum")
+        parts = [slice(0, rows), slice(0, rows // 2), slice(rows // 2, rows)]
+        for i, h in enumerate(parts):
+            dx, loss, logps, rest = outs[min(i, 1)]
+            cd.conduit_distill_loss(opts, x[:, h], ids[:, h], y[:, h], loss[:, h], stats[i], dlogits=dx[:, h], mask=mask[:, h])
+            cd.conduit_listed_logprobs(x[:, h], ids[:, h], logps[:, h], rest=rest[:, h], mask=mask[:, h])
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+        s = host(stats).astype(np.float64)
+        _close(s[0, 0], s[1, 0] + s[2, 0], 2.0 ** -22 * s[0, 0])
+        assert s[0, 2] == s[1, 2] + s[2, 2] == int(mask.sum())
+
+
 @pytest.mark.parametrize("V", [6, 50, 900, 5000, 40000])
 @pytest.mark.parametrize("opts", FORMS)
 def test_distill_entries_that_do_not_count(V, opts):
