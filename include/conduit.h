@@ -783,10 +783,11 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * Listed choices: a few choices of every token instead of all of them.  A
  * listed array holds K numbers of choices (ids: I32) or K values (F32) a token,
  * rows of 1 <= K <= 128 elements in the layout of the logits' rows.  Scores,
- * workspaces, masks and errors as above.  A row with a NaN or +inf gives NaN in
- * all that it is asked for (in its own outputs, and in the sums it counts in).  A
- * row is summed in an order that goes by its alignment in memory: a call gives the
- * same bits every time, the same values elsewhere may differ in the last places.
+ * workspaces, masks and errors as above.  A row with a NaN or +inf gives NaN
+ * wherever its scores count (not for entries without a choice, nor in what a
+ * token of weight 0 adds).  A row is summed in an order that goes by its alignment
+ * in memory: a call gives the same bits every time, the same values elsewhere may
+ * differ in the last places.
  * ------------------------------------------------------------------------- */
 
 /*
@@ -796,10 +797,10 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * falling order of their logits, the lowest number first among equal ones (-0
  * and 0 are equal), choices at -inf among them; beyond V choices the number -1
  * with log-probability -inf.  Masked tokens have 0 in both, and so have tokens
- * outside [0, V), which are flagged.  A row with a NaN or
- * +inf has no ranking: its numbers are -1 and its log-probabilities NaN.  tokens
- * may be NULL (then logp must be); logp, lse and entropy may be.  ids and logps
- * are apart from each other and from every other array of the call.
+ * outside [0, V), which are flagged.  A row with a NaN or +inf has no ranking: its
+ * numbers are -1 and its log-probabilities NaN.  tokens may be NULL (then logp must
+ * be); logp, lse and entropy may be.  ids and logps are apart from each other and
+ * from every other array of the call.
  * Rows of up to 4,096 choices share a wavefront or take one, wider ones a
  * workgroup; fewer rows than the GPU has compute units, and rows of more than 2^18
  * bf16 (2^17 float) choices, are split into parts that the row's last workgroup
