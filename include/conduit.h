@@ -798,7 +798,8 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * and 0 are equal), choices at -inf among them; beyond V choices the number -1
  * with log-probability -inf.  Masked tokens have 0 in both, and so have tokens
  * outside [0, V), which are flagged.  A row with a NaN or +inf has no ranking: its
- * numbers are -1 and its log-probabilities NaN.  tokens may be NULL (then logp must
+ * numbers are -1 and its log-probabilities NaN; finite logits have theirs whatever
+ * their size and the temperature.  tokens may be NULL (then logp must
  * be); logp, lse and entropy may be.  ids and logps are apart from each other and
  * from every other array of the call.
  * Rows of up to 4,096 choices share a wavefront or take one, wider ones a
