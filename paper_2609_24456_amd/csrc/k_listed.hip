@@ -348,7 +348,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
     const float p_rest = r.some ? exp_fast(r.rest) : 0.0f;
     if (!a.with_rest) {
         o.loss = loss + p_rest;
-        o.coef = r.some ? o.w * r.share : 0.0f;
+        o.coef = r.some && o.w != 0.0f ? o.w * r.share : 0.0f;  // (a share that is no number counts for nothing at weight 0)
         return o;
     }
     const double kept = r.some ? (t.left > kLeastRest ? t.left : kLeastRest) : 0.0;
