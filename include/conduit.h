@@ -787,7 +787,8 @@ conduit_status conduit_head_logprobs_backward(const conduit_rows* hidden, const 
  * wherever its scores count (not for entries without a choice, nor in what a
  * token of weight 0 adds).  A row is summed in an order that goes by its alignment
  * in memory: a call gives the same bits every time, the same values elsewhere may
- * differ in the last places.
+ * differ in the last places.  Wide rows are worked on in parts (of 1,024 elements
+ * or more); a batch that would take 2^31 of them is refused.
  * ------------------------------------------------------------------------- */
 
 /*

@@ -1151,10 +1151,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
 
 template <bool BF16, bool SPLIT>
 hipError_t launch_gradient(const ListedArgs& a, hipStream_t s) {
-    const int64_t nv = a.V / Elem<BF16>::kPer;
-    const int64_t per_row = nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
-    const int64_t items = a.shape.B * a.shape.T * per_row;
-    if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
+    const int64_t per_row = gradient_parts(a.V, BF16);
+    const int64_t items = a.shape.B * a.shape.T * per_row;  // fewer than 2^31 (the caller's check)
     auto go = [&](auto past) {
         hipLaunchKernelGGL((k_listed_gradient<BF16, SPLIT, decltype(past)::value>),
                            grid_of((items + kListedThreads / kWave - 1) / (kListedThreads / kWave), kListedThreads), dim3(kListedThreads), 0,
@@ -1194,8 +1192,7 @@ hipError_t launch_short(const ListedArgs& a, hipStream_t s) {
 template <bool BF16, int MODE>
 hipError_t launch_scan(const ListedArgs& a, hipStream_t s) {
     constexpr int kPer = Elem<BF16>::kPer;
-    const int64_t rows = a.shape.B * a.shape.T, items = rows * a.parts;
-    if (items >= 1ll << 31) return hipErrorInvalidValue;  // (the division's range)
+    const int64_t rows = a.shape.B * a.shape.T, items = rows * a.parts;  // fewer than 2^31 (the caller's check)
     constexpr int kTile = kListedThreads * kScanVectors;
     const unsigned lds = (a.per + kTile - 1) / kTile * (kTile * kPer / 8);
     // (with a gradient to come the rows are read again)
@@ -1274,6 +1271,11 @@ RowParts listed_parts(int64_t rows, int64_t V, bool bf16, bool whole_rows) {
         if (split > parts) parts = split;
     }
     return RowParts{(int32_t)parts, (int32_t)((nv + parts - 1) / parts)};
+}
+
+int64_t gradient_parts(int64_t V, bool bf16) {
+    const int64_t nv = V / (bf16 ? 8 : 4);
+    return nv > 0 ? (nv + kGradK * kWave - 1) / (kGradK * kWave) : 1;
 }
 
 hipError_t launch_listed_logprobs(const ListedArgs& a, bool bf16, hipStream_t s) {

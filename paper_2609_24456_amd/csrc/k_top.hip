@@ -792,9 +792,7 @@ hipError_t alternatives(const TopArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((k_top_wave<BF16>), each, dim3(kTopThreads), 0, s, a);
         return hipGetLastError();
     }
-    // one launch takes fewer than 2^31 parts (the division's range)
-    const int64_t items = rows * a.parts;
-    if (items >= 1ll << 31) return hipErrorInvalidValue;
+    const int64_t items = rows * a.parts;  // fewer than 2^31 (the caller's check)
     auto go = [&](auto once) {
         hipLaunchKernelGGL((k_top_rows<BF16, decltype(once)::value>), grid_of(items, kTopThreads), dim3(kTopThreads),
                            sizeof(float) * (a.per / kGroup), s, a);

@@ -49,6 +49,13 @@ conduit_status check_outputs_apart(std::initializer_list<const void*> outs, std:
     return CONDUIT_OK;
 }
 
+// One launch takes fewer than 2^31 parts of rows (the range of the division that finds a part's row).  Checked before
+// anything is enqueued: a call that has begun leaves the workspace's counters for its last launch to clear.
+conduit_status check_parts(int64_t B, int64_t T, int64_t parts) {
+    if (B * T * parts >= 1ll << 31) return bad("the rows of the batch must take fewer than 2^31 parts in all");
+    return CONDUIT_OK;
+}
+
 conduit_status check_K(int64_t K) {
     if (K < 1 || K > kMostListed) return bad("the number of choices a token must be in [1, 128]");
     return CONDUIT_OK;
@@ -159,6 +166,7 @@ conduit_status conduit_token_alternatives(const conduit_rows* logits, int64_t B,
     CONDUIT_TRY(check_apart(logps, "logps", {logits}, {tokens, logp, lse, entropy}, mask, B, T, stride));
     CONDUIT_TRY(check_outputs_apart({logp, lse, entropy}, {logits}, mask, B, T, stride));
     const ListedLayout l = top_layout(B, T, logits, ids->width);
+    CONDUIT_TRY(check_parts(B, T, l.split.parts));
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));
     uint32_t* err = nullptr;
     CONDUIT_TRY(standalone_error_words(&err));
@@ -195,6 +203,7 @@ conduit_status conduit_listed_logprobs(const conduit_rows* logits, int64_t B, in
     CONDUIT_TRY(check_apart(logps, "logps", {logits, ids}, {rest, lse}, mask, B, T, stride));
     CONDUIT_TRY(check_outputs_apart({rest, lse}, {logits, ids}, mask, B, T, stride));
     const ListedLayout l = listed_layout(B, T, logits, false);
+    CONDUIT_TRY(check_parts(B, T, l.split.parts));
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));
     uint32_t* err = nullptr;
     CONDUIT_TRY(standalone_error_words(&err));
@@ -222,6 +231,7 @@ conduit_status conduit_listed_logprobs_backward(const conduit_rows* logits, int6
     if (drest && !rest) return bad("the gradient of the rest needs the rest");
     CONDUIT_TRY(check_outputs({}, {lse, rest, drest}, nullptr, B, T, stride));
     CONDUIT_TRY(check_apart(dlogits, "dlogits", {ids, dlogps}, {lse, rest, drest}, mask, B, T, stride));
+    CONDUIT_TRY(check_parts(B, T, gradient_parts(logits->width, logits->dtype == CONDUIT_BF16)));
     uint32_t* err = nullptr;
     CONDUIT_TRY(standalone_error_words(&err));
     ListedArgs a{};
@@ -280,6 +290,8 @@ conduit_status conduit_distill_loss(const conduit_distill_opts* opts, const cond
         if (mask && !apart(stats, 12, mask, each)) return bad("stats must be apart from the call's other arrays");
     }
     const ListedLayout l = distill_layout(B, T, logits, dlogits != nullptr);
+    CONDUIT_TRY(check_parts(B, T, l.split.parts));
+    if (dlogits && l.split.parts > 1) CONDUIT_TRY(check_parts(B, T, gradient_parts(logits->width, logits->dtype == CONDUIT_BF16)));
     CONDUIT_TRY(check_workspace(workspace, workspace_bytes, l.l.bytes));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (empty) return launched(launch_fill_u32(reinterpret_cast<uint32_t*>(stats), 0u, 3, s), "distillation launch");

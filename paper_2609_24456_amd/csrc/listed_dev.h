@@ -17,6 +17,7 @@ struct RowParts {
 };
 RowParts top_parts(int64_t rows, int64_t V, bool bf16);
 RowParts listed_parts(int64_t rows, int64_t V, bool bf16, bool whole_rows);
+int64_t gradient_parts(int64_t V, bool bf16);  // wavefronts that a row's gradient takes where it has a launch of its own
 
 // The K most probable choices of every token.
 struct TopArgs {
