@@ -1185,7 +1185,9 @@ hipError_t launch_short(const ListedArgs& a, hipStream_t s) {
     using Elems = std::integral_constant<int, kShortElems>;
     // (a sequence's tokens are counted by whole wavefronts where no launch has counted them, up to kPolicyBlocks rows)
     const bool few = rows > kPolicyBlocks && a.V <= kFewElems * kFewLanes && a.K <= kLists * kFewLanes;
-    if (MODE == DISTILL && rows > (few ? 32 : 8) * kPolicyBlocks) return few ? go(Large{}, Part{}, Few{}) : go(Large{}, Wave{}, Elems{});
+    if constexpr (MODE == DISTILL) {
+        if (rows > (few ? 32 : 8) * kPolicyBlocks) return few ? go(Large{}, Part{}, Few{}) : go(Large{}, Wave{}, Elems{});
+    }
     return few ? go(Small{}, Part{}, Few{}) : go(Small{}, Wave{}, Elems{});
 }
 
