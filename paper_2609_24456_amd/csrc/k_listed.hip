@@ -388,7 +388,7 @@ __device__ __forceinline__ void write_scores(const ListedArgs& a, uint32_t n, in
     }
     if (group_lane<LANES>() != 0) return;
     if (a.rest) a.rest[at] = r.rest;
-    if (a.lse) a.lse[at] = r.weight ? fmaf(r.top, a.inv_t, fmaf(r.top, a.inv_lo, r.log2_s * kLn2)) : kNone;
+    if (a.lse) a.lse[at] = r.weight ? log_normaliser(r.top, r.log2_s * kLn2, a.inv_t, a.inv_lo) : kNone;
 }
 
 // per-token outputs of a token that does not count, by LANES lanes

@@ -84,8 +84,15 @@ struct RowValues {
     float lse, entropy, logp, one_minus_p;
 };
 
-// inv_lo: what the rounding of 1 / temperature to inv_t left, which at a large
-// maximum is as much as the rounding of lse itself (0: not counted)
+// max x / temperature + log_s.  inv_lo: what the rounding of 1 / temperature to inv_t
+// left, which at a large maximum is as much as the rounding of lse itself (0: not
+// counted).  Where its share is past the largest float the score is by far, and lse is
+// the score's infinity, whatever the share's sign.
+__device__ __forceinline__ float log_normaliser(float m, float log_s, float inv_t, float inv_lo) {
+    const float lo = fmaf(m, inv_lo, log_s);
+    return fabsf(lo) == INFINITY ? m * inv_t : fmaf(m, inv_t, lo);
+}
+
 __device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float c, float inv_t, float inv_lo) {
     RowValues r;
     if (st.s == 0.0f) {
@@ -96,7 +103,7 @@ __device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float 
     r.base = st.m;
     r.inv_s = 1.0f / st.s;
     r.log2_s = log2_fast(st.s);
-    r.lse = fmaf(st.m, inv_t, fmaf(st.m, inv_lo, r.log2_s * kLn2));
+    r.lse = log_normaliser(st.m, r.log2_s * kLn2, inv_t, inv_lo);
     r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
     r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
     r.one_minus_p = -expm1_fast(r.logp);
