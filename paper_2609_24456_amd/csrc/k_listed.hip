@@ -1111,9 +1111,8 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     if (twice) find_first<!SPLIT>(e, a.K);
     wave_fence();
     const uint32_t marked = bits[lane], marked_beside = bits[kWave + lane / 32] >> lane % 32 & 1;
-    auto log_p = [&](float f) {  // as FromLse in k_logits.hip, for what may be far from 0
-        return fmaf(f, a.inv_t, fmaf(fmaxf(f, -3.4028235e38f), a.inv_lo, -lse));
-    };
+    const LogP by{a.inv_t, a.inv_lo, a.lowest, lse};
+    auto log_p = [&](float f) { return by.of(f); };
     // of any other choice: coef times its share of the rest (with h), or its probability
     float coef, shift = 0.0f;
     if constexpr (SPLIT) {

@@ -383,13 +383,10 @@ constexpr int kGradK = 4;
 
 // by the log-normaliser given
 struct FromLse {
-    float inv_t, inv_lo, lse, entropy;
+    float inv_t, entropy;
+    LogP by;
     RowGrad g;
-    // The scores are far from 0 where log p_j need not be, so a rounded 1 / temperature would cost |z_j| 2^-25 of p_j:
-    // its rest goes along (of the lowest finite value for a choice at -inf: the rest may be 0).
-    __device__ __forceinline__ float log_p(float f) const {
-        return fmaf(f, inv_t, fmaf(fmaxf(f, -3.4028235e38f), inv_lo, -lse));
-    }
+    __device__ __forceinline__ float log_p(float f) const { return by.of(f); }
     __device__ __forceinline__ bool with_entropy() const { return g.h != 0.0f; }
     template <bool ENT>
     __device__ __forceinline__ float of(float f, float gj) const {
@@ -442,12 +439,11 @@ __global__ __launch_bounds__(kGradThreads) void k_rows_gradient(LogitsArgs a, ui
         if (ok) grad.r = a.split[n];
     } else {
         grad.inv_t = a.inv_t;
-        grad.inv_lo = a.inv_lo;
-        grad.lse = ok ? a.lse_in[at] : 0.0f;
+        grad.by = LogP{a.inv_t, a.inv_lo, a.lowest, ok ? a.lse_in[at] : 0.0f};
         grad.g.g = ok && a.g ? a.g[at] : 0.0f;
         grad.g.h = ok && a.h ? a.h[at] : 0.0f;
         grad.entropy = ok && a.entropy_in ? a.entropy_in[at] : 0.0f;
-        weight = ok && grad.lse != kNone;
+        weight = ok && grad.by.lse != kNone;
     }
     if (!weight) {  // nothing counts, or a row without weight
 #pragma unroll

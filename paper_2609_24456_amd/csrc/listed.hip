@@ -236,6 +236,7 @@ conduit_status conduit_listed_logprobs_backward(const conduit_rows* logits, int6
     CONDUIT_TRY(standalone_error_words(&err));
     ListedArgs a{};
     common_args(a, logits, B, T, stride, ids, mask, temperature, err);
+    a.lowest = lowest_score(a.inv_lo);
     a.lse_in = lse;
     a.rest_in = rest;
     a.g = view(dlogps);

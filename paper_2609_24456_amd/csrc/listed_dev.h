@@ -63,7 +63,7 @@ struct ListedArgs {
     TokenShape shape;
     RowsView x, dx;
     int64_t V;
-    float c, inv_t, inv_lo;
+    float c, inv_t, inv_lo, lowest;
     bool once;  // as in TopArgs
     const uint8_t* mask;
     RowsView ids;

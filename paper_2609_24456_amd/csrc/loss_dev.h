@@ -91,6 +91,7 @@ struct LogitsArgs {
     float c;      // log2(e) / temperature
     float inv_t;  // 1 / temperature
     float inv_lo; // what its rounding left
+    float lowest; // logits below it have no weight (lowest_score)
     const int32_t* tokens;
     const uint8_t* mask;
     float* logp;

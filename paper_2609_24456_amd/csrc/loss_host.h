@@ -133,6 +133,13 @@ inline conduit_status check_temperature(double t) {
     return CONDUIT_OK;
 }
 
+// The lowest logit whose product with inv_lo, what rounding 1 / temperature left, is a float: the type's lowest, or one
+// whose score is past the largest float by far (times 1 / temperature, which is at least 2^23 times inv_lo).
+inline float lowest_score(float inv_lo) {
+    constexpr float kMost = 3.4028235e38f;
+    return std::fabs(inv_lo) < 1.0f ? -kMost : -0.5f * kMost / std::fabs(inv_lo);
+}
+
 inline conduit_status check_workspace(const void* ws, uint64_t bytes, uint64_t need) {
     if (!ws) return bad("NULL workspace");
     if (misaligned(ws, 256)) return bad("the workspace must be 256-byte aligned");

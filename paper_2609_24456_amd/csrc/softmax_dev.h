@@ -76,6 +76,15 @@ __device__ __forceinline__ Stat join_lanes(const Stat& a, float c) {
     return r;
 }
 
+// log p of a score, by the log-normaliser given.  The scores are far from 0 where log p
+// need not be, so a rounded 1 / temperature would cost |z| 2^-25 of p: its rest goes
+// along, from the score `lowest` on (below, -infinity among them, p is 0 whatever the
+// rest, which times the score could be no number, or the other infinity).
+struct LogP {
+    float inv_t, inv_lo, lowest, lse;
+    __device__ __forceinline__ float of(float x) const { return fmaf(x, inv_t, fmaf(fmaxf(x, lowest), inv_lo, -lse)); }
+};
+
 // what a row's statistics say
 struct RowValues {
     float base;     // m, or 0 in a row without weight
