@@ -157,6 +157,17 @@ def _row_of(row, listed, temperature):
     return z - log_sum, logrest, top / temperature + log_sum
 
 
+def _shares(row, listed, temperature):
+    """Every choice's share of the probability of those not in `listed`, 0 for these: by the others' own largest score (a
+    difference of log-probabilities of 1e30 holds nothing of it)."""
+    out, others = np.zeros(row.shape), np.ones(row.shape, bool)
+    others[sorted(set(listed))] = False
+    if others.any() and row[others].max() > -np.inf:
+        out[others] = np.exp((row[others] - row[others].max()) / temperature)
+        out /= out.sum()
+    return out
+
+
 def listed_logprobs(logits, ids, mask=None, temperature=1.0):
     """(log-probabilities of ids, log-probability of all others, log-normaliser)."""
     x = np.asarray(logits, np.float64)
@@ -186,9 +197,7 @@ def listed_gradient(logits, ids, g, h=None, mask=None, temperature=1.0):
             d[at] -= g[at][k] * p
             d[at][j] += g[at][k]
         if h is not None and rest > -np.inf:
-            share = np.exp(logp - rest)
-            share[[j for _, j in entries]] = 0
-            d[at] += h[at] * (share - p)
+            d[at] += h[at] * (_shares(x[at], [j for _, j in entries], temperature) - p)
     return d / temperature
 
 
@@ -238,7 +247,7 @@ def distill_loss(logits, ids, teacher, loss="forward", rest=False, teacher_tempe
             g = p * (q.sum() + q_rest)
             g[js] -= q
             if some:
-                g[others] -= np.exp(logp[others] - logrest) * q_rest
+                g -= _shares(x[at], js, temperature) * q_rest
             used = q > 0
         else:
             used = p[js] > 0
