@@ -257,11 +257,11 @@ struct RowMass {
     float top, log2_s;   // M (0 in a row without weight), log2 S
     float share, rest;   // 2^(c (m - M)) / S, log p_rest
     bool weight, some;   // anything but -infinity in the row, among the others
-    __device__ __forceinline__ float logp(float x, float c) const { return ((x - top) * c - log2_s) * kLn2; }
+    __device__ __forceinline__ float logp(float x, float c, float inv_t) const { return log_p_from(x - top, c, inv_t, log2_s); }
 };
 
 template <int LANES = kWave>
-__device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others, float c) {
+__device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others, float c, float inv_t) {
     RowMass r;
     float top = kNone;
 #pragma unroll
@@ -271,13 +271,14 @@ __device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others,
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.x[i] - r.top) * c) : 0.0f;
-    const float d = others.m == top ? 0.0f : (others.m - top) * c, k = exp2_fast(d);
+    const float away = others.m == top ? 0.0f : others.m - top, d = away * c, k = exp2_fast(d);
     const float S = fmaf(others.s, k, group_first<LANES>(lanes_sum<LANES>(sum)));
     r.weight = !(S == 0.0f);  // (a row of NaN alone has no largest score either)
     r.log2_s = r.weight ? log2_fast(S) : 0.0f;
     r.some = !(others.s == 0.0f);
     r.share = r.weight ? k / S : 0.0f;
     r.rest = r.some ? (log2_fast(others.s) + d - r.log2_s) * kLn2 : kNone;
+    if (r.some && r.rest == kNone) r.rest = away * inv_t;  // (as in log_p_from: the logarithms are nothing beside it)
     return r;
 }
 
@@ -340,7 +341,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         if (!e.first[i]) continue;
-        const float lq = (e.y[i] - t.top) * a.q_inv_t - t.log, lp = r.logp(e.x[i], a.c);
+        const float lq = (e.y[i] - t.top) * a.q_inv_t - t.log, lp = r.logp(e.x[i], a.c, a.inv_t);
         const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
         loss += a.reverse ? curve(p, q, u) : curve(q, p, -u);
     }
@@ -379,12 +380,12 @@ __device__ __forceinline__ float listed_gradient(const ListedArgs& a, const List
 
 template <int LANES = kWave>
 __device__ __forceinline__ void write_scores(const ListedArgs& a, uint32_t n, int64_t at, const Listed& e, const Mass& others) {
-    const RowMass r = row_mass<LANES>(e, others, a.c);
+    const RowMass r = row_mass<LANES>(e, others, a.c, a.inv_t);
     float* out = static_cast<float*>(a.logps.data) + a.logps.at(n, a.shape);
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         const int32_t k = i * LANES + group_lane<LANES>();
-        if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.c) : kNone;
+        if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.c, a.inv_t) : kNone;
     }
     if (group_lane<LANES>() != 0) return;
     if (a.rest) a.rest[at] = r.rest;
@@ -622,7 +623,7 @@ __global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
             write_scores<LANES>(a, n, at, e, others);
         } else {
             const double part = token_part(a, n, at, counts);
-            const ListedRow o = distill_row<LANES>(a, e, others, row_mass<LANES>(e, others, a.c), teacher_row<LANES>(a, e), (float)(part * a.scale));
+            const ListedRow o = distill_row<LANES>(a, e, others, row_mass<LANES>(e, others, a.c, a.inv_t), teacher_row<LANES>(a, e), (float)(part * a.scale));
             if (l == 0) a.loss[at] = o.loss;
             sums[0] += part == 0.0 ? 0.0 : part * (double)o.loss;
             sums[1] += (double)o.loss;
@@ -701,7 +702,7 @@ __device__ __forceinline__ void finish_listed(const ListedArgs& a, uint32_t n, i
     if constexpr (MODE == SCORES) {
         write_scores(a, n, at, r.e, others);
     } else {
-        const ListedRow o = distill_row(a, r.e, others, row_mass(r.e, others, a.c), r.t, (float)(r.part * a.scale));
+        const ListedRow o = distill_row(a, r.e, others, row_mass(r.e, others, a.c, a.inv_t), r.t, (float)(r.part * a.scale));
         if (lane_id() == 0) a.loss[at] = o.loss;
         if (lane_id() == 0 && a.has_dx) a.row[n] = o;
         finish_token(a, n, r.part, o.loss, r.tokens);
@@ -982,7 +983,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void k_listed_row
     }
     ListedRow o{};
     if (tid < kWave) {
-        o = distill_row(a, r.e, others, row_mass(r.e, others, a.c), r.t, (float)(r.part * a.scale));
+        o = distill_row(a, r.e, others, row_mass(r.e, others, a.c, a.inv_t), r.t, (float)(r.part * a.scale));
         if (tid == 0) {
             if constexpr (WAVES > 1) s_row = o;
             a.loss[at] = o.loss;

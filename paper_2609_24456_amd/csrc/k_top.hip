@@ -142,7 +142,7 @@ __device__ __forceinline__ void write_ranked(const TopArgs& a, uint32_t row, con
     const float base = uniform(r.base), log2_s = uniform(r.log2_s);
     rank<NT>(cand, n, a.K, tid, [&](uint32_t k, uint64_t key) {
         o.ids[k] = (int32_t)~(uint32_t)key;
-        o.logps[k] = weight ? ((key_score((uint32_t)(key >> 32)) - base) * a.c - log2_s) * kLn2 : kNone;
+        o.logps[k] = weight ? log_p_from(key_score((uint32_t)(key >> 32)) - base, a.c, a.inv_t, log2_s) : kNone;
     });
     if (n < (uint32_t)a.K) fill_row<NT>(a, o, tid, (int32_t)n, -1, kNone);  // fewer choices than K
 }
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_few(TopArgs a) {
     for (int i = 0; i < kFewElems; ++i) {
         if (key[i] == 0 || rank[i] >= (uint32_t)a.K) continue;
         o.ids[rank[i]] = l + i * LANES;
-        o.logps[rank[i]] = r.inv_s != 0.0f ? ((v[i] - r.base) * a.c - r.log2_s) * kLn2 : kNone;
+        o.logps[rank[i]] = r.inv_s != 0.0f ? log_p_from(v[i] - r.base, a.c, a.inv_t, r.log2_s) : kNone;
     }
     if (a.V < a.K) fill_row<LANES>(a, o, l, (int32_t)a.V, -1, kNone);
 }

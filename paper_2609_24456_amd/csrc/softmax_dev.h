@@ -93,6 +93,13 @@ struct RowValues {
     float lse, entropy, logp, one_minus_p;
 };
 
+// log p of a score that is `d` from the largest (0 or below).  In powers of two it may be
+// past the largest float where log p is not: choices at the type's lowest value.
+__device__ __forceinline__ float log_p_from(float d, float c, float inv_t, float log2_s) {
+    const float r = (d * c - log2_s) * kLn2;
+    return r == kNone ? fmaf(d, inv_t, -log2_s * kLn2) : r;
+}
+
 // max x / temperature + log_s.  inv_lo: what the rounding of 1 / temperature to inv_t
 // left, which at a large maximum is as much as the rounding of lse itself (0: not
 // counted).  Where its share is past the largest float the score is by far, and lse is
@@ -114,7 +121,7 @@ __device__ __forceinline__ RowValues row_values(const Stat& st, float xa, float 
     r.log2_s = log2_fast(st.s);
     r.lse = log_normaliser(st.m, r.log2_s * kLn2, inv_t, inv_lo);
     r.entropy = (r.log2_s - st.u * r.inv_s) * kLn2;
-    r.logp = ((xa - st.m) * c - r.log2_s) * kLn2;
+    r.logp = log_p_from(xa - st.m, c, inv_t, r.log2_s);
     r.one_minus_p = -expm1_fast(r.logp);
     return r;
 }
