@@ -8,7 +8,7 @@
 // often far smaller than what the listed ones hold, and would be lost in the
 // difference of two sums.  With m, s the others' maximum and sum, and M, S the
 // whole row's, in powers of two as in k_logits.hip:
-//     log p_k = ln2 (c (x_k - M) - log2 S),   log p_rest = ln2 (log2 s + c (m - M) - log2 S).
+//     log p_k = (x_k - M) / temperature - log S,   log p_rest = (m - M) / temperature + log s - log S.
 // The divergence goes by u = log q - log p of each listed choice, and of the rest
 // where it counts as one more:
 //     forward  sum q log (q / p) = sum q (exp(-u) - 1 + u) + sum q - sum p
@@ -254,10 +254,10 @@ __device__ __forceinline__ float apart_by(float a, float b, float s) {
 
 // what a row's sums say
 struct RowMass {
-    float top, log2_s;   // M (0 in a row without weight), log2 S
+    float top, log_s;    // M (0 in a row without weight), log S
     float share, rest;   // 2^(c (m - M)) / S, log p_rest
     bool weight, some;   // anything but -infinity in the row, among the others
-    __device__ __forceinline__ float logp(float x, float c, float inv_t) const { return log_p_from(x - top, c, inv_t, log2_s); }
+    __device__ __forceinline__ float logp(float x, float inv_t) const { return fmaf(x - top, inv_t, -log_s); }
 };
 
 template <int LANES = kWave>
@@ -271,14 +271,14 @@ __device__ __forceinline__ RowMass row_mass(const Listed& e, const Mass& others,
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLists; ++i) sum += e.first[i] ? exp2_fast((e.x[i] - r.top) * c) : 0.0f;
-    const float away = others.m == top ? 0.0f : others.m - top, d = away * c, k = exp2_fast(d);
+    const float d = others.m == top ? 0.0f : others.m - top, k = exp2_fast(d * c);
     const float S = fmaf(others.s, k, group_first<LANES>(lanes_sum<LANES>(sum)));
     r.weight = !(S == 0.0f);  // (a row of NaN alone has no largest score either)
-    r.log2_s = r.weight ? log2_fast(S) : 0.0f;
+    const float log2_s = r.weight ? log2_fast(S) : 0.0f;
+    r.log_s = log2_s * kLn2;
     r.some = !(others.s == 0.0f);
     r.share = r.weight ? k / S : 0.0f;
-    r.rest = r.some ? (log2_fast(others.s) + d - r.log2_s) * kLn2 : kNone;
-    if (r.some && r.rest == kNone) r.rest = away * inv_t;  // (as in log_p_from: the logarithms are nothing beside it)
+    r.rest = r.some ? fmaf(d, inv_t, (log2_fast(others.s) - log2_s) * kLn2) : kNone;
     return r;
 }
 
@@ -317,13 +317,29 @@ __device__ __forceinline__ Teacher teacher_row(const ListedArgs& a, const Listed
 
 constexpr double kLeastRest = 1.0 / 8388608.0;  // 2^-23: what 32-bit log-probabilities say of a rest at best
 
+// The forward divergence of a row in which a log-probability is past the largest float (choices at the type's lowest
+// value, small temperatures): its product with the teacher's probability need not be.  What is left out of it, sum q log
+// q, is nothing beside it.
+template <int LANES>
+__device__ __forceinline__ float far_divergence(const ListedArgs& a, const Listed& e, const Mass& others, const RowMass& r,
+                                                const Teacher& t, float q_rest) {
+    float loss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+        const float q = e.first[i] ? exp_fast((e.y[i] - t.top) * a.q_inv_t - t.log) : 0.0f;
+        if (q != 0.0f) loss = e.x[i] == kNone ? INFINITY : fmaf(q * a.inv_t, r.top - e.x[i], loss);
+    }
+    loss = group_first<LANES>(lanes_sum<LANES>(loss));
+    return r.some && q_rest != 0.0f ? fmaf(q_rest * a.inv_t, r.top - others.m, loss) : loss;
+}
+
 // The divergence of a row and what its gradient needs; w: the token's weight.
 template <int LANES = kWave>
 __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const Listed& e, const Mass& others, const RowMass& r,
                                                  const Teacher& t, float w) {
     ListedRow o{};
     o.top = r.top;
-    o.log2_s = r.log2_s;
+    o.log_s = r.log_s;
     o.q_top = t.top;
     o.q_log = t.log;
     o.base = others.m == kNone ? 0.0f : others.m;
@@ -341,7 +357,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         if (!e.first[i]) continue;
-        const float lq = (e.y[i] - t.top) * a.q_inv_t - t.log, lp = r.logp(e.x[i], a.c, a.inv_t);
+        const float lq = (e.y[i] - t.top) * a.q_inv_t - t.log, lp = r.logp(e.x[i], a.inv_t);
         const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
         loss += a.reverse ? curve(p, q, u) : curve(q, p, -u);
     }
@@ -349,6 +365,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
     const float p_rest = r.some ? exp_fast(r.rest) : 0.0f;
     if (!a.with_rest) {
         o.loss = loss + p_rest;
+        if (o.loss == INFINITY) o.loss = far_divergence<LANES>(a, e, others, r, t, 0.0f);
         o.coef = r.some && o.w != 0.0f ? o.w * r.share : 0.0f;  // (a share that is no number counts for nothing at weight 0)
         return o;
     }
@@ -357,9 +374,11 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
     const float q_rest = (float)kept, away = r.some ? log2_fast(q_rest) * kLn2 - r.rest : 0.0f;
     if (a.reverse) {
         o.loss = loss + (r.some ? curve(p_rest, q_rest, away) : 0.0f) - o.over;
-        o.coef = r.some && o.w != 0.0f ? -o.w * (r.share * (away + o.loss)) : 0.0f;
+        // (others without weight have none of the gradient however far away they are: 0 times infinity)
+        o.coef = r.some && o.w != 0.0f && r.share != 0.0f ? -o.w * (r.share * (away + o.loss)) : 0.0f;
     } else {
         o.loss = loss + (r.some ? curve(q_rest, p_rest, -away) : 0.0f) + o.over;
+        if (o.loss == INFINITY) o.loss = far_divergence<LANES>(a, e, others, r, t, q_rest);
         // (1 + over) share - q_rest / s
         float k, em1;
         exp_remainder(away, &k, &em1);
@@ -372,7 +391,7 @@ __device__ __forceinline__ ListedRow distill_row(const ListedArgs& a, const List
 // the gradient of a listed choice of score x and teacher's value y
 __device__ __forceinline__ float listed_gradient(const ListedArgs& a, const ListedRow& o, float x, float y) {
     if (o.w == 0.0f) return 0.0f;
-    const float lq = (y - o.q_top) * a.q_inv_t - o.q_log, lp = ((x - o.top) * a.c - o.log2_s) * kLn2;
+    const float lq = (y - o.q_top) * a.q_inv_t - o.q_log, lp = fmaf(x - o.top, a.inv_t, -o.log_s);
     const float q = exp_fast(lq), p = exp_fast(lp), u = lq - lp;
     if (a.reverse) return p == 0.0f ? 0.0f : -o.w * p * (u + o.loss);
     return o.w * fmaf(p, o.over, apart_by(q, p, -u));
@@ -385,11 +404,11 @@ __device__ __forceinline__ void write_scores(const ListedArgs& a, uint32_t n, in
 #pragma unroll
     for (int i = 0; i < kLists; ++i) {
         const int32_t k = i * LANES + group_lane<LANES>();
-        if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.c, a.inv_t) : kNone;
+        if (k < a.K) out[k] = e.on[i] ? r.logp(e.x[i], a.inv_t) : kNone;
     }
     if (group_lane<LANES>() != 0) return;
     if (a.rest) a.rest[at] = r.rest;
-    if (a.lse) a.lse[at] = r.weight ? log_normaliser(r.top, r.log2_s * kLn2, a.inv_t, a.inv_lo) : kNone;
+    if (a.lse) a.lse[at] = r.weight ? log_normaliser(r.top, r.log_s, a.inv_t, a.inv_lo) : kNone;
 }
 
 // per-token outputs of a token that does not count, by LANES lanes
@@ -571,9 +590,10 @@ __global__ __launch_bounds__(kSumThreads) void k_distill_sum(ListedArgs a) {
 // So many rows of up to 64 choices with short lists share a wavefront, 16 lanes each
 // (65,536 rows of 18, K = 8: 23 us, a wavefront each 77; scores of 5 choices 8.6 against
 // 29).  The loss's workgroups are few, since each draws a ticket; a large batch has
-// them of 1,024 threads (256: 103 us for the 77).
+// them of 1,024 threads (256: 103 us for the 77).  Five wavefronts a SIMD (96
+// registers) cover each other; four take 2 to 4% longer.
 template <bool BF16, int MODE, int NT, int LANES, int E>
-__global__ __launch_bounds__(NT) void k_listed_short(ListedArgs a) {
+__global__ __launch_bounds__(NT, MODE == DISTILL ? 5 : 1) void k_listed_short(ListedArgs a) {
     using T = typename Elem<BF16>::T;
     constexpr int kRows = NT / LANES;
     static_assert(E <= 32 && kRows <= kWave, "a word of bits a lane");

@@ -50,7 +50,7 @@ hipError_t launch_token_alternatives(const TopArgs& a, bool bf16, hipStream_t s)
 // by its own and the teacher's probability.
 struct ListedRow {
     float base, coef;
-    float top, log2_s;  // log p = ln2 (c (x - top) - log2_s)
+    float top, log_s;   // log p = (x - top) / temperature - log_s
     float q_top, q_log; // log q = (y - q_top) / teacher's temperature - q_log
     float loss, over, w;
 };

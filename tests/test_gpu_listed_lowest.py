@@ -83,3 +83,73 @@ def test_log_probabilities_of_forbidden_choices(V, B, T, dtype):
             _close(host(lp), w, tol(w))
             cd.conduit_token_logprobs(x, _gpu(tok), lp, temperature=tau)
             _close(host(lp), w, tol(w))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,B,T", SHAPES)
+def test_distillation_where_all_others_are_forbidden(V, B, T, dtype):
+    rng = np.random.default_rng(V + 1)
+    for low in _lows(dtype):
+        x, z, ids = _batch(V, B, T, dtype, low)
+        q = rng.random((B, T, ALLOWED)) + 0.05
+        y = np.full((B, T, K), -np.inf, np.float32)
+        y[..., :ALLOWED] = np.log(q / q.sum(-1, keepdims=True) * rng.choice([0.7, 0.99, 1.0], (B, T, 1)))
+        for tau in (0.9, 1.0, 1.3):
+            for opts in FORMS:
+                e = _e(z, tau)
+                want = ref.distill_loss(z, ids, y, temperature=tau, **opts)
+                dx = torch.full_like(x, float("nan"))
+                loss, stats = torch.empty((B, T), device="cuda"), torch.empty(3, device="cuda")
+                cd.conduit_distill_loss(cd.distill_opts(**opts), x, _gpu(ids), _gpu(y), loss, stats, dlogits=dx, temperature=tau)
+                logp, rest, _ = ref.listed_logprobs(z, ids, temperature=tau)
+                t = y[..., :ALLOWED].astype(np.float64) / (opts.get("teacher_temperature", 1.0))
+                if not opts.get("rest"):
+                    t = t - np.log(np.exp(t).sum(-1, keepdims=True))
+                U = 1 + np.abs(t - logp[..., :ALLOWED]).max(-1)
+                far = 16 * 2.0 ** -24 * np.abs(want[0]) if opts["loss"] == "forward" else 0.0
+                _close(host(loss), want[0], 4 * e * U + far)
+                total = abs(opts.get("scale", 1.0)) * (B * T if opts.get("reduction") == "sum" else 1)
+                _close(host(stats)[0], want[1][0], total * (4 * e * U.max() + 2.0 ** -22 * np.abs(want[0]).max()))
+                size = np.zeros(z.shape)
+                np.put_along_axis(size, ids[..., :ALLOWED].astype(np.int64), np.exp(t) + np.exp(logp[..., :ALLOWED]), -1)
+                if opts.get("rest") and V > ALLOWED:
+                    others = np.ones(z.shape, bool)
+                    np.put_along_axis(others, ids[..., :ALLOWED].astype(np.int64), False, -1)
+                    size[others] = 1.0 / (V - ALLOWED)
+                w = abs(opts.get("scale", 1.0)) / (1 if opts.get("reduction") == "sum" else B * T)
+                _close(host(dx.float()), want[2],
+                       8 * e * U[..., None] * size * w / tau + 1e-44 + (2.0 ** -8 * np.abs(want[2]) if dtype == BF16 else 0.0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,B,T", SHAPES)
+def test_distillation_towards_a_forbidden_choice(V, B, T, dtype):
+    """The teacher gives weight to a choice that the student's logits forbid; at -infinity the divergence is infinite."""
+    rng = np.random.default_rng(V + 3)
+    for low in _lows(dtype)[1:] + [-np.inf]:
+        x, z, ids = _batch(V, B, T, dtype, low)
+        free = np.ones(z.shape, bool)
+        np.put_along_axis(free, ids[..., :ALLOWED].astype(np.int64), False, -1)
+        ids[..., ALLOWED] = free.argmax(-1)  # the first forbidden one
+        q = rng.random((B, T, ALLOWED + 1)) + 0.05
+        y = np.full((B, T, K), -np.inf, np.float32)
+        y[..., :ALLOWED + 1] = np.log(q / q.sum(-1, keepdims=True))
+        for tau in (0.9, 1.0, 1.3):
+            for opts in FORMS[:2]:
+                want = ref.distill_loss(z, ids, y, temperature=tau, **opts)
+                dx = torch.full_like(x, float("nan"))
+                loss, stats = torch.empty((B, T), device="cuda"), torch.empty(3, device="cuda")
+                cd.conduit_distill_loss(cd.distill_opts(**opts), x, _gpu(ids), _gpu(y), loss, stats, dlogits=dx, temperature=tau)
+                # (sums of up to 11 terms of one sign, each of 4 roundings and the exponential's)
+                _close(host(loss), want[0], 32 * 2.0 ** -24 * np.abs(np.where(np.isfinite(want[0]), want[0], 0)) + _e(z, tau) * 100)
+                e = _e(z, tau)
+                logp = ref.listed_logprobs(z, ids, temperature=tau)[0][..., :ALLOWED + 1]
+                t = y[..., :ALLOWED + 1].astype(np.float64) / opts.get("teacher_temperature", 1.0)
+                if not opts.get("rest"):
+                    t = t - np.log(np.exp(t).sum(-1, keepdims=True))
+                U = 1 + np.abs(t - logp)[..., :ALLOWED].max(-1)
+                size = np.full(z.shape, 1.0 / V)
+                np.put_along_axis(size, ids[..., :ALLOWED + 1].astype(np.int64), np.exp(t) + np.exp(logp), -1)
+                w = abs(opts.get("scale", 1.0)) / (B * T)
+                _close(host(dx.float()), want[2],
+                       8 * e * U[..., None] * size * w / tau + 1e-44 + (2.0 ** -8 * np.abs(want[2]) if dtype == BF16 else 0.0))
