@@ -843,7 +843,9 @@ conduit_status conduit_listed_logprobs(const conduit_rows* logits, int64_t B, in
  * dlogits: rows of the logits' dtype and width, rounded once; it may be the
  * logits themselves (in place), and is apart from every other array.  Masked
  * rows are written as 0, and so are rows whose lse is -inf; a rest of -inf has no
- * gradient.  Errors: EINVAL, EDEVICE, ESTATE.
+ * gradient.  p_j and p_j / exp(rest) go by lse and rest as given, so that they are
+ * off by the rounding of these, 2^-24 of their size, and are 1 at most.
+ * Errors: EINVAL, EDEVICE, ESTATE.
  */
 conduit_status conduit_listed_logprobs_backward(const conduit_rows* logits, int64_t B, int64_t T, int64_t stride,
                                                 const conduit_rows* ids, const uint8_t* mask, double temperature,

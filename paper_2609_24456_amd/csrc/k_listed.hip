@@ -1133,7 +1133,6 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
     wave_fence();
     const uint32_t marked = bits[lane], marked_beside = bits[kWave + lane / 32] >> lane % 32 & 1;
     const LogP by{a.inv_t, a.inv_lo, a.lowest, lse};
-    auto log_p = [&](float f) { return by.of(f); };
     // of any other choice: coef times its share of the rest (with h), or its probability
     float coef, shift = 0.0f;
     if constexpr (SPLIT) {
@@ -1144,29 +1143,40 @@ __global__ __launch_bounds__(kListedThreads) void k_listed_gradient(ListedArgs a
         shift = rest;
         coef = -fmaf(sum, exp_fast(rest), h * expm1_fast(rest)) * a.inv_t;
     }
-    auto other = [&](float f) {
-        if (coef == 0.0f) return 0.0f;
-        if constexpr (SPLIT) return coef * exp2_fast((f - o.base) * a.c);
-        return coef * exp2_fast((log_p(f) - shift) * kLog2e);
+    // (held: the log-probability of a choice, or of one among the others, is 0 at most, which the rounding of a large lse
+    // or rest would pass: 2^-24 of it, 64 at 1e9.  NaN stays.)
+    auto log_p = [&](float f, float less, auto held) {
+        const float q = by.of(f) - less;
+        return held && q > 0.0f ? 0.0f : q;
     };
+    auto write = [&](auto held) {
+        auto other = [&](float f) {
+            if (coef == 0.0f) return 0.0f;
+            if constexpr (SPLIT) return coef * exp2_fast((f - o.base) * a.c);
+            return coef * exp2_fast(log_p(f, shift, held) * kLog2e);
+        };
 #pragma unroll
-    for (int k = 0; k < kGradK; ++k) {
-        const uint32_t i = base + k * kWave;
-        float f[kPer];
-        E::unpack(v[k], f);
+        for (int k = 0; k < kGradK; ++k) {
+            const uint32_t i = base + k * kWave;
+            float f[kPer];
+            E::unpack(v[k], f);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) f[j] = other(f[j]);
-        if (i < nv) store_others<BF16, PAST>(vdx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
-    }
-    if (mine && !marked_beside) dx[row.beside_at(lane)] = E::round(other(xt));
+            for (int j = 0; j < kPer; ++j) f[j] = other(f[j]);
+            if (i < nv) store_others<BF16, PAST>(vdx + (size_t)i * kPer, f, marked >> k * kPer & ((1u << kPer) - 1));
+        }
+        if (mine && !marked_beside) dx[row.beside_at(lane)] = E::round(other(xt));
 #pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-        if (!e.first[i]) continue;
-        float d;
-        if constexpr (SPLIT) d = listed_gradient(a, o, e.x[i], e.y[i]);
-        else d = (e.y[i] - (sum + h) * exp_fast(log_p(e.x[i]))) * a.inv_t;
-        dx[e.id[i]] = E::round(d);
-    }
+        for (int i = 0; i < kLists; ++i) {
+            if (!e.first[i]) continue;
+            float d;
+            if constexpr (SPLIT) d = listed_gradient(a, o, e.x[i], e.y[i]);
+            else d = (e.y[i] - (sum + h) * exp_fast(log_p(e.x[i], 0.0f, held))) * a.inv_t;
+            dx[e.id[i]] = E::round(d);
+        }
+    };
+    constexpr float kHeld = 65536.0f;  // (off by 2^-8 at most below; held always, 65,536 rows of 18 choices take 7 to 10% longer)
+    if (SPLIT || fabsf(lse) + fabsf(shift) < kHeld) write(std::false_type{});
+    else write(std::true_type{});
 }
 
 template <bool BF16, bool SPLIT>

@@ -153,3 +153,33 @@ def test_distillation_towards_a_forbidden_choice(V, B, T, dtype):
                 w = abs(opts.get("scale", 1.0)) / (B * T)
                 _close(host(dx.float()), want[2],
                        8 * e * U[..., None] * size * w / tau + 1e-44 + (2.0 ** -8 * np.abs(want[2]) if dtype == BF16 else 0.0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,B,T", SHAPES)
+def test_gradient_of_a_rest_without_weight(V, B, T, dtype):
+    """By lse and rest as they are given, whose roundings are as large as |rest| 2^-24: an other's share of the rest is
+    within them, and never above 1."""
+    rng = np.random.default_rng(V + 2)
+    for low in _lows(dtype):
+        x, z, ids = _batch(V, B, T, dtype, low)
+        g, h = rng.standard_normal((B, T, K)).astype(np.float32), rng.standard_normal((B, T)).astype(np.float32)
+        gz = np.where(ids < 0, 0, g)
+        for tau in (0.9, 1.0, 1.2, 3.0):
+            out = [torch.empty(s, device="cuda") for s in ((B, T, K), (B, T), (B, T))]
+            cd.conduit_listed_logprobs(x, _gpu(ids), out[0], rest=out[1], lse=out[2], temperature=tau)
+            dx = torch.full_like(x, float("nan"))
+            cd.conduit_listed_logprobs_backward(x, _gpu(ids), out[2], _gpu(g), dx, rest=out[1], drest=_gpu(h), temperature=tau)
+            got, rest = host(dx.float()).astype(np.float64), host(out[1])
+            # (a rest past the largest float is -infinity as given, and has no gradient)
+            want = ref.listed_gradient(z, ids, gz, np.where(rest > -np.inf, h, 0), temperature=tau)
+            half = 1 + (2.0 ** -8 if dtype == BF16 else 2.0 ** -24)
+            others = np.ones(z.shape, bool)
+            np.put_along_axis(others, ids[..., :ALLOWED].astype(np.int64), False, -1)
+            most = np.broadcast_to(np.where(rest > -np.inf, np.abs(h), 0)[..., None] / tau * half * (1 + 2.0 ** -20), z.shape)
+            assert np.isfinite(got).all() and (np.abs(got)[others] <= most[others]).all(), (low, tau)
+            size = (np.abs(gz).sum(-1) + np.abs(h))[..., None] / tau
+            _close(got[~others], want[~others], np.broadcast_to(4 * _e(z, tau) * size, z.shape)[~others] + 2.0 ** -8 * (dtype == BF16) * np.abs(want[~others]))
+            if low == -1e4:  # 4 roundings of |rest| and |lse|
+                tol = np.expm1(8 * 2.0 ** -24 * 1.2e4 / tau) + _e(z, tau)
+                _close(got[others], want[others], (tol + half - 1) * np.abs(want[others]))
