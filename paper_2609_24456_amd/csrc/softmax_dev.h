@@ -1,5 +1,5 @@
 // Softmax statistics of rows of scores, in parts that can be joined
-// (k_logits.hip, k_head.hip).  The scores are c x, c = log2(e) / temperature.
+// (k_logits.hip, k_head.hip, k_top.hip, k_listed.hip).  The scores are c x, c = log2(e) / temperature.
 #pragma once
 
 #include "loss_dev.h"

@@ -186,7 +186,7 @@ bool rows_like(PyObject* o, const at::Tensor& ids, Rows* r) {
 // log-probabilities: rest, lse; 2 their gradient: lse, rest, drest; 3 distillation:
 // loss, weight) whose arguments are all plain ones, and its status; None, and no
 // call, if anything is otherwise.  (Argument by argument through ctypes a call takes
-// 7.4 us on the host, this way 4.9, most of it the launch.)
+// 7.4 us on the host, this way 4.8 to 4.9, most of it the launch.)
 PyObject* listed(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 16) {
         PyErr_SetString(PyExc_TypeError, "listed takes 16 arguments");
